@@ -391,6 +391,144 @@ tr_status tr_project_kept(const tr_tokens *in, const int32_t *d_cu_k, const int3
 tr_status tr_project(const void *y, int32_t rows, int32_t d, const void *w, const float *bias, int32_t d_out,
                      int32_t act, void *z, int32_t *d_error, void *stream);
 
+/*
+ * ---- Into the language model: rotary positions and the paged cache ----
+ *
+ * The kept tokens Z* = P(X*) enter the LLM's attention layers (Section
+ * III-A: E_l consumes Z* and the text).  These calls take one layer's
+ * queries, keys and values from there to the attention output: the rotation
+ * of queries and keys by positions with several axes (kept tokens are a
+ * subset of their image's grid, so each token carries its own coordinates),
+ * the append of keys and values to a paged cache, and the attention of the
+ * new tokens over that cache.
+ *
+ * tr_heads: rows of one projection, element [t, h, c] at
+ * p + t * token_stride + h * head_stride + c (strides in elements; the
+ * channels are contiguous), so slices of a fused q/k/v projection pass as
+ * they are.  Bases are 16-byte aligned and strides multiples of 16 bytes.
+ */
+typedef struct {
+  void *p;               /* device; NULL where the argument is optional and absent */
+  int64_t token_stride;  /* elements                                               */
+  int64_t head_stride;
+  int32_t heads;
+} tr_heads;
+
+/*
+ * Rotary positions.  Frequency i < rot_dim / 2 turns one pair of channels by
+ * the angle pos[axis[i]] * f_i: the pair (i, i + rot_dim / 2) with
+ * TR_ROTARY_HALF, (2 i, 2 i + 1) with TR_ROTARY_PAIRS; channels >= rot_dim
+ * keep their values.  turns[i] = f_i / (2 pi) * 2^64 modulo 2^64, an exact
+ * fixed-point fraction of a turn: position times turns, modulo 2^64, is the
+ * angle without any loss at large positions (int32, negative ones too).
+ * tr_rotary_turns fills it on the host from the angular frequencies f_i.
+ * head_dim and rot_dim are multiples of 8, rot_dim <= head_dim <= 256.  An
+ * axis outside [0, axes) turns by nothing.
+ */
+#define TR_ROTARY_HALF 0
+#define TR_ROTARY_PAIRS 1
+#define TR_ROTARY_MAX_DIM 256
+typedef struct {
+  const uint64_t *turns;  /* device [rot_dim / 2] */
+  const int32_t *axis;    /* device [rot_dim / 2] */
+  int32_t head_dim, rot_dim;
+  int32_t axes;           /* rows of pos          */
+  int32_t layout;         /* TR_ROTARY_HALF or TR_ROTARY_PAIRS */
+} tr_rotary;
+
+/* Host only: h_turns[i] from h_freq[i] (radians per position, finite). */
+tr_status tr_rotary_turns(const double *h_freq, int32_t n, uint64_t *h_turns);
+
+/*
+ * y = rotate(norm(x)) for every head of the queries and of the keys, in one
+ * pass: norm(x) = x / sqrt(mean(x^2) + eps) * weight over the head's
+ * channels where a weight (device fp32 [head_dim], 16-byte aligned, shared
+ * by all heads) is given, x where it is NULL.  fp32 arithmetic, rounded once
+ * into `dtype` (any tr_dtype), the type of all rows.
+ *   pos:  device int32 [axes, tokens]
+ *   q, q_out; k, k_out:  tr_heads of `tokens` rows; k and k_out may both be
+ *         NULL.  Out may be the input itself (the same pointer and strides).
+ */
+tr_status tr_rotary_apply(const tr_rotary *r, int32_t dtype, int32_t tokens, const int32_t *pos, const tr_heads *q,
+                          const float *q_weight, const tr_heads *q_out, const tr_heads *k, const float *k_weight,
+                          const tr_heads *k_out, float eps, void *stream);
+
+/*
+ * The gradient of tr_rotary_apply: dq_out / dk_out with respect to q / k
+ * from dq / dk with respect to its outputs, and where a weight is given its
+ * gradient (device fp32 [head_dim], overwritten), the sum over all tokens
+ * and heads taken in a fixed order (the same bits on every call on one GPU
+ * model).  q and k (the forward inputs) are read only where their weight is
+ * given and may be NULL otherwise.  ws: tr_rotary_backward_workspace_bytes
+ * device bytes, 256-byte aligned (0 bytes, NULL allowed, without weights).
+ */
+size_t tr_rotary_backward_workspace_bytes(const tr_rotary *r, int32_t tokens);
+tr_status tr_rotary_backward(const tr_rotary *r, int32_t dtype, int32_t tokens, const int32_t *pos,
+                             const tr_heads *dq, const tr_heads *q, const float *q_weight, const tr_heads *dq_out,
+                             float *dq_weight, const tr_heads *dk, const tr_heads *k, const float *k_weight,
+                             const tr_heads *dk_out, float *dk_weight, float eps, void *ws, size_t ws_bytes,
+                             void *stream);
+
+/*
+ * A paged key/value cache and one step's new tokens.  k and v are
+ * [pages, heads, page, head_dim] in `dtype` (TR_BF16 or TR_F16); key j of
+ * sequence b lies in page table[b, j / page] at slot j % page.  lens[b]
+ * counts the keys of sequence b with the step's new tokens, which are its
+ * last: new token t, cu_new[b] <= t < cu_new[b+1], is key
+ * lens[b] - cu_new[b+1] + t.  All of this may change on the device between
+ * replays of a captured graph.  page is a power of two from 16 to 256,
+ * head_dim a multiple of 16 up to 128.  Nothing outside the cache is
+ * touched whatever the device arrays hold: keys beyond max_pages * page do
+ * not exist, a page id outside [0, pages) takes no append and reads as
+ * zeros.  d_error (optional device int32, zero it first) then gets
+ * TR_CACHE_ERR_PAGE, or TR_CACHE_ERR_WAIT when a pipeline wait inside the
+ * attention timed out (not expected in a correct run; outputs incomplete).
+ */
+#define TR_CACHE_ERR_PAGE 1
+#define TR_CACHE_ERR_WAIT 2
+typedef struct {
+  void *k, *v;             /* device [pages, heads, page, head_dim], 16-byte aligned */
+  int32_t dtype;
+  int32_t pages, heads, page, head_dim;
+  const int32_t *table;    /* device [batch, max_pages] page ids   */
+  int32_t batch, max_pages;
+  const int32_t *lens;     /* device [batch]                       */
+  const int32_t *cu_new;   /* device [batch + 1], cu_new[0] = 0    */
+  int32_t total_new;       /* host: cu_new[batch]                  */
+} tr_cache;
+
+/*
+ * Appends the new tokens' keys and values: k is normed (k_weight) and
+ * rotated (r, pos) as in tr_rotary_apply on the way (r and k_weight may be
+ * NULL), v is copied.  q, if given, holds the queries of the same tokens:
+ * q_out = rotate(norm(q)) in the same launch.  All rows in the cache's dtype.
+ */
+tr_status tr_cache_append(const tr_cache *c, const tr_heads *k, const tr_heads *v, const tr_rotary *r,
+                          const int32_t *pos, const float *k_weight, const tr_heads *q, const float *q_weight,
+                          const tr_heads *q_out, float eps, int32_t *d_error, void *stream);
+
+/*
+ * Attention of the new tokens over the cache (their own keys appended
+ * first): o[t, h] = sum_j p_j v_j with p = softmax(scale q[t, h] . k_j) over
+ * the visible keys j of key head h / (q heads / key heads).  With
+ * i = lens[b] - cu_new[b+1] + t the token's own key, key j is visible when
+ *   0 <= j < lens[b],  j <= i if causal,  j > i - window if window > 0.
+ * A row that sees no key gives zeros (lse = -inf).
+ *   q, o:     tr_heads of total_new rows, the same number of heads, a
+ *             multiple of the cache's
+ *   lse:      device fp32 [total_new, q heads] or NULL: log sum exp of the
+ *             scaled scores
+ *   max_new, max_len: host upper bounds of a sequence's new tokens and of
+ *             lens (they size the launch; tokens or keys beyond them are
+ *             not served, and a bound that is too high costs only time)
+ *   ws:       device workspace of tr_cache_attend_workspace_bytes bytes,
+ *             256-byte aligned
+ */
+size_t tr_cache_attend_workspace_bytes(const tr_cache *c, int32_t q_heads, int32_t max_new, int32_t max_len);
+tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *o, float *lse, float scale,
+                          int32_t causal, int32_t window, int32_t max_new, int32_t max_len, void *ws,
+                          size_t ws_bytes, int32_t *d_error, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

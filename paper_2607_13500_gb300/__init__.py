@@ -12,9 +12,13 @@ encoder's final-layer MLP (Eq. 5) on the tensor cores with the scoring fused
 into its second GEMM, for callers that own that MLP; ``project_kept`` runs the
 projector's first layer on the kept tokens, reading them from x by index, and
 ``project`` the same layer on the gathered rows y (the faster route).
+``Rotary`` and ``PagedCache`` take the kept tokens on through an attention
+layer of the language model: rotary positions with several axes, the append of
+keys and values to a paged cache, and the attention over it.
 """
 from .api import (Mlp, MlpResult, Pipeline, Reducer, ReduceResult, budgets, mlp, project, project_kept, reduce,
                   score, select, workspace_bytes)
+from .attention import PagedCache, Rotary, RotaryGrads
 
-__all__ = ["Mlp", "MlpResult", "Pipeline", "Reducer", "ReduceResult", "budgets", "mlp", "project", "project_kept",
-           "reduce", "score", "select", "workspace_bytes"]
+__all__ = ["Mlp", "MlpResult", "PagedCache", "Pipeline", "Reducer", "ReduceResult", "Rotary", "RotaryGrads", "budgets",
+           "mlp", "project", "project_kept", "reduce", "score", "select", "workspace_bytes"]

@@ -54,6 +54,48 @@ class TrMlp(ctypes.Structure):
     ]
 
 
+TR_ROTARY_LAYOUT = {"half": 0, "pairs": 1}
+TR_CACHE_ERR_PAGE, TR_CACHE_ERR_WAIT = 1, 2
+
+
+class TrHeads(ctypes.Structure):
+    _fields_ = [
+        ("p", ctypes.c_void_p),
+        ("token_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+        ("heads", ctypes.c_int32),
+    ]
+
+
+class TrRotary(ctypes.Structure):
+    _fields_ = [
+        ("turns", ctypes.c_void_p),
+        ("axis", ctypes.c_void_p),
+        ("head_dim", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32),
+        ("axes", ctypes.c_int32),
+        ("layout", ctypes.c_int32),
+    ]
+
+
+class TrCache(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("dtype", ctypes.c_int32),
+        ("pages", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("page", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("table", ctypes.c_void_p),
+        ("batch", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("lens", ctypes.c_void_p),
+        ("cu_new", ctypes.c_void_p),
+        ("total_new", ctypes.c_int32),
+    ]
+
+
 class TrError(RuntimeError):
     def __init__(self, fn, code, lib):
         self.code = code
@@ -103,6 +145,21 @@ def load() -> ctypes.CDLL:
     lib.tr_project_kept.restype = I32
     lib.tr_project.argtypes = [VP, I32, I32, VP, VP, I32, I32, VP, VP, VP]
     lib.tr_project.restype = I32
+    F32, rot, cache, heads = ctypes.c_float, P(TrRotary), P(TrCache), P(TrHeads)
+    lib.tr_rotary_turns.argtypes, lib.tr_rotary_turns.restype = [P(ctypes.c_double), I32, P(ctypes.c_uint64)], I32
+    lib.tr_rotary_apply.argtypes = [rot, I32, I32, VP, heads, VP, heads, heads, VP, heads, F32, VP]
+    lib.tr_rotary_apply.restype = I32
+    lib.tr_rotary_backward_workspace_bytes.argtypes = [rot, I32]
+    lib.tr_rotary_backward_workspace_bytes.restype = SZ
+    lib.tr_rotary_backward.argtypes = [rot, I32, I32, VP, heads, heads, VP, heads, VP, heads, heads, VP, heads, VP, F32,
+                                       VP, SZ, VP]
+    lib.tr_rotary_backward.restype = I32
+    lib.tr_cache_append.argtypes = [cache, heads, heads, rot, VP, VP, heads, VP, heads, F32, VP, VP]
+    lib.tr_cache_append.restype = I32
+    lib.tr_cache_attend_workspace_bytes.argtypes = [cache, I32, I32, I32]
+    lib.tr_cache_attend_workspace_bytes.restype = SZ
+    lib.tr_cache_attend.argtypes = [cache, heads, heads, VP, F32, I32, I32, I32, I32, VP, SZ, VP, VP]
+    lib.tr_cache_attend.restype = I32
     _lib = lib
     return lib
 
