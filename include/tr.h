@@ -513,18 +513,23 @@ tr_status tr_cache_append(const tr_cache *c, const tr_heads *k, const tr_heads *
  * the visible keys j of key head h / (q heads / key heads).  With
  * i = lens[b] - cu_new[b+1] + t the token's own key, key j is visible when
  *   0 <= j < lens[b],  j <= i if causal,  j > i - window if window > 0.
- * A row that sees no key gives zeros (lse = -inf).
+ * A row that sees no key (or only scores of -inf) gives zeros (lse = -inf).
+ * A key that a row does not see takes no part in it, whatever it holds (a
+ * row whose tiles hold a hidden non-finite value is computed again without
+ * it, slowly).  Probabilities are rounded to the cache's type for their
+ * product with V; their sum and everything else is fp32.
  *   q, o:     tr_heads of total_new rows, the same number of heads, a
  *             multiple of the cache's
  *   lse:      device fp32 [total_new, q heads] or NULL: log sum exp of the
  *             scaled scores
- *   max_new, max_len: host upper bounds of a sequence's new tokens and of
- *             lens (they size the launch; tokens or keys beyond them are
- *             not served, and a bound that is too high costs only time)
+ *   max_new, max_len: what the host knows of a sequence's new tokens and of
+ *             lens at most.  They only choose the launch (rows of a block,
+ *             parts of the keys): a bound that is off costs time, no more
  *   ws:       device workspace of tr_cache_attend_workspace_bytes bytes,
  *             256-byte aligned
  */
-size_t tr_cache_attend_workspace_bytes(const tr_cache *c, int32_t q_heads, int32_t max_new, int32_t max_len);
+size_t tr_cache_attend_workspace_bytes(const tr_cache *c, int32_t q_heads, int32_t window, int32_t max_new,
+                                       int32_t max_len);
 tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *o, float *lse, float scale,
                           int32_t causal, int32_t window, int32_t max_new, int32_t max_len, void *ws,
                           size_t ws_bytes, int32_t *d_error, void *stream);

@@ -156,7 +156,7 @@ def load() -> ctypes.CDLL:
     lib.tr_rotary_backward.restype = I32
     lib.tr_cache_append.argtypes = [cache, heads, heads, rot, VP, VP, heads, VP, heads, F32, VP, VP]
     lib.tr_cache_append.restype = I32
-    lib.tr_cache_attend_workspace_bytes.argtypes = [cache, I32, I32, I32]
+    lib.tr_cache_attend_workspace_bytes.argtypes = [cache, I32, I32, I32, I32]
     lib.tr_cache_attend_workspace_bytes.restype = SZ
     lib.tr_cache_attend.argtypes = [cache, heads, heads, VP, F32, I32, I32, I32, I32, VP, SZ, VP, VP]
     lib.tr_cache_attend.restype = I32

@@ -245,9 +245,9 @@ class PagedCache:
         """Attention of the new tokens' queries q [T, q heads, head_dim] over
         the cache (tr_cache_attend), their own keys appended first.  With
         ``causal`` a token sees the keys up to its own, with ``window`` > 0 only
-        the last ``window`` of those.  ``max_new`` and ``max_len`` bound a
-        sequence's new tokens and its length (defaults: all T, and what the
-        table can hold; tighter bounds give a better launch).  Returns
+        the last ``window`` of those.  ``max_new`` and ``max_len``, what the
+        host knows of a sequence's new tokens and length at most, only choose
+        the launch (defaults: all T, and what the table can hold).  Returns
         out, or (out, lse fp32 [T, q heads])."""
         t, d, dev = q.shape[0], self.head_dim, self.device
         c = self._struct(table, lens, cu_new, t)
@@ -259,7 +259,7 @@ class PagedCache:
             return (out, lse) if return_lse else out
         max_new = t if max_new is None else int(max_new)
         max_len = table.shape[1] * self.page if max_len is None else int(max_len)
-        nbytes = self.lib.tr_cache_attend_workspace_bytes(c, hq.heads, max_new, max_len)
+        nbytes = self.lib.tr_cache_attend_workspace_bytes(c, hq.heads, window, max_new, max_len)
         ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
         check("tr_cache_attend", self.lib.tr_cache_attend(
             c, hq, ho, None if lse is None else lse.data_ptr(), 1.0 / math.sqrt(d) if scale is None else scale,

@@ -1,15 +1,49 @@
-// Attention of new tokens over the paged cache (tr_cache_attend):
-//   o = sum_j p_j v_j,  p = softmax over the visible keys of scale q . k_j.
+// Attention of new tokens over the paged cache (tr_cache_attend) on the
+// 5th-generation tensor cores:
+//   o = sum_j p_j v_j,  p = softmax over the visible keys of scale q . k_j,
+// in one pass over the keys with the running maximum and sum of the softmax.
+//
+// The query heads of one key head and the new tokens of one sequence make up
+// the rows of a block (row r: token r / group, head r % group), so a page is
+// read once for the whole group, and a single token of a grouped layer still
+// fills several rows.  A CTA takes 128 MT rows of one sequence and key head
+// and walks the keys in tiles of 128:
+//   softmax warps   one warpgroup per 128 rows, one thread per row: scores
+//                   from tensor memory, mask, maximum, exponentials; the
+//                   probabilities go back to tensor memory as the A operand
+//                   of the second product, in the place of the scores;
+//   producer warp   TMA loads of K and V tiles, page by page, into a ring of
+//                   128-byte-swizzled tiles; zeroes the value rows past the
+//                   sequence's end (stale memory there may hold NaN);
+//   MMA warp        S = Q K^T and O += P V from one thread.  The products of
+//                   the two 128-row blocks alternate, so one block's softmax
+//                   runs while the tensor cores work on the other.
+//
+// The maximum that the exponentials are taken against is only renewed (and
+// O rescaled) when it has grown by more than 8 powers of two: p <= 2^8 is as
+// exact as p <= 1 in floating point, and the rescaling, which reads and
+// writes all of O, almost never runs after the first tiles.
+//
+// Probabilities are rounded to the cache's 16-bit type for the second
+// product (the tensor cores take both operands in one type); their sum is
+// taken before that rounding, and everything else is fp32.
+#include <cfloat>
 #include <climits>
 #include <cmath>
+
+#include <atomic>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "tr_cache.cuh"
+#include "tr_map.cuh"
+#include "tr_tc.cuh"
 
 namespace tr {
 namespace {
+
+constexpr int kTile = 128;  // keys of a tile, rows of a block
 
 struct AttendArgs {
   CacheView c;
@@ -18,57 +52,184 @@ struct AttendArgs {
   long long q_tok, q_head, o_tok, o_head;  // elements
   int q_heads, group;                      // group: query heads of a key head
   float *lse;
-  float scale;
+  float scale;      // |scale| log2(e), never zero
+  int negate;       // scale < 0: the queries enter negated
   int causal, window;
+  int splits;       // parts of the key range, each a CTA's
+  float *part;      // splits > 1: [splits][total_new * q_heads][d] unnormalised sums,
+  float2 *part_ml;  //             [splits][total_new * q_heads] (maximum, sum)
   int32_t *err;
 };
 
+template <int D, int MT>
+struct Shape {
+  static constexpr int kHalves = D / 64;             // 64-column halves of a row
+  static constexpr int kTileBytes = kTile * D * 2;   // one K or V tile, or one block's Q
+  static constexpr int kBudget = 227 * 1024 - 2048;  // shared memory less barriers and alignment
+  static constexpr int kFit = (kBudget - MT * kTileBytes) / kTileBytes;
+  static constexpr int kStages = kFit < 12 ? kFit : 12;
+  static constexpr int kSBuf = MT == 1 ? 2 : 1;      // score buffers of a block
+  static constexpr int kThreads = 32 * (4 * MT + 2);
+  static constexpr int kColO = 256;                  // tensor-memory columns: scores below, sums from here
+  static constexpr int kCols = 512;
+  static constexpr size_t kSmem = (size_t)(MT + kStages) * kTileBytes + 1024 + 512;
+  static_assert(kColO + MT * D <= kCols, "scores and sums fit the tensor memory");
+  static_assert(kStages >= 4, "two tiles in use and two on their way");
+};
+
+template <typename T>
+struct Bits;
+template <>
+struct Bits<__nv_bfloat16> {
+  static constexpr bool kBf16 = true;
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  }
+};
+template <>
+struct Bits<__half> {
+  static constexpr bool kBf16 = false;
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  }
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 of_pair(unsigned long long v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// ---------------------------------------------------------------- where a CTA works
+// Sequence b's row blocks occupy the slots from floor(cu_new[b] group / R) + b
+// on (R rows a block), which leaves room for all of them whatever cu_new
+// holds; the last slot of a sequence may stay empty.
+struct Block {
+  int seq, first;     // sequence, first row (token * group + head) of the block
+  int rows;           // rows of the sequence: new tokens * group
+  int tok0;           // first new token of the sequence
+  int base;           // key of new token 0
+  int len;            // keys of the sequence
+};
+
+// All lanes of a warp together; seq = -1 for an empty slot.
+__device__ __forceinline__ Block find_block(const AttendArgs &g, int slot, int rows_per_block) {
+  const int lane = threadIdx.x & 31;
+  const CacheView &c = g.c;
+  int b = 0;  // sequences whose slots start at or before this one, less one
+  for (int i0 = 0; i0 < c.batch; i0 += 32) {
+    const int i = i0 + lane;
+    const bool before =
+        i < c.batch && ((long long)__ldg(c.cu_new + i) * g.group) / rows_per_block + i <= (long long)slot;
+    const unsigned m = __ballot_sync(0xffffffffu, before);
+    b += __popc(m);
+    if (m != 0xffffffffu) break;
+  }
+  b -= 1;
+  Block k;
+  k.seq = -1;
+  k.rows = k.first = k.tok0 = k.base = k.len = 0;
+  if (b < 0) return k;
+  const int t0 = __ldg(c.cu_new + b), t1 = min(__ldg(c.cu_new + b + 1), c.total_new);
+  const int n = t1 > t0 ? t1 - t0 : 0;
+  const long long start = ((long long)t0 * g.group) / rows_per_block + b;
+  k.first = (int)((slot - start) * rows_per_block);
+  k.rows = n * g.group;
+  if (t0 < 0 || k.first < 0 || k.first >= k.rows) return k;
+  k.seq = b;
+  k.tok0 = t0;
+  k.len = cache_len(c, b);
+  k.base = max(__ldg(c.lens + b), 0) - n;
+  return k;
+}
+
+// First key of the window that ends with key `own`.
+__device__ __forceinline__ int window_start(int own, int window) { return own >= window ? own - window + 1 : 0; }
+
+// Keys [lo, hi) that some row of [r0, r1) sees.
+struct Range {
+  int lo, hi;
+};
+__device__ __forceinline__ Range keys_of_rows(const AttendArgs &g, const Block &k, int r0, int r1) {
+  Range r{0, 0};
+  if (r0 >= r1) return r;
+  r.hi = g.causal ? min(k.len, k.base + (r1 - 1) / g.group + 1) : k.len;
+  r.lo = g.window > 0 ? window_start(k.base + r0 / g.group, g.window) : 0;
+  if (r.hi <= r.lo) r.lo = r.hi = 0;
+  return r;
+}
+
+// One row by one warp on the plain cores, four channels a lane: the running
+// maximum (powers of two), sum and weighted values over the keys [lo, hi).
 template <typename T>
 __device__ __forceinline__ float4 load4(const char *p) {
   const uint2 v = *reinterpret_cast<const uint2 *>(p);
   const T *h = reinterpret_cast<const T *>(&v);
   return make_float4((float)h[0], (float)h[1], (float)h[2], (float)h[3]);
 }
-
-// One warp per row (token, query head): four channels a lane, one key at a
-// time, the running maximum and sum of the softmax in registers.
+__device__ __forceinline__ bool finite4(const float4 &v) {
+  return fabsf(v.x) <= FLT_MAX && fabsf(v.y) <= FLT_MAX && fabsf(v.z) <= FLT_MAX && fabsf(v.w) <= FLT_MAX;
+}
 template <typename T>
-__global__ void __launch_bounds__(128) k_attend_rows(const __grid_constant__ AttendArgs g) {
-  const int lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row >= (long long)g.c.total_new * g.q_heads) return;
-  const int t = (int)(row / g.q_heads), h = (int)(row - (long long)t * g.q_heads);
-  const NewToken at = find_token(g.c, t);
-  int lo = 0, hi = 0;
-  if (at.seq >= 0) {
-    hi = cache_len(g.c, at.seq);
-    if (g.causal) hi = min(hi, at.key + 1);
-    if (g.window > 0) lo = max(0, at.key - g.window + 1);
-  }
-  const int d = g.c.d, ch = 4 * lane, hk = h / g.group;
-  const bool holds = ch < d;
-  float4 q = make_float4(0.f, 0.f, 0.f, 0.f), acc = q;
-  if (holds) q = load4<T>(g.q + 2 * ((long long)t * g.q_tok + (long long)h * g.q_head + ch));
-  float m = -INFINITY, l = 0.f;
+__device__ __noinline__ bool hidden_values_finite(const AttendArgs &g, int seq, int hk, int lo, int hi) {
+  const int ch = 4 * (threadIdx.x & 31);
+  bool ok = true;
   for (int j = lo; j < hi; ++j) {
-    const int page = page_of(g.c, at.seq, j);
+    const int page = page_of(g.c, seq, j);
+    if (page >= 0 && ch < g.c.d)
+      ok &= finite4(load4<T>(static_cast<const char *>(g.c.v) +
+                             2 * ((((long long)page * g.c.heads + hk) * g.c.page + (j & (g.c.page - 1))) * g.c.d + ch)));
+  }
+  return __all_sync(0xffffffffu, ok);
+}
+template <typename T>
+__device__ __noinline__ float4 row_by_warp(const AttendArgs &g, int seq, int hk, const char *q, int lo, int hi, float &m,
+                                           float &l) {
+  const int d = g.c.d, ch = 4 * (threadIdx.x & 31);
+  const bool holds = ch < d;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f), acc = x;
+  if (holds) x = load4<T>(q + 2 * ch);
+  const float sc = g.negate ? -g.scale : g.scale;
+  m = -INFINITY;
+  l = 0.f;
+  for (int j = lo; j < hi; ++j) {
+    const int page = page_of(g.c, seq, j);
     float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-    if (page >= 0) {
-      if (holds) {
-        const long long off =
-            2 * ((((long long)page * g.c.heads + hk) * g.c.page + (j & (g.c.page - 1))) * d + ch);
-        k = load4<T>(static_cast<const char *>(g.c.k) + off);
-        v = load4<T>(static_cast<const char *>(g.c.v) + off);
-      }
-    } else if (g.err && lane == 0) {
-      atomicOr(g.err, TR_CACHE_ERR_PAGE);
+    if (page >= 0 && holds) {
+      const long long off = 2 * ((((long long)page * g.c.heads + hk) * g.c.page + (j & (g.c.page - 1))) * d + ch);
+      k = load4<T>(static_cast<const char *>(g.c.k) + off);
+      v = load4<T>(static_cast<const char *>(g.c.v) + off);
     }
-    float s = q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
+    float s = x.x * k.x + x.y * k.y + x.z * k.z + x.w * k.w;
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    s *= g.scale;
+    s *= sc;
     const float mn = fmaxf(m, s);
-    const float f = m == mn ? 1.f : __expf(m - mn), p = s == -INFINITY ? 0.f : __expf(s - mn);
+    const float f = m == mn ? 1.f : exp2_fast(m - mn), p = s == -INFINITY ? 0.f : exp2_fast(s - mn);
     m = mn;
     l = l * f + p;
     acc.x = acc.x * f + p * v.x;
@@ -76,13 +237,525 @@ __global__ void __launch_bounds__(128) k_attend_rows(const __grid_constant__ Att
     acc.z = acc.z * f + p * v.z;
     acc.w = acc.w * f + p * v.w;
   }
-  const float inv = hi > lo ? 1.f / l : 0.f;
-  if (holds) {
-    T out[4] = {(T)(acc.x * inv), (T)(acc.y * inv), (T)(acc.z * inv), (T)(acc.w * inv)};
-    *reinterpret_cast<uint2 *>(g.o + 2 * ((long long)t * g.o_tok + (long long)h * g.o_head + ch)) =
-        *reinterpret_cast<uint2 *>(out);
+  return acc;
+}
+
+__device__ __forceinline__ void flag(const AttendArgs &g, int bit) {
+  if (g.err) atomicOr(g.err, bit);
+}
+
+// ---------------------------------------------------------------- the kernel
+template <typename T, int D, int MT>
+__global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
+    k_attend(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+             const __grid_constant__ AttendArgs g) {
+  using S = Shape<D, MT>;
+  constexpr int kRows = kTile * MT;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t sbase = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;  // the swizzle atom
+  const uint32_t ring = sbase + MT * S::kTileBytes;
+  const uint32_t bars = ring + S::kStages * S::kTileBytes;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 8u * (S::kStages + s); };
+  auto q_full = [&](int m) { return bars + 8u * (2 * S::kStages + m); };
+  auto s_full = [&](int m, int b) { return bars + 8u * (2 * S::kStages + MT + m * S::kSBuf + b); };
+  auto p_full = [&](int m, int b) { return bars + 8u * (2 * S::kStages + MT + MT * S::kSBuf + m * S::kSBuf + b); };
+  auto o_done = [&](int m) { return bars + 8u * (2 * S::kStages + MT + 2 * MT * S::kSBuf + m); };
+  const uint32_t tail = bars + 8u * (2 * S::kStages + 2 * MT + 2 * MT * S::kSBuf);
+  const uint32_t tmem_slot = tail + 8;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_wait();  // q and the cache come from the kernels before
+  const int slot = gridDim.x - 1 - blockIdx.x;  // causal chunks: the longest key ranges first
+  const int hk = blockIdx.y, split = blockIdx.z;
+  const Block k = find_block(g, slot, kRows);
+  if (k.seq < 0) return;
+
+  // tiles of the whole CTA and of each 128-row block, cut to this split
+  int t0, t1, a[MT], b[MT];
+  {
+    const Range r = keys_of_rows(g, k, k.first, min(k.first + kRows, k.rows));
+    const int u0 = r.lo / kTile, u1 = (r.hi + kTile - 1) / kTile;
+    const int per = (u1 - u0 + g.splits - 1) / g.splits;
+    t0 = min(u0 + split * per, u1);
+    t1 = min(t0 + per, u1);
+    int lo = INT_MAX, hi = 0;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const Range q = keys_of_rows(g, k, k.first + m * kTile, min(k.first + (m + 1) * kTile, k.rows));
+      a[m] = max(t0, q.lo / kTile);
+      b[m] = min(t1, (q.hi + kTile - 1) / kTile);
+      if (b[m] <= a[m]) a[m] = b[m] = t0;
+      else lo = min(lo, a[m]), hi = max(hi, b[m]);
+    }
+    t0 = lo < hi ? lo : 0;
+    t1 = lo < hi ? hi : 0;
   }
-  if (g.lse && lane == 0) g.lse[(long long)t * g.q_heads + h] = hi > lo ? m + logf(l) : -INFINITY;
+
+  if (t0 < t1) {
+    if (threadIdx.x == 0) {
+      for (int s = 0; s < S::kStages; ++s) {
+        tc::mbar_init(full(s), 1);
+        tc::mbar_init(empty(s), 1);
+      }
+      for (int m = 0; m < MT; ++m) {
+        tc::mbar_init(q_full(m), kTile);
+        for (int i = 0; i < S::kSBuf; ++i) {
+          tc::mbar_init(s_full(m, i), 1);
+          tc::mbar_init(p_full(m, i), kTile);
+        }
+        tc::mbar_init(o_done(m), 1);
+      }
+      tc::mbar_init(tail, 1);
+      tc::mbar_fence_init();
+      tc::tma_prefetch_map(&map_k);
+      tc::tma_prefetch_map(&map_v);
+    }
+    if (warp == 4 * MT) {
+      tc::tmem_alloc(tmem_slot, S::kCols);
+      tc::tmem_relinquish();
+    }
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+  }
+  uint32_t tmem = 0;
+  if (t0 < t1) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
+
+  if (warp == 4 * MT) {
+    // ---------------------------------------------------------------- TMA producer
+    const int page = g.c.page, piece = page < kTile ? page : kTile;  // keys of one load
+    const int none = max(1, g.c.pages * g.c.heads * page);           // a row past the cache: reads as zeros
+    int stage = 0;
+    uint32_t phase = 0, tails = 0, filled = 0, parity = 0;
+    bool ok = true;
+    for (int t = t0; t < t1 && ok; ++t) {
+      const int key0 = t * kTile, left = min(k.len - key0, kTile);
+      const int pieces = (left + piece - 1) / piece;
+      // lane: (half, piece) of the tile; its page's first row
+      const int pc = lane % (kTile / piece), half = lane / (kTile / piece);
+      const bool mine = pc < pieces && half < S::kHalves;
+      int row = none;
+      if (mine) {
+        const int key = key0 + pc * piece, id = page_of(g.c, k.seq, key);
+        if (id >= 0) row = (id * g.c.heads + hk) * page + (key & (page - 1));
+        else flag(g, TR_CACHE_ERR_PAGE);
+      }
+      const uint32_t bytes = (uint32_t)pieces * piece * 128u * S::kHalves;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        if (!tc::mbar_wait_warp(empty(stage), phase ^ 1u)) {
+          ok = false;
+          break;
+        }
+        const uint32_t dst = ring + stage * S::kTileBytes;
+        const bool cut = kv == 1 && left < kTile;  // the sequence ends inside this value tile
+        const uint32_t bar = cut ? tail : full(stage);
+        if (lane == 0) tc::mbar_expect_tx(bar, bytes);
+        __syncwarp();
+        if (mine) tc::tma_load_2d(dst + half * (kTile * 128) + pc * piece * 128, kv ? &map_v : &map_k, half * 64, row, bar);
+        if (cut) {
+          if (!tc::mbar_wait(tail, tails)) ok = false;
+          ok = __all_sync(0xffffffffu, ok);
+          tails ^= 1u;
+          for (int i = lane + left * 8; i < kTile * 8; i += 32)
+#pragma unroll
+            for (int h = 0; h < S::kHalves; ++h) tc::st_shared_v4(dst + h * (kTile * 128) + i * 16, 0, 0, 0, 0);
+          tc::fence_async_shared();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(full(stage));
+        }
+        filled |= 1u << stage;
+        parity = (parity & ~(1u << stage)) | (phase << stage);
+        if (++stage == S::kStages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+    // the loads already issued land before the CTA may exit
+    for (int s = 0; s < S::kStages; ++s)
+      if (filled >> s & 1u) tc::mbar_wait_warp(full(s), parity >> s & 1u);
+  } else if (warp == 4 * MT + 1) {
+    // ---------------------------------------------------------------- MMA issuer
+    if (lane == 0) {
+      const uint32_t idesc_s = tc::idesc_16(kTile, kTile, Bits<T>::kBf16, false);
+      const uint32_t idesc_o = tc::idesc_16(kTile, g.c.d, Bits<T>::kBf16, true);
+      const int ksteps = g.c.d / 16;
+      uint32_t sn[MT], pn[MT];  // products issued so far, of each kind
+      bool ok = true, have_q[MT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) sn[m] = pn[m] = 0, have_q[m] = false;
+      // The ring holds K and V of tile t as fills 2 (t - t0) and 2 (t - t0) + 1.
+      auto landed = [&](uint32_t fill) {
+        ok &= tc::mbar_wait(full((int)(fill % S::kStages)), fill / S::kStages & 1u);
+        return true;
+      };
+      // S_m = Q_m K^T
+      auto scores = [&](int m, uint32_t fill) {
+        const uint32_t qa = sbase + m * S::kTileBytes, kb = ring + fill % S::kStages * S::kTileBytes;
+        const int buf = S::kSBuf == 2 ? (int)(sn[m] & 1u) : 0;
+        const uint32_t dst = tmem + (uint32_t)((MT == 1 ? buf : m) * kTile);
+        for (int i = 0; i < ksteps; ++i) {
+          const uint32_t off = (uint32_t)((i >> 2) * (kTile * 128) + (i & 3) * 32);
+          tc::mma_bf16(dst, tc::sw128_desc(qa + off), tc::sw128_desc(kb + off), idesc_s, i > 0);
+        }
+        tc::mma_commit(s_full(m, buf));
+        ++sn[m];
+      };
+      // O_m (+)= P_m V
+      auto values = [&](int m, uint32_t fill) {
+        const uint32_t vb = ring + fill % S::kStages * S::kTileBytes;
+        const int buf = S::kSBuf == 2 ? (int)(pn[m] & 1u) : 0;
+        const uint32_t p = tmem + (uint32_t)((MT == 1 ? buf : m) * kTile), dst = tmem + (uint32_t)(S::kColO + m * D);
+#pragma unroll
+        for (int i = 0; i < kTile / 16; ++i)
+          tc::mma_bf16_ta(dst, p + 8 * i, tc::sw128_desc_mn(vb + 2048 * i, kTile * 128), idesc_o, pn[m] > 0 || i > 0);
+        tc::mma_commit(o_done(m));
+        ++pn[m];
+      };
+      // Step t issues P V of tile t - 1 and the scores of tile t.  The tensor
+      // cores run the products in the order of issue, so scores may overwrite
+      // probabilities that the product issued before them reads.  One block
+      // (MT = 1) has two score buffers and issues the scores first: its
+      // softmax of tile t runs during the products of tile t - 1.
+      for (int t = t0; t <= t1 && ok; ++t) {
+        const uint32_t kf = 2u * (uint32_t)(t - t0), vf = kf - 1;
+        bool have_k = t == t1, have_v = t == t0;
+        if (MT == 1 && t < t1) {
+          have_k = landed(kf);
+          if (!have_q[0]) ok &= tc::mbar_wait(q_full(0), 0), have_q[0] = true;
+          if (!ok) break;
+          tc::fence_after_sync();
+          scores(0, kf);
+          tc::mma_commit(empty((int)(kf % S::kStages)));
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          if (t > a[m] && t <= b[m]) {
+            if (!have_v) have_v = landed(vf);
+            ok &= tc::mbar_wait(p_full(m, S::kSBuf == 2 ? (int)(pn[m] & 1u) : 0),
+                                S::kSBuf == 2 ? pn[m] >> 1 & 1u : pn[m] & 1u);
+            if (!ok) break;
+            tc::fence_after_sync();
+            values(m, vf);
+          }
+          if (MT > 1 && t >= a[m] && t < b[m]) {
+            if (!have_k) have_k = landed(kf);
+            if (!have_q[m]) ok &= tc::mbar_wait(q_full(m), 0), have_q[m] = true;
+            if (!ok) break;
+            tc::fence_after_sync();
+            scores(m, kf);
+          }
+        }
+        if (!ok) break;
+        if (!have_v) have_v = landed(vf);  // a tile that no block used (the ranges of two blocks touch: not expected)
+        if (!have_k) have_k = landed(kf);
+        if (t > t0) tc::mma_commit(empty((int)(vf % S::kStages)));
+        if (MT > 1 && t < t1) tc::mma_commit(empty((int)(kf % S::kStages)));
+      }
+      if (!ok) flag(g, TR_CACHE_ERR_WAIT);
+    }
+    __syncwarp();
+  } else {
+    // ---------------------------------------------------------------- softmax
+    const int m = MT == 1 ? 0 : warp >> 2, quarter = warp & 3;
+    const int row = 32 * quarter + lane, r = k.first + m * kTile + row;  // row of the block, of the sequence
+    const bool valid = r < k.rows;
+    const int tok = valid ? r / g.group : 0, head = hk * g.group + (valid ? r - tok * g.group : 0);
+    const char *qrow = g.q + 2 * ((long long)(k.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
+    const int own = k.base + tok;
+    // keys this row sees; rows that do not exist mask nothing and are dropped at the end
+    const int hi = !valid ? INT_MAX : g.causal ? min(k.len, own + 1) : k.len;
+    const int lo = valid && g.window > 0 ? window_start(own, g.window) : 0;
+    const bool live = __any_sync(0xffffffffu, valid);
+    const int ta = MT > 1 && m == 1 ? a[MT - 1] : a[0], tb = MT > 1 && m == 1 ? b[MT - 1] : b[0];
+    float mx = -INFINITY, sum = 0.f;
+    bool ok = true;
+    const uint32_t lane_col = (uint32_t)(32 * quarter) << 16;
+    const uint32_t o_col = tmem + lane_col + (uint32_t)(S::kColO + m * D);
+    if (ta < tb) {
+      // this row of Q into the swizzled layout that TMA would write
+      const uint32_t dst = sbase + m * S::kTileBytes + row * 128;
+      const uint32_t flip = g.negate ? 0x80008000u : 0u;
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (valid && 8 * c < g.c.d) {
+          v = *reinterpret_cast<const uint4 *>(qrow + 16 * c);
+          v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
+        }
+        tc::st_shared_v4(dst + (c >> 3) * (kTile * 128) + (((c & 7) ^ (row & 7)) << 4), v.x, v.y, v.z, v.w);
+      }
+      tc::fence_async_shared();
+      tc::mbar_arrive(q_full(m));
+
+      for (int t = ta; t < tb; ++t) {
+        const int n = t - ta;
+        const int buf = S::kSBuf == 2 ? n & 1 : 0;
+        const uint32_t s_par = S::kSBuf == 2 ? (uint32_t)(n >> 1) & 1u : (uint32_t)n & 1u;
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(s_full(m, buf), s_par));
+        if (!ok) break;
+        tc::fence_after_sync();
+        if (live) {
+          const uint32_t s_col = tmem + lane_col + (uint32_t)((MT == 1 ? buf : m) * kTile);
+          uint32_t s[kTile];
+#pragma unroll
+          for (int i = 0; i < kTile; i += 32) tc::tmem_ld32_issue(s_col + i, s + i);
+#pragma unroll
+          for (int i = 0; i < kTile; i += 32) tc::tmem_ld32_wait(s + i);
+          const int key0 = t * kTile;
+          if (__any_sync(0xffffffffu, lo > key0 || hi < key0 + kTile)) {
+            const int c0 = lo - key0, c1 = hi - key0;
+#pragma unroll
+            for (int i = 0; i < kTile; ++i)
+              if (i < c0 || i >= c1) s[i] = 0xff800000u;  // -inf
+          }
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < kTile; i += 8)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              top[j] = fmaxf(top[j], fmaxf(__uint_as_float(s[i + 2 * j]), __uint_as_float(s[i + 2 * j + 1])));
+          const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * g.scale;
+          if (n == 0) {
+            mx = now;
+          } else if (__any_sync(0xffffffffu, now > mx + 8.f)) {
+            // the sums so far (all products up to the last tile's are in) move to the new maximum
+            const bool up = now > mx + 8.f;
+            const float f = up ? exp2_fast(mx - now) : 1.f;
+            ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 1) & 1u));
+            if (!ok) break;
+            tc::fence_after_sync();
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              uint32_t o[32];
+              tc::tmem_ld32_issue(o_col + c, o);
+              tc::tmem_ld32_wait(o);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tc::tmem_st32(o_col + c, o);
+            }
+            tc::tmem_st_wait();
+            if (up) mx = now;
+            sum *= f;
+          }
+          const float neg = mx == -INFINITY ? 0.f : -mx;  // a row that has seen nothing: exp2(-inf) = 0
+          const unsigned long long sc2 = pair_of(g.scale, g.scale), neg2 = pair_of(neg, neg);
+          unsigned long long acc[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+          for (int i = 0; i < kTile; i += 2) {
+            const float2 e = of_pair(fma2(pair_of(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), sc2, neg2));
+            const float p0 = exp2_fast(e.x), p1 = exp2_fast(e.y);
+            acc[(i >> 1) & 3] = add2(acc[(i >> 1) & 3], pair_of(p0, p1));
+            s[i >> 1] = Bits<T>::pack(p0, p1);
+          }
+          const float2 x = of_pair(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])));
+          sum += x.x + x.y;
+          tc::tmem_st32(s_col, s);
+          tc::tmem_st32(s_col + 32, s + 32);
+          tc::tmem_st_wait();
+        }
+        tc::fence_before_sync();
+        tc::mbar_arrive(p_full(m, buf));
+      }
+      // One phase after the other: the last scores say that all products but
+      // the last two are in (MT = 1 issues scores ahead of a product).
+      const int n = tb - ta;
+      if (ok && MT == 1 && n > 1) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 2) & 1u));
+      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 1) & 1u));
+      tc::fence_after_sync();
+      if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+    }
+
+    // ---------------------------------------------------------------- the rows' results
+    if (live && ok) {
+      const long long out_row = (long long)(k.tok0 + tok) * g.q_heads + head;
+      char *orow = g.o + 2 * ((long long)(k.tok0 + tok) * g.o_tok + (long long)head * g.o_head);
+      const bool parts = g.splits > 1;
+      const long long all_rows = (long long)g.c.total_new * g.q_heads;
+      float *prow = g.part + ((long long)split * all_rows + out_row) * g.c.d;
+      const float inv = parts ? 1.f : sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+      bool finite = true;
+#pragma unroll 1
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        if (ta < tb) {
+          tc::tmem_ld32_issue(o_col + c, o);
+          tc::tmem_ld32_wait(o);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = 0u;
+        }
+        if (valid && (ta < tb || !parts)) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            if (c + i >= g.c.d) break;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              v[j] = __uint_as_float(o[i + j]) * inv;
+              finite &= fabsf(v[j]) <= FLT_MAX;
+            }
+            if (parts) {
+              *reinterpret_cast<float4 *>(prow + c + i) = make_float4(v[0], v[1], v[2], v[3]);
+              *reinterpret_cast<float4 *>(prow + c + i + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+              *reinterpret_cast<uint4 *>(orow + 2 * (c + i)) =
+                  make_uint4(Bits<T>::pack(v[0], v[1]), Bits<T>::pack(v[2], v[3]), Bits<T>::pack(v[4], v[5]),
+                             Bits<T>::pack(v[6], v[7]));
+            }
+          }
+        }
+      }
+      if (valid) {
+        if (parts) g.part_ml[(long long)split * all_rows + out_row] = make_float2(mx, sum);
+        else if (g.lse) g.lse[out_row] = sum > 0.f || sum != sum ? mx * 0.693147180559945309f + logf(sum) : -INFINITY;
+      }
+      // A non-finite value of a key hidden from a row reaches it all the same
+      // as 0 * inf in the product over the tile.  Such rows are taken again
+      // without it: only when a row came out non-finite and a value hidden
+      // from it inside its tiles is.
+      unsigned bad = __ballot_sync(0xffffffffu, valid && !finite);
+      while (bad) {
+        const int src = __ffs(bad) - 1;
+        bad &= bad - 1;
+        const int rlo = max(__shfl_sync(0xffffffffu, lo, src), ta * kTile);
+        const int rhi = min(__shfl_sync(0xffffffffu, hi, src), tb * kTile);
+        const int end = min(tb * kTile, k.len);
+        if (hidden_values_finite<T>(g, k.seq, hk, ta * kTile, min(rlo, end)) &&
+            hidden_values_finite<T>(g, k.seq, hk, max(rhi, ta * kTile), end))
+          continue;
+        const unsigned long long qp = __shfl_sync(0xffffffffu, (unsigned long long)qrow, src);
+        const unsigned long long op = __shfl_sync(0xffffffffu, (unsigned long long)orow, src);
+        const unsigned long long pp = __shfl_sync(0xffffffffu, (unsigned long long)prow, src);
+        const long long orow_id = __shfl_sync(0xffffffffu, out_row, src);
+        float m1, l1;
+        float4 v = row_by_warp<T>(g, k.seq, hk, reinterpret_cast<const char *>(qp), rlo, rhi, m1, l1);
+        const float f = parts ? 1.f : l1 > 0.f || l1 != l1 ? 1.f / l1 : 0.f;
+        v.x *= f, v.y *= f, v.z *= f, v.w *= f;
+        if (4 * lane < g.c.d) {
+          if (parts) reinterpret_cast<float4 *>(pp)[lane] = v;
+          else
+            reinterpret_cast<uint2 *>(op)[lane] = make_uint2(Bits<T>::pack(v.x, v.y), Bits<T>::pack(v.z, v.w));
+        }
+        if (lane == 0) {
+          if (parts) g.part_ml[(long long)split * all_rows + orow_id] = make_float2(m1, l1);
+          else if (g.lse) g.lse[orow_id] = l1 > 0.f || l1 != l1 ? m1 * 0.693147180559945309f + logf(l1) : -INFINITY;
+        }
+      }
+    }
+  }
+
+  if (t0 < t1) {
+    tc::fence_before_sync();
+    __syncthreads();
+    if (warp == 4 * MT) {
+      tc::fence_after_sync();
+      tc::tmem_dealloc(tmem, S::kCols);
+    }
+  }
+}
+
+// Joins the splits of each row: one warp per row, in the splits' order.
+template <typename T>
+__global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ AttendArgs g) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const long long rows = (long long)g.c.total_new * g.q_heads;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const int t = (int)(row / g.q_heads), h = (int)(row - (long long)t * g.q_heads);
+  char *orow = g.o + 2 * ((long long)t * g.o_tok + (long long)h * g.o_head);
+  const bool holds = 4 * lane < g.c.d;
+  float m = -INFINITY, l = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (find_token(g.c, t).seq >= 0) {
+    for (int s = 0; s < g.splits; ++s) m = fmaxf(m, g.part_ml[s * rows + row].x);
+    for (int s = 0; s < g.splits; ++s) {
+      const float2 ml = g.part_ml[s * rows + row];
+      if (ml.y == 0.f) continue;  // saw no key
+      const float f = exp2_fast(ml.x - m);
+      l += ml.y * f;
+      if (holds) {
+        const float4 v = reinterpret_cast<const float4 *>(g.part + (s * rows + row) * g.c.d)[lane];
+        acc.x += v.x * f, acc.y += v.y * f, acc.z += v.z * f, acc.w += v.w * f;
+      }
+    }
+  }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  if (holds)
+    reinterpret_cast<uint2 *>(orow)[lane] =
+        make_uint2(Bits<T>::pack(acc.x * inv, acc.y * inv), Bits<T>::pack(acc.z * inv, acc.w * inv));
+  if (g.lse && lane == 0) g.lse[row] = l > 0.f || l != l ? m * 0.693147180559945309f + logf(l) : -INFINITY;
+}
+
+// ---------------------------------------------------------------- host side
+struct Plan {
+  int mt, splits, slots;
+  size_t part, part_ml, total;  // workspace
+};
+
+Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_len) {
+  Plan p{};
+  const int group = q_heads / c->heads;
+  const long long most = (long long)(max_new < c->total_new ? max_new : c->total_new) * group;
+  p.mt = most <= kTile ? 1 : 2;
+  const int rows = kTile * p.mt;
+  p.slots = (int)((long long)c->total_new * group / rows) + c->batch;
+  // Split the keys when the row blocks alone would not fill the GPU.
+  const int sms = sm_count() > 0 ? sm_count() : 1;
+  const long long blocks = (long long)p.slots * c->heads;
+  const long long cap = (long long)c->max_pages * c->page;
+  long long keys = max_len < cap ? max_len : cap;
+  if (window > 0 && keys > (long long)window + max_new) keys = (long long)window + max_new;
+  const long long tiles = (keys + kTile - 1) / kTile;
+  long long s = blocks > 0 ? sms / blocks : 1;
+  if (s > tiles) s = tiles;
+  if (s > 64) s = 64;
+  p.splits = s < 1 ? 1 : (int)s;
+  if (p.splits > 1) {
+    const size_t r = (size_t)c->total_new * q_heads * p.splits;
+    p.part_ml = align_up(r * c->head_dim * sizeof(float), 256);
+    p.total = p.part_ml + align_up(r * sizeof(float2), 256);
+  }
+  return p;
+}
+
+std::atomic<int> g_attend_smem_set[64];
+
+template <typename T, int D, int MT>
+cudaError_t launch_attend_t(const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &g, int slots, int variant,
+                            cudaStream_t st) {
+  using S = Shape<D, MT>;
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  const int bit = 1 << variant;
+  if (!(g_attend_smem_set[dev & 63].load() & bit)) {
+    err = cudaFuncSetAttribute(k_attend<T, D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
+    if (err != cudaSuccess) return err;
+    g_attend_smem_set[dev & 63].fetch_or(bit);
+  }
+  return launch_kernel(k_attend<T, D, MT>, dim3(slots, g.c.heads, g.splits), dim3(S::kThreads), S::kSmem, st, false, mk,
+                       mv, g);
+}
+
+template <typename T>
+cudaError_t launch_attend(const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &g, const Plan &p,
+                          cudaStream_t st) {
+  const int base = Bits<T>::kBf16 ? 0 : 4;
+  cudaError_t err;
+  if (g.c.d <= 64)
+    err = p.mt == 1 ? launch_attend_t<T, 64, 1>(mk, mv, g, p.slots, base, st)
+                    : launch_attend_t<T, 64, 2>(mk, mv, g, p.slots, base + 1, st);
+  else
+    err = p.mt == 1 ? launch_attend_t<T, 128, 1>(mk, mv, g, p.slots, base + 2, st)
+                    : launch_attend_t<T, 128, 2>(mk, mv, g, p.slots, base + 3, st);
+  if (err != cudaSuccess || g.splits == 1) return err;
+  const long long rows = (long long)g.c.total_new * g.q_heads;
+  return launch_kernel(k_attend_join<T>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, true, g);
 }
 
 }  // namespace
@@ -92,9 +765,11 @@ using namespace tr;
 
 extern "C" {
 
-size_t tr_cache_attend_workspace_bytes(const tr_cache *c, int32_t q_heads, int32_t max_new, int32_t max_len) {
-  if (check_cache(c) != TR_OK || q_heads <= 0 || q_heads % c->heads || max_new < 0 || max_len < 0) return 0;
-  return 0;
+size_t tr_cache_attend_workspace_bytes(const tr_cache *c, int32_t q_heads, int32_t window, int32_t max_new,
+                                       int32_t max_len) {
+  if (check_cache(c) != TR_OK || q_heads <= 0 || q_heads % c->heads || window < 0 || max_new < 0 || max_len < 0)
+    return 0;
+  return plan_of(c, q_heads, window, max_new, max_len).total;
 }
 
 tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *o, float *lse, float scale,
@@ -106,8 +781,11 @@ tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *
   if ((rc = check_heads(q, 2)) != TR_OK || (rc = check_heads(o, 2)) != TR_OK) return rc;
   if (q->heads != o->heads || q->heads % c->heads) return TR_ERR_ARG;
   if (reinterpret_cast<uintptr_t>(lse) & 3u) return TR_ERR_ALIGN;
-  if ((long long)c->total_new * q->heads > INT_MAX) return TR_ERR_UNSUPPORTED;
+  if ((long long)c->total_new * q->heads > INT_MAX - 65536) return TR_ERR_UNSUPPORTED;
+  if (c->heads > 65535) return TR_ERR_UNSUPPORTED;
   if (c->total_new == 0 || c->batch == 0) return TR_OK;
+  const Plan p = plan_of(c, q->heads, window, max_new, max_len);
+  if (p.total && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < p.total)) return TR_ERR_WORKSPACE;
   AttendArgs g{};
   g.c = cache_view(c);
   g.q = static_cast<const char *>(q->p);
@@ -116,14 +794,27 @@ tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *
   g.o_tok = o->token_stride, g.o_head = o->head_stride;
   g.q_heads = q->heads, g.group = q->heads / c->heads;
   g.lse = lse;
-  g.scale = scale;
+  // A zero scale becomes a factor too small to matter: -inf marks masked
+  // scores, and -inf * 0 would be NaN.
+  g.scale = fmaxf(fabsf(scale) * 1.44269504088896341f, 1e-30f);
+  g.negate = scale < 0.f;
   g.causal = causal, g.window = window;
+  g.splits = p.splits;
+  g.part = static_cast<float *>(ws);
+  g.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.part_ml);
   g.err = d_error;
-  const int grid = (int)(((long long)c->total_new * q->heads + 3) / 4);
+  CUtensorMap mk{}, mv{};
+  const long long rows = (long long)c->pages * c->heads * c->page;
+  const int box = c->page < kTile ? c->page : kTile;
+  const CUtensorMapDataType type =
+      c->dtype == TR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  // an empty cache keeps one row in the maps' extents: no page id is valid, so nothing reads it
+  if (!make_map(&mk, c->k, rows > 0 ? rows : 1, c->head_dim, box, 64, CU_TENSOR_MAP_SWIZZLE_128B, type) ||
+      !make_map(&mv, c->v, rows > 0 ? rows : 1, c->head_dim, box, 64, CU_TENSOR_MAP_SWIZZLE_128B, type))
+    return TR_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t err = c->dtype == TR_BF16
-                              ? launch_kernel(k_attend_rows<__nv_bfloat16>, dim3(grid), dim3(128), 0, st, false, g)
-                              : launch_kernel(k_attend_rows<__half>, dim3(grid), dim3(128), 0, st, false, g);
+  const cudaError_t err =
+      c->dtype == TR_BF16 ? launch_attend<__nv_bfloat16>(mk, mv, g, p, st) : launch_attend<__half>(mk, mv, g, p, st);
   return err == cudaSuccess ? TR_OK : TR_ERR_CUDA;
 }
 

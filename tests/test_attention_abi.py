@@ -147,7 +147,7 @@ def test_attend_refusals(lib):
     assert call(window=-1) == ARG
     assert call(max_new=-1) == ARG
     assert call(max_len=-1) == ARG
-    assert lib.tr_cache_attend_workspace_bytes(_cache(page=5), 28, 1, 100) == 0
+    assert lib.tr_cache_attend_workspace_bytes(_cache(page=5), 28, 0, 1, 100) == 0
 
 
 def test_binding_refuses_before_the_library(lib):
