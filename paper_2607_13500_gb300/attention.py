@@ -10,53 +10,103 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 from dataclasses import dataclass
 
 import torch
 
-from ._lib import TR_BF16, TR_F16, TR_F32, TR_ROTARY_LAYOUT, TrCache, TrHeads, TrRotary, check, load
+from . import _lib
+from ._lib import TR_BF16, TR_F16, TR_F32, TR_ROTARY_LAYOUT, check, load
 
 _CODES = {torch.bfloat16: TR_BF16, torch.float16: TR_F16, torch.float32: TR_F32}
-_byref = ctypes.byref
+
+# The C structs are packed with struct.Struct and passed as bytes through
+# function objects of their own (void pointers throughout): a call on one
+# token takes the GPU two or three microseconds, so what the binding spends
+# per argument counts.
+_pack_heads = struct.Struct("@Pqqi0q").pack           # tr_heads
+_pack_rotary = struct.Struct("@PPiiii").pack          # tr_rotary
+_pack_cache = struct.Struct("@PPiiiiiPiiPPi0q").pack  # tr_cache
+assert len(_pack_heads(0, 0, 0, 0)) == ctypes.sizeof(_lib.TrHeads)
+assert len(_pack_rotary(0, 0, 0, 0, 0, 0)) == ctypes.sizeof(_lib.TrRotary)
+assert len(_pack_cache(*([0] * 13))) == ctypes.sizeof(_lib.TrCache)
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+class _Calls:
+    """The library's attention entry points with raw argument types."""
+
+    def __init__(self, lib):
+        for name in ("tr_rotary_apply", "tr_rotary_backward", "tr_rotary_backward_workspace_bytes", "tr_cache_append",
+                     "tr_cache_attend", "tr_cache_attend_workspace_bytes"):
+            known, fn = getattr(lib, name), lib[name]  # indexing gives a function object of our own
+            fn.argtypes = [a if a in (ctypes.c_int32, ctypes.c_float, ctypes.c_size_t) else ctypes.c_void_p
+                           for a in known.argtypes]
+            fn.restype = known.restype
+            setattr(self, name[3:], fn)
 
 
-def _heads(t, name, tokens, heads, d, dtype, device):
-    """A [tokens, heads, d] tensor (its channels contiguous) as a tr_heads."""
-    if t.dim() != 3 or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be a {dtype} tensor [tokens, heads, {d}] on {device}")
-    shape, stride = t.shape, t.stride()
-    if shape[0] != tokens or (heads is not None and shape[1] != heads) or shape[2] != d:
-        raise ValueError(f"{name} must be [{tokens}, {'heads' if heads is None else heads}, {d}], not {tuple(shape)}")
-    if stride[2] != 1 and d > 1:
+_calls = None
+
+
+def _library():
+    global _calls
+    lib = load()
+    if _calls is None or _calls.lib is not lib:
+        _calls = _Calls(lib)
+        _calls.lib = lib
+    return _calls
+
+
+def _device(device):
+    dev = torch.device(device)
+    if dev.type != "cuda":
+        raise ValueError("a CUDA device is needed (libtr has no CPU path)")
+    return torch.device("cuda", torch.cuda.current_device()) if dev.index is None else dev
+
+
+try:  # the raw handle without a Stream object around it
+    from torch._C import _cuda_getCurrentRawStream as _stream
+except ImportError:
+    def _stream(index):
+        return torch.cuda.current_stream(index).cuda_stream
+
+
+def _heads(t, name, tokens, heads, d, dtype, index):
+    """A [tokens, heads, d] tensor (its channels contiguous) on CUDA device
+    `index` as a tr_heads; heads None: any number."""
+    shape = t.shape
+    if (len(shape) != 3 or shape[0] != tokens or shape[2] != d or t.dtype is not dtype or t.get_device() != index
+            or (heads is not None and shape[1] != heads)):
+        raise ValueError(f"{name} must be {dtype} [{tokens}, {'heads' if heads is None else heads}, {d}] on CUDA device "
+                         f"{index}, not {t.dtype} {list(shape)} on {t.device}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and d > 1:
         raise ValueError(f"{name}'s channels must be contiguous")
-    return TrHeads(t.data_ptr(), stride[0], stride[1], shape[1])
+    return _pack_heads(t.data_ptr(), s0, s1, shape[1])
 
 
-def _vector(t, name, d, device):
+def _vector(t, name, d, index):
     """An fp32 [d] device vector's address (None passes)."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.shape != (d,) or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous fp32 tensor [{d}] on {device}")
+    if t.dtype is not torch.float32 or t.shape != (d,) or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous fp32 tensor [{d}] on CUDA device {index}")
     return t.data_ptr()
 
 
-def _ints(t, name, shape, device):
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+def _ints(t, name, shape, index):
+    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on CUDA device {index}")
     return t.data_ptr()
 
 
-def _out(t, like, name):
-    if t is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
-    if t.shape != like.shape:
-        raise ValueError(f"{name} must have the shape {tuple(like.shape)}")
-    return t
+def _output(out, like, name, index):
+    """`out`, or a new contiguous tensor like `like`, with its tr_heads."""
+    t, h, d = like.shape
+    if out is None:
+        out = torch.empty((t, h, d), dtype=like.dtype, device=like.device)
+        return out, _pack_heads(out.data_ptr(), h * d, d, h)
+    return out, _heads(out, name, t, h, d, like.dtype, index)
 
 
 @dataclass
@@ -79,12 +129,10 @@ class Rotary:
     2 i + 1).  Positions are int32 and may be of any size and sign."""
 
     def __init__(self, head_dim, device, base=10000.0, rot_dim=None, sections=None, layout="half", inv_freq=None):
-        lib = self.lib = load()
-        self.device = torch.device(device)
-        if self.device.type != "cuda":
-            raise ValueError("Rotary needs a CUDA device (libtr has no CPU path)")
-        if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
+        lib = load()
+        self.calls = _library()
+        self.device = _device(device)
+        self.index = self.device.index
         if layout not in TR_ROTARY_LAYOUT:
             raise ValueError(f"layout must be one of {sorted(TR_ROTARY_LAYOUT)}")
         self.head_dim, self.rot_dim = int(head_dim), int(head_dim if rot_dim is None else rot_dim)
@@ -100,14 +148,13 @@ class Rotary:
         self.turns = torch.tensor(signed, dtype=torch.int64, device=self.device)
         self.axis = torch.tensor([a for a, n in enumerate(sections) for _ in range(n)] or [0], dtype=torch.int32,
                                  device=self.device)
-        self._s = TrRotary(self.turns.data_ptr(), self.axis.data_ptr(), self.head_dim, self.rot_dim, self.axes,
-                           TR_ROTARY_LAYOUT[layout])
-        self._ref = _byref(self._s)
+        self._struct = _pack_rotary(self.turns.data_ptr(), self.axis.data_ptr(), self.head_dim, self.rot_dim, self.axes,
+                                    TR_ROTARY_LAYOUT[layout])
 
     def _pos(self, pos, tokens):
-        if pos.dim() == 1 and self.axes == 1:
-            return _ints(pos, "pos", (tokens,), self.device)
-        return _ints(pos, "pos", (self.axes, tokens), self.device)
+        if self.axes == 1 and pos.dim() == 1:
+            return _ints(pos, "pos", (tokens,), self.index)
+        return _ints(pos, "pos", (self.axes, tokens), self.index)
 
     def apply(self, q, k, pos, q_weight=None, k_weight=None, eps=1e-6, q_out=None, k_out=None):
         """rotate(norm(q)), rotate(norm(k)) for q [T, q heads, head_dim] and k
@@ -115,64 +162,62 @@ class Rotary:
         channels; ``pos`` int32 [axes, T].  A head is normed where its fp32
         [head_dim] weight is given.  ``q_out`` / ``k_out`` may be q / k
         themselves.  Returns (q_out, k_out)."""
-        code = _CODES.get(q.dtype)
+        dt, i, d = q.dtype, self.index, self.head_dim
+        code = _CODES.get(dt)
         if code is None:
             raise TypeError("q must be bf16, fp16 or fp32")
-        t, d, dev = q.shape[0], self.head_dim, self.device
-        hq = _heads(q, "q", t, None, d, q.dtype, dev)
+        t = q.shape[0]
+        hq = _heads(q, "q", t, None, d, dt, i)
         p = self._pos(pos, t)
-        qo = _out(q_out, q, "q_out")
-        hqo = _heads(qo, "q_out", t, hq.heads, d, q.dtype, dev)
-        hk = hko = ko = None
+        q_out, hqo = _output(q_out, q, "q_out", i)
+        hk = hko = None
         if k is not None:
-            hk = _heads(k, "k", t, None, d, q.dtype, dev)
-            ko = _out(k_out, k, "k_out")
-            hko = _heads(ko, "k_out", t, hk.heads, d, q.dtype, dev)
-        if t == 0:
-            return qo, ko
-        check("tr_rotary_apply", self.lib.tr_rotary_apply(
-            self._ref, code, t, p, hq, _vector(q_weight, "q_weight", d, dev), hqo, hk,
-            _vector(k_weight, "k_weight", d, dev), hko, eps, _stream(dev)))
-        return qo, ko
+            hk = _heads(k, "k", t, None, d, dt, i)
+            k_out, hko = _output(k_out, k, "k_out", i)
+        wq, wk = _vector(q_weight, "q_weight", d, i), _vector(k_weight, "k_weight", d, i)
+        if t:
+            rc = self.calls.rotary_apply(self._struct, code, t, p, hq, wq, hqo, hk, wk, hko, eps, _stream(i))
+            if rc:
+                check("tr_rotary_apply", rc)
+        return q_out, k_out
 
     def backward(self, dq, dk, pos, q=None, k=None, q_weight=None, k_weight=None, eps=1e-6) -> RotaryGrads:
         """Gradients of ``apply`` from those of its outputs (tr_rotary_backward);
         the forward inputs q and k are needed where their weight was given."""
-        code = _CODES.get(dq.dtype)
+        dt, i, d = dq.dtype, self.index, self.head_dim
+        code = _CODES.get(dt)
         if code is None:
             raise TypeError("dq must be bf16, fp16 or fp32")
-        t, d, dev = dq.shape[0], self.head_dim, self.device
-        hdq = _heads(dq, "dq", t, None, d, dq.dtype, dev)
+        t = dq.shape[0]
+        hdq = _heads(dq, "dq", t, None, d, dt, i)
         p = self._pos(pos, t)
-        gq = torch.empty(dq.shape, dtype=dq.dtype, device=dev)
-        hgq = _heads(gq, "dq", t, hdq.heads, d, dq.dtype, dev)
-        hq = hk = hdk = hgk = gk = wq = wk = None
+        gq, hgq = _output(None, dq, "dq", i)
+        hq = hk = hdk = hgk = gk = wq = wk = ws = None
         if q_weight is not None:
             if q is None:
                 raise ValueError("q (the forward input) is needed for the gradient through its norm")
-            hq = _heads(q, "q", t, hdq.heads, d, dq.dtype, dev)
-            wq = torch.empty(d, dtype=torch.float32, device=dev)
+            hq = _heads(q, "q", t, dq.shape[1], d, dt, i)
+            wq = torch.empty(d, dtype=torch.float32, device=self.device)
         if dk is not None:
-            hdk = _heads(dk, "dk", t, None, d, dq.dtype, dev)
-            gk = torch.empty(dk.shape, dtype=dq.dtype, device=dev)
-            hgk = _heads(gk, "dk", t, hdk.heads, d, dq.dtype, dev)
+            hdk = _heads(dk, "dk", t, None, d, dt, i)
+            gk, hgk = _output(None, dk, "dk", i)
         if k_weight is not None:
             if dk is None or k is None:
                 raise ValueError("dk and k (the forward input) are needed for the gradient through the keys' norm")
-            hk = _heads(k, "k", t, hdk.heads, d, dq.dtype, dev)
-            wk = torch.empty(d, dtype=torch.float32, device=dev)
-        if t == 0:
+            hk = _heads(k, "k", t, dk.shape[1], d, dt, i)
+            wk = torch.empty(d, dtype=torch.float32, device=self.device)
+        pq, pk = _vector(q_weight, "q_weight", d, i), _vector(k_weight, "k_weight", d, i)
+        if t == 0:  # empty sums
             return RotaryGrads(gq, gk, None if wq is None else wq.zero_(), None if wk is None else wk.zero_())
-        ws = ws_ptr = None
         nbytes = 0
         if wq is not None or wk is not None:
-            nbytes = self.lib.tr_rotary_backward_workspace_bytes(self._ref, t)
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-            ws_ptr = ws.data_ptr()
-        check("tr_rotary_backward", self.lib.tr_rotary_backward(
-            self._ref, code, t, p, hdq, hq, _vector(q_weight, "q_weight", d, dev), hgq,
-            None if wq is None else wq.data_ptr(), hdk, hk, _vector(k_weight, "k_weight", d, dev), hgk,
-            None if wk is None else wk.data_ptr(), eps, ws_ptr, nbytes, _stream(dev)))
+            nbytes = self.calls.rotary_backward_workspace_bytes(self._struct, t)
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        ptr = lambda x: None if x is None else x.data_ptr()
+        rc = self.calls.rotary_backward(self._struct, code, t, p, hdq, hq, pq, hgq, ptr(wq), hdk, hk, pk, hgk, ptr(wk),
+                                        eps, ptr(ws), nbytes, _stream(i))
+        if rc:
+            check("tr_rotary_backward", rc)
         return RotaryGrads(gq, gk, wq, wk)
 
 
@@ -189,16 +234,18 @@ class PagedCache:
     collects TR_CACHE_ERR_PAGE / TR_CACHE_ERR_WAIT."""
 
     def __init__(self, k, v):
-        self.lib = load()
+        self.calls = _library()
         if k.device.type != "cuda" or v.device != k.device:
             raise ValueError("the cache must live on one CUDA device (libtr has no CPU path)")
         if k.dtype not in (torch.bfloat16, torch.float16) or v.dtype != k.dtype:
             raise TypeError("the cache must be bf16 or fp16")
         if k.dim() != 4 or v.shape != k.shape or not k.is_contiguous() or not v.is_contiguous():
             raise ValueError("k and v must be contiguous [pages, heads, page, head_dim]")
-        self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
+        self.k, self.v, self.device, self.dtype, self.index = k, v, k.device, k.dtype, k.get_device()
         self.pages, self.heads, self.page, self.head_dim = k.shape
         self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._fixed = (k.data_ptr(), v.data_ptr(), _CODES[k.dtype], *k.shape)
+        self._sizes = {}  # workspace bytes by the sizes they follow from
 
     @classmethod
     def empty(cls, pages, heads, page, head_dim, dtype=torch.bfloat16, device="cuda"):
@@ -207,12 +254,11 @@ class PagedCache:
         return cls(mk(), mk())
 
     def _struct(self, table, lens, cu_new, tokens):
-        dev, batch = self.device, lens.shape[0]
-        if table.dim() != 2:
-            raise ValueError("table must be [batch, max_pages]")
-        return TrCache(self.k.data_ptr(), self.v.data_ptr(), _CODES[self.dtype], self.pages, self.heads, self.page,
-                       self.head_dim, _ints(table, "table", (batch, table.shape[1]), dev), batch, table.shape[1],
-                       _ints(lens, "lens", (batch,), dev), _ints(cu_new, "cu_new", (batch + 1,), dev), tokens)
+        i, batch, shape = self.index, lens.shape[0], table.shape
+        if len(shape) != 2 or shape[0] != batch:
+            raise ValueError("table must be [batch, max_pages], lens [batch]")
+        return _pack_cache(*self._fixed, _ints(table, "table", shape, i), batch, shape[1],
+                           _ints(lens, "lens", (batch,), i), _ints(cu_new, "cu_new", (batch + 1,), i), tokens)
 
     def append(self, k, v, table, lens, cu_new, rotary=None, pos=None, k_weight=None, q=None, q_weight=None,
                q_out=None, eps=1e-6):
@@ -221,24 +267,23 @@ class PagedCache:
         Rotary, with ``pos``) and ``k_weight`` are optional.  ``q`` [T, q
         heads, head_dim], when given, is normed and rotated in the same
         launch; returns it (``q_out``, which may be q), else None."""
-        t, d, dev, dt = k.shape[0], self.head_dim, self.device, self.dtype
+        t, d, i, dt = k.shape[0], self.head_dim, self.index, self.dtype
         c = self._struct(table, lens, cu_new, t)
-        hk, hv = _heads(k, "k", t, self.heads, d, dt, dev), _heads(v, "v", t, self.heads, d, dt, dev)
+        hk, hv = _heads(k, "k", t, self.heads, d, dt, i), _heads(v, "v", t, self.heads, d, dt, i)
         r = p = hq = hqo = None
         if rotary is not None:
-            if rotary.device != dev or pos is None:
+            if rotary.index != i or pos is None:
                 raise ValueError("rotary must live on the cache's device and needs pos")
-            r, p = rotary._ref, rotary._pos(pos, t)
+            r, p = rotary._struct, rotary._pos(pos, t)
         if q is not None:
-            hq = _heads(q, "q", t, None, d, dt, dev)
-            q_out = _out(q_out, q, "q_out")
-            hqo = _heads(q_out, "q_out", t, hq.heads, d, dt, dev)
-        if t == 0:
-            return q_out if q is not None else None
-        check("tr_cache_append", self.lib.tr_cache_append(
-            c, hk, hv, r, p, _vector(k_weight, "k_weight", d, dev), hq, _vector(q_weight, "q_weight", d, dev), hqo,
-            eps, self.error.data_ptr(), _stream(dev)))
-        return q_out if q is not None else None
+            hq = _heads(q, "q", t, None, d, dt, i)
+            q_out, hqo = _output(q_out, q, "q_out", i)
+        wq, wk = _vector(q_weight, "q_weight", d, i), _vector(k_weight, "k_weight", d, i)
+        if t:
+            rc = self.calls.cache_append(c, hk, hv, r, p, wk, hq, wq, hqo, eps, self.error.data_ptr(), _stream(i))
+            if rc:
+                check("tr_cache_append", rc)
+        return None if q is None else q_out
 
     def attend(self, q, table, lens, cu_new, scale=None, causal=True, window=0, max_new=None, max_len=None, out=None,
                return_lse=False):
@@ -249,20 +294,29 @@ class PagedCache:
         host knows of a sequence's new tokens and length at most, only choose
         the launch (defaults: all T, and what the table can hold).  Returns
         out, or (out, lse fp32 [T, q heads])."""
-        t, d, dev = q.shape[0], self.head_dim, self.device
+        t, d, i = q.shape[0], self.head_dim, self.index
         c = self._struct(table, lens, cu_new, t)
-        hq = _heads(q, "q", t, None, d, self.dtype, dev)
-        out = _out(out, q, "out")
-        ho = _heads(out, "out", t, hq.heads, d, self.dtype, dev)
-        lse = torch.empty(t, hq.heads, dtype=torch.float32, device=dev) if return_lse else None
-        if t == 0:
-            return (out, lse) if return_lse else out
-        max_new = t if max_new is None else int(max_new)
-        max_len = table.shape[1] * self.page if max_len is None else int(max_len)
-        nbytes = self.lib.tr_cache_attend_workspace_bytes(c, hq.heads, window, max_new, max_len)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        check("tr_cache_attend", self.lib.tr_cache_attend(
-            c, hq, ho, None if lse is None else lse.data_ptr(), 1.0 / math.sqrt(d) if scale is None else scale,
-            1 if causal else 0, window, max_new, max_len, None if ws is None else ws.data_ptr(), nbytes,
-            self.error.data_ptr(), _stream(dev)))
+        hq = _heads(q, "q", t, None, d, self.dtype, i)
+        out, ho = _output(out, q, "out", i)
+        heads = q.shape[1]
+        lse = torch.empty((t, heads), dtype=torch.float32, device=self.device) if return_lse else None
+        if t:
+            if max_new is None:
+                max_new = t
+            if max_len is None:
+                max_len = min(table.shape[1] * self.page, 2 ** 31 - 1)
+            key = (t, lens.shape[0], table.shape[1], heads, window, max_new, max_len)
+            nbytes = self._sizes.get(key)
+            if nbytes is None:
+                if len(self._sizes) >= 4096:
+                    self._sizes.clear()
+                nbytes = self.calls.cache_attend_workspace_bytes(c, heads, window, max_new, max_len)
+                self._sizes[key] = nbytes
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
+            rc = self.calls.cache_attend(
+                c, hq, ho, None if lse is None else lse.data_ptr(), 1.0 / math.sqrt(d) if scale is None else scale,
+                1 if causal else 0, window, max_new, max_len, None if ws is None else ws.data_ptr(), nbytes,
+                self.error.data_ptr(), _stream(i))
+            if rc:
+                check("tr_cache_attend", rc)
         return (out, lse) if return_lse else out

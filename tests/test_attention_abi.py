@@ -157,12 +157,14 @@ def test_binding_refuses_before_the_library(lib):
     with pytest.raises(ValueError, match="CUDA"):
         altr.PagedCache(torch.zeros(2, 1, 16, 64), torch.zeros(2, 1, 16, 64))
     from paper_2607_13500_gb300 import attention
-    cpu = torch.device("cpu")
+    cpu = -1  # the device index of host tensors
     x = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
-    h = attention._heads(x[:, 1:3], "q", 3, 2, 64, torch.bfloat16, cpu)
+    h = _lib.TrHeads.from_buffer_copy(attention._heads(x[:, 1:3], "q", 3, 2, 64, torch.bfloat16, cpu))
     assert (h.token_stride, h.head_stride, h.heads) == (256, 64, 2) and h.p == x.data_ptr() + 128
+    with pytest.raises(ValueError, match="q must"):  # on another device
+        attention._heads(x, "q", 3, None, 64, torch.bfloat16, 0)
     for bad in (x[0], x.float(), x[:2], x[..., :32], x.transpose(1, 2)):
-        with pytest.raises(ValueError, match="q must|channels"):
+        with pytest.raises(ValueError, match="q must"):
             attention._heads(bad, "q", 3, None, 64, torch.bfloat16, cpu)
     with pytest.raises(ValueError, match="channels"):
         attention._heads(torch.zeros(3, 64, 4, dtype=torch.bfloat16).transpose(1, 2), "q", 3, 4, 64, torch.bfloat16,
@@ -172,3 +174,8 @@ def test_binding_refuses_before_the_library(lib):
             attention._ints(bad, "lens", (4,), cpu)
     with pytest.raises(ValueError, match="weight must"):
         attention._vector(torch.zeros(64, dtype=torch.bfloat16), "weight", 64, cpu)
+    # the packed structs are the C structs
+    c = _lib.TrCache.from_buffer_copy(attention._pack_cache(1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13))
+    assert [getattr(c, n) for n, _ in c._fields_] == list(range(1, 14))
+    r = _lib.TrRotary.from_buffer_copy(attention._pack_rotary(1, 2, 3, 4, 5, 6))
+    assert [getattr(r, n) for n, _ in r._fields_] == list(range(1, 7))
