@@ -36,30 +36,12 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "tr_cache.cuh"
-#include "tr_map.cuh"
-#include "tr_tc.cuh"
+#include "tr_attend.cuh"
 
 namespace tr {
 namespace {
 
-constexpr int kTile = 128;  // keys of a tile, rows of a block
-
-struct AttendArgs {
-  CacheView c;
-  const char *q;
-  char *o;
-  long long q_tok, q_head, o_tok, o_head;  // elements
-  int q_heads, group;                      // group: query heads of a key head
-  float *lse;
-  float scale;      // |scale| log2(e), never zero
-  int negate;       // scale < 0: the queries enter negated
-  int causal, window;
-  int splits;       // parts of the key range, each a CTA's
-  float *part;      // splits > 1: [splits][total_new * q_heads][d] unnormalised sums,
-  float2 *part_ml;  //             [splits][total_new * q_heads] (maximum, sum)
-  int32_t *err;
-};
+using namespace attend;
 
 template <int D, int MT>
 struct Shape {
@@ -77,32 +59,6 @@ struct Shape {
   static_assert(kStages >= 4, "two tiles in use and two on their way");
 };
 
-template <typename T>
-struct Bits;
-template <>
-struct Bits<__nv_bfloat16> {
-  static constexpr bool kBf16 = true;
-  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-  }
-};
-template <>
-struct Bits<__half> {
-  static constexpr bool kBf16 = false;
-  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-  }
-};
-
-__device__ __forceinline__ float exp2_fast(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 __device__ __forceinline__ unsigned long long pair_of(float a, float b) {
   unsigned long long r;
   asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
@@ -122,126 +78,6 @@ __device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigne
   unsigned long long r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
-}
-
-// ---------------------------------------------------------------- where a CTA works
-// Sequence b's row blocks occupy the slots from floor(cu_new[b] group / R) + b
-// on (R rows a block), which leaves room for all of them whatever cu_new
-// holds; the last slot of a sequence may stay empty.
-struct Block {
-  int seq, first;     // sequence, first row (token * group + head) of the block
-  int rows;           // rows of the sequence: new tokens * group
-  int tok0;           // first new token of the sequence
-  int base;           // key of new token 0
-  int len;            // keys of the sequence
-};
-
-// All lanes of a warp together; seq = -1 for an empty slot.
-__device__ __forceinline__ Block find_block(const AttendArgs &g, int slot, int rows_per_block) {
-  const int lane = threadIdx.x & 31;
-  const CacheView &c = g.c;
-  int b = 0;  // sequences whose slots start at or before this one, less one
-  for (int i0 = 0; i0 < c.batch; i0 += 32) {
-    const int i = i0 + lane;
-    const bool before =
-        i < c.batch && ((long long)__ldg(c.cu_new + i) * g.group) / rows_per_block + i <= (long long)slot;
-    const unsigned m = __ballot_sync(0xffffffffu, before);
-    b += __popc(m);
-    if (m != 0xffffffffu) break;
-  }
-  b -= 1;
-  Block k;
-  k.seq = -1;
-  k.rows = k.first = k.tok0 = k.base = k.len = 0;
-  if (b < 0) return k;
-  const int t0 = __ldg(c.cu_new + b), t1 = min(__ldg(c.cu_new + b + 1), c.total_new);
-  const int n = t1 > t0 ? t1 - t0 : 0;
-  const long long start = ((long long)t0 * g.group) / rows_per_block + b;
-  k.first = (int)((slot - start) * rows_per_block);
-  k.rows = n * g.group;
-  if (t0 < 0 || k.first < 0 || k.first >= k.rows) return k;
-  k.seq = b;
-  k.tok0 = t0;
-  k.len = cache_len(c, b);
-  k.base = max(__ldg(c.lens + b), 0) - n;
-  return k;
-}
-
-// First key of the window that ends with key `own`.
-__device__ __forceinline__ int window_start(int own, int window) { return own >= window ? own - window + 1 : 0; }
-
-// Keys [lo, hi) that some row of [r0, r1) sees.
-struct Range {
-  int lo, hi;
-};
-__device__ __forceinline__ Range keys_of_rows(const AttendArgs &g, const Block &k, int r0, int r1) {
-  Range r{0, 0};
-  if (r0 >= r1) return r;
-  r.hi = g.causal ? min(k.len, k.base + (r1 - 1) / g.group + 1) : k.len;
-  r.lo = g.window > 0 ? window_start(k.base + r0 / g.group, g.window) : 0;
-  if (r.hi <= r.lo) r.lo = r.hi = 0;
-  return r;
-}
-
-// One row by one warp on the plain cores, four channels a lane: the running
-// maximum (powers of two), sum and weighted values over the keys [lo, hi).
-template <typename T>
-__device__ __forceinline__ float4 load4(const char *p) {
-  const uint2 v = *reinterpret_cast<const uint2 *>(p);
-  const T *h = reinterpret_cast<const T *>(&v);
-  return make_float4((float)h[0], (float)h[1], (float)h[2], (float)h[3]);
-}
-__device__ __forceinline__ bool finite4(const float4 &v) {
-  return fabsf(v.x) <= FLT_MAX && fabsf(v.y) <= FLT_MAX && fabsf(v.z) <= FLT_MAX && fabsf(v.w) <= FLT_MAX;
-}
-template <typename T>
-__device__ __noinline__ bool hidden_values_finite(const AttendArgs &g, int seq, int hk, int lo, int hi) {
-  const int ch = 4 * (threadIdx.x & 31);
-  bool ok = true;
-  for (int j = lo; j < hi; ++j) {
-    const int page = page_of(g.c, seq, j);
-    if (page >= 0 && ch < g.c.d)
-      ok &= finite4(load4<T>(static_cast<const char *>(g.c.v) +
-                             2 * ((((long long)page * g.c.heads + hk) * g.c.page + (j & (g.c.page - 1))) * g.c.d + ch)));
-  }
-  return __all_sync(0xffffffffu, ok);
-}
-template <typename T>
-__device__ __noinline__ float4 row_by_warp(const AttendArgs &g, int seq, int hk, const char *q, int lo, int hi, float &m,
-                                           float &l) {
-  const int d = g.c.d, ch = 4 * (threadIdx.x & 31);
-  const bool holds = ch < d;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f), acc = x;
-  if (holds) x = load4<T>(q + 2 * ch);
-  const float sc = g.negate ? -g.scale : g.scale;
-  m = -INFINITY;
-  l = 0.f;
-  for (int j = lo; j < hi; ++j) {
-    const int page = page_of(g.c, seq, j);
-    float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-    if (page >= 0 && holds) {
-      const long long off = 2 * ((((long long)page * g.c.heads + hk) * g.c.page + (j & (g.c.page - 1))) * d + ch);
-      k = load4<T>(static_cast<const char *>(g.c.k) + off);
-      v = load4<T>(static_cast<const char *>(g.c.v) + off);
-    }
-    float s = x.x * k.x + x.y * k.y + x.z * k.z + x.w * k.w;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    s *= sc;
-    const float mn = fmaxf(m, s);
-    const float f = m == mn ? 1.f : exp2_fast(m - mn), p = s == -INFINITY ? 0.f : exp2_fast(s - mn);
-    m = mn;
-    l = l * f + p;
-    acc.x = acc.x * f + p * v.x;
-    acc.y = acc.y * f + p * v.y;
-    acc.z = acc.z * f + p * v.z;
-    acc.w = acc.w * f + p * v.w;
-  }
-  return acc;
-}
-
-__device__ __forceinline__ void flag(const AttendArgs &g, int bit) {
-  if (g.err) atomicOr(g.err, bit);
 }
 
 // ---------------------------------------------------------------- the kernel
@@ -324,59 +160,12 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
 
   if (warp == 4 * MT) {
     // ---------------------------------------------------------------- TMA producer
-    const int page = g.c.page, piece = page < kTile ? page : kTile;  // keys of one load
-    const int none = max(1, g.c.pages * g.c.heads * page);           // a row past the cache: reads as zeros
-    int stage = 0;
-    uint32_t phase = 0, tails = 0, filled = 0, parity = 0;
+    TileRing<D, S::kStages> tiles;
+    tiles.base = ring, tiles.full0 = full(0), tiles.empty0 = empty(0), tiles.tail = tail;
     bool ok = true;
-    for (int t = t0; t < t1 && ok; ++t) {
-      const int key0 = t * kTile, left = min(k.len - key0, kTile);
-      const int pieces = (left + piece - 1) / piece;
-      // lane: (half, piece) of the tile; its page's first row
-      const int pc = lane % (kTile / piece), half = lane / (kTile / piece);
-      const bool mine = pc < pieces && half < S::kHalves;
-      int row = none;
-      if (mine) {
-        const int key = key0 + pc * piece, id = page_of(g.c, k.seq, key);
-        if (id >= 0) row = (id * g.c.heads + hk) * page + (key & (page - 1));
-        else flag(g, TR_CACHE_ERR_PAGE);
-      }
-      const uint32_t bytes = (uint32_t)pieces * piece * 128u * S::kHalves;
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        if (!tc::mbar_wait_warp(empty(stage), phase ^ 1u)) {
-          ok = false;
-          break;
-        }
-        const uint32_t dst = ring + stage * S::kTileBytes;
-        const bool cut = kv == 1 && left < kTile;  // the sequence ends inside this value tile
-        const uint32_t bar = cut ? tail : full(stage);
-        if (lane == 0) tc::mbar_expect_tx(bar, bytes);
-        __syncwarp();
-        if (mine) tc::tma_load_2d(dst + half * (kTile * 128) + pc * piece * 128, kv ? &map_v : &map_k, half * 64, row, bar);
-        if (cut) {
-          if (!tc::mbar_wait(tail, tails)) ok = false;
-          ok = __all_sync(0xffffffffu, ok);
-          tails ^= 1u;
-          for (int i = lane + left * 8; i < kTile * 8; i += 32)
-#pragma unroll
-            for (int h = 0; h < S::kHalves; ++h) tc::st_shared_v4(dst + h * (kTile * 128) + i * 16, 0, 0, 0, 0);
-          tc::fence_async_shared();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(full(stage));
-        }
-        filled |= 1u << stage;
-        parity = (parity & ~(1u << stage)) | (phase << stage);
-        if (++stage == S::kStages) {
-          stage = 0;
-          phase ^= 1u;
-        }
-      }
-    }
+    for (int t = t0; t < t1 && ok; ++t) ok = tiles.load(g, &map_k, &map_v, k.seq, k.len, hk, t);
     if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
-    // the loads already issued land before the CTA may exit
-    for (int s = 0; s < S::kStages; ++s)
-      if (filled >> s & 1u) tc::mbar_wait_warp(full(s), parity >> s & 1u);
+    tiles.drain();
   } else if (warp == 4 * MT + 1) {
     // ---------------------------------------------------------------- MMA issuer
     if (lane == 0) {
@@ -693,19 +482,25 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
 
 // ---------------------------------------------------------------- host side
 struct Plan {
-  int mt, splits, slots;
-  size_t part, part_ml, total;  // workspace
+  bool few;               // tr_attend_few.cu's kernel
+  int mt, splits, slots;  // else k_attend's blocks of 128 mt rows and parts of the keys
+  size_t part_ml, total;  // workspace
 };
 
 Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_len) {
   Plan p{};
   const int group = q_heads / c->heads;
   const long long most = (long long)(max_new < c->total_new ? max_new : c->total_new) * group;
+  const int sms = sm_count() > 0 ? sm_count() : 1;
+  if (most <= kFewRows && c->batch <= kFewMaxBatch) {
+    p.few = true;
+    p.total = few_workspace_bytes(c->head_dim, sms);
+    return p;
+  }
   p.mt = most <= kTile ? 1 : 2;
   const int rows = kTile * p.mt;
   p.slots = (int)((long long)c->total_new * group / rows) + c->batch;
   // Split the keys when the row blocks alone would not fill the GPU.
-  const int sms = sm_count() > 0 ? sm_count() : 1;
   const long long blocks = (long long)p.slots * c->heads;
   const long long cap = (long long)c->max_pages * c->page;
   long long keys = max_len < cap ? max_len : cap;
@@ -813,6 +608,10 @@ tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *
       !make_map(&mv, c->v, rows > 0 ? rows : 1, c->head_dim, box, 64, CU_TENSOR_MAP_SWIZZLE_128B, type))
     return TR_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (p.few) {
+    g.ctas = sm_count();
+    return launch_few(mk, mv, g, c->dtype == TR_BF16, ws, st) == cudaSuccess ? TR_OK : TR_ERR_CUDA;
+  }
   const cudaError_t err =
       c->dtype == TR_BF16 ? launch_attend<__nv_bfloat16>(mk, mv, g, p, st) : launch_attend<__half>(mk, mv, g, p, st);
   return err == cudaSuccess ? TR_OK : TR_ERR_CUDA;

@@ -1,0 +1,548 @@
+// Attention of few rows per key head (single tokens, short drafts) over the
+// paged cache: bound by reading K and V once, so everything serves that.
+//
+// Work is counted in units of one 128-key tile of one key head (and block of
+// 16 rows) and cut into equal shares, one per CTA and one CTA per SM,
+// whatever the sequences' lengths: a share covers a run of tiles that may
+// cross heads and sequences.  The lengths are read on the device, so a
+// captured graph stays balanced as they grow.  An item (block, key head)
+// that lies in one share is finished there; one that is cut leaves a partial
+// (maximum, sum, weighted values) per share, joined by k_few_join.
+//
+// One warp fills the tile ring by TMA; eight warps take 16 keys of each tile
+// and run both products on warp-level tensor-core instructions (m16n8k16)
+// from registers: at up to 16 rows the 128-row tcgen05 shapes would compute
+// mostly padding and put a tensor-memory round trip between the products,
+// while here the scores never leave the registers of the warp.  The order of
+// channels inside a product is free, so each lane takes whole 16-byte chunks
+// of K rows (chunk 2 c + s of lane (g, c): the 128-byte swizzle spreads them
+// over all banks) and the queries are laid out to match; for V a lane takes
+// 8 channels of four keys and pairs keys with byte permutes.
+#include <atomic>
+
+#include "tr_attend.cuh"
+
+namespace tr {
+namespace {
+
+using namespace attend;
+
+constexpr int kWarps = 8;                     // consumer warps: 16 keys of a tile each
+constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kPass = 32;                     // channels joined per pass at an item's end
+
+template <int D>
+struct Few {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kTileBytes = kTile * D * 2;
+  static constexpr int kJoinBytes = kWarps * kFewRows * (kPass + 1) * 4;
+  static constexpr int kFit = (227 * 1024 - 4096 - 1024 - kJoinBytes) / kTileBytes;
+  static constexpr int kStages = kFit < 12 ? kFit : 12;
+  static constexpr size_t kSmem = (size_t)kStages * kTileBytes + kJoinBytes + 1024 + 4096;
+};
+
+// What a sequence brings: its rows and the tiles that some row of it sees.
+struct Seq {
+  int tok0, rows, len, base;
+  int tile0, tiles;  // first tile, tiles
+  int items;         // blocks of rows x key heads
+};
+__device__ __forceinline__ Seq seq_of(const AttendArgs &g, int b) {
+  Seq s{0, 0, 0, 0, 0, 0, 0};
+  if (b >= g.c.batch) return s;
+  const int t0 = __ldg(g.c.cu_new + b), t1 = min(__ldg(g.c.cu_new + b + 1), g.c.total_new);
+  if (t0 < 0 || t1 <= t0) return s;
+  Block k;
+  k.len = cache_len(g.c, b);
+  k.base = max(__ldg(g.c.lens + b), 0) - (t1 - t0);
+  s.tok0 = t0;
+  s.rows = (t1 - t0) * g.group;
+  s.len = k.len;
+  s.base = k.base;
+  const Range r = keys_of_rows(g, k, 0, s.rows);
+  s.tile0 = r.lo / kTile;
+  s.tiles = (r.hi + kTile - 1) / kTile - s.tile0;
+  s.items = (s.rows + kFewRows - 1) / kFewRows * g.c.heads;
+  return s;
+}
+__device__ __forceinline__ long long units_of(const Seq &s) { return (long long)s.items * s.tiles; }
+
+// Units of each run of 32 sequences, left in shared memory by all warps of
+// the CTA together; returns their total.
+__device__ __forceinline__ long long count_units(const AttendArgs &g, long long *runs, int warps) {
+  const int lane = threadIdx.x & 31;
+  const int n = (g.c.batch + 31) / 32;
+  for (int i = threadIdx.x >> 5; i < n; i += warps) {
+    long long u = units_of(seq_of(g, 32 * i + lane));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
+    if (lane == 0) runs[i] = u;
+  }
+  __syncthreads();
+  long long all = 0;
+  for (int i = lane; i < n; i += 32) all += runs[i];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+  return all;
+}
+
+// A walk over the units of a share, item by item; the same in all lanes.
+struct Walk {
+  long long u, end;   // next unit, end of the share
+  long long first;    // first unit of sequence b
+  int b;
+  Seq s;
+  // the current piece
+  int item, tile, count;  // item of the sequence, first tile (absolute), tiles
+  bool whole;             // the piece is the whole item
+  bool inside;            // the item starts after the share does
+
+  __device__ __forceinline__ void seek(const AttendArgs &g, const long long *runs, long long from, long long to) {
+    const int lane = threadIdx.x & 31;
+    u = from;
+    end = to;
+    first = 0;
+    int i = 0;
+    const int n = (g.c.batch + 31) / 32;
+    while (i + 1 < n && u >= first + runs[i]) first += runs[i++];
+    const Seq mine = seq_of(g, 32 * i + lane);
+    long long before = units_of(mine);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long v = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += v;
+    }
+    const int at = max(__ffs(__ballot_sync(0xffffffffu, u < first + before)), 1) - 1;
+    first += __shfl_sync(0xffffffffu, before - units_of(mine), at);
+    b = 32 * i + at;
+    s = seq_of(g, b);
+  }
+  // The next piece; false at the end of the share.
+  __device__ __forceinline__ bool next(const AttendArgs &g, long long share) {
+    if (u >= end) return false;
+    if (u >= first + units_of(s)) {  // on to the next sequence that has units
+      const int lane = threadIdx.x & 31;
+      first += units_of(s);
+      unsigned any = 0;
+      for (int i = b + 1; i < g.c.batch && !any; i += 32) {
+        any = __ballot_sync(0xffffffffu, units_of(seq_of(g, i + lane)) > 0);
+        if (any) b = i + __ffs(any) - 1;
+      }
+      if (!any) return false;
+      s = seq_of(g, b);
+    }
+    if (s.tiles <= 0) return false;
+    const long long rel = u - first;
+    item = (int)(rel / s.tiles);
+    const int t = (int)(rel - (long long)item * s.tiles);
+    const long long left = end - u;
+    count = (long long)(s.tiles - t) < left ? s.tiles - t : (int)left;
+    tile = s.tile0 + t;
+    whole = count == s.tiles;
+    inside = u - t > share;
+    u += count;
+    return true;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  if (Bits<T>::kBf16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+                 "{%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+                 "{%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ void named_sync(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_attend_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                 const __grid_constant__ AttendArgs g) {
+  using F = Few<D>;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ long long runs[kFewMaxBatch / 32];  // units of 32 sequences each
+  __shared__ float top[kWarps][kFewRows], tot[kWarps][kFewRows];
+  __shared__ unsigned bad_rows;
+  const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
+  float *join = reinterpret_cast<float *>(smem_raw + (base - tc::smem_u32(smem_raw)) + F::kStages * F::kTileBytes);
+  const uint32_t bars = tc::smem_u32(join) + F::kJoinBytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  TileRing<D, F::kStages> ring;
+  ring.base = base, ring.full0 = bars, ring.empty0 = bars + 8u * F::kStages, ring.tail = bars + 16u * F::kStages;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < F::kStages; ++s) {
+      tc::mbar_init(ring.full(s), 1);
+      tc::mbar_init(ring.empty(s), kWarps);
+    }
+    tc::mbar_init(ring.tail, 1);
+    tc::mbar_fence_init();
+    tc::tma_prefetch_map(&map_k);
+    tc::tma_prefetch_map(&map_v);
+    bad_rows = 0;
+  }
+  pdl_wait();  // q and the cache come from the kernels before
+  pdl_trigger();
+  const long long all = count_units(g, runs, kWarps + 1);  // (its barrier also publishes the mbarriers)
+  const long long share = all * blockIdx.x / g.ctas, share_end = all * (blockIdx.x + 1) / g.ctas;
+  if (share >= share_end) return;
+  Walk w;
+  w.seek(g, runs, share, share_end);
+
+  if (warp == kWarps) {
+    bool ok = true;
+    while (ok && w.next(g, share)) {
+      const int hk = w.item % g.c.heads;
+      for (int i = 0; i < w.count && ok; ++i) ok = ring.load(g, &map_k, &map_v, w.b, w.s.len, hk, w.tile + i);
+    }
+    if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+    ring.drain();
+    return;
+  }
+
+  // ------------------------------------------------------------------ consumers
+  const int gq = lane >> 2, c = lane & 3;  // quad (row or key of a fragment), lane of the quad
+  int stage = 0;
+  uint32_t phase = 0;
+  bool ok = true;  // once a wait has timed out the warp only keeps up with the others' barriers
+  while (w.next(g, share)) {
+    const int hk = w.item % g.c.heads, block0 = w.item / g.c.heads * kFewRows;
+    const int rows = min(kFewRows, w.s.rows - block0);
+    // this lane's two rows of a fragment, and the keys they see
+    const char *qrow[2];
+    int lo[2], hi[2];
+    uint32_t q[F::kHalves * 2][8];  // [half, chunk parity][row g: 4 words, row g + 8: 4 words]
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = gq + 8 * i, row = block0 + r;
+      const bool valid = r < rows;
+      const int tok = valid ? row / g.group : 0, head = hk * g.group + (valid ? row - tok * g.group : 0);
+      const int own = w.s.base + tok;
+      hi[i] = !valid ? INT_MAX : g.causal ? min(w.s.len, own + 1) : w.s.len;
+      lo[i] = valid && g.window > 0 ? window_start(own, g.window) : 0;
+      qrow[i] = g.q + 2 * ((long long)(w.s.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
+      const uint32_t flip = g.negate ? 0x80008000u : 0u;
+#pragma unroll
+      for (int s = 0; s < F::kHalves * 2; ++s) {
+        const int ch = (s >> 1) * 64 + (2 * c + (s & 1)) * 8;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (valid && ch < g.c.d) {
+          v = *reinterpret_cast<const uint4 *>(qrow[i] + 2 * ch);
+          v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
+        }
+        q[s][4 * i] = v.x, q[s][4 * i + 1] = v.y, q[s][4 * i + 2] = v.z, q[s][4 * i + 3] = v.w;
+      }
+    }
+    float o[F::kHalves][8][4];
+#pragma unroll
+    for (int h = 0; h < F::kHalves; ++h)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[h][i][j] = 0.f;
+    float mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+
+    for (int t = w.tile; ok && t < w.tile + w.count; ++t) {
+      // ---- scores of 16 keys: two products of 8 keys
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(stage), phase));
+      if (!ok) {
+        if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+        break;
+      }
+      const uint32_t kt = base + stage * F::kTileBytes + (uint32_t)(16 * warp) * 128u;
+      float s[2][4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < F::kHalves * 2; ++j) {
+          const uint4 v = lds128(kt + (j >> 1) * (kTile * 128) + (8 * n + gq) * 128 + (((2 * c + (j & 1)) ^ gq) << 4));
+          mma16816<T>(s[n], q[j][0], q[j][4], q[j][1], q[j][5], v.x, v.y);
+          mma16816<T>(s[n], q[j][2], q[j][6], q[j][3], q[j][7], v.z, v.w);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(ring.empty(stage));
+      if (++stage == F::kStages) stage = 0, phase ^= 1u;
+
+      // ---- softmax: s[n][0..1] row g, s[n][2..3] row g + 8, keys 8 n + 2 c and + 1
+      const int key0 = t * kTile + 16 * warp;
+      const bool cut = lo[0] > key0 || hi[0] < key0 + 16 || lo[1] > key0 || hi[1] < key0 + 16;
+      if (__any_sync(0xffffffffu, cut)) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int key = key0 + 8 * n + 2 * c + (j & 1);
+            if (key < lo[j >> 1] || key >= hi[j >> 1]) s[n][j] = -INFINITY;
+          }
+      }
+      float now[2], f[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        now[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1])) * g.scale;
+        now[i] = fmaxf(now[i], __shfl_xor_sync(0xffffffffu, now[i], 1));
+        now[i] = fmaxf(now[i], __shfl_xor_sync(0xffffffffu, now[i], 2));
+      }
+      if (__any_sync(0xffffffffu, now[0] > mx[0] + 8.f || now[1] > mx[1] + 8.f)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const bool up = now[i] > mx[i] + 8.f;
+          f[i] = up ? exp2_fast(mx[i] - now[i]) : 1.f;
+          if (up) mx[i] = now[i];
+          sum[i] *= f[i];
+        }
+#pragma unroll
+        for (int h = 0; h < F::kHalves; ++h)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            o[h][i][0] *= f[0], o[h][i][1] *= f[0];
+            o[h][i][2] *= f[1], o[h][i][3] *= f[1];
+          }
+      }
+      uint32_t p[4];  // the A fragment of the second product
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float neg = mx[i] == -INFINITY ? 0.f : -mx[i];
+          const float p0 = exp2_fast(fmaf(s[n][2 * i], g.scale, neg)), p1 = exp2_fast(fmaf(s[n][2 * i + 1], g.scale, neg));
+          sum[i] += p0 + p1;
+          p[2 * n + i] = Bits<T>::pack(p0, p1);
+        }
+
+      // ---- o += p V: n-tile i of a half holds channels 8 g + i
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(stage), phase));
+      if (!ok) {
+        if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+        break;
+      }
+      const uint32_t vt = base + stage * F::kTileBytes + (uint32_t)(16 * warp) * 128u;
+#pragma unroll
+      for (int h = 0; h < F::kHalves; ++h) {
+        uint4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = 2 * c + (j & 1) + 8 * (j >> 1);
+          v[j] = lds128(vt + h * (kTile * 128) + key * 128 + ((gq ^ (key & 7)) << 4));
+        }
+        const uint32_t *v0 = &v[0].x, *v1 = &v[1].x, *v2 = &v[2].x, *v3 = &v[3].x;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t sel = i & 1 ? 0x7632u : 0x5410u;
+          mma16816<T>(o[h][i], p[0], p[1], p[2], p[3], __byte_perm(v0[i >> 1], v1[i >> 1], sel),
+                      __byte_perm(v2[i >> 1], v3[i >> 1], sel));
+        }
+      }
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(ring.empty(stage));
+      if (++stage == F::kStages) stage = 0, phase ^= 1u;
+    }
+
+    // ------------------------------------------------------------------ the piece's result
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
+      sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+      if (c == 0) top[warp][gq + 8 * i] = mx[i], tot[warp][gq + 8 * i] = sum[i];
+    }
+    named_sync(32 * kWarps);
+    float f[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < kWarps; ++j) m = fmaxf(m, top[j][gq + 8 * i]);
+      f[i] = mx[i] == -INFINITY ? 0.f : exp2_fast(mx[i] - m);
+    }
+    const int part = 2 * blockIdx.x + (w.inside ? 1 : 0);
+    for (int pass = 0; pass < F::kHalves * 2; ++pass) {
+      // half pass / 2, n-tiles 4 (pass & 1) .. + 3: channels 8 k + 4 (pass & 1) .. + 3 for k < 8
+#pragma unroll
+      for (int pp = 0; pp < F::kHalves * 2; ++pp) {
+        if (pp != pass) continue;
+        const int h = pp >> 1, i0 = (pp & 1) * 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            // accumulator column 2 c + (j & 1) of n-tile i0 + i is channel 8 (2 c + (j & 1)) + i0 + i
+            const int col = (2 * c + (j & 1)) * 4 + i;
+            join[(warp * kFewRows + gq + 8 * (j >> 1)) * (kPass + 1) + col] = o[h][i0 + i][j] * f[j >> 1];
+          }
+      }
+      named_sync(32 * kWarps);
+      for (int e = threadIdx.x; e < rows * (kPass / 4); e += 32 * kWarps) {
+        const int r = e / (kPass / 4), q4 = e % (kPass / 4);  // row, channel group 8 q4 + i0 .. + 3
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int j = 0; j < kWarps; ++j) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] += join[(j * kFewRows + r) * (kPass + 1) + 4 * q4 + i];
+          m = fmaxf(m, top[j][r]);
+        }
+#pragma unroll
+        for (int j = 0; j < kWarps; ++j)
+          if (top[j][r] != -INFINITY) l += tot[j][r] * exp2_fast(top[j][r] - m);
+        const int ch = (pass >> 1) * 64 + 8 * q4 + (pass & 1) * 4;
+        if (ch >= g.c.d) continue;
+        const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
+        const long long out = (long long)(w.s.tok0 + tok) * g.q_heads + head;
+        if (!finite4(make_float4(v[0], v[1], v[2], v[3]))) atomicOr(&bad_rows, 1u << r);
+        if (w.whole) {
+          const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+          *reinterpret_cast<uint2 *>(g.o + 2 * ((long long)(w.s.tok0 + tok) * g.o_tok + (long long)head * g.o_head + ch)) =
+              make_uint2(Bits<T>::pack(v[0] * inv, v[1] * inv), Bits<T>::pack(v[2] * inv, v[3] * inv));
+          if (ch == 0 && g.lse)
+            g.lse[out] = l > 0.f || l != l ? m * 0.693147180559945309f + logf(l) : -INFINITY;
+        } else {
+          *reinterpret_cast<float4 *>(g.part + ((long long)part * kFewRows + r) * g.c.d + ch) =
+              make_float4(v[0], v[1], v[2], v[3]);
+          if (ch == 0) g.part_ml[part * kFewRows + r] = make_float2(m, l);
+        }
+      }
+      named_sync(32 * kWarps);
+    }
+    // Rows that came out non-finite because of a value they do not see (see
+    // k_attend) are taken again without it.
+    const unsigned bad = bad_rows;
+    if (bad) {
+      named_sync(32 * kWarps);
+      if (threadIdx.x == 0) bad_rows = 0;
+      for (int r = warp; r < rows; r += kWarps) {
+        if (!(bad >> r & 1u)) continue;
+        const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
+        const int own = w.s.base + tok, from = w.tile * kTile, end = min((w.tile + w.count) * kTile, w.s.len);
+        const int rlo = max(g.window > 0 ? window_start(own, g.window) : 0, from);
+        const int rhi = min(g.causal ? min(w.s.len, own + 1) : w.s.len, end);
+        if (hidden_values_finite<T>(g, w.b, hk, from, min(rlo, end)) &&
+            hidden_values_finite<T>(g, w.b, hk, max(rhi, from), end))
+          continue;
+        const char *qr = g.q + 2 * ((long long)(w.s.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
+        float m, l;
+        float4 v = row_by_warp<T>(g, w.b, hk, qr, rlo, rhi, m, l);
+        const long long out = (long long)(w.s.tok0 + tok) * g.q_heads + head;
+        if (w.whole) {
+          const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+          if (4 * lane < g.c.d)
+            reinterpret_cast<uint2 *>(g.o + 2 * ((long long)(w.s.tok0 + tok) * g.o_tok + (long long)head * g.o_head))[lane] =
+                make_uint2(Bits<T>::pack(v.x * inv, v.y * inv), Bits<T>::pack(v.z * inv, v.w * inv));
+          if (lane == 0 && g.lse)
+            g.lse[out] = l > 0.f || l != l ? m * 0.693147180559945309f + logf(l) : -INFINITY;
+        } else {
+          if (4 * lane < g.c.d)
+            reinterpret_cast<float4 *>(g.part + ((long long)part * kFewRows + r) * g.c.d)[lane] = v;
+          if (lane == 0) g.part_ml[part * kFewRows + r] = make_float2(m, l);
+        }
+      }
+      named_sync(32 * kWarps);
+    }
+  }
+}
+
+// Joins the pieces of the items that several shares cover, one warp per row,
+// in the shares' order; rows of sequences without a visible tile get zeros.
+template <typename T>
+__global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ AttendArgs g) {
+  __shared__ long long runs[kFewMaxBatch / 32];
+  const int lane = threadIdx.x & 31;
+  const long long all = count_units(g, runs, 8);  // reads nothing that k_attend_few writes
+  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  pdl_wait();
+  if (row >= (long long)g.c.total_new * g.q_heads) return;
+  const int t = (int)(row / g.q_heads), h = (int)(row - (long long)t * g.q_heads);
+  const int b = find_token(g.c, t).seq;
+  float m = -INFINITY, l = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  const bool holds = 4 * lane < g.c.d;
+  const Seq s = b >= 0 ? seq_of(g, b) : Seq{0, 0, 0, 0, 0, 0, 0};
+  if (s.tiles > 0) {
+    long long u0 = 0;
+    for (int i = 0; i < b / 32; ++i) u0 += runs[i];
+    long long x = lane < b % 32 ? units_of(seq_of(g, b / 32 * 32 + lane)) : 0;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    const int local = (t - s.tok0) * g.group + h % g.group, r = local % kFewRows;
+    u0 += x + (long long)(local / kFewRows * g.c.heads + h / g.group) * s.tiles;
+    // the share of unit u is the largest c with floor(c all / ctas) <= u
+    const int c0 = (int)(((u0 + 1) * g.ctas - 1) / all), c1 = (int)(((u0 + s.tiles) * g.ctas - 1) / all);
+    if (c0 == c1) return;  // finished by its share
+    for (int c = c0; c <= c1; ++c) {
+      const long long from = all * c / g.ctas;
+      if (from == all * (c + 1) / g.ctas) continue;  // an empty share (fewer units than CTAs)
+      const int slot = 2 * c + (from < u0 ? 1 : 0);
+      const float2 ml = g.part_ml[slot * kFewRows + r];
+      if (ml.y == 0.f) continue;  // saw no key
+      const float top = fmaxf(m, ml.x);
+      const float f = m == -INFINITY ? 0.f : exp2_fast(m - top), e = exp2_fast(ml.x - top);
+      m = top;
+      l = l * f + ml.y * e;
+      if (holds) {
+        const float4 v = reinterpret_cast<const float4 *>(g.part + ((long long)slot * kFewRows + r) * g.c.d)[lane];
+        acc.x = acc.x * f + v.x * e;
+        acc.y = acc.y * f + v.y * e;
+        acc.z = acc.z * f + v.z * e;
+        acc.w = acc.w * f + v.w * e;
+      }
+    }
+  }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  if (holds)
+    reinterpret_cast<uint2 *>(g.o + 2 * ((long long)t * g.o_tok + (long long)h * g.o_head))[lane] =
+        make_uint2(Bits<T>::pack(acc.x * inv, acc.y * inv), Bits<T>::pack(acc.z * inv, acc.w * inv));
+  if (g.lse && lane == 0) g.lse[row] = l > 0.f || l != l ? m * 0.693147180559945309f + logf(l) : -INFINITY;
+}
+
+std::atomic<int> g_few_smem_set[64];
+
+template <typename T, int D>
+cudaError_t launch_few_t(const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &g, int variant,
+                         cudaStream_t st) {
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  if (!(g_few_smem_set[dev & 63].load() & (1 << variant))) {
+    err = cudaFuncSetAttribute(k_attend_few<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Few<D>::kSmem);
+    if (err != cudaSuccess) return err;
+    g_few_smem_set[dev & 63].fetch_or(1 << variant);
+  }
+  err = launch_kernel(k_attend_few<T, D>, dim3(g.ctas), dim3(kThreads), Few<D>::kSmem, st, false, mk, mv, g);
+  if (err != cudaSuccess) return err;
+  const long long rows = (long long)g.c.total_new * g.q_heads;
+  return launch_kernel(k_few_join<T>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, true, g);
+}
+
+size_t few_part_bytes(int d, int ctas) { return align_up((size_t)2 * ctas * kFewRows * d * sizeof(float), 256); }
+
+}  // namespace
+
+namespace attend {
+
+size_t few_workspace_bytes(int d, int ctas) {
+  return few_part_bytes(d, ctas) + align_up((size_t)2 * ctas * kFewRows * sizeof(float2), 256);
+}
+
+cudaError_t launch_few(const CUtensorMap &mk, const CUtensorMap &mv, AttendArgs g, bool bf16, void *ws, cudaStream_t st) {
+  g.part = static_cast<float *>(ws);
+  g.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + few_part_bytes(g.c.d, g.ctas));
+  if (bf16)
+    return g.c.d <= 64 ? launch_few_t<__nv_bfloat16, 64>(mk, mv, g, 0, st)
+                       : launch_few_t<__nv_bfloat16, 128>(mk, mv, g, 1, st);
+  return g.c.d <= 64 ? launch_few_t<__half, 64>(mk, mv, g, 2, st) : launch_few_t<__half, 128>(mk, mv, g, 3, st);
+}
+
+}  // namespace attend
+}  // namespace tr
