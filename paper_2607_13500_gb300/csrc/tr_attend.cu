@@ -163,7 +163,12 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
     TileRing<D, S::kStages> tiles;
     tiles.base = ring, tiles.full0 = full(0), tiles.empty0 = empty(0), tiles.tail = tail;
     bool ok = true;
-    for (int t = t0; t < t1 && ok; ++t) ok = tiles.load(g, &map_k, &map_v, k.seq, k.len, hk, t);
+    int id = t0 < t1 ? tiles.page_id(g, k.seq, k.len, t0) : -1;
+    for (int t = t0; t < t1 && ok; ++t) {
+      const int next = t + 1 < t1 ? tiles.page_id(g, k.seq, k.len, t + 1) : -1;
+      ok = tiles.load(g, &map_k, &map_v, id, k.len, hk, t);
+      id = next;
+    }
     if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
     tiles.drain();
   } else if (warp == 4 * MT + 1) {
@@ -492,7 +497,11 @@ Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_le
   const int group = q_heads / c->heads;
   const long long most = (long long)(max_new < c->total_new ? max_new : c->total_new) * group;
   const int sms = sm_count() > 0 ? sm_count() : 1;
-  if (most <= kFewRows && c->batch <= kFewMaxBatch) {
+  // (its units, tiles of all blocks and key heads, are counted in 31 bits)
+  const long long blocks16 = (long long)c->total_new * group / kFewRows + c->batch;
+  const long long table_tiles = ((long long)c->max_pages * c->page + kTile - 1) / kTile;
+  if (most <= kFewRows && c->batch <= kFewMaxBatch && blocks16 * c->heads <= INT_MAX &&
+      (table_tiles == 0 || blocks16 * c->heads <= INT_MAX / table_tiles)) {
     p.few = true;
     p.total = few_workspace_bytes(c->head_dim, sms);
     return p;
@@ -595,6 +604,7 @@ tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *
   g.negate = scale < 0.f;
   g.causal = causal, g.window = window;
   g.splits = p.splits;
+  while ((1 << g.page_log2) < c->page) ++g.page_log2;
   g.part = static_cast<float *>(ws);
   g.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.part_ml);
   g.err = d_error;

@@ -31,6 +31,7 @@ struct AttendArgs {
   int splits;       // parts of the key range, each a CTA's
   float *part;      // splits > 1: [splits][total_new * q_heads][d] unnormalised sums,
   float2 *part_ml;  //             [splits][total_new * q_heads] (maximum, sum)
+  int page_log2;
   int ctas;         // few rows: CTAs that share the work; part [2 ctas][16][d], part_ml [2 ctas][16]
   int32_t *err;
 };
@@ -196,21 +197,28 @@ struct TileRing {
   __device__ __forceinline__ uint32_t full(int s) const { return full0 + 8u * s; }
   __device__ __forceinline__ uint32_t empty(int s) const { return empty0 + 8u * s; }
 
+  // The page id that this lane's part of tile t needs (part: one half of
+  // the rows of one page).  Asked for one tile ahead of its load, so that
+  // the table's latency is not in the loads' way.
+  __device__ __forceinline__ int page_id(const AttendArgs &g, int seq, int len, int t) const {
+    const int piece = min(g.c.page, kTile), key = t * kTile + (int)(threadIdx.x & 31) % (kTile / piece) * piece;
+    const int i = key >> g.page_log2;
+    return key < len && i < g.c.max_pages ? __ldg(g.c.table + (long long)seq * g.c.max_pages + i) : -1;
+  }
   // K and V of tile t of the sequence; false when a wait timed out.  Value
   // rows past the sequence's end are zeroed: stale memory may hold NaN there,
   // and 0 * NaN would reach every row.
-  __device__ __forceinline__ bool load(const AttendArgs &g, const CUtensorMap *map_k, const CUtensorMap *map_v, int seq,
+  __device__ __forceinline__ bool load(const AttendArgs &g, const CUtensorMap *map_k, const CUtensorMap *map_v, int id,
                                        int len, int hk, int t) {
     const int lane = threadIdx.x & 31;
-    const int page = g.c.page, piece = page < kTile ? page : kTile;  // keys of one load
+    const int page = g.c.page, piece = min(page, kTile);  // keys of one load
     const int key0 = t * kTile, left = min(len - key0, kTile);
     const int pieces = (left + piece - 1) / piece;
     const int pc = lane % (kTile / piece), half = lane / (kTile / piece);
     const bool mine = pc < pieces && half < kHalves;
     int row = max(1, g.c.pages * g.c.heads * page);  // a row past the cache: reads as zeros
     if (mine) {
-      const int key = key0 + pc * piece, id = page_of(g.c, seq, key);
-      if (id >= 0) row = (id * g.c.heads + hk) * page + (key & (page - 1));
+      if ((unsigned)id < (unsigned)g.c.pages) row = (id * g.c.heads + hk) * page + ((key0 + pc * piece) & (page - 1));
       else flag(g, TR_CACHE_ERR_PAGE);
     }
     const uint32_t bytes = (uint32_t)pieces * piece * 128u * kHalves;

@@ -65,31 +65,39 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs &g, int b) {
   s.items = (s.rows + kFewRows - 1) / kFewRows * g.c.heads;
   return s;
 }
-__device__ __forceinline__ long long units_of(const Seq &s) { return (long long)s.items * s.tiles; }
+__device__ __forceinline__ int units_of(const Seq &s) { return s.items * s.tiles; }
+
+// Share c of `all` units over `ctas` CTAs: the first all % ctas shares are
+// one unit longer.
+struct Shares {
+  int size, longer;
+  __device__ __forceinline__ Shares(int all, int ctas) : size(all / ctas), longer(all % ctas) {}
+  __device__ __forceinline__ int start(int c) const { return c * size + min(c, longer); }
+  __device__ __forceinline__ int of(int unit) const {
+    const int head = longer * (size + 1);
+    return unit < head ? unit / (size + 1) : longer + (unit - head) / max(size, 1);
+  }
+};
 
 // Units of each run of 32 sequences, left in shared memory by all warps of
 // the CTA together; returns their total.
-__device__ __forceinline__ long long count_units(const AttendArgs &g, long long *runs, int warps) {
+__device__ __forceinline__ int count_units(const AttendArgs &g, int *runs, int warps) {
   const int lane = threadIdx.x & 31;
   const int n = (g.c.batch + 31) / 32;
   for (int i = threadIdx.x >> 5; i < n; i += warps) {
-    long long u = units_of(seq_of(g, 32 * i + lane));
-#pragma unroll
-    for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
+    const int u = (int)__reduce_add_sync(0xffffffffu, (unsigned)units_of(seq_of(g, 32 * i + lane)));
     if (lane == 0) runs[i] = u;
   }
   __syncthreads();
-  long long all = 0;
+  int all = 0;
   for (int i = lane; i < n; i += 32) all += runs[i];
-#pragma unroll
-  for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-  return all;
+  return (int)__reduce_add_sync(0xffffffffu, (unsigned)all);
 }
 
 // A walk over the units of a share, item by item; the same in all lanes.
 struct Walk {
-  long long u, end;   // next unit, end of the share
-  long long first;    // first unit of sequence b
+  int u, end;   // next unit, end of the share
+  int first;    // first unit of sequence b
   int b;
   Seq s;
   // the current piece
@@ -97,7 +105,7 @@ struct Walk {
   bool whole;             // the piece is the whole item
   bool inside;            // the item starts after the share does
 
-  __device__ __forceinline__ void seek(const AttendArgs &g, const long long *runs, long long from, long long to) {
+  __device__ __forceinline__ void seek(const AttendArgs &g, const int *runs, int from, int to) {
     const int lane = threadIdx.x & 31;
     u = from;
     end = to;
@@ -106,10 +114,10 @@ struct Walk {
     const int n = (g.c.batch + 31) / 32;
     while (i + 1 < n && u >= first + runs[i]) first += runs[i++];
     const Seq mine = seq_of(g, 32 * i + lane);
-    long long before = units_of(mine);
+    int before = units_of(mine);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long v = __shfl_up_sync(0xffffffffu, before, o);
+      const int v = __shfl_up_sync(0xffffffffu, before, o);
       if (lane >= o) before += v;
     }
     const int at = max(__ffs(__ballot_sync(0xffffffffu, u < first + before)), 1) - 1;
@@ -118,7 +126,7 @@ struct Walk {
     s = seq_of(g, b);
   }
   // The next piece; false at the end of the share.
-  __device__ __forceinline__ bool next(const AttendArgs &g, long long share) {
+  __device__ __forceinline__ bool next(const AttendArgs &g, int share) {
     if (u >= end) return false;
     if (u >= first + units_of(s)) {  // on to the next sequence that has units
       const int lane = threadIdx.x & 31;
@@ -132,11 +140,10 @@ struct Walk {
       s = seq_of(g, b);
     }
     if (s.tiles <= 0) return false;
-    const long long rel = u - first;
-    item = (int)(rel / s.tiles);
-    const int t = (int)(rel - (long long)item * s.tiles);
-    const long long left = end - u;
-    count = (long long)(s.tiles - t) < left ? s.tiles - t : (int)left;
+    const int rel = u - first;
+    item = rel / s.tiles;
+    const int t = rel - item * s.tiles;
+    count = min(s.tiles - t, end - u);
     tile = s.tile0 + t;
     whole = count == s.tiles;
     inside = u - t > share;
@@ -172,7 +179,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                  const __grid_constant__ AttendArgs g) {
   using F = Few<D>;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ long long runs[kFewMaxBatch / 32];  // units of 32 sequences each
+  __shared__ int runs[kFewMaxBatch / 32];  // units of 32 sequences each
   __shared__ float top[kWarps][kFewRows], tot[kWarps][kFewRows];
   __shared__ unsigned bad_rows;
   const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -195,8 +202,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   pdl_wait();  // q and the cache come from the kernels before
   pdl_trigger();
-  const long long all = count_units(g, runs, kWarps + 1);  // (its barrier also publishes the mbarriers)
-  const long long share = all * blockIdx.x / g.ctas, share_end = all * (blockIdx.x + 1) / g.ctas;
+  const Shares shares(count_units(g, runs, kWarps + 1), g.ctas);  // (its barrier also publishes the mbarriers)
+  const int share = shares.start(blockIdx.x), share_end = shares.start(blockIdx.x + 1);
   if (share >= share_end) return;
   Walk w;
   w.seek(g, runs, share, share_end);
@@ -204,8 +211,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kWarps) {
     bool ok = true;
     while (ok && w.next(g, share)) {
-      const int hk = w.item % g.c.heads;
-      for (int i = 0; i < w.count && ok; ++i) ok = ring.load(g, &map_k, &map_v, w.b, w.s.len, hk, w.tile + i);
+      const int hk = w.item % g.c.heads, end = w.tile + w.count;
+      int id = ring.page_id(g, w.b, w.s.len, w.tile);
+      for (int t = w.tile; t < end && ok; ++t) {
+        const int next = t + 1 < end ? ring.page_id(g, w.b, w.s.len, t + 1) : -1;
+        ok = ring.load(g, &map_k, &map_v, id, w.s.len, hk, t);
+        id = next;
+      }
     }
     if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
     ring.drain();
@@ -265,13 +277,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       float s[2][4];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        // two chains of products, so that one's latency hides the other's
+        float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < F::kHalves * 2; ++j) {
           const uint4 v = lds128(kt + (j >> 1) * (kTile * 128) + (8 * n + gq) * 128 + (((2 * c + (j & 1)) ^ gq) << 4));
-          mma16816<T>(s[n], q[j][0], q[j][4], q[j][1], q[j][5], v.x, v.y);
-          mma16816<T>(s[n], q[j][2], q[j][6], q[j][3], q[j][7], v.z, v.w);
+          mma16816<T>(x, q[j][0], q[j][4], q[j][1], q[j][5], v.x, v.y);
+          mma16816<T>(y, q[j][2], q[j][6], q[j][3], q[j][7], v.z, v.w);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] = x[i] + y[i];
       }
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(ring.empty(stage));
@@ -457,12 +472,14 @@ __global__ void __launch_bounds__(kThreads, 1)
 // in the shares' order; rows of sequences without a visible tile get zeros.
 template <typename T>
 __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ AttendArgs g) {
-  __shared__ long long runs[kFewMaxBatch / 32];
+  __shared__ int runs[kFewMaxBatch / 32];
   const int lane = threadIdx.x & 31;
-  const long long all = count_units(g, runs, 8);  // reads nothing that k_attend_few writes
+  const Shares shares(count_units(g, runs, 8), g.ctas);  // reads nothing that k_attend_few writes
   const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  pdl_wait();
-  if (row >= (long long)g.c.total_new * g.q_heads) return;
+  if (row >= (long long)g.c.total_new * g.q_heads) {
+    pdl_wait();
+    return;
+  }
   const int t = (int)(row / g.q_heads), h = (int)(row - (long long)t * g.q_heads);
   const int b = find_token(g.c, t).seq;
   float m = -INFINITY, l = 0.f;
@@ -470,35 +487,60 @@ __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ Attend
   const bool holds = 4 * lane < g.c.d;
   const Seq s = b >= 0 ? seq_of(g, b) : Seq{0, 0, 0, 0, 0, 0, 0};
   if (s.tiles > 0) {
-    long long u0 = 0;
-    for (int i = 0; i < b / 32; ++i) u0 += runs[i];
-    long long x = lane < b % 32 ? units_of(seq_of(g, b / 32 * 32 + lane)) : 0;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    unsigned x = lane < b % 32 ? units_of(seq_of(g, b / 32 * 32 + lane)) : 0;
+    for (int i = lane; i < b / 32; i += 32) x += runs[i];
     const int local = (t - s.tok0) * g.group + h % g.group, r = local % kFewRows;
-    u0 += x + (long long)(local / kFewRows * g.c.heads + h / g.group) * s.tiles;
-    // the share of unit u is the largest c with floor(c all / ctas) <= u
-    const int c0 = (int)(((u0 + 1) * g.ctas - 1) / all), c1 = (int)(((u0 + s.tiles) * g.ctas - 1) / all);
+    const int u0 = (int)__reduce_add_sync(0xffffffffu, x) + (local / kFewRows * g.c.heads + h / g.group) * s.tiles;
+    const int c0 = shares.of(u0), c1 = shares.of(u0 + s.tiles - 1);
+    pdl_wait();
     if (c0 == c1) return;  // finished by its share
-    for (int c = c0; c <= c1; ++c) {
-      const long long from = all * c / g.ctas;
-      if (from == all * (c + 1) / g.ctas) continue;  // an empty share (fewer units than CTAs)
-      const int slot = 2 * c + (from < u0 ? 1 : 0);
-      const float2 ml = g.part_ml[slot * kFewRows + r];
-      if (ml.y == 0.f) continue;  // saw no key
-      const float top = fmaxf(m, ml.x);
-      const float f = m == -INFINITY ? 0.f : exp2_fast(m - top), e = exp2_fast(ml.x - top);
-      m = top;
-      l = l * f + ml.y * e;
-      if (holds) {
-        const float4 v = reinterpret_cast<const float4 *>(g.part + ((long long)slot * kFewRows + r) * g.c.d)[lane];
-        acc.x = acc.x * f + v.x * e;
-        acc.y = acc.y * f + v.y * e;
-        acc.z = acc.z * f + v.z * e;
-        acc.w = acc.w * f + v.w * e;
+    // 32 shares at a time: a lane each for (maximum, sum), then the values,
+    // several loads in flight
+    for (int i0 = c0; i0 <= c1; i0 += 32) {
+      const int c = i0 + lane;
+      const int slot = 2 * c + (shares.start(c) < u0 ? 1 : 0);
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (c <= c1) ml = g.part_ml[slot * kFewRows + r];
+      const bool seen = ml.y != 0.f;  // NaN counts
+      float now = seen ? ml.x : -INFINITY;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, o));
+      const float before = m;
+      m = fmaxf(m, now);
+      const float f = before == -INFINITY ? 0.f : exp2_fast(before - m);
+      const float e = seen ? exp2_fast(ml.x - m) : 0.f;
+      float add = seen ? ml.y * e : 0.f;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) add += __shfl_xor_sync(0xffffffffu, add, o);
+      l = l * f + add;
+      acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
+      unsigned left = __ballot_sync(0xffffffffu, seen);
+      while (left) {
+        constexpr int kU = 4;
+        float4 v[kU];
+        float w[kU];
+#pragma unroll
+        for (int k = 0; k < kU; ++k) {
+          const int src = left ? __ffs(left) - 1 : 0;
+          const bool have = left != 0;
+          left &= left - 1;
+          const int from_slot = __shfl_sync(0xffffffffu, slot, src);
+          w[k] = __shfl_sync(0xffffffffu, e, src);
+          v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (have && holds)
+            v[k] = reinterpret_cast<const float4 *>(g.part + ((long long)from_slot * kFewRows + r) * g.c.d)[lane];
+        }
+#pragma unroll
+        for (int k = 0; k < kU; ++k) {
+          acc.x += v[k].x * w[k];
+          acc.y += v[k].y * w[k];
+          acc.z += v[k].z * w[k];
+          acc.w += v[k].w * w[k];
+        }
       }
     }
   }
+  if (s.tiles <= 0) pdl_wait();  // o may still be read by the kernel before last
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
   if (holds)
     reinterpret_cast<uint2 *>(g.o + 2 * ((long long)t * g.o_tok + (long long)h * g.o_head))[lane] =
