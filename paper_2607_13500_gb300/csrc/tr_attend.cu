@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
 
   if (warp == 4 * MT) {
     // ---------------------------------------------------------------- TMA producer
-    TileRing<D, S::kStages> tiles;
+    TileRing<D, S::kStages, true> tiles;
     tiles.base = ring, tiles.full0 = full(0), tiles.empty0 = empty(0), tiles.tail = tail;
     bool ok = true;
     int id = t0 < t1 ? tiles.page_id(g, k.seq, k.len, t0) : -1;

@@ -186,7 +186,12 @@ __device__ __forceinline__ void flag(const AttendArgs &g, int bit) {
 // A ring of 128-key tiles (D / 64 halves of 128 rows x 128 bytes, 128-byte
 // swizzle), K and V in turn, filled by one warp.  A tile is loaded page by
 // page; the lanes of the warp issue its loads side by side.
-template <int D, int STAGES>
+// ZERO_TAIL: value rows past the sequence's end are zeroed before the tile is
+// handed on -- stale memory may hold NaN there, and 0 * NaN would reach every
+// row of a product that reads the tile from shared memory.  That waits for
+// the tile, so it suits a CTA that ends with it; consumers that read the
+// tile into registers drop those rows themselves.
+template <int D, int STAGES, bool ZERO_TAIL>
 struct TileRing {
   static constexpr int kHalves = D / 64;
   static constexpr uint32_t kBytes = kTile * D * 2;
@@ -205,9 +210,7 @@ struct TileRing {
     const int i = key >> g.page_log2;
     return key < len && i < g.c.max_pages ? __ldg(g.c.table + (long long)seq * g.c.max_pages + i) : -1;
   }
-  // K and V of tile t of the sequence; false when a wait timed out.  Value
-  // rows past the sequence's end are zeroed: stale memory may hold NaN there,
-  // and 0 * NaN would reach every row.
+  // K and V of tile t of the sequence; false when a wait timed out.
   __device__ __forceinline__ bool load(const AttendArgs &g, const CUtensorMap *map_k, const CUtensorMap *map_v, int id,
                                        int len, int hk, int t) {
     const int lane = threadIdx.x & 31;
@@ -226,7 +229,7 @@ struct TileRing {
     for (int kv = 0; kv < 2; ++kv) {
       if (!tc::mbar_wait_warp(empty(stage), phase ^ 1u)) return false;
       const uint32_t dst = base + stage * kBytes;
-      const bool cut = kv == 1 && left < kTile;  // the sequence ends inside this value tile
+      const bool cut = ZERO_TAIL && kv == 1 && left < kTile;  // the sequence ends inside this value tile
       const uint32_t bar = cut ? tail : full(stage);
       if (lane == 0) tc::mbar_expect_tx(bar, bytes);
       __syncwarp();

@@ -29,13 +29,14 @@ using namespace attend;
 
 constexpr int kWarps = 8;                     // consumer warps: 16 keys of a tile each
 constexpr int kThreads = 32 * (kWarps + 1);
-constexpr int kPass = 32;                     // channels joined per pass at an item's end
+constexpr int kPass = 4;                      // rows joined per pass at an item's end
 
 template <int D>
 struct Few {
   static constexpr int kHalves = D / 64;
   static constexpr int kTileBytes = kTile * D * 2;
-  static constexpr int kJoinBytes = kWarps * kFewRows * (kPass + 1) * 4;
+  static constexpr int kJoinRow = D + 4;  // floats
+  static constexpr int kJoinBytes = kWarps * kPass * kJoinRow * 4;
   static constexpr int kFit = (227 * 1024 - 4096 - 1024 - kJoinBytes) / kTileBytes;
   static constexpr int kStages = kFit < 12 ? kFit : 12;
   static constexpr size_t kSmem = (size_t)kStages * kTileBytes + kJoinBytes + 1024 + 4096;
@@ -79,11 +80,26 @@ struct Shares {
   }
 };
 
-// Units of each run of 32 sequences, left in shared memory by all warps of
-// the CTA together; returns their total.
-__device__ __forceinline__ int count_units(const AttendArgs &g, int *runs, int warps) {
+// The sequences 32 at a time, a lane each.
+__device__ __forceinline__ Seq seq_from(const Seq &mine, int lane) {
+  Seq s;
+  s.tok0 = __shfl_sync(0xffffffffu, mine.tok0, lane);
+  s.rows = __shfl_sync(0xffffffffu, mine.rows, lane);
+  s.len = __shfl_sync(0xffffffffu, mine.len, lane);
+  s.base = __shfl_sync(0xffffffffu, mine.base, lane);
+  s.tile0 = __shfl_sync(0xffffffffu, mine.tile0, lane);
+  s.tiles = __shfl_sync(0xffffffffu, mine.tiles, lane);
+  s.items = __shfl_sync(0xffffffffu, mine.items, lane);
+  return s;
+}
+
+// Total units, and `mine` = this lane's sequence of the first run.  With more
+// than one run their units are left in shared memory by all warps together.
+__device__ __forceinline__ int count_units(const AttendArgs &g, int *runs, int warps, Seq &mine) {
   const int lane = threadIdx.x & 31;
   const int n = (g.c.batch + 31) / 32;
+  mine = seq_of(g, lane);
+  if (n <= 1) return (int)__reduce_add_sync(0xffffffffu, (unsigned)units_of(mine));
   for (int i = threadIdx.x >> 5; i < n; i += warps) {
     const int u = (int)__reduce_add_sync(0xffffffffu, (unsigned)units_of(seq_of(g, 32 * i + lane)));
     if (lane == 0) runs[i] = u;
@@ -94,50 +110,55 @@ __device__ __forceinline__ int count_units(const AttendArgs &g, int *runs, int w
   return (int)__reduce_add_sync(0xffffffffu, (unsigned)all);
 }
 
-// A walk over the units of a share, item by item; the same in all lanes.
+// A walk over the units of a share, item by item; the same in all lanes
+// (but `mine`).
 struct Walk {
-  int u, end;   // next unit, end of the share
-  int first;    // first unit of sequence b
-  int b;
-  Seq s;
+  int u, end;  // next unit, end of the share
+  int first;   // first unit of the sequence
+  int run, at; // the sequence: its run of 32, its lane
+  Seq mine;    // this lane's sequence of the run
+  Seq s;       // the sequence
   // the current piece
   int item, tile, count;  // item of the sequence, first tile (absolute), tiles
   bool whole;             // the piece is the whole item
   bool inside;            // the item starts after the share does
 
-  __device__ __forceinline__ void seek(const AttendArgs &g, const int *runs, int from, int to) {
-    const int lane = threadIdx.x & 31;
+  __device__ __forceinline__ int seq() const { return 32 * run + at; }
+  __device__ __forceinline__ void seek(const AttendArgs &g, const int *runs, const Seq &run0, int from, int to) {
+    const int lane = threadIdx.x & 31, n = (g.c.batch + 31) / 32;
     u = from;
     end = to;
     first = 0;
-    int i = 0;
-    const int n = (g.c.batch + 31) / 32;
-    while (i + 1 < n && u >= first + runs[i]) first += runs[i++];
-    const Seq mine = seq_of(g, 32 * i + lane);
-    int before = units_of(mine);
+    run = 0;
+    mine = run0;
+    if (n > 1) {
+      while (run + 1 < n && u >= first + runs[run]) first += runs[run++];
+      if (run) mine = seq_of(g, 32 * run + lane);
+    }
+    const int own = units_of(mine);
+    int before = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, before, o);
       if (lane >= o) before += v;
     }
-    const int at = max(__ffs(__ballot_sync(0xffffffffu, u < first + before)), 1) - 1;
-    first += __shfl_sync(0xffffffffu, before - units_of(mine), at);
-    b = 32 * i + at;
-    s = seq_of(g, b);
+    at = max(__ffs(__ballot_sync(0xffffffffu, u < first + before)), 1) - 1;
+    first += __shfl_sync(0xffffffffu, before - own, at);
+    s = seq_from(mine, at);
   }
   // The next piece; false at the end of the share.
   __device__ __forceinline__ bool next(const AttendArgs &g, int share) {
     if (u >= end) return false;
     if (u >= first + units_of(s)) {  // on to the next sequence that has units
-      const int lane = threadIdx.x & 31;
       first += units_of(s);
-      unsigned any = 0;
-      for (int i = b + 1; i < g.c.batch && !any; i += 32) {
-        any = __ballot_sync(0xffffffffu, units_of(seq_of(g, i + lane)) > 0);
-        if (any) b = i + __ffs(any) - 1;
+      unsigned any = __ballot_sync(0xffffffffu, units_of(mine) > 0) & ~(at == 31 ? 0xffffffffu : (2u << at) - 1u);
+      while (!any && 32 * (run + 1) < g.c.batch) {
+        mine = seq_of(g, 32 * ++run + (threadIdx.x & 31));
+        any = __ballot_sync(0xffffffffu, units_of(mine) > 0);
       }
       if (!any) return false;
-      s = seq_of(g, b);
+      at = __ffs(any) - 1;
+      s = seq_from(mine, at);
     }
     if (s.tiles <= 0) return false;
     const int rel = u - first;
@@ -173,6 +194,24 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 }
 __device__ __forceinline__ void named_sync(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
 
+// Four channels of row r of the piece: into the output, or into its share's
+// partial result.
+template <typename T>
+__device__ __forceinline__ void put_row(const AttendArgs &g, const Walk &w, int part, int block0, int hk, int r, int ch,
+                                        const float4 &v, float m, float l) {
+  if (w.whole) {
+    const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
+    const long long t = w.s.tok0 + tok;
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+    *reinterpret_cast<uint2 *>(g.o + 2 * (t * g.o_tok + (long long)head * g.o_head + ch)) =
+        make_uint2(Bits<T>::pack(v.x * inv, v.y * inv), Bits<T>::pack(v.z * inv, v.w * inv));
+    if (ch == 0 && g.lse) g.lse[t * g.q_heads + head] = l > 0.f || l != l ? m * 0.693147180559945309f + logf(l) : -INFINITY;
+  } else {
+    *reinterpret_cast<float4 *>(g.part + ((long long)part * kFewRows + r) * g.c.d + ch) = v;
+    if (ch == 0) g.part_ml[part * kFewRows + r] = make_float2(m, l);
+  }
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attend_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -187,14 +226,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t bars = tc::smem_u32(join) + F::kJoinBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-  TileRing<D, F::kStages> ring;
-  ring.base = base, ring.full0 = bars, ring.empty0 = bars + 8u * F::kStages, ring.tail = bars + 16u * F::kStages;
+  TileRing<D, F::kStages, false> ring;
+  ring.base = base, ring.full0 = bars, ring.empty0 = bars + 8u * F::kStages, ring.tail = 0;
   if (threadIdx.x == 0) {
     for (int s = 0; s < F::kStages; ++s) {
       tc::mbar_init(ring.full(s), 1);
       tc::mbar_init(ring.empty(s), kWarps);
     }
-    tc::mbar_init(ring.tail, 1);
     tc::mbar_fence_init();
     tc::tma_prefetch_map(&map_k);
     tc::tma_prefetch_map(&map_v);
@@ -202,19 +240,21 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   pdl_wait();  // q and the cache come from the kernels before
   pdl_trigger();
-  const Shares shares(count_units(g, runs, kWarps + 1), g.ctas);  // (its barrier also publishes the mbarriers)
+  __syncthreads();  // the barriers are ready
+  Walk w;
+  Seq run0;
+  const Shares shares(count_units(g, runs, kWarps + 1, run0), g.ctas);
   const int share = shares.start(blockIdx.x), share_end = shares.start(blockIdx.x + 1);
   if (share >= share_end) return;
-  Walk w;
-  w.seek(g, runs, share, share_end);
+  w.seek(g, runs, run0, share, share_end);
 
   if (warp == kWarps) {
     bool ok = true;
     while (ok && w.next(g, share)) {
       const int hk = w.item % g.c.heads, end = w.tile + w.count;
-      int id = ring.page_id(g, w.b, w.s.len, w.tile);
+      int id = ring.page_id(g, w.seq(), w.s.len, w.tile);
       for (int t = w.tile; t < end && ok; ++t) {
-        const int next = t + 1 < end ? ring.page_id(g, w.b, w.s.len, t + 1) : -1;
+        const int next = t + 1 < end ? ring.page_id(g, w.seq(), w.s.len, t + 1) : -1;
         ok = ring.load(g, &map_k, &map_v, id, w.s.len, hk, t);
         id = next;
       }
@@ -344,6 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
         break;
       }
+      const bool ends = key0 + 16 > w.s.len;
       const uint32_t vt = base + stage * F::kTileBytes + (uint32_t)(16 * warp) * 128u;
 #pragma unroll
       for (int h = 0; h < F::kHalves; ++h) {
@@ -352,6 +393,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int j = 0; j < 4; ++j) {
           const int key = 2 * c + (j & 1) + 8 * (j >> 1);
           v[j] = lds128(vt + h * (kTile * 128) + key * 128 + ((gq ^ (key & 7)) << 4));
+        }
+        if (ends) {  // the sequence ends among these keys: what lies behind may be NaN
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (key0 + 2 * c + (j & 1) + 8 * (j >> 1) >= w.s.len) v[j] = make_uint4(0u, 0u, 0u, 0u);
         }
         const uint32_t *v0 = &v[0].x, *v1 = &v[1].x, *v2 = &v[2].x, *v3 = &v[3].x;
 #pragma unroll
@@ -383,51 +429,42 @@ __global__ void __launch_bounds__(kThreads, 1)
       f[i] = mx[i] == -INFINITY ? 0.f : exp2_fast(mx[i] - m);
     }
     const int part = 2 * blockIdx.x + (w.inside ? 1 : 0);
-    for (int pass = 0; pass < F::kHalves * 2; ++pass) {
-      // half pass / 2, n-tiles 4 (pass & 1) .. + 3: channels 8 k + 4 (pass & 1) .. + 3 for k < 8
+    for (int r0 = 0; r0 < rows; r0 += kPass) {
+      // accumulator column 2 c + (j & 1) of n-tile i is channel 8 (2 c + (j & 1)) + i
+      const int mine = gq - (r0 & 7);  // row of the pass that this quad holds (of its rows g or g + 8)
+      if (mine >= 0 && mine < kPass) {
+        float *dst = join + (warp * kPass + mine) * F::kJoinRow + 16 * c;
 #pragma unroll
-      for (int pp = 0; pp < F::kHalves * 2; ++pp) {
-        if (pp != pass) continue;
-        const int h = pp >> 1, i0 = (pp & 1) * 4;
+        for (int h = 0; h < F::kHalves; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            // accumulator column 2 c + (j & 1) of n-tile i0 + i is channel 8 (2 c + (j & 1)) + i0 + i
-            const int col = (2 * c + (j & 1)) * 4 + i;
-            join[(warp * kFewRows + gq + 8 * (j >> 1)) * (kPass + 1) + col] = o[h][i0 + i][j] * f[j >> 1];
-          }
+            for (int i = 0; i < 8; i += 4) {
+              float4 v;
+              if (r0 < 8)
+                v = make_float4(o[h][i][b] * f[0], o[h][i + 1][b] * f[0], o[h][i + 2][b] * f[0], o[h][i + 3][b] * f[0]);
+              else
+                v = make_float4(o[h][i][2 + b] * f[1], o[h][i + 1][2 + b] * f[1], o[h][i + 2][2 + b] * f[1],
+                                o[h][i + 3][2 + b] * f[1]);
+              *reinterpret_cast<float4 *>(dst + 64 * h + 8 * b + i) = v;
+            }
       }
       named_sync(32 * kWarps);
-      for (int e = threadIdx.x; e < rows * (kPass / 4); e += 32 * kWarps) {
-        const int r = e / (kPass / 4), q4 = e % (kPass / 4);  // row, channel group 8 q4 + i0 .. + 3
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
+      const int r = r0 + (int)threadIdx.x / (D / 4), ch = (int)threadIdx.x % (D / 4) * 4;
+      if ((int)threadIdx.x < kPass * (D / 4) && r < rows && ch < g.c.d) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         float m = -INFINITY, l = 0.f;
 #pragma unroll
         for (int j = 0; j < kWarps; ++j) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] += join[(j * kFewRows + r) * (kPass + 1) + 4 * q4 + i];
+          const float4 x = *reinterpret_cast<const float4 *>(join + (j * kPass + r - r0) * F::kJoinRow + ch);
+          v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
           m = fmaxf(m, top[j][r]);
         }
 #pragma unroll
         for (int j = 0; j < kWarps; ++j)
           if (top[j][r] != -INFINITY) l += tot[j][r] * exp2_fast(top[j][r] - m);
-        const int ch = (pass >> 1) * 64 + 8 * q4 + (pass & 1) * 4;
-        if (ch >= g.c.d) continue;
-        const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
-        const long long out = (long long)(w.s.tok0 + tok) * g.q_heads + head;
-        if (!finite4(make_float4(v[0], v[1], v[2], v[3]))) atomicOr(&bad_rows, 1u << r);
-        if (w.whole) {
-          const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-          *reinterpret_cast<uint2 *>(g.o + 2 * ((long long)(w.s.tok0 + tok) * g.o_tok + (long long)head * g.o_head + ch)) =
-              make_uint2(Bits<T>::pack(v[0] * inv, v[1] * inv), Bits<T>::pack(v[2] * inv, v[3] * inv));
-          if (ch == 0 && g.lse)
-            g.lse[out] = l > 0.f || l != l ? m * 0.693147180559945309f + logf(l) : -INFINITY;
-        } else {
-          *reinterpret_cast<float4 *>(g.part + ((long long)part * kFewRows + r) * g.c.d + ch) =
-              make_float4(v[0], v[1], v[2], v[3]);
-          if (ch == 0) g.part_ml[part * kFewRows + r] = make_float2(m, l);
-        }
+        if (!finite4(v)) atomicOr(&bad_rows, 1u << r);
+        put_row<T>(g, w, part, block0, hk, r, ch, v, m, l);
       }
       named_sync(32 * kWarps);
     }
@@ -443,25 +480,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int own = w.s.base + tok, from = w.tile * kTile, end = min((w.tile + w.count) * kTile, w.s.len);
         const int rlo = max(g.window > 0 ? window_start(own, g.window) : 0, from);
         const int rhi = min(g.causal ? min(w.s.len, own + 1) : w.s.len, end);
-        if (hidden_values_finite<T>(g, w.b, hk, from, min(rlo, end)) &&
-            hidden_values_finite<T>(g, w.b, hk, max(rhi, from), end))
+        if (hidden_values_finite<T>(g, w.seq(), hk, from, min(rlo, end)) &&
+            hidden_values_finite<T>(g, w.seq(), hk, max(rhi, from), end))
           continue;
         const char *qr = g.q + 2 * ((long long)(w.s.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
         float m, l;
-        float4 v = row_by_warp<T>(g, w.b, hk, qr, rlo, rhi, m, l);
-        const long long out = (long long)(w.s.tok0 + tok) * g.q_heads + head;
-        if (w.whole) {
-          const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-          if (4 * lane < g.c.d)
-            reinterpret_cast<uint2 *>(g.o + 2 * ((long long)(w.s.tok0 + tok) * g.o_tok + (long long)head * g.o_head))[lane] =
-                make_uint2(Bits<T>::pack(v.x * inv, v.y * inv), Bits<T>::pack(v.z * inv, v.w * inv));
-          if (lane == 0 && g.lse)
-            g.lse[out] = l > 0.f || l != l ? m * 0.693147180559945309f + logf(l) : -INFINITY;
-        } else {
-          if (4 * lane < g.c.d)
-            reinterpret_cast<float4 *>(g.part + ((long long)part * kFewRows + r) * g.c.d)[lane] = v;
-          if (lane == 0) g.part_ml[part * kFewRows + r] = make_float2(m, l);
-        }
+        float4 v = row_by_warp<T>(g, w.seq(), hk, qr, rlo, rhi, m, l);
+        if (4 * lane < g.c.d) put_row<T>(g, w, part, block0, hk, r, 4 * lane, v, m, l);
       }
       named_sync(32 * kWarps);
     }
@@ -474,7 +499,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ AttendArgs g) {
   __shared__ int runs[kFewMaxBatch / 32];
   const int lane = threadIdx.x & 31;
-  const Shares shares(count_units(g, runs, 8), g.ctas);  // reads nothing that k_attend_few writes
+  Seq run0;
+  const Shares shares(count_units(g, runs, 8, run0), g.ctas);  // reads nothing that k_attend_few writes
   const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= (long long)g.c.total_new * g.q_heads) {
     pdl_wait();
@@ -485,9 +511,11 @@ __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ Attend
   float m = -INFINITY, l = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   const bool holds = 4 * lane < g.c.d;
-  const Seq s = b >= 0 ? seq_of(g, b) : Seq{0, 0, 0, 0, 0, 0, 0};
+  const Seq mine = b < 32 ? run0 : seq_of(g, b / 32 * 32 + lane);
+  Seq s = seq_from(mine, b & 31);
+  if (b < 0) s.tiles = 0;
   if (s.tiles > 0) {
-    unsigned x = lane < b % 32 ? units_of(seq_of(g, b / 32 * 32 + lane)) : 0;
+    unsigned x = lane < b % 32 ? units_of(mine) : 0;
     for (int i = lane; i < b / 32; i += 32) x += runs[i];
     const int local = (t - s.tok0) * g.group + h % g.group, r = local % kFewRows;
     const int u0 = (int)__reduce_add_sync(0xffffffffu, x) + (local / kFewRows * g.c.heads + h / g.group) * s.tiles;
