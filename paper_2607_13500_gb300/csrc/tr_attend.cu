@@ -499,9 +499,8 @@ Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_le
   const int sms = sm_count() > 0 ? sm_count() : 1;
   // (its units, tiles of all blocks and key heads, are counted in 31 bits)
   const long long blocks16 = (long long)c->total_new * group / kFewRows + c->batch;
-  const long long table_tiles = ((long long)c->max_pages * c->page + kTile - 1) / kTile;
-  if (most <= kFewRows && c->batch <= kFewMaxBatch && blocks16 * c->heads <= INT_MAX &&
-      (table_tiles == 0 || blocks16 * c->heads <= INT_MAX / table_tiles)) {
+  const long long table_tiles = ((long long)c->max_pages * c->page + kTile - 1) / kTile + kFewItemCost;
+  if (most <= kFewRows && c->batch <= kFewMaxBatch && blocks16 * c->heads <= INT_MAX / table_tiles) {
     p.few = true;
     p.total = few_workspace_bytes(c->head_dim, sms);
     return p;

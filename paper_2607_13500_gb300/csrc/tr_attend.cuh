@@ -264,6 +264,7 @@ struct TileRing {
 
 // ---------------------------------------------------------------- few rows (tr_attend_few.cu)
 constexpr int kFewRows = 16;         // rows of a block there
+constexpr int kFewItemCost = 2;      // units that an item counts besides its tiles
 constexpr int kFewMaxBatch = 8192;   // sequences its unit count handles
 // Workspace bytes, and the launch (work and join kernels); g.part and
 // g.part_ml are carved from ws by the launch.

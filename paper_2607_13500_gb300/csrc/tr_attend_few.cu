@@ -66,7 +66,11 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs &g, int b) {
   s.items = (s.rows + kFewRows - 1) / kFewRows * g.c.heads;
   return s;
 }
-__device__ __forceinline__ int units_of(const Seq &s) { return s.items * s.tiles; }
+// An item counts kExtra units before its tiles', the time that taking it up
+// and finishing it cost (about 3 us against 1.3 us a tile): without them the
+// shares that hold many short items end last.
+constexpr int kExtra = kFewItemCost;
+__device__ __forceinline__ int units_of(const Seq &s) { return s.tiles > 0 ? s.items * (s.tiles + kExtra) : 0; }
 
 // Share c of `all` units over `ctas` CTAs: the first all % ctas shares are
 // one unit longer.
@@ -121,7 +125,7 @@ struct Walk {
   // the current piece
   int item, tile, count;  // item of the sequence, first tile (absolute), tiles
   bool whole;             // the piece is the whole item
-  bool inside;            // the item starts after the share does
+  bool starts;            // it holds the item's first tile
 
   __device__ __forceinline__ int seq() const { return 32 * run + at; }
   __device__ __forceinline__ void seek(const AttendArgs &g, const int *runs, const Seq &run0, int from, int to) {
@@ -147,29 +151,32 @@ struct Walk {
     s = seq_from(mine, at);
   }
   // The next piece; false at the end of the share.
-  __device__ __forceinline__ bool next(const AttendArgs &g, int share) {
-    if (u >= end) return false;
-    if (u >= first + units_of(s)) {  // on to the next sequence that has units
-      first += units_of(s);
-      unsigned any = __ballot_sync(0xffffffffu, units_of(mine) > 0) & ~(at == 31 ? 0xffffffffu : (2u << at) - 1u);
-      while (!any && 32 * (run + 1) < g.c.batch) {
-        mine = seq_of(g, 32 * ++run + (threadIdx.x & 31));
-        any = __ballot_sync(0xffffffffu, units_of(mine) > 0);
+  __device__ __forceinline__ bool next(const AttendArgs &g) {
+    while (u < end) {
+      if (u >= first + units_of(s)) {  // on to the next sequence that has units
+        first += units_of(s);
+        unsigned any = __ballot_sync(0xffffffffu, units_of(mine) > 0) & ~(at == 31 ? 0xffffffffu : (2u << at) - 1u);
+        while (!any && 32 * (run + 1) < g.c.batch) {
+          mine = seq_of(g, 32 * ++run + (threadIdx.x & 31));
+          any = __ballot_sync(0xffffffffu, units_of(mine) > 0);
+        }
+        if (!any) return false;
+        at = __ffs(any) - 1;
+        s = seq_from(mine, at);
       }
-      if (!any) return false;
-      at = __ffs(any) - 1;
-      s = seq_from(mine, at);
+      if (s.tiles <= 0) return false;
+      const int rel = u - first, each = s.tiles + kExtra;
+      item = rel / each;
+      const int t = rel - item * each, n = min(each - t, end - u);
+      const int from = max(t - kExtra, 0);
+      count = t + n - kExtra - from;
+      tile = s.tile0 + from;
+      whole = count == s.tiles;
+      starts = from == 0;
+      u += n;
+      if (count > 0) return true;  // (else only the item's own units: its tiles are the next share's)
     }
-    if (s.tiles <= 0) return false;
-    const int rel = u - first;
-    item = rel / s.tiles;
-    const int t = rel - item * s.tiles;
-    count = min(s.tiles - t, end - u);
-    tile = s.tile0 + t;
-    whole = count == s.tiles;
-    inside = u - t > share;
-    u += count;
-    return true;
+    return false;
   }
 };
 
@@ -250,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == kWarps) {
     bool ok = true;
-    while (ok && w.next(g, share)) {
+    while (ok && w.next(g)) {
       const int hk = w.item % g.c.heads, end = w.tile + w.count;
       int id = ring.page_id(g, w.seq(), w.s.len, w.tile);
       for (int t = w.tile; t < end && ok; ++t) {
@@ -269,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   int stage = 0;
   uint32_t phase = 0;
   bool ok = true;  // once a wait has timed out the warp only keeps up with the others' barriers
-  while (w.next(g, share)) {
+  while (w.next(g)) {
     const int hk = w.item % g.c.heads, block0 = w.item / g.c.heads * kFewRows;
     const int rows = min(kFewRows, w.s.rows - block0);
     // this lane's two rows of a fragment, and the keys they see
@@ -428,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int j = 0; j < kWarps; ++j) m = fmaxf(m, top[j][gq + 8 * i]);
       f[i] = mx[i] == -INFINITY ? 0.f : exp2_fast(mx[i] - m);
     }
-    const int part = 2 * blockIdx.x + (w.inside ? 1 : 0);
+    const int part = 2 * blockIdx.x + (w.starts ? 1 : 0);
     for (int r0 = 0; r0 < rows; r0 += kPass) {
       // accumulator column 2 c + (j & 1) of n-tile i is channel 8 (2 c + (j & 1)) + i
       const int mine = gq - (r0 & 7);  // row of the pass that this quad holds (of its rows g or g + 8)
@@ -518,7 +525,7 @@ __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ Attend
     unsigned x = lane < b % 32 ? units_of(mine) : 0;
     for (int i = lane; i < b / 32; i += 32) x += runs[i];
     const int local = (t - s.tok0) * g.group + h % g.group, r = local % kFewRows;
-    const int u0 = (int)__reduce_add_sync(0xffffffffu, x) + (local / kFewRows * g.c.heads + h / g.group) * s.tiles;
+    const int u0 = (int)__reduce_add_sync(0xffffffffu, x) + (local / kFewRows * g.c.heads + h / g.group) * (s.tiles + kExtra) + kExtra;
     const int c0 = shares.of(u0), c1 = shares.of(u0 + s.tiles - 1);
     pdl_wait();
     if (c0 == c1) return;  // finished by its share
@@ -526,7 +533,7 @@ __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ Attend
     // several loads in flight
     for (int i0 = c0; i0 <= c1; i0 += 32) {
       const int c = i0 + lane;
-      const int slot = 2 * c + (shares.start(c) < u0 ? 1 : 0);
+      const int slot = 2 * c + (shares.start(c) <= u0 ? 1 : 0);
       float2 ml = make_float2(-INFINITY, 0.f);
       if (c <= c1) ml = g.part_ml[slot * kFewRows + r];
       const bool seen = ml.y != 0.f;  // NaN counts
