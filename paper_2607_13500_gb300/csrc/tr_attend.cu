@@ -51,7 +51,9 @@ struct Shape {
   static constexpr int kFit = (kBudget - MT * kTileBytes) / kTileBytes;
   static constexpr int kStages = kFit < 12 ? kFit : 12;
   static constexpr int kSBuf = MT == 1 ? 2 : 1;      // score buffers of a block
-  static constexpr int kThreads = 32 * (4 * MT + 2);
+  // MT = 2: three warpgroups, so that registers can move between them: 168 a
+  // thread at launch, 216 for the softmax (a row of scores is 128), 56 for the rest.
+  static constexpr int kThreads = MT == 2 ? 384 : 32 * 6;
   static constexpr int kColO = 256;                  // tensor-memory columns: scores below, sums from here
   static constexpr int kCols = 512;
   static constexpr size_t kSmem = (size_t)(MT + kStages) * kTileBytes + 1024 + 512;
@@ -67,6 +69,11 @@ __device__ __forceinline__ unsigned long long pair_of(float a, float b) {
 __device__ __forceinline__ float2 of_pair(unsigned long long v) {
   float2 r;
   asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
   return r;
 }
 __device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
@@ -112,9 +119,8 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
   {
     const Range r = keys_of_rows(g, k, k.first, min(k.first + kRows, k.rows));
     const int u0 = r.lo / kTile, u1 = (r.hi + kTile - 1) / kTile;
-    const int per = (u1 - u0 + g.splits - 1) / g.splits;
-    t0 = min(u0 + split * per, u1);
-    t1 = min(t0 + per, u1);
+    t0 = min(u0 + split * g.split_tiles, u1);
+    t1 = split + 1 < g.splits ? min(t0 + g.split_tiles, u1) : u1;
     int lo = INT_MAX, hi = 0;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -158,6 +164,8 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
   uint32_t tmem = 0;
   if (t0 < t1) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
 
+  if (warp >= 4 * MT) {
+  if (MT == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   if (warp == 4 * MT) {
     // ---------------------------------------------------------------- TMA producer
     TileRing<D, S::kStages, true> tiles;
@@ -252,7 +260,9 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
       if (!ok) flag(g, TR_CACHE_ERR_WAIT);
     }
     __syncwarp();
+  }
   } else {
+    if (MT == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ---------------------------------------------------------------- softmax
     const int m = MT == 1 ? 0 : warp >> 2, quarter = warp & 3;
     const int row = 32 * quarter + lane, r = k.first + m * kTile + row;  // row of the block, of the sequence
@@ -310,8 +320,7 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
 #pragma unroll
           for (int i = 0; i < kTile; i += 8)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              top[j] = fmaxf(top[j], fmaxf(__uint_as_float(s[i + 2 * j]), __uint_as_float(s[i + 2 * j + 1])));
+            for (int j = 0; j < 4; ++j) top[j] = max3(top[j], s[i + 2 * j], s[i + 2 * j + 1]);
           const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * g.scale;
           if (n == 0) {
             mx = now;
@@ -488,7 +497,8 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
 // ---------------------------------------------------------------- host side
 struct Plan {
   bool few;               // tr_attend_few.cu's kernel
-  int mt, splits, slots;  // else k_attend's blocks of 128 mt rows and parts of the keys
+  int mt, slots;          // else k_attend's blocks of 128 mt rows
+  int splits, split_tiles;  // and the parts of the keys, in tiles
   size_t part_ml, total;  // workspace
 };
 
@@ -508,16 +518,27 @@ Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_le
   p.mt = most <= kTile ? 1 : 2;
   const int rows = kTile * p.mt;
   p.slots = (int)((long long)c->total_new * group / rows) + c->batch;
-  // Split the keys when the row blocks alone would not fill the GPU.
-  const long long blocks = (long long)p.slots * c->heads;
+  // Parts of the keys: as many as finish earliest when `sms` CTAs run at a
+  // time, one costing its tiles and about kCtaTiles more, and the join
+  // writing and reading a row's fp32 sums once per part (kJoinRows rows in
+  // the time of one tile).
+  constexpr double kCtaTiles = 4.0, kJoinRows = 8192.0;
+  const double blocks = (double)p.slots * c->heads;
   const long long cap = (long long)c->max_pages * c->page;
   long long keys = max_len < cap ? max_len : cap;
   if (window > 0 && keys > (long long)window + max_new) keys = (long long)window + max_new;
-  const long long tiles = (keys + kTile - 1) / kTile;
-  long long s = blocks > 0 ? sms / blocks : 1;
-  if (s > tiles) s = tiles;
-  if (s > 64) s = 64;
-  p.splits = s < 1 ? 1 : (int)s;
+  const int tiles = (int)((keys + kTile - 1) / kTile);
+  double best = 0;
+  for (int s = 1; s <= 64 && s <= (tiles > 1 ? tiles : 1); ++s) {
+    const double waves = std::ceil(blocks * s / sms);
+    const double t = waves * ((tiles + s - 1) / s + kCtaTiles) +
+                     (s > 1 ? kCtaTiles + (double)c->total_new * q_heads * s / kJoinRows : 0.0);
+    if (s == 1 || t < best) {
+      best = t;
+      p.splits = s;
+    }
+  }
+  p.split_tiles = (tiles + p.splits - 1) / p.splits;
   if (p.splits > 1) {
     const size_t r = (size_t)c->total_new * q_heads * p.splits;
     p.part_ml = align_up(r * c->head_dim * sizeof(float), 256);
@@ -603,6 +624,7 @@ tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *
   g.negate = scale < 0.f;
   g.causal = causal, g.window = window;
   g.splits = p.splits;
+  g.split_tiles = p.split_tiles;
   while ((1 << g.page_log2) < c->page) ++g.page_log2;
   g.part = static_cast<float *>(ws);
   g.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.part_ml);

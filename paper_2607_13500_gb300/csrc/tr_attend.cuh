@@ -28,7 +28,8 @@ struct AttendArgs {
   float scale;      // |scale| log2(e), never zero
   int negate;       // scale < 0: the queries enter negated
   int causal, window;
-  int splits;       // parts of the key range, each a CTA's
+  int splits;       // parts of the keys, each a CTA's: split_tiles tiles (the last: the rest)
+  int split_tiles;
   float *part;      // splits > 1: [splits][total_new * q_heads][d] unnormalised sums,
   float2 *part_ml;  //             [splits][total_new * q_heads] (maximum, sum)
   int page_log2;
@@ -133,7 +134,7 @@ __device__ __forceinline__ bool finite4(const float4 &v) {
   return fabsf(v.x) <= FLT_MAX && fabsf(v.y) <= FLT_MAX && fabsf(v.z) <= FLT_MAX && fabsf(v.w) <= FLT_MAX;
 }
 template <typename T>
-__device__ __noinline__ bool hidden_values_finite(const AttendArgs &g, int seq, int hk, int lo, int hi) {
+__device__ __forceinline__ bool hidden_values_finite(const AttendArgs &g, int seq, int hk, int lo, int hi) {
   const int ch = 4 * (threadIdx.x & 31);
   bool ok = true;
   for (int j = lo; j < hi; ++j) {
@@ -145,7 +146,7 @@ __device__ __noinline__ bool hidden_values_finite(const AttendArgs &g, int seq, 
   return __all_sync(0xffffffffu, ok);
 }
 template <typename T>
-__device__ __noinline__ float4 row_by_warp(const AttendArgs &g, int seq, int hk, const char *q, int lo, int hi, float &m,
+__device__ __forceinline__ float4 row_by_warp(const AttendArgs &g, int seq, int hk, const char *q, int lo, int hi, float &m,
                                            float &l) {
   const int d = g.c.d, ch = 4 * (threadIdx.x & 31);
   const bool holds = ch < d;
