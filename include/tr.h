@@ -405,7 +405,8 @@ tr_status tr_project(const void *y, int32_t rows, int32_t d, const void *w, cons
  * tr_heads: rows of one projection, element [t, h, c] at
  * p + t * token_stride + h * head_stride + c (strides in elements; the
  * channels are contiguous), so slices of a fused q/k/v projection pass as
- * they are.  Bases are 16-byte aligned and strides multiples of 16 bytes.
+ * they are.  Bases are 16-byte aligned, strides multiples of 16 bytes and
+ * below 2^31 elements.
  */
 typedef struct {
   void *p;               /* device; NULL where the argument is optional and absent */

@@ -37,6 +37,7 @@
 #include <cuda_fp16.h>
 
 #include "tr_attend.cuh"
+#include "tr_pack.cuh"
 
 namespace tr {
 namespace {
@@ -61,33 +62,11 @@ struct Shape {
   static_assert(kStages >= 4, "two tiles in use and two on their way");
 };
 
-__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
-  unsigned long long r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 of_pair(unsigned long long v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
 __device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
   return r;
 }
-__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
-  unsigned long long r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
-  unsigned long long r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-
-// ---------------------------------------------------------------- the kernel
 template <typename T, int D, int MT>
 __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
     k_attend(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -345,16 +324,16 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
             sum *= f;
           }
           const float neg = mx == -INFINITY ? 0.f : -mx;  // a row that has seen nothing: exp2(-inf) = 0
-          const unsigned long long sc2 = pair_of(g.scale, g.scale), neg2 = pair_of(neg, neg);
-          unsigned long long acc[4] = {0ull, 0ull, 0ull, 0ull};
+          const pack::f2 sc2 = pack::make(g.scale, g.scale), neg2 = pack::make(neg, neg);
+          pack::f2 acc[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
           for (int i = 0; i < kTile; i += 2) {
-            const float2 e = of_pair(fma2(pair_of(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), sc2, neg2));
+            const float2 e = pack::split(pack::fma(pack::make(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), sc2, neg2));
             const float p0 = exp2_fast(e.x), p1 = exp2_fast(e.y);
-            acc[(i >> 1) & 3] = add2(acc[(i >> 1) & 3], pair_of(p0, p1));
+            acc[(i >> 1) & 3] = pack::add(acc[(i >> 1) & 3], pack::make(p0, p1));
             s[i >> 1] = Bits<T>::pack(p0, p1);
           }
-          const float2 x = of_pair(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])));
+          const float2 x = pack::split(pack::add(pack::add(acc[0], acc[1]), pack::add(acc[2], acc[3])));
           sum += x.x + x.y;
           tc::tmem_st32(s_col, s);
           tc::tmem_st32(s_col + 32, s + 32);

@@ -77,6 +77,7 @@ inline tr_status check_heads(const tr_heads *h, int es) {
   if (!h || !h->p || h->heads <= 0 || h->token_stride < 0 || h->head_stride < 0) return TR_ERR_ARG;
   if ((reinterpret_cast<uintptr_t>(h->p) & 15u) || (h->token_stride * es) % 16 || (h->head_stride * es) % 16)
     return TR_ERR_ALIGN;
+  if (h->token_stride > INT32_MAX || h->head_stride > INT32_MAX) return TR_ERR_UNSUPPORTED;  // the kernels multiply 32 x 32 bits
   return TR_OK;
 }
 

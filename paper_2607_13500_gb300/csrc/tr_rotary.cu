@@ -22,39 +22,50 @@
 
 #include "tr_cache.cuh"
 #include "tr_internal.cuh"
+#include "tr_pack.cuh"
 
 namespace tr {
 namespace {
 
 constexpr int kRotThreads = 256;
-constexpr int kMaxTokens = 8;                       // tokens of one CTA at most
-constexpr int kMaxTrig = kRotThreads;               // angles a CTA holds (tokens x frequencies)
+constexpr int kMaxTokens = 32;                      // tokens a CTA takes at a time at most
+constexpr int kMaxTrig = 4 * kRotThreads;           // angles it holds (tokens x frequencies)
+
+using pack::f2;
 
 struct Rows {
   const char *in;   // NULL: segment absent
   char *out;        // NULL: into the cache
-  long long in_tok, in_head, out_tok, out_head;  // elements
+  int in_tok, in_head, out_tok, out_head;  // elements
   int heads;
   const float *w;   // norm weight or NULL
   int turn;         // rows are rotated
   int cache;        // 0: out, 1: the cache's keys, 2: its values
+  int tokens;       // that a CTA takes at a time
+  int toks, rest;   // a step of one row per lane group: whole tokens, and heads
+  int cta0;         // first CTA of the segment
 };
 
 struct RotArgs {
   const unsigned long long *turns;
   const int32_t *axis;
   const int32_t *pos;
-  int d, half, axes, tokens, tokens_per_cta;
+  int d, half, axes, tokens;
   int lanes_log2;   // lanes of a row's group
   int slots;        // lanes of it that hold channels: d / (2 V)
+  int trig_toks, trig_rest;  // a step of kRotThreads angles
   float sign;       // -1 turns backwards
-  float eps;
+  float eps, inv_d;
   Rows seg[3];      // queries, keys, values
   CacheView cache;
   int32_t *err;
 };
 
 // ---------------------------------------------------------------- elements
+template <typename T>
+__device__ __forceinline__ long long row_bytes(int tok, int tok_stride, int head, int head_stride) {
+  return (long long)sizeof(T) * ((long long)tok * tok_stride + (long long)head * head_stride);
+}
 template <typename T>
 __device__ __forceinline__ float2 unpack2(uint32_t v);
 template <>
@@ -100,27 +111,47 @@ struct Chunk {
     else
       *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
   }
-  __device__ __forceinline__ void get(float (&f)[V]) const {
+  __device__ __forceinline__ void get(f2 (&f)[V / 2]) const {
 #pragma unroll
-    for (int i = 0; i < V / (4 / (int)sizeof(T)); ++i) {
+    for (int i = 0; i < V / 2; ++i) {
       if constexpr (sizeof(T) == 4) {
-        f[i] = __uint_as_float(w[i]);
+        f[i] = pack::make(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
       } else {
         const float2 t = unpack2<T>(w[i]);
-        f[2 * i] = t.x, f[2 * i + 1] = t.y;
+        f[i] = pack::make(t.x, t.y);
       }
     }
   }
-  __device__ __forceinline__ void set(const float (&f)[V]) {
+  __device__ __forceinline__ void set(const f2 (&f)[V / 2]) {
 #pragma unroll
-    for (int i = 0; i < V / (4 / (int)sizeof(T)); ++i) {
+    for (int i = 0; i < V / 2; ++i) {
+      const float2 t = pack::split(f[i]);
       if constexpr (sizeof(T) == 4)
-        w[i] = __float_as_uint(f[i]);
+        w[2 * i] = __float_as_uint(t.x), w[2 * i + 1] = __float_as_uint(t.y);
       else
-        w[i] = pack2<T>(f[2 * i], f[2 * i + 1]);
+        w[i] = pack2<T>(t.x, t.y);
     }
   }
 };
+
+// 2 V floats of a vector at the slot's channels, as pairs.
+template <int V>
+__device__ __forceinline__ void get_weights(const float *w, int a, int b, f2 (&wa)[V / 2], f2 (&wb)[V / 2]) {
+#pragma unroll
+  for (int i = 0; i < V; i += 4) {
+    const float4 x = __ldg(reinterpret_cast<const float4 *>(w + a + i)), y = __ldg(reinterpret_cast<const float4 *>(w + b + i));
+    wa[i / 2] = pack::make(x.x, x.y), wa[i / 2 + 1] = pack::make(x.z, x.w);
+    wb[i / 2] = pack::make(y.x, y.y), wb[i / 2 + 1] = pack::make(y.z, y.w);
+  }
+}
+
+// Sum over the 2^log2 lanes of a row's group.
+__device__ __forceinline__ float group_sum(float v, int log2) {
+#pragma unroll
+  for (int i = 0; i < 5; ++i)
+    if (i < log2) v += __shfl_xor_sync(0xffffffffu, v, 1 << i);
+  return v;
+}
 
 // The slot's two chunks: first halves and second halves of V pairs
 // (TR_ROTARY_HALF), or 2 V neighbouring channels (TR_ROTARY_PAIRS, and the
@@ -143,26 +174,54 @@ __device__ __forceinline__ SlotPlace slot_place(int slot, int half) {
   return p;
 }
 
-// Turns the slot's pairs in place by (c, s); with PAIRS a pair is two
-// neighbours of the 2 V channels, else the same place in both chunks.
+// Turns the slot's pairs in place by V angles (16-byte aligned in shared
+// memory); with PAIRS a pair is two neighbours of the 2 V channels, else the
+// same place in both chunks.
 template <int V, bool PAIRS>
-__device__ __forceinline__ void turn(float (&x)[V], float (&y)[V], const float *c, const float *s) {
+__device__ __forceinline__ void turn(f2 (&x)[V / 2], f2 (&y)[V / 2], const float *cs, const float *sn) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    float &a = PAIRS ? (2 * i < V ? x[2 * i % V] : y[2 * i % V]) : x[i];
-    float &b = PAIRS ? (2 * i < V ? x[(2 * i + 1) % V] : y[(2 * i + 1) % V]) : y[i];
-    const float a0 = a, b0 = b;
-    a = a0 * c[i] - b0 * s[i];
-    b = b0 * c[i] + a0 * s[i];
+  for (int j = 0; j < V; j += 4) {
+    const float4 c = *reinterpret_cast<const float4 *>(cs + j), s = *reinterpret_cast<const float4 *>(sn + j);
+    if (PAIRS) {
+      const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        f2 &v = j + k < V / 2 ? x[(j + k) % (V / 2)] : y[(j + k) % (V / 2)];
+        const float2 t = pack::split(v);
+        v = pack::fma(v, pack::make(cc[k], cc[k]), pack::mul(pack::make(t.y, t.x), pack::make(-ss[k], ss[k])));
+      }
+    } else {
+      const f2 c2[2] = {pack::make(c.x, c.y), pack::make(c.z, c.w)}, s2[2] = {pack::make(s.x, s.y), pack::make(s.z, s.w)};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const f2 a = x[j / 2 + k], b = y[j / 2 + k];
+        x[j / 2 + k] = pack::sub(pack::mul(a, c2[k]), pack::mul(b, s2[k]));
+        y[j / 2 + k] = pack::fma(b, c2[k], pack::mul(a, s2[k]));
+      }
+    }
   }
 }
+
+// A group's walk over the rows (token, head) of its CTA, `groups` rows on
+// each time.
+struct RowWalk {
+  int tok, head;
+  __device__ __forceinline__ RowWalk(int r, int heads) : tok(r < heads ? 0 : r / heads), head(r - tok * heads) {}
+  __device__ __forceinline__ void step(int toks, int rest, int heads) {
+    tok += toks;
+    head += rest;
+    if (head >= heads) head -= heads, ++tok;
+  }
+};
 
 // Cosines and sines of the CTA's tokens into shared memory.  position *
 // turns modulo 2^64 is the angle as a fraction of a turn, exactly; its top 32
 // bits, signed, are the angle in units of pi / 2^31.
 __device__ __forceinline__ void fill_trig(const RotArgs &g, int t0, int nt, float *cs, float *sn) {
-  for (int i = threadIdx.x; i < nt * g.half; i += kRotThreads) {
-    const int lt = i / g.half, f = i - lt * g.half;
+  if (!g.half) return;
+  RowWalk w(threadIdx.x, g.half);
+  for (int i = threadIdx.x; i < nt * g.half; i += kRotThreads, w.step(g.trig_toks, g.trig_rest, g.half)) {
+    const int lt = w.tok, f = w.head;
     const int ax = __ldg(g.axis + f);
     const long long p = (unsigned)ax < (unsigned)g.axes ? (long long)__ldg(g.pos + (long long)ax * g.tokens + t0 + lt) : 0;
     const unsigned long long frac = (unsigned long long)p * __ldg(g.turns + f);
@@ -173,103 +232,119 @@ __device__ __forceinline__ void fill_trig(const RotArgs &g, int t0, int nt, floa
   }
 }
 
+// Two (normed) or four rows per lane group in flight, the first asked for
+// before the angles: a CTA has few rows per group, so the latency of its
+// first loads would otherwise stand alone.
+// Rows of all three segments in one CTA took three times the instructions
+// (which segment, whose weight, where to): 6272 tokens x 32 normed heads 26.3
+// us, issue-bound, against what the host part's comment gives.
 template <typename T, int V, bool PAIRS, bool NORM>
-__global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ RotArgs g) {
+__global__ void __launch_bounds__(kRotThreads, V == 8 ? 3 : 4) k_rotate(const __grid_constant__ RotArgs g) {
   __shared__ __align__(16) float cs[kMaxTrig], sn[kMaxTrig];
   __shared__ long long home[kMaxTokens];  // the token's first key row in the cache (head 0), or -1
   pdl_wait();  // q, k, v come from the kernel before
-  const int t0 = blockIdx.x * g.tokens_per_cta;
-  const int nt = min(g.tokens_per_cta, g.tokens - t0);
-  fill_trig(g, t0, nt, cs, sn);
-  if (g.cache.k && (int)threadIdx.x < nt) {
-    const NewToken at = find_token(g.cache, t0 + threadIdx.x);
-    long long row = -1;
-    if (at.seq >= 0 && at.key >= 0) {
-      const int page = page_of(g.cache, at.seq, at.key);
-      if (page >= 0)
-        row = (long long)page * g.cache.heads * g.cache.page + (at.key & (g.cache.page - 1));
-      else if (g.err)
-        atomicOr(g.err, TR_CACHE_ERR_PAGE);
-    } else if (at.seq >= 0 && g.err) {
-      atomicOr(g.err, TR_CACHE_ERR_PAGE);
-    }
-    home[threadIdx.x] = row;
-  }
-  __syncthreads();
+  const int sg = (int)blockIdx.x < g.seg[1].cta0 ? 0 : (int)blockIdx.x < g.seg[2].cta0 ? 1 : 2;
+  const Rows &s = sg == 0 ? g.seg[0] : sg == 1 ? g.seg[1] : g.seg[2];
+  const int heads = s.heads, t0 = (blockIdx.x - s.cta0) * s.tokens;
+  const int nt = min(s.tokens, g.tokens - t0), rows = nt * heads;
   const int slot = threadIdx.x & ((1 << g.lanes_log2) - 1);
   const int group = threadIdx.x >> g.lanes_log2, groups = kRotThreads >> g.lanes_log2;
   const bool holds = slot < g.slots;
   const SlotPlace at = slot_place<V, PAIRS>(slot, g.half);
-  const int q_heads = g.seg[0].heads, k_heads = g.seg[1].heads;
-  const int heads = q_heads + k_heads + g.seg[2].heads;
-  const int rows = nt * heads;
-  constexpr int kU = 2;  // rows in flight per group
-  for (int r0 = 0; r0 < rows; r0 += kU * groups) {  // the same trips for every lane of a warp
-    Chunk<T, V> ca[kU], cb[kU];
-    int tok[kU], head[kU], which[kU];
-    bool live[kU];
+  const char *src = s.in + (long long)sizeof(T) * ((long long)t0 * s.in_tok + at.a);
+  const int ab = (int)sizeof(T) * (at.b - at.a);
+  constexpr int kU = NORM ? 2 : 4;
+  Chunk<T, V> na[kU], nb[kU];
+  RowWalk ahead(group, heads);
+  auto ask = [&]() {
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      const int r = r0 + u * groups + group;
-      live[u] = holds && r < rows;
-      tok[u] = r / heads;
-      int h = r - tok[u] * heads;
-      which[u] = h < q_heads ? 0 : h < q_heads + k_heads ? 1 : 2;
-      head[u] = which[u] == 0 ? h : which[u] == 1 ? h - q_heads : h - q_heads - k_heads;
-      if (live[u]) {
-        const Rows &s = g.seg[which[u]];
-        const char *src =
-            s.in + (long long)sizeof(T) * ((long long)(t0 + tok[u]) * s.in_tok + (long long)head[u] * s.in_head);
-        ca[u].load(src + sizeof(T) * at.a);
-        cb[u].load(src + sizeof(T) * at.b);
+      if (holds && ahead.tok < nt) {
+        const char *p = src + row_bytes<T>(ahead.tok, s.in_tok, ahead.head, s.in_head);
+        na[u].load(p);
+        nb[u].load(p + ab);
+      }
+      ahead.step(s.toks, s.rest, heads);
+    }
+  };
+  ask();
+  if (s.turn) fill_trig(g, t0, nt, cs, sn);
+  if (s.cache) {  // a warp per token
+    const int lane = threadIdx.x & 31;
+    for (int i = threadIdx.x >> 5; i < nt; i += kRotThreads / 32) {
+      const int t = t0 + i;
+      int b = -1;  // the last sequence that starts at or before the token
+      for (int i0 = 0; i0 < g.cache.batch; i0 += 32) {
+        const bool before = i0 + lane < g.cache.batch && __ldg(g.cache.cu_new + i0 + lane) <= t;
+        const unsigned m = __ballot_sync(0xffffffffu, before);
+        b += __popc(m);
+        if (m != 0xffffffffu) break;
+      }
+      if (lane == 0) {
+        long long row = -1;
+        const int end = b >= 0 ? __ldg(g.cache.cu_new + b + 1) : 0;
+        if (t < end) {
+          const int key = max(__ldg(g.cache.lens + b), 0) - end + t;
+          const int page = key >= 0 ? page_of(g.cache, b, key) : -1;
+          if (page >= 0)
+            row = (long long)page * g.cache.heads * g.cache.page + (key & (g.cache.page - 1));
+          else if (g.err)
+            atomicOr(g.err, TR_CACHE_ERR_PAGE);
+        }
+        home[i] = row;
       }
     }
+  }
+  f2 wa[V / 2] = {}, wb[V / 2] = {};
+  if (NORM && s.w && holds) get_weights<V>(s.w, at.a, at.b, wa, wb);
+  __syncthreads();
+  RowWalk now(group, heads);
+  for (int r0 = 0; r0 < rows; r0 += kU * groups) {  // the same trips for every lane of a warp
+    if (r0) ask();
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      const Rows &s = g.seg[which[u]];
-      if (NORM || s.turn) {
-        float x[V], y[V];
-        ca[u].get(x);
-        cb[u].get(y);
-        if (NORM) {
-          float ss = 0.f;
-          if (live[u]) {
+      const bool live = holds && now.tok < nt;
+      if (s.w || s.turn) {  // (values pass bit for bit)
+        f2 x[V / 2], y[V / 2];
+        na[u].get(x);
+        nb[u].get(y);
+        if (NORM && s.w) {
+          f2 s2 = 0ull;
 #pragma unroll
-            for (int i = 0; i < V; ++i) ss += x[i] * x[i] + y[i] * y[i];
-          }
-          for (int o = 1 << g.lanes_log2 >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-          if (s.w && live[u]) {
-            const float r = rsqrtf(ss / (float)g.d + g.eps);
+          for (int i = 0; i < V / 2; ++i) s2 = pack::fma(x[i], x[i], pack::fma(y[i], y[i], s2));
+          const float2 t = pack::split(s2);
+          float ss = live ? t.x + t.y : 0.f;
+          ss = group_sum(ss, g.lanes_log2);
+          const float f = rsqrtf(ss * g.inv_d + g.eps);
+          const f2 f2f = pack::make(f, f);
 #pragma unroll
-            for (int i = 0; i < V; i += 4) {
-              const float4 wa = __ldg(reinterpret_cast<const float4 *>(s.w + at.a + i));
-              const float4 wb = __ldg(reinterpret_cast<const float4 *>(s.w + at.b + i));
-              x[i] *= r * wa.x, x[i + 1] *= r * wa.y, x[i + 2] *= r * wa.z, x[i + 3] *= r * wa.w;
-              y[i] *= r * wb.x, y[i + 1] *= r * wb.y, y[i + 2] *= r * wb.z, y[i + 3] *= r * wb.w;
-            }
+          for (int i = 0; i < V / 2; ++i) {
+            x[i] = pack::mul(x[i], pack::mul(f2f, wa[i]));
+            y[i] = pack::mul(y[i], pack::mul(f2f, wb[i]));
           }
         }
-        if (live[u]) {
-          if (s.turn && at.turns) turn<V, PAIRS>(x, y, cs + tok[u] * g.half + slot * V, sn + tok[u] * g.half + slot * V);
-          if (s.turn || s.w) {  // values pass bit for bit
-            ca[u].set(x);
-            cb[u].set(y);
-          }
-        }
+        if (live && s.turn && at.turns)
+          turn<V, PAIRS>(x, y, cs + now.tok * g.half + slot * V, sn + now.tok * g.half + slot * V);
+        na[u].set(x);
+        nb[u].set(y);
       }
-      if (live[u]) {
+      if (live) {
         char *dst;
+        bool there = true;
         if (s.cache == 0) {
-          dst = s.out + (long long)sizeof(T) * ((long long)(t0 + tok[u]) * s.out_tok + (long long)head[u] * s.out_head);
+          dst = s.out + row_bytes<T>(t0 + now.tok, s.out_tok, now.head, s.out_head);
         } else {
-          const long long row = home[tok[u]];
-          if (row < 0) continue;
+          const long long row = home[now.tok];
+          there = row >= 0;
           dst = static_cast<char *>(s.cache == 1 ? g.cache.k : g.cache.v) +
-                (long long)sizeof(T) * (row + (long long)head[u] * g.cache.page) * g.d;
+                (long long)sizeof(T) * ((row + now.head * g.cache.page) * g.d);
         }
-        ca[u].store(dst + sizeof(T) * at.a);
-        cb[u].store(dst + sizeof(T) * at.b);
+        if (there) {
+          na[u].store(dst + sizeof(T) * at.a);
+          nb[u].store(dst + sizeof(T) * at.b);
+        }
       }
+      now.step(s.toks, s.rest, heads);
     }
   }
 }
@@ -278,132 +353,131 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
 struct RotBackArgs {
   RotArgs g;          // seg[].in = dy, seg[].out = dx
   const char *x[2];   // the forward inputs
-  long long x_tok[2], x_head[2];
-  float *part;        // [CTAs][2][d]
-  int ctas;
+  int x_tok[2], x_head[2];
+  float *part;        // [CTAs][d]
+  int ctas, q_ctas;   // the first q_ctas take the queries' rows, the others the keys'
 };
 
-// The weights' gradients stay in registers (a lane's channels never change)
-// over all the rows a CTA takes, are summed over its groups once at the end
-// and leave as one row per CTA and weight; k_rotate_weight_sum adds those in
-// a fixed order.
+// A CTA takes the rows of one of the two segments, so that a lane's weights
+// and its share of their gradients (its channels never change) stay in
+// registers over all of them; the gradients are summed over the CTA once at
+// the end and leave as one row per CTA, which k_rotate_weight_sum adds in a
+// fixed order.  The next row is asked for before the present one is worked
+// on.
 template <typename T, int V, bool PAIRS>
-__global__ void __launch_bounds__(kRotThreads) k_rotate_back(const __grid_constant__ RotBackArgs a) {
+__global__ void __launch_bounds__(kRotThreads, 2) k_rotate_back(const __grid_constant__ RotBackArgs a) {
   __shared__ __align__(16) float cs[kMaxTrig], sn[kMaxTrig];
   __shared__ float sums[kRotThreads / 32][TR_ROTARY_MAX_DIM];
   const RotArgs &g = a.g;
   pdl_wait();
+  const int sg = (int)blockIdx.x < a.q_ctas ? 0 : 1;
+  const int cta = sg ? blockIdx.x - a.q_ctas : blockIdx.x, ctas = sg ? a.ctas - a.q_ctas : a.q_ctas;
+  const Rows &s = sg ? g.seg[1] : g.seg[0];
+  const bool normed = s.w != nullptr;
   const int slot = threadIdx.x & ((1 << g.lanes_log2) - 1);
   const int group = threadIdx.x >> g.lanes_log2, groups = kRotThreads >> g.lanes_log2;
   const bool holds = slot < g.slots;
   const SlotPlace at = slot_place<V, PAIRS>(slot, g.half);
-  float wa[2][V], wb[2][V], da[2][V], db[2][V];
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const bool have = holds && g.seg[s].w;
-      wa[s][i] = have ? __ldg(g.seg[s].w + at.a + i) : 0.f;
-      wb[s][i] = have ? __ldg(g.seg[s].w + at.b + i) : 0.f;
-      da[s][i] = db[s][i] = 0.f;
-    }
-  for (int t0 = blockIdx.x * g.tokens_per_cta; t0 < g.tokens; t0 += gridDim.x * g.tokens_per_cta) {
-    const int nt = min(g.tokens_per_cta, g.tokens - t0);
+  f2 wa[V / 2] = {}, wb[V / 2] = {}, da[V / 2] = {}, db[V / 2] = {};
+  if (normed && holds) get_weights<V>(s.w, at.a, at.b, wa, wb);
+  Chunk<T, V> ga, gb, xa, xb;
+  const int heads = s.heads, toks = s.toks, rest = s.rest;
+  for (int t0 = cta * s.tokens; t0 < g.tokens; t0 += ctas * s.tokens) {
+    const int nt = min(s.tokens, g.tokens - t0), rows = nt * heads;
+    RowWalk ahead(group, heads), now = ahead;
+    auto ask = [&]() {
+      const int tok = ahead.tok, head = ahead.head;
+      ahead.step(toks, rest, heads);
+      if (!holds || tok >= nt) return;
+      const char *src = s.in + row_bytes<T>(t0 + tok, s.in_tok, head, s.in_head);
+      ga.load(src + sizeof(T) * at.a);
+      gb.load(src + sizeof(T) * at.b);
+      if (normed) {
+        const char *xs = (sg ? a.x[1] : a.x[0]) + row_bytes<T>(t0 + tok, sg ? a.x_tok[1] : a.x_tok[0], head,
+                                                               sg ? a.x_head[1] : a.x_head[0]);
+        xa.load(xs + sizeof(T) * at.a);
+        xb.load(xs + sizeof(T) * at.b);
+      }
+    };
+    ask();
     __syncthreads();  // the last tokens' angles are used up
     fill_trig(g, t0, nt, cs, sn);
     __syncthreads();
+    for (int r0 = 0; r0 < rows; r0 += groups) {
+      const int tok = now.tok, head = now.head;
+      const bool live = holds && tok < nt;
+      now.step(toks, rest, heads);
+      f2 x[V / 2], y[V / 2], p[V / 2], q[V / 2];
+      ga.get(p);
+      gb.get(q);
+      xa.get(x);
+      xb.get(y);
+      ask();
+      if (live && at.turns) turn<V, PAIRS>(p, q, cs + tok * g.half + slot * V, sn + tok * g.half + slot * V);
+      if (normed) {
+        f2 s2 = 0ull, d2 = 0ull;
 #pragma unroll
-    for (int sg = 0; sg < 2; ++sg) {
-      const Rows &s = g.seg[sg];
-      const int rows = nt * s.heads;
-      for (int r0 = 0; r0 < rows; r0 += groups) {
-        const int r = r0 + group;
-        const bool live = holds && r < rows;
-        const int tok = live ? r / s.heads : 0, head = live ? r - tok * s.heads : 0;
-        Chunk<T, V> ga, gb, xa, xb;
-        float x[V], y[V], p[V], q[V];
-        float ss = 0.f, dot = 0.f;
+        for (int i = 0; i < V / 2; ++i) {
+          s2 = pack::fma(x[i], x[i], pack::fma(y[i], y[i], s2));
+          d2 = pack::fma(x[i], pack::mul(wa[i], p[i]), pack::fma(y[i], pack::mul(wb[i], q[i]), d2));
+        }
+        const float2 st = pack::split(s2), dt = pack::split(d2);
+        float ss = live ? st.x + st.y : 0.f, dot = live ? dt.x + dt.y : 0.f;
+        ss = group_sum(ss, g.lanes_log2);
+        dot = group_sum(dot, g.lanes_log2);
         if (live) {
-          const char *src = s.in + (long long)sizeof(T) * ((long long)(t0 + tok) * s.in_tok + (long long)head * s.in_head);
-          ga.load(src + sizeof(T) * at.a);
-          gb.load(src + sizeof(T) * at.b);
-          if (s.w) {
-            const char *xs = a.x[sg] +
-                             (long long)sizeof(T) * ((long long)(t0 + tok) * a.x_tok[sg] + (long long)head * a.x_head[sg]);
-            xa.load(xs + sizeof(T) * at.a);
-            xb.load(xs + sizeof(T) * at.b);
-          }
-          ga.get(p);
-          gb.get(q);
-          if (at.turns) turn<V, PAIRS>(p, q, cs + tok * g.half + slot * V, sn + tok * g.half + slot * V);
-          if (s.w) {
-            xa.get(x);
-            xb.get(y);
+          const float r1 = rsqrtf(ss * g.inv_d + g.eps);
+          const float k = r1 * r1 * r1 * (dot * g.inv_d);
+          const f2 r2 = pack::make(r1, r1), k2 = pack::make(k, k);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-              ss += x[i] * x[i] + y[i] * y[i];
-              dot += x[i] * (wa[sg][i] * p[i]) + y[i] * (wb[sg][i] * q[i]);
-            }
+          for (int i = 0; i < V / 2; ++i) {
+            da[i] = pack::fma(p[i], pack::mul(x[i], r2), da[i]);
+            db[i] = pack::fma(q[i], pack::mul(y[i], r2), db[i]);
+            p[i] = pack::sub(pack::mul(r2, pack::mul(wa[i], p[i])), pack::mul(x[i], k2));
+            q[i] = pack::sub(pack::mul(r2, pack::mul(wb[i], q[i])), pack::mul(y[i], k2));
           }
         }
-        if (s.w) {
-          for (int o = 1 << g.lanes_log2 >> 1; o; o >>= 1) {
-            ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            dot += __shfl_xor_sync(0xffffffffu, dot, o);
-          }
-          if (live) {
-            const float r1 = rsqrtf(ss / (float)g.d + g.eps);
-            const float k = r1 * r1 * r1 * (dot / (float)g.d);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-              da[sg][i] += p[i] * (x[i] * r1);
-              db[sg][i] += q[i] * (y[i] * r1);
-              p[i] = r1 * (wa[sg][i] * p[i]) - x[i] * k;
-              q[i] = r1 * (wb[sg][i] * q[i]) - y[i] * k;
-            }
-          }
-        }
-        if (live) {
-          ga.set(p);
-          gb.set(q);
-          char *dst = s.out + (long long)sizeof(T) * ((long long)(t0 + tok) * s.out_tok + (long long)head * s.out_head);
-          ga.store(dst + sizeof(T) * at.a);
-          gb.store(dst + sizeof(T) * at.b);
-        }
+      }
+      if (live) {
+        Chunk<T, V> oa, ob;
+        oa.set(p);
+        ob.set(q);
+        char *dst = s.out + row_bytes<T>(t0 + tok, s.out_tok, head, s.out_head);
+        oa.store(dst + sizeof(T) * at.a);
+        ob.store(dst + sizeof(T) * at.b);
       }
     }
   }
+  if (!normed) return;
   // over the groups of each warp by shuffles, over the warps through shared memory
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
-  for (int sg = 0; sg < 2; ++sg) {
-    if (!g.seg[sg].w) continue;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      for (int o = 1 << g.lanes_log2; o < 32; o <<= 1) {
-        da[sg][i] += __shfl_xor_sync(0xffffffffu, da[sg][i], o);
-        db[sg][i] += __shfl_xor_sync(0xffffffffu, db[sg][i], o);
-      }
-    __syncthreads();
-    if (holds && lane < 1 << g.lanes_log2)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        sums[warp][at.a + i] = da[sg][i];
-        sums[warp][at.b + i] = db[sg][i];
-      }
-    __syncthreads();
-    if ((int)threadIdx.x < g.d) {
-      float t = 0.f;
-#pragma unroll
-      for (int w = 0; w < kRotThreads / 32; ++w) t += sums[w][threadIdx.x];
-      a.part[((long long)blockIdx.x * 2 + sg) * g.d + threadIdx.x] = t;
+  for (int i = 0; i < V / 2; ++i) {
+    float2 u = pack::split(da[i]), v = pack::split(db[i]);
+    for (int o = 1 << g.lanes_log2; o < 32; o <<= 1) {
+      u.x += __shfl_xor_sync(0xffffffffu, u.x, o);
+      u.y += __shfl_xor_sync(0xffffffffu, u.y, o);
+      v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+      v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
     }
+    if (holds && lane < 1 << g.lanes_log2) {
+      sums[warp][at.a + 2 * i] = u.x, sums[warp][at.a + 2 * i + 1] = u.y;
+      sums[warp][at.b + 2 * i] = v.x, sums[warp][at.b + 2 * i + 1] = v.y;
+    }
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < g.d) {
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRotThreads / 32; ++w) t += sums[w][threadIdx.x];
+    a.part[(long long)blockIdx.x * g.d + threadIdx.x] = t;
   }
 }
 
 // dw[c] = the sum of the CTAs' rows: 1024 / 32 slices of rows for 32 channels
 // per CTA, each slice in order, then the slices in order.
-__global__ void __launch_bounds__(1024) k_rotate_weight_sum(const float *part, int ctas, int d, float *dq, float *dk) {
+__global__ void __launch_bounds__(1024)
+    k_rotate_weight_sum(const float *part, int q_ctas, int ctas, int d, float *dq, float *dk) {
   __shared__ float sums[32][33];
   pdl_wait();
   const int sg = blockIdx.y, c = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5;
@@ -411,7 +485,7 @@ __global__ void __launch_bounds__(1024) k_rotate_weight_sum(const float *part, i
   if (!out) return;
   float t = 0.f;
   if (c < d)
-    for (int i = slice; i < ctas; i += 32) t += part[((long long)i * 2 + sg) * d + c];
+    for (int i = (sg ? q_ctas : 0) + slice; i < (sg ? ctas : q_ctas); i += 32) t += part[(long long)i * d + c];
   sums[slice][threadIdx.x & 31] = t;
   __syncthreads();
   if (slice == 0 && c < d) {
@@ -443,29 +517,60 @@ int pairs_per_lane(int dtype, int d, int rot) {
 void shape(RotArgs &g, int dtype, int d, int rot, int tokens) {
   const int v = pairs_per_lane(dtype, d, rot);
   g.d = d;
+  g.inv_d = 1.f / (float)d;
   g.half = rot / 2;
   g.tokens = tokens;
   g.slots = d / (2 * v);
   g.lanes_log2 = 0;
   while ((1 << g.lanes_log2) < g.slots) ++g.lanes_log2;
-  // A few tokens a CTA share the angles' cost and keep every thread busy
-  // with them; fewer when the GPU would not be filled.
-  const int sms = sm_count();
-  int per = kMaxTrig / (g.half > 32 ? g.half : 32);
-  if (per > kMaxTokens) per = kMaxTokens;
-  const int fill = sms > 0 ? tokens / (4 * sms) : 1;
-  g.tokens_per_cta = fill < 1 ? 1 : fill < per ? fill : per;
+  if (g.half) g.trig_toks = kRotThreads / g.half, g.trig_rest = kRotThreads % g.half;
+}
+
+void set_steps(RotArgs &g) {
+  const int groups = kRotThreads >> g.lanes_log2;
+  for (Rows &s : g.seg)
+    if (s.heads) s.toks = groups / s.heads, s.rest = groups % s.heads;
+}
+
+// The tokens that a CTA takes of each segment: four rows for every lane
+// group, all asked for at once (12288 tokens x 64 heads: 65 us, with sixteen
+// 82 us), eight where they are normed, so that what a CTA costs besides its
+// rows (addresses, weights) is spread over more; fewer when the three CTAs an
+// SM holds would not all get some, and within the room for angles.  Returns
+// the CTAs of all segments.
+int cut_segments(RotArgs &g) {
+  const bool norm = g.seg[0].w || g.seg[1].w;
+  const int sms = sm_count() > 0 ? sm_count() : 1, groups = kRotThreads >> g.lanes_log2;
+  int room = g.half ? kMaxTrig / g.half : kMaxTokens;
+  if (room > kMaxTokens) room = kMaxTokens;
+  long long all = 0;
+  for (int i = 0; i < 3; ++i) all += (long long)g.tokens * g.seg[i].heads;
+  long long rows = all / (3 * sms);
+  if (rows < groups) rows = groups;
+  const int most = norm ? 8 * groups : 4 * groups;
+  if (rows > most) rows = most;
+  set_steps(g);
+  int ctas = 0;
+  for (int i = 0; i < 3; ++i) {
+    Rows &s = g.seg[i];
+    s.cta0 = ctas;
+    if (!s.in) continue;
+    const long long n = rows / s.heads;
+    s.tokens = n < 1 ? 1 : n > room ? room : (int)n;
+    ctas += (g.tokens + s.tokens - 1) / s.tokens;
+  }
+  return ctas;
 }
 
 template <typename T, int V, bool PAIRS>
-cudaError_t launch_rotate_t(const RotArgs &g, cudaStream_t st) {
-  const dim3 grid((g.tokens + g.tokens_per_cta - 1) / g.tokens_per_cta);
-  const bool norm = g.seg[0].w || g.seg[1].w;
-  return norm ? launch_kernel(k_rotate<T, V, PAIRS, true>, grid, dim3(kRotThreads), 0, st, false, g)
-              : launch_kernel(k_rotate<T, V, PAIRS, false>, grid, dim3(kRotThreads), 0, st, false, g);
+cudaError_t launch_rotate_t(RotArgs &g, cudaStream_t st) {
+  const int ctas = cut_segments(g);
+  return g.seg[0].w || g.seg[1].w
+             ? launch_kernel(k_rotate<T, V, PAIRS, true>, dim3(ctas), dim3(kRotThreads), 0, st, false, g)
+             : launch_kernel(k_rotate<T, V, PAIRS, false>, dim3(ctas), dim3(kRotThreads), 0, st, false, g);
 }
 
-cudaError_t launch_rotate(const RotArgs &g, int dtype, int rot, int layout, cudaStream_t st) {
+cudaError_t launch_rotate(RotArgs &g, int dtype, int rot, int layout, cudaStream_t st) {
   const bool wide = pairs_per_lane(dtype, g.d, rot) == 8, pairs = layout == TR_ROTARY_PAIRS;
   if (dtype == TR_F32) return pairs ? launch_rotate_t<float, 4, true>(g, st) : launch_rotate_t<float, 4, false>(g, st);
   if (dtype == TR_BF16) {
@@ -497,13 +602,13 @@ Rows rows_of(const tr_heads *in, const tr_heads *out, const float *w, int turn, 
   Rows r{};
   if (!in || !in->p) return r;
   r.in = static_cast<const char *>(in->p);
-  r.in_tok = in->token_stride;
-  r.in_head = in->head_stride;
+  r.in_tok = (int)in->token_stride;
+  r.in_head = (int)in->head_stride;
   r.heads = in->heads;
   if (out) {
     r.out = static_cast<char *>(out->p);
-    r.out_tok = out->token_stride;
-    r.out_head = out->head_stride;
+    r.out_tok = (int)out->token_stride;
+    r.out_head = (int)out->head_stride;
   }
   r.w = w;
   r.turn = turn;
@@ -522,10 +627,11 @@ tr_status check_pair(const tr_heads *in, const tr_heads *out, const float *w, in
   return rc;
 }
 
-int back_ctas(int tokens) {
+// CTAs of the backward pass: one wave of two per SM, at least one for each
+// segment.
+int back_ctas() {
   const int sms = sm_count();
-  const int most = 4 * (sms > 0 ? sms : 1);  // four resident CTAs per SM
-  return tokens < most ? tokens : most;
+  return 2 * (sms > 0 ? sms : 1);
 }
 
 }  // namespace
@@ -576,7 +682,7 @@ tr_status tr_rotary_apply(const tr_rotary *r, int32_t dtype, int32_t tokens, con
 
 size_t tr_rotary_backward_workspace_bytes(const tr_rotary *r, int32_t tokens) {
   if (check_rotary(r) != TR_OK || tokens < 0) return 0;
-  return align_up((size_t)back_ctas(tokens) * 2 * r->head_dim * sizeof(float), 256);
+  return align_up((size_t)back_ctas() * r->head_dim * sizeof(float), 256);
 }
 
 tr_status tr_rotary_backward(const tr_rotary *r, int32_t dtype, int32_t tokens, const int32_t *pos,
@@ -628,13 +734,28 @@ tr_status tr_rotary_backward(const tr_rotary *r, int32_t dtype, int32_t tokens, 
   g.seg[1] = rows_of(dk, dk_out, k_weight, 1, 0);
   if (!norm)  // a rotation's gradient is the rotation back
     return launch_rotate(g, dtype, r->rot_dim, r->layout, st) == cudaSuccess ? TR_OK : TR_ERR_CUDA;
-  a.ctas = back_ctas(tokens);
+  // tokens a CTA takes at a time: as many as the angles' room holds, fewer
+  // when the CTAs would not all get some
+  const int q_heads = g.seg[0].heads, k_heads = g.seg[1].heads;
+  a.ctas = back_ctas();
+  a.q_ctas = k_heads ? (int)((long long)a.ctas * q_heads / (q_heads + k_heads)) : a.ctas;
+  if (a.q_ctas < 1) a.q_ctas = 1;
+  if (k_heads && a.q_ctas == a.ctas) --a.q_ctas;
+  int per = g.half ? kMaxTrig / g.half : kMaxTokens;
+  if (per > kMaxTokens) per = kMaxTokens;
+  for (int i = 0; i < 2; ++i) {
+    // equal rounds: n tokens for each CTA in as few rounds as the room allows
+    const int ctas = i ? (a.ctas - a.q_ctas > 0 ? a.ctas - a.q_ctas : 1) : a.q_ctas;
+    const int n = (tokens + ctas - 1) / ctas, rounds = (n + per - 1) / per;
+    g.seg[i].tokens = (n + rounds - 1) / rounds;
+  }
   a.part = static_cast<float *>(ws);
-  if (q_weight) a.x[0] = static_cast<const char *>(q->p), a.x_tok[0] = q->token_stride, a.x_head[0] = q->head_stride;
-  if (k_weight) a.x[1] = static_cast<const char *>(k->p), a.x_tok[1] = k->token_stride, a.x_head[1] = k->head_stride;
+  set_steps(g);
+  if (q_weight) a.x[0] = static_cast<const char *>(q->p), a.x_tok[0] = (int)q->token_stride, a.x_head[0] = (int)q->head_stride;
+  if (k_weight) a.x[1] = static_cast<const char *>(k->p), a.x_tok[1] = (int)k->token_stride, a.x_head[1] = (int)k->head_stride;
   if (launch_back(a, dtype, r->rot_dim, r->layout, st) != cudaSuccess) return TR_ERR_CUDA;
-  return launch_kernel(k_rotate_weight_sum, dim3((r->head_dim + 31) / 32, 2), dim3(1024), 0, st, false,
-                       (const float *)a.part, a.ctas, (int)r->head_dim, dq_weight, dk_weight) == cudaSuccess
+  return launch_kernel(k_rotate_weight_sum, dim3((r->head_dim + 31) / 32, 2), dim3(1024), 0, st, true,
+                       (const float *)a.part, a.q_ctas, a.ctas, (int)r->head_dim, dq_weight, dk_weight) == cudaSuccess
              ? TR_OK
              : TR_ERR_CUDA;
 }
