@@ -161,80 +161,87 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
   } else if (warp == 4 * MT + 1) {
     // ---------------------------------------------------------------- MMA issuer
     if (lane == 0) {
+      // The tensor cores hold only a product or two beyond the one they run,
+      // so every cycle this thread spends between two products is theirs
+      // too: descriptors are sums with constants, ring positions are
+      // counted, and what can be waited for early is.
       const uint32_t idesc_s = tc::idesc_16(kTile, kTile, Bits<T>::kBf16, false);
       const uint32_t idesc_o = tc::idesc_16(kTile, g.c.d, Bits<T>::kBf16, true);
       const int ksteps = g.c.d / 16;
+      const uint64_t q_desc = tc::sw128_desc(sbase), k_desc = tc::sw128_desc(ring),
+                     v_desc = tc::sw128_desc_mn(ring, kTile * 128);
+      constexpr uint32_t kStep = S::kTileBytes >> 4;  // a tile on, in a descriptor's address field
       uint32_t sn[MT], pn[MT];  // products issued so far, of each kind
       bool ok = true, have_q[MT];
 #pragma unroll
       for (int m = 0; m < MT; ++m) sn[m] = pn[m] = 0, have_q[m] = false;
-      // The ring holds K and V of tile t as fills 2 (t - t0) and 2 (t - t0) + 1.
-      auto landed = [&](uint32_t fill) {
-        ok &= tc::mbar_wait(full((int)(fill % S::kStages)), fill / S::kStages & 1u);
-        return true;
-      };
-      // S_m = Q_m K^T
-      auto scores = [&](int m, uint32_t fill) {
-        const uint32_t qa = sbase + m * S::kTileBytes, kb = ring + fill % S::kStages * S::kTileBytes;
+      // S_m = Q_m K^T of the tile in ring position st
+      auto scores = [&](int m, int st) {
+        const uint64_t qd = q_desc + (uint64_t)(m * kStep), kd = k_desc + (uint64_t)((uint32_t)st * kStep);
         const int buf = S::kSBuf == 2 ? (int)(sn[m] & 1u) : 0;
         const uint32_t dst = tmem + (uint32_t)((MT == 1 ? buf : m) * kTile);
-        for (int i = 0; i < ksteps; ++i) {
-          const uint32_t off = (uint32_t)((i >> 2) * (kTile * 128) + (i & 3) * 32);
-          tc::mma_bf16(dst, tc::sw128_desc(qa + off), tc::sw128_desc(kb + off), idesc_s, i > 0);
-        }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+          if (i < ksteps) {
+            const uint64_t off = (uint64_t)(((i >> 2) * (kTile * 128) + (i & 3) * 32) >> 4);
+            tc::mma_bf16(dst, qd + off, kd + off, idesc_s, i > 0);
+          }
         tc::mma_commit(s_full(m, buf));
         ++sn[m];
       };
-      // O_m (+)= P_m V
-      auto values = [&](int m, uint32_t fill) {
-        const uint32_t vb = ring + fill % S::kStages * S::kTileBytes;
+      // O_m (+)= P_m V of the tile in ring position st
+      auto values = [&](int m, int st, bool last) {
+        const uint64_t vd = v_desc + (uint64_t)((uint32_t)st * kStep);
         const int buf = S::kSBuf == 2 ? (int)(pn[m] & 1u) : 0;
         const uint32_t p = tmem + (uint32_t)((MT == 1 ? buf : m) * kTile), dst = tmem + (uint32_t)(S::kColO + m * D);
+        const uint32_t more = pn[m] > 0;
 #pragma unroll
         for (int i = 0; i < kTile / 16; ++i)
-          tc::mma_bf16_ta(dst, p + 8 * i, tc::sw128_desc_mn(vb + 2048 * i, kTile * 128), idesc_o, pn[m] > 0 || i > 0);
-        tc::mma_commit(o_done(m));
+          tc::mma_bf16_ta(dst, p + 8 * i, vd + (uint64_t)(2048 * i >> 4), idesc_o, i > 0 ? 1u : more);
+        // MT = 2: the next scores, issued after this product, say as much
+        if (MT == 1 || last) tc::mma_commit(o_done(m));
         ++pn[m];
       };
       // Step t issues P V of tile t - 1 and the scores of tile t.  The tensor
       // cores run the products in the order of issue, so scores may overwrite
       // probabilities that the product issued before them reads.  One block
       // (MT = 1) has two score buffers and issues the scores first: its
-      // softmax of tile t runs during the products of tile t - 1.
-      for (int t = t0; t <= t1 && ok; ++t) {
-        const uint32_t kf = 2u * (uint32_t)(t - t0), vf = kf - 1;
-        bool have_k = t == t1, have_v = t == t0;
+      // softmax of tile t runs during the products of tile t - 1.  The ring
+      // holds K and V of a tile one after the other.
+      int kst = 0, vst = 0;
+      uint32_t kph = 0, vph = 0;
+      for (int t = t0; t <= t1; ++t) {
+        if (t > t0) ok &= tc::mbar_wait(full(vst), vph);
+        if (t < t1) ok &= tc::mbar_wait(full(kst), kph);
+        if (!ok) break;
+        tc::fence_after_sync();
         if (MT == 1 && t < t1) {
-          have_k = landed(kf);
           if (!have_q[0]) ok &= tc::mbar_wait(q_full(0), 0), have_q[0] = true;
           if (!ok) break;
-          tc::fence_after_sync();
-          scores(0, kf);
-          tc::mma_commit(empty((int)(kf % S::kStages)));
+          scores(0, kst);
+          tc::mma_commit(empty(kst));
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
+          if (MT > 1 && t >= a[m] && t < b[m] && !have_q[m]) ok &= tc::mbar_wait(q_full(m), 0), have_q[m] = true;
           if (t > a[m] && t <= b[m]) {
-            if (!have_v) have_v = landed(vf);
             ok &= tc::mbar_wait(p_full(m, S::kSBuf == 2 ? (int)(pn[m] & 1u) : 0),
                                 S::kSBuf == 2 ? pn[m] >> 1 & 1u : pn[m] & 1u);
             if (!ok) break;
             tc::fence_after_sync();
-            values(m, vf);
+            values(m, vst, t == b[m]);
           }
-          if (MT > 1 && t >= a[m] && t < b[m]) {
-            if (!have_k) have_k = landed(kf);
-            if (!have_q[m]) ok &= tc::mbar_wait(q_full(m), 0), have_q[m] = true;
-            if (!ok) break;
-            tc::fence_after_sync();
-            scores(m, kf);
-          }
+          if (!ok) break;
+          if (MT > 1 && t >= a[m] && t < b[m]) scores(m, kst);
         }
         if (!ok) break;
-        if (!have_v) have_v = landed(vf);  // a tile that no block used (the ranges of two blocks touch: not expected)
-        if (!have_k) have_k = landed(kf);
-        if (t > t0) tc::mma_commit(empty((int)(vf % S::kStages)));
-        if (MT > 1 && t < t1) tc::mma_commit(empty((int)(kf % S::kStages)));
+        if (t > t0) tc::mma_commit(empty(vst));
+        if (MT > 1 && t < t1) tc::mma_commit(empty(kst));
+        // V of this tile, K of the next
+        vst = kst, vph = kph;
+        if (++vst == S::kStages) vst = 0, vph ^= 1u;
+        kst = vst, kph = vph;
+        if (++kst == S::kStages) kst = 0, kph ^= 1u;
       }
       if (!ok) flag(g, TR_CACHE_ERR_WAIT);
     }
@@ -307,9 +314,11 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
             // the sums so far (all products up to the last tile's are in) move to the new maximum
             const bool up = now > mx + 8.f;
             const float f = up ? exp2_fast(mx - now) : 1.f;
-            ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 1) & 1u));
-            if (!ok) break;
-            tc::fence_after_sync();
+            if (MT == 1) {  // (two blocks: these scores came after the last tile's product)
+              ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 1) & 1u));
+              if (!ok) break;
+              tc::fence_after_sync();
+            }
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
               uint32_t o[32];
@@ -346,7 +355,7 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
       // the last two are in (MT = 1 issues scores ahead of a product).
       const int n = tb - ta;
       if (ok && MT == 1 && n > 1) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 2) & 1u));
-      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 1) & 1u));
+      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), MT == 1 ? (uint32_t)(n - 1) & 1u : 0u));
       tc::fence_after_sync();
       if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
     }
