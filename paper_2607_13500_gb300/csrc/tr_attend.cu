@@ -12,9 +12,10 @@
 //                   from tensor memory, mask, maximum, exponentials; the
 //                   probabilities go back to tensor memory as the A operand
 //                   of the second product, in the place of the scores;
-//   producer warp   TMA loads of K and V tiles, page by page, into a ring of
-//                   128-byte-swizzled tiles; zeroes the value rows past the
-//                   sequence's end (stale memory there may hold NaN);
+//   producer warps  TMA loads of K (one warp) and V (another) tiles, page by
+//                   page, into a ring of 128-byte-swizzled tiles; the value
+//                   rows past the sequence's end are zeroed (stale memory
+//                   there may hold NaN);
 //   MMA warp        S = Q K^T and O += P V from one thread.  The products of
 //                   the two 128-row blocks alternate, so one block's softmax
 //                   runs while the tensor cores work on the other.
@@ -54,7 +55,7 @@ struct Shape {
   static constexpr int kSBuf = MT == 1 ? 2 : 1;      // score buffers of a block
   // MT = 2: three warpgroups, so that registers can move between them: 168 a
   // thread at launch, 216 for the softmax (a row of scores is 128), 56 for the rest.
-  static constexpr int kThreads = MT == 2 ? 384 : 32 * 6;
+  static constexpr int kThreads = MT == 2 ? 384 : 32 * 7;
   static constexpr int kColO = 256;                  // tensor-memory columns: scores below, sums from here
   static constexpr int kCols = 512;
   static constexpr size_t kSmem = (size_t)(MT + kStages) * kTileBytes + 1024 + 512;
@@ -67,6 +68,12 @@ __device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
   return r;
 }
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
 template <typename T, int D, int MT>
 __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
     k_attend(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -145,15 +152,17 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
 
   if (warp >= 4 * MT) {
   if (MT == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-  if (warp == 4 * MT) {
-    // ---------------------------------------------------------------- TMA producer
+  if (warp == 4 * MT || warp == 4 * MT + 2) {
+    // ---------------------------------------------------------------- TMA producers
     TileRing<D, S::kStages, true> tiles;
     tiles.base = ring, tiles.full0 = full(0), tiles.empty0 = empty(0), tiles.tail = tail;
+    tiles.take(warp == 4 * MT ? 0 : 1);
+    const CUtensorMap *map = warp == 4 * MT ? &map_k : &map_v;
     bool ok = true;
     int id = t0 < t1 ? tiles.page_id(g, k.seq, k.len, t0) : -1;
     for (int t = t0; t < t1 && ok; ++t) {
       const int next = t + 1 < t1 ? tiles.page_id(g, k.seq, k.len, t + 1) : -1;
-      ok = tiles.load(g, &map_k, &map_v, id, k.len, hk, t);
+      ok = tiles.load(g, map, id, k.len, hk, t);
       id = next;
     }
     if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
@@ -206,9 +215,9 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
       // cores run the products in the order of issue, so scores may overwrite
       // probabilities that the product issued before them reads.  One block
       // (MT = 1) has two score buffers and issues the scores first: its
-      // softmax of tile t runs during the products of tile t - 1.  The ring
-      // holds K and V of a tile one after the other.
-      int kst = 0, vst = 0;
+      // softmax of tile t runs during the products of tile t - 1.
+      using Ring = TileRing<D, S::kStages, true>;
+      int kst = Ring::first(0), vst = Ring::first(1);
       uint32_t kph = 0, vph = 0;
       for (int t = t0; t <= t1; ++t) {
         if (t > t0) ok &= tc::mbar_wait(full(vst), vph);
@@ -237,11 +246,8 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
         if (!ok) break;
         if (t > t0) tc::mma_commit(empty(vst));
         if (MT > 1 && t < t1) tc::mma_commit(empty(kst));
-        // V of this tile, K of the next
-        vst = kst, vph = kph;
-        if (++vst == S::kStages) vst = 0, vph ^= 1u;
-        kst = vst, kph = vph;
-        if (++kst == S::kStages) kst = 0, kph ^= 1u;
+        if (t > t0) Ring::on(1, vst, vph);
+        Ring::on(0, kst, kph);
       }
       if (!ok) flag(g, TR_CACHE_ERR_WAIT);
     }
@@ -266,17 +272,24 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
     const uint32_t lane_col = (uint32_t)(32 * quarter) << 16;
     const uint32_t o_col = tmem + lane_col + (uint32_t)(S::kColO + m * D);
     if (ta < tb) {
-      // this row of Q into the swizzled layout that TMA would write
-      const uint32_t dst = sbase + m * S::kTileBytes + row * 128;
+      // The warp's 32 rows of Q into the swizzled layout that TMA would
+      // write; D / 8 neighbouring lanes take a row, so that a load reads
+      // whole lines.
+      const uint32_t dst = sbase + m * S::kTileBytes + 32 * quarter * 128;
       const uint32_t flip = g.negate ? 0x80008000u : 0u;
-#pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
+      constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+      const int c = lane % kLanes;
+      const long long qoff = valid ? qrow - g.q : -1;
+#pragma unroll 4
+      for (int i = 0; i < 32; i += kAtOnce) {
+        const int r1 = i + lane / kLanes;
+        const long long off = __shfl_sync(0xffffffffu, qoff, r1);
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (valid && 8 * c < g.c.d) {
-          v = *reinterpret_cast<const uint4 *>(qrow + 16 * c);
+        if (off >= 0 && 8 * c < g.c.d) {
+          v = *reinterpret_cast<const uint4 *>(g.q + off + 16 * c);
           v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
         }
-        tc::st_shared_v4(dst + (c >> 3) * (kTile * 128) + (((c & 7) ^ (row & 7)) << 4), v.x, v.y, v.z, v.w);
+        tc::st_shared_v4(dst + (c >> 3) * (kTile * 128) + r1 * 128 + (((c & 7) ^ (r1 & 7)) << 4), v.x, v.y, v.z, v.w);
       }
       tc::fence_async_shared();
       tc::mbar_arrive(q_full(m));
@@ -369,6 +382,8 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
       float *prow = g.part + ((long long)split * all_rows + out_row) * g.c.d;
       const float inv = parts ? 1.f : sum > 0.f || sum != sum ? 1.f / sum : 0.f;
       bool finite = true;
+      // staged in the place of this row's queries, whose products are done
+      const uint32_t stage_row = sbase + m * S::kTileBytes + row * 128;
 #pragma unroll 1
       for (int c = 0; c < D; c += 32) {
         uint32_t o[32];
@@ -393,12 +408,28 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
               *reinterpret_cast<float4 *>(prow + c + i) = make_float4(v[0], v[1], v[2], v[3]);
               *reinterpret_cast<float4 *>(prow + c + i + 4) = make_float4(v[4], v[5], v[6], v[7]);
             } else {
-              *reinterpret_cast<uint4 *>(orow + 2 * (c + i)) =
-                  make_uint4(Bits<T>::pack(v[0], v[1]), Bits<T>::pack(v[2], v[3]), Bits<T>::pack(v[4], v[5]),
-                             Bits<T>::pack(v[6], v[7]));
+              const int ch = (c + i) >> 3;
+              tc::st_shared_v4(stage_row + (ch >> 3) * (kTile * 128) + (((ch & 7) ^ (row & 7)) << 4),
+                               Bits<T>::pack(v[0], v[1]), Bits<T>::pack(v[2], v[3]), Bits<T>::pack(v[4], v[5]),
+                               Bits<T>::pack(v[6], v[7]));
             }
           }
         }
+      }
+      if (!parts) {  // rows leave as whole lines, as they came
+        __syncwarp();
+        constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+        const int c = lane % kLanes;
+        const long long ooff = valid ? orow - g.o : -1;
+#pragma unroll 4
+        for (int i = 0; i < 32; i += kAtOnce) {
+          const int r1 = i + lane / kLanes;
+          const long long off = __shfl_sync(0xffffffffu, ooff, r1);
+          const uint32_t src = sbase + m * S::kTileBytes + (32 * quarter + r1) * 128 + (c >> 3) * (kTile * 128) +
+                               (((c & 7) ^ (r1 & 7)) << 4);
+          if (off >= 0 && 8 * c < g.c.d) *reinterpret_cast<uint4 *>(g.o + off + 16 * c) = ld_shared_v4(src);
+        }
+        __syncwarp();
       }
       if (valid) {
         if (parts) g.part_ml[(long long)split * all_rows + out_row] = make_float2(mx, sum);

@@ -185,8 +185,11 @@ __device__ __forceinline__ void flag(const AttendArgs &g, int bit) {
 
 // ---------------------------------------------------------------- K and V tiles
 // A ring of 128-key tiles (D / 64 halves of 128 rows x 128 bytes, 128-byte
-// swizzle), K and V in turn, filled by one warp.  A tile is loaded page by
-// page; the lanes of the warp issue its loads side by side.
+// swizzle), the first kK of them for K, the others for V, each kind filled by
+// a warp of its own (positions that both filled in turn would need one warp
+// to follow the other's laps: a barrier tells only two phases apart).  A tile
+// is loaded page by page, the halves apart; the lanes of the warp issue its
+// loads (one warp for both kinds took 3 us a tile of 16-key pages).
 // ZERO_TAIL: value rows past the sequence's end are zeroed before the tile is
 // handed on -- stale memory may hold NaN there, and 0 * NaN would reach every
 // row of a product that reads the tile from shared memory.  That waits for
@@ -196,10 +199,23 @@ template <int D, int STAGES, bool ZERO_TAIL>
 struct TileRing {
   static constexpr int kHalves = D / 64;
   static constexpr uint32_t kBytes = kTile * D * 2;
+  static constexpr int kK = (STAGES + 1) / 2;
   uint32_t base, full0, empty0, tail;
-  int stage = 0;
+  int kv = 0, stage = 0;  // 0: K, 1: V; position of the next tile
   uint32_t phase = 0, tails = 0, filled = 0, parity = 0;
 
+  __device__ __forceinline__ void take(int kind) {
+    kv = kind;
+    stage = first(kind);
+  }
+  // The positions of a kind, and the walk over them.
+  static __device__ __forceinline__ int first(int kind) { return kind ? kK : 0; }
+  static __device__ __forceinline__ void on(int kind, int &st, uint32_t &ph) {
+    if (++st == (kind ? STAGES : kK)) {
+      st = first(kind);
+      ph ^= 1u;
+    }
+  }
   __device__ __forceinline__ uint32_t full(int s) const { return full0 + 8u * s; }
   __device__ __forceinline__ uint32_t empty(int s) const { return empty0 + 8u * s; }
 
@@ -211,9 +227,8 @@ struct TileRing {
     const int i = key >> g.page_log2;
     return key < len && i < g.c.max_pages ? __ldg(g.c.table + (long long)seq * g.c.max_pages + i) : -1;
   }
-  // K and V of tile t of the sequence; false when a wait timed out.
-  __device__ __forceinline__ bool load(const AttendArgs &g, const CUtensorMap *map_k, const CUtensorMap *map_v, int id,
-                                       int len, int hk, int t) {
+  // Tile t of the sequence; false when a wait timed out.
+  __device__ __forceinline__ bool load(const AttendArgs &g, const CUtensorMap *map, int id, int len, int hk, int t) {
     const int lane = threadIdx.x & 31;
     const int page = g.c.page, piece = min(page, kTile);  // keys of one load
     const int key0 = t * kTile, left = min(len - key0, kTile);
@@ -226,35 +241,28 @@ struct TileRing {
       else flag(g, TR_CACHE_ERR_PAGE);
     }
     const uint32_t bytes = (uint32_t)pieces * piece * 128u * kHalves;
+    if (!tc::mbar_wait_warp(empty(stage), phase ^ 1u)) return false;
+    const uint32_t dst = base + stage * kBytes;
+    const bool cut = ZERO_TAIL && kv == 1 && left < kTile;  // the sequence ends inside this value tile
+    const uint32_t bar = cut ? tail : full(stage);
+    if (lane == 0) tc::mbar_expect_tx(bar, bytes);
+    __syncwarp();
+    if (mine) tc::tma_load_2d(dst + half * (kTile * 128) + pc * piece * 128, map, half * 64, row, bar);
+    bool ok = true;
+    if (cut) {
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(tail, tails));
+      tails ^= 1u;
+      for (int i = lane + left * 8; i < kTile * 8; i += 32)
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      if (!tc::mbar_wait_warp(empty(stage), phase ^ 1u)) return false;
-      const uint32_t dst = base + stage * kBytes;
-      const bool cut = ZERO_TAIL && kv == 1 && left < kTile;  // the sequence ends inside this value tile
-      const uint32_t bar = cut ? tail : full(stage);
-      if (lane == 0) tc::mbar_expect_tx(bar, bytes);
+        for (int h = 0; h < kHalves; ++h) tc::st_shared_v4(dst + h * (kTile * 128) + i * 16, 0, 0, 0, 0);
+      tc::fence_async_shared();
       __syncwarp();
-      if (mine) tc::tma_load_2d(dst + half * (kTile * 128) + pc * piece * 128, kv ? map_v : map_k, half * 64, row, bar);
-      bool ok = true;
-      if (cut) {
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(tail, tails));
-        tails ^= 1u;
-        for (int i = lane + left * 8; i < kTile * 8; i += 32)
-#pragma unroll
-          for (int h = 0; h < kHalves; ++h) tc::st_shared_v4(dst + h * (kTile * 128) + i * 16, 0, 0, 0, 0);
-        tc::fence_async_shared();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(full(stage));
-      }
-      filled |= 1u << stage;
-      parity = (parity & ~(1u << stage)) | (phase << stage);
-      if (++stage == STAGES) {
-        stage = 0;
-        phase ^= 1u;
-      }
-      if (!ok) return false;
+      if (lane == 0) tc::mbar_arrive(full(stage));
     }
-    return true;
+    filled |= 1u << stage;
+    parity = (parity & ~(1u << stage)) | (phase << stage);
+    on(kv, stage, phase);
+    return ok;
   }
   // The loads already issued land before the CTA may exit.
   __device__ __forceinline__ void drain() const {

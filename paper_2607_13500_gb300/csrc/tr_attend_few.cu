@@ -9,7 +9,7 @@
 // that lies in one share is finished there; one that is cut leaves a partial
 // (maximum, sum, weighted values) per share, joined by k_few_join.
 //
-// One warp fills the tile ring by TMA; eight warps take 16 keys of each tile
+// Two warps fill the tile ring by TMA; eight warps take 16 keys of each tile
 // and run both products on warp-level tensor-core instructions (m16n8k16)
 // from registers: at up to 16 rows the 128-row tcgen05 shapes would compute
 // mostly padding and put a tensor-memory round trip between the products,
@@ -28,7 +28,7 @@ namespace {
 using namespace attend;
 
 constexpr int kWarps = 8;                     // consumer warps: 16 keys of a tile each
-constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kThreads = 32 * (kWarps + 2);   // and the producers of K and of V
 constexpr int kPass = 4;                      // rows joined per pass at an item's end
 
 template <int D>
@@ -250,19 +250,21 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();  // the barriers are ready
   Walk w;
   Seq run0;
-  const Shares shares(count_units(g, runs, kWarps + 1, run0), g.ctas);
+  const Shares shares(count_units(g, runs, kWarps + 2, run0), g.ctas);
   const int share = shares.start(blockIdx.x), share_end = shares.start(blockIdx.x + 1);
   if (share >= share_end) return;
   w.seek(g, runs, run0, share, share_end);
 
-  if (warp == kWarps) {
+  if (warp >= kWarps) {
+    ring.take(warp - kWarps);
+    const CUtensorMap *map = warp == kWarps ? &map_k : &map_v;
     bool ok = true;
     while (ok && w.next(g)) {
       const int hk = w.item % g.c.heads, end = w.tile + w.count;
       int id = ring.page_id(g, w.seq(), w.s.len, w.tile);
       for (int t = w.tile; t < end && ok; ++t) {
         const int next = t + 1 < end ? ring.page_id(g, w.seq(), w.s.len, t + 1) : -1;
-        ok = ring.load(g, &map_k, &map_v, id, w.s.len, hk, t);
+        ok = ring.load(g, map, id, w.s.len, hk, t);
         id = next;
       }
     }
@@ -273,8 +275,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   // ------------------------------------------------------------------ consumers
   const int gq = lane >> 2, c = lane & 3;  // quad (row or key of a fragment), lane of the quad
-  int stage = 0;
-  uint32_t phase = 0;
+  using Ring = TileRing<D, F::kStages, false>;
+  int kst = Ring::first(0), vst = Ring::first(1);
+  uint32_t kph = 0, vph = 0;
   bool ok = true;  // once a wait has timed out the warp only keeps up with the others' barriers
   while (w.next(g)) {
     const int hk = w.item % g.c.heads, block0 = w.item / g.c.heads * kFewRows;
@@ -315,12 +318,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     for (int t = w.tile; ok && t < w.tile + w.count; ++t) {
       // ---- scores of 16 keys: two products of 8 keys
-      ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(stage), phase));
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(kst), kph));
       if (!ok) {
         if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
         break;
       }
-      const uint32_t kt = base + stage * F::kTileBytes + (uint32_t)(16 * warp) * 128u;
+      const uint32_t kt = base + kst * F::kTileBytes + (uint32_t)(16 * warp) * 128u;
       float s[2][4];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
@@ -336,8 +339,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < 4; ++i) s[n][i] = x[i] + y[i];
       }
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(ring.empty(stage));
-      if (++stage == F::kStages) stage = 0, phase ^= 1u;
+      if (lane == 0) tc::mbar_arrive(ring.empty(kst));
+      Ring::on(0, kst, kph);
 
       // ---- softmax: s[n][0..1] row g, s[n][2..3] row g + 8, keys 8 n + 2 c and + 1
       const int key0 = t * kTile + 16 * warp;
@@ -386,13 +389,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
 
       // ---- o += p V: n-tile i of a half holds channels 8 g + i
-      ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(stage), phase));
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(vst), vph));
       if (!ok) {
         if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
         break;
       }
       const bool ends = key0 + 16 > w.s.len;
-      const uint32_t vt = base + stage * F::kTileBytes + (uint32_t)(16 * warp) * 128u;
+      const uint32_t vt = base + vst * F::kTileBytes + (uint32_t)(16 * warp) * 128u;
 #pragma unroll
       for (int h = 0; h < F::kHalves; ++h) {
         uint4 v[4];
@@ -415,8 +418,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(ring.empty(stage));
-      if (++stage == F::kStages) stage = 0, phase ^= 1u;
+      if (lane == 0) tc::mbar_arrive(ring.empty(vst));
+      Ring::on(1, vst, vph);
     }
 
     // ------------------------------------------------------------------ the piece's result
