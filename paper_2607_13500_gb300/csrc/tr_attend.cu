@@ -93,7 +93,8 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
   const uint32_t tail = bars + 8u * (2 * S::kStages + 2 * MT + 2 * MT * S::kSBuf);
   const uint32_t tmem_slot = tail + 8;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // (the warp's index by shuffle: the compiler then knows it to be uniform)
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   pdl_wait();  // q and the cache come from the kernels before
   const int slot = gridDim.x - 1 - blockIdx.x;  // causal chunks: the longest key ranges first
   const int hk = blockIdx.y, split = blockIdx.z;
@@ -169,9 +170,10 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
     tiles.drain();
   } else if (warp == 4 * MT + 1) {
     // ---------------------------------------------------------------- MMA issuer
-    if (lane == 0) {
+    {
+      const uint32_t lead = tc::elect_lane();
       // The tensor cores hold only a product or two beyond the one they run,
-      // so every cycle this thread spends between two products is theirs
+      // so every cycle this warp spends between two products is theirs
       // too: descriptors are sums with constants, ring positions are
       // counted, and what can be waited for early is.
       const uint32_t idesc_s = tc::idesc_16(kTile, kTile, Bits<T>::kBf16, false);
@@ -193,9 +195,9 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
         for (int i = 0; i < D / 16; ++i)
           if (i < ksteps) {
             const uint64_t off = (uint64_t)(((i >> 2) * (kTile * 128) + (i & 3) * 32) >> 4);
-            tc::mma_bf16(dst, qd + off, kd + off, idesc_s, i > 0);
+            tc::mma_16_warp(dst, qd + off, kd + off, idesc_s, i > 0, lead);
           }
-        tc::mma_commit(s_full(m, buf));
+        tc::mma_commit_warp(s_full(m, buf), lead);
         ++sn[m];
       };
       // O_m (+)= P_m V of the tile in ring position st
@@ -206,9 +208,9 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
         const uint32_t more = pn[m] > 0;
 #pragma unroll
         for (int i = 0; i < kTile / 16; ++i)
-          tc::mma_bf16_ta(dst, p + 8 * i, vd + (uint64_t)(2048 * i >> 4), idesc_o, i > 0 ? 1u : more);
+          tc::mma_16_ta_warp(dst, p + 8 * i, vd + (uint64_t)(2048 * i >> 4), idesc_o, i > 0 ? 1u : more, lead);
         // MT = 2: the next scores, issued after this product, say as much
-        if (MT == 1 || last) tc::mma_commit(o_done(m));
+        if (MT == 1 || last) tc::mma_commit_warp(o_done(m), lead);
         ++pn[m];
       };
       // Step t issues P V of tile t - 1 and the scores of tile t.  The tensor
@@ -220,21 +222,21 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
       int kst = Ring::first(0), vst = Ring::first(1);
       uint32_t kph = 0, vph = 0;
       for (int t = t0; t <= t1; ++t) {
-        if (t > t0) ok &= tc::mbar_wait(full(vst), vph);
-        if (t < t1) ok &= tc::mbar_wait(full(kst), kph);
+        if (t > t0) ok &= tc::mbar_wait_warp(full(vst), vph);
+        if (t < t1) ok &= tc::mbar_wait_warp(full(kst), kph);
         if (!ok) break;
         tc::fence_after_sync();
         if (MT == 1 && t < t1) {
-          if (!have_q[0]) ok &= tc::mbar_wait(q_full(0), 0), have_q[0] = true;
+          if (!have_q[0]) ok &= tc::mbar_wait_warp(q_full(0), 0), have_q[0] = true;
           if (!ok) break;
           scores(0, kst);
-          tc::mma_commit(empty(kst));
+          tc::mma_commit_warp(empty(kst), lead);
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          if (MT > 1 && t >= a[m] && t < b[m] && !have_q[m]) ok &= tc::mbar_wait(q_full(m), 0), have_q[m] = true;
+          if (MT > 1 && t >= a[m] && t < b[m] && !have_q[m]) ok &= tc::mbar_wait_warp(q_full(m), 0), have_q[m] = true;
           if (t > a[m] && t <= b[m]) {
-            ok &= tc::mbar_wait(p_full(m, S::kSBuf == 2 ? (int)(pn[m] & 1u) : 0),
+            ok &= tc::mbar_wait_warp(p_full(m, S::kSBuf == 2 ? (int)(pn[m] & 1u) : 0),
                                 S::kSBuf == 2 ? pn[m] >> 1 & 1u : pn[m] & 1u);
             if (!ok) break;
             tc::fence_after_sync();
@@ -244,12 +246,12 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
           if (MT > 1 && t >= a[m] && t < b[m]) scores(m, kst);
         }
         if (!ok) break;
-        if (t > t0) tc::mma_commit(empty(vst));
-        if (MT > 1 && t < t1) tc::mma_commit(empty(kst));
+        if (t > t0) tc::mma_commit_warp(empty(vst), lead);
+        if (MT > 1 && t < t1) tc::mma_commit_warp(empty(kst), lead);
         if (t > t0) Ring::on(1, vst, vph);
         Ring::on(0, kst, kph);
       }
-      if (!ok) flag(g, TR_CACHE_ERR_WAIT);
+      if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
     }
     __syncwarp();
   }
@@ -280,7 +282,7 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
       constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
       const int c = lane % kLanes;
       const long long qoff = valid ? qrow - g.q : -1;
-#pragma unroll 4
+#pragma unroll
       for (int i = 0; i < 32; i += kAtOnce) {
         const int r1 = i + lane / kLanes;
         const long long off = __shfl_sync(0xffffffffu, qoff, r1);
