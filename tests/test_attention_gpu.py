@@ -349,6 +349,30 @@ def test_attend(case, mode):
                   window=0 if mode in ("causal", "full") else 50, strided=mode == "window")
 
 
+def test_attend_many_sequences():
+    # more sequences than a warp has lanes, idle and empty ones among them, few and many rows
+    lens = [(37 * i * i) % 900 for i in range(75)]
+    seqs = [(0 if i % 7 == 3 else 1, n) for i, n in enumerate(lens)]
+    _check_attend(seqs, 8, 2, 64, 16, torch.bfloat16, max_new=1)
+    _check_attend([(0, 50)] * 40 + [(1, 300)] + [(0, 0)] * 30 + [(1, 20)], 7, 1, 128, 16, torch.float16, max_new=1)
+    _check_attend([(n % 5, n) for n in lens], 12, 2, 64, 32, torch.bfloat16)
+
+
+@pytest.mark.parametrize("case", [(8, 1, 128, 16), (8, 1, 128, 64), (2, 2, 128, 256), (8, 1, 64, 32), (2, 2, 80, 16)],
+                         ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}-p{c[3]}")
+def test_attend_long_runs_repeat(case):
+    # dozens of tiles per CTA: every ring position is filled many times over; the
+    # same bits every time, alone and back to back
+    hq, hk, d, page = case
+    for seqs, new in (([(600, 9000), (64, 6001)], 600), ([(1, 20000), (1, 9999), (1, 3)], 1)):
+        first = _check_attend(seqs, hq, hk, d, page, torch.bfloat16, max_new=new, max_len=20000, seed=3)
+        cache, table, lens, cu, _, _ = _step(seqs, hk, page, d, torch.bfloat16, 3)
+        q = _randn(int(cu[-1]), hq, d, dtype=torch.bfloat16, seed=4, gain=1.5)
+        outs = [cache.attend(q, table, lens, cu, max_new=new, max_len=20000) for _ in range(12)]
+        assert all(torch.equal(o, first) for o in outs)
+        assert int(cache.error) == 0
+
+
 @pytest.mark.parametrize("bounds", [(None, None), (20, 700), (1000, 100000)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_attend_bounds_and_splits(bounds, dtype):
