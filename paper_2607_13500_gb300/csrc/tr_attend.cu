@@ -282,16 +282,22 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
       constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
       const int c = lane % kLanes;
       const long long qoff = valid ? qrow - g.q : -1;
+      constexpr int kLoads = 32 / kAtOnce, kBatch = kLoads < 8 ? kLoads : 8;  // all loads of a batch before its stores
+#pragma unroll 1
+      for (int i0 = 0; i0 < kLoads; i0 += kBatch) {
+        uint4 v[kBatch];
 #pragma unroll
-      for (int i = 0; i < 32; i += kAtOnce) {
-        const int r1 = i + lane / kLanes;
-        const long long off = __shfl_sync(0xffffffffu, qoff, r1);
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (off >= 0 && 8 * c < g.c.d) {
-          v = *reinterpret_cast<const uint4 *>(g.q + off + 16 * c);
-          v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
+        for (int i = 0; i < kBatch; ++i) {
+          const long long off = __shfl_sync(0xffffffffu, qoff, (i0 + i) * kAtOnce + lane / kLanes);
+          v[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (off >= 0 && 8 * c < g.c.d) v[i] = *reinterpret_cast<const uint4 *>(g.q + off + 16 * c);
         }
-        tc::st_shared_v4(dst + (c >> 3) * (kTile * 128) + r1 * 128 + (((c & 7) ^ (r1 & 7)) << 4), v.x, v.y, v.z, v.w);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int r1 = (i0 + i) * kAtOnce + lane / kLanes;
+          tc::st_shared_v4(dst + (c >> 3) * (kTile * 128) + r1 * 128 + (((c & 7) ^ (r1 & 7)) << 4), v[i].x ^ flip,
+                           v[i].y ^ flip, v[i].z ^ flip, v[i].w ^ flip);
+        }
       }
       tc::fence_async_shared();
       tc::mbar_arrive(q_full(m));
