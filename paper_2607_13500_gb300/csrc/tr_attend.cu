@@ -45,22 +45,29 @@ namespace {
 
 using namespace attend;
 
-template <int D, int MT>
+// MT blocks of 128 rows a CTA.  PAIRED (MT = 1): two CTAs share an SM, each
+// with room for little more than the tile in use, so that one's start and
+// end run beside the other's work: for keys of a few tiles, where a CTA is
+// mostly start and end (16 prompts of 227 tokens, 32 heads: 48 us against 54
+// us with MT = 2).
+template <int D, int MT, bool PAIRED>
 struct Shape {
-  static constexpr int kHalves = D / 64;             // 64-column halves of a row
+  static_assert(MT == 2 || MT == 1, "");
   static constexpr int kTileBytes = kTile * D * 2;   // one K or V tile, or one block's Q
   static constexpr int kBudget = 227 * 1024 - 2048;  // shared memory less barriers and alignment
   static constexpr int kFit = (kBudget - MT * kTileBytes) / kTileBytes;
-  static constexpr int kStages = kFit < 12 ? kFit : 12;
-  static constexpr int kSBuf = MT == 1 ? 2 : 1;      // score buffers of a block
-  // MT = 2: three warpgroups, so that registers can move between them: 168 a
-  // thread at launch, 216 for the softmax (a row of scores is 128), 56 for the rest.
-  static constexpr int kThreads = MT == 2 ? 384 : 32 * 7;
-  static constexpr int kColO = 256;                  // tensor-memory columns: scores below, sums from here
-  static constexpr int kCols = 512;
+  static constexpr int kStages = PAIRED ? (D == 128 ? 2 : 4) : kFit < 12 ? kFit : 12;
+  static constexpr int kSBuf = MT == 1 && !PAIRED ? 2 : 1;  // score buffers of a block
+  // Whole warpgroups, so that registers can move between them where a thread
+  // would have too few for a row of scores (128): of 168 at launch (MT = 2)
+  // 216 for the softmax and 56 for the rest, of 128 (PAIRED) 200 and 48.
+  static constexpr int kThreads = MT == 2 ? 384 : 256;
+  static constexpr bool kMove = MT == 2 || PAIRED;
+  static constexpr int kColO = PAIRED ? 128 : 256;  // tensor-memory columns: scores below, sums from here
+  static constexpr int kCols = PAIRED ? 256 : 512;
   static constexpr size_t kSmem = (size_t)(MT + kStages) * kTileBytes + 1024 + 512;
-  static_assert(kColO + MT * D <= kCols, "scores and sums fit the tensor memory");
-  static_assert(kStages >= 4, "two tiles in use and two on their way");
+  static_assert(kColO + MT * D <= kCols && kColO >= MT * kSBuf * kTile, "scores and sums fit the tensor memory");
+  static_assert(!PAIRED || 2 * (kSmem + 1024) <= 228 * 1024, "two CTAs fit an SM");
 };
 
 __device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
@@ -74,11 +81,11 @@ __device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
   return v;
 }
 
-template <typename T, int D, int MT>
-__global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
+template <typename T, int D, int MT, bool PAIRED>
+__global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1)
     k_attend(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
              const __grid_constant__ AttendArgs g) {
-  using S = Shape<D, MT>;
+  using S = Shape<D, MT, PAIRED>;
   constexpr int kRows = kTile * MT;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t sbase = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;  // the swizzle atom
@@ -152,7 +159,10 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
   if (t0 < t1) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
 
   if (warp >= 4 * MT) {
-  if (MT == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  if (S::kMove) {
+    if (PAIRED) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  }
   if (warp == 4 * MT || warp == 4 * MT + 2) {
     // ---------------------------------------------------------------- TMA producers
     TileRing<D, S::kStages, true> tiles;
@@ -209,15 +219,15 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
 #pragma unroll
         for (int i = 0; i < kTile / 16; ++i)
           tc::mma_16_ta_warp(dst, p + 8 * i, vd + (uint64_t)(2048 * i >> 4), idesc_o, i > 0 ? 1u : more, lead);
-        // MT = 2: the next scores, issued after this product, say as much
-        if (MT == 1 || last) tc::mma_commit_warp(o_done(m), lead);
+        // one score buffer: the next scores, issued after this product, say as much
+        if (S::kSBuf == 2 || last) tc::mma_commit_warp(o_done(m), lead);
         ++pn[m];
       };
       // Step t issues P V of tile t - 1 and the scores of tile t.  The tensor
       // cores run the products in the order of issue, so scores may overwrite
       // probabilities that the product issued before them reads.  One block
-      // (MT = 1) has two score buffers and issues the scores first: its
-      // softmax of tile t runs during the products of tile t - 1.
+      // with two score buffers issues the scores first: its softmax of tile t
+      // runs during the products of tile t - 1.
       using Ring = TileRing<D, S::kStages, true>;
       int kst = Ring::first(0), vst = Ring::first(1);
       uint32_t kph = 0, vph = 0;
@@ -226,7 +236,7 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
         if (t < t1) ok &= tc::mbar_wait_warp(full(kst), kph);
         if (!ok) break;
         tc::fence_after_sync();
-        if (MT == 1 && t < t1) {
+        if (S::kSBuf == 2 && t < t1) {
           if (!have_q[0]) ok &= tc::mbar_wait_warp(q_full(0), 0), have_q[0] = true;
           if (!ok) break;
           scores(0, kst);
@@ -234,7 +244,7 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          if (MT > 1 && t >= a[m] && t < b[m] && !have_q[m]) ok &= tc::mbar_wait_warp(q_full(m), 0), have_q[m] = true;
+          if (S::kSBuf == 1 && t >= a[m] && t < b[m] && !have_q[m]) ok &= tc::mbar_wait_warp(q_full(m), 0), have_q[m] = true;
           if (t > a[m] && t <= b[m]) {
             ok &= tc::mbar_wait_warp(p_full(m, S::kSBuf == 2 ? (int)(pn[m] & 1u) : 0),
                                 S::kSBuf == 2 ? pn[m] >> 1 & 1u : pn[m] & 1u);
@@ -243,11 +253,11 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
             values(m, vst, t == b[m]);
           }
           if (!ok) break;
-          if (MT > 1 && t >= a[m] && t < b[m]) scores(m, kst);
+          if (S::kSBuf == 1 && t >= a[m] && t < b[m]) scores(m, kst);
         }
         if (!ok) break;
         if (t > t0) tc::mma_commit_warp(empty(vst), lead);
-        if (MT > 1 && t < t1) tc::mma_commit_warp(empty(kst), lead);
+        if (S::kSBuf == 1 && t < t1) tc::mma_commit_warp(empty(kst), lead);
         if (t > t0) Ring::on(1, vst, vph);
         Ring::on(0, kst, kph);
       }
@@ -256,7 +266,10 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
     __syncwarp();
   }
   } else {
-    if (MT == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    if (S::kMove) {
+      if (PAIRED) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+      else asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    }
     // ---------------------------------------------------------------- softmax
     const int m = MT == 1 ? 0 : warp >> 2, quarter = warp & 3;
     const int row = 32 * quarter + lane, r = k.first + m * kTile + row;  // row of the block, of the sequence
@@ -335,7 +348,7 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
             // the sums so far (all products up to the last tile's are in) move to the new maximum
             const bool up = now > mx + 8.f;
             const float f = up ? exp2_fast(mx - now) : 1.f;
-            if (MT == 1) {  // (two blocks: these scores came after the last tile's product)
+            if (S::kSBuf == 2) {  // (one buffer: these scores came after the last tile's product)
               ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 1) & 1u));
               if (!ok) break;
               tc::fence_after_sync();
@@ -373,10 +386,10 @@ __global__ void __launch_bounds__(Shape<D, MT>::kThreads, 1)
         tc::mbar_arrive(p_full(m, buf));
       }
       // One phase after the other: the last scores say that all products but
-      // the last two are in (MT = 1 issues scores ahead of a product).
+      // the last two are in (with two buffers scores are ahead of a product).
       const int n = tb - ta;
-      if (ok && MT == 1 && n > 1) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 2) & 1u));
-      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), MT == 1 ? (uint32_t)(n - 1) & 1u : 0u));
+      if (ok && S::kSBuf == 2 && n > 1) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 2) & 1u));
+      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), S::kSBuf == 2 ? (uint32_t)(n - 1) & 1u : 0u));
       tc::fence_after_sync();
       if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
     }
@@ -522,9 +535,12 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
 }
 
 // ---------------------------------------------------------------- host side
+constexpr int kPairedTiles = 4;  // see Shape
+
 struct Plan {
   bool few;               // tr_attend_few.cu's kernel
   int mt, slots;          // else k_attend's blocks of 128 mt rows
+  bool paired;            // two CTAs an SM
   int splits, split_tiles;  // and the parts of the keys, in tiles
   size_t part_ml, total;  // workspace
 };
@@ -542,19 +558,25 @@ Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_le
     p.total = few_workspace_bytes(c->head_dim, sms);
     return p;
   }
-  p.mt = most <= kTile ? 1 : 2;
+  const long long cap = (long long)c->max_pages * c->page;
+  long long keys = max_len < cap ? max_len : cap;
+  if (window > 0 && keys > (long long)window + max_new) keys = (long long)window + max_new;
+  const int tiles = (int)((keys + kTile - 1) / kTile);
+  p.paired = tiles <= kPairedTiles;
+  p.mt = most <= kTile || p.paired ? 1 : 2;
   const int rows = kTile * p.mt;
   p.slots = (int)((long long)c->total_new * group / rows) + c->batch;
+  if (p.paired) {
+    p.splits = 1;
+    p.split_tiles = tiles;
+    return p;
+  }
   // Parts of the keys: as many as finish earliest when `sms` CTAs run at a
   // time, one costing its tiles and about kCtaTiles more, and the join
   // writing and reading a row's fp32 sums once per part (kJoinRows rows in
   // the time of one tile).
   constexpr double kCtaTiles = 4.0, kJoinRows = 8192.0;
   const double blocks = (double)p.slots * c->heads;
-  const long long cap = (long long)c->max_pages * c->page;
-  long long keys = max_len < cap ? max_len : cap;
-  if (window > 0 && keys > (long long)window + max_new) keys = (long long)window + max_new;
-  const int tiles = (int)((keys + kTile - 1) / kTile);
   double best = 0;
   for (int s = 1; s <= 64 && s <= (tiles > 1 ? tiles : 1); ++s) {
     const double waves = std::ceil(blocks * s / sms);
@@ -576,34 +598,36 @@ Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_le
 
 std::atomic<int> g_attend_smem_set[64];
 
-template <typename T, int D, int MT>
-cudaError_t launch_attend_t(const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &g, int slots, int variant,
+template <typename T, int D, int MT, bool PAIRED>
+cudaError_t launch_attend_t(const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &g, int slots,
                             cudaStream_t st) {
-  using S = Shape<D, MT>;
+  using S = Shape<D, MT, PAIRED>;
   int dev = 0;
   cudaError_t err = cudaGetDevice(&dev);
   if (err != cudaSuccess) return err;
-  const int bit = 1 << variant;
+  const int bit = 1 << (Bits<T>::kBf16 * 6 + (D == 128) * 3 + (PAIRED ? 2 : MT - 1));
   if (!(g_attend_smem_set[dev & 63].load() & bit)) {
-    err = cudaFuncSetAttribute(k_attend<T, D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
+    err = cudaFuncSetAttribute(k_attend<T, D, MT, PAIRED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
     if (err != cudaSuccess) return err;
     g_attend_smem_set[dev & 63].fetch_or(bit);
   }
-  return launch_kernel(k_attend<T, D, MT>, dim3(slots, g.c.heads, g.splits), dim3(S::kThreads), S::kSmem, st, false, mk,
-                       mv, g);
+  return launch_kernel(k_attend<T, D, MT, PAIRED>, dim3(slots, g.c.heads, g.splits), dim3(S::kThreads), S::kSmem, st,
+                       false, mk, mv, g);
+}
+
+template <typename T, int D>
+cudaError_t launch_attend_d(const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &g, const Plan &p,
+                            cudaStream_t st) {
+  return p.paired    ? launch_attend_t<T, D, 1, true>(mk, mv, g, p.slots, st)
+         : p.mt == 1 ? launch_attend_t<T, D, 1, false>(mk, mv, g, p.slots, st)
+                     : launch_attend_t<T, D, 2, false>(mk, mv, g, p.slots, st);
 }
 
 template <typename T>
 cudaError_t launch_attend(const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &g, const Plan &p,
                           cudaStream_t st) {
-  const int base = Bits<T>::kBf16 ? 0 : 4;
-  cudaError_t err;
-  if (g.c.d <= 64)
-    err = p.mt == 1 ? launch_attend_t<T, 64, 1>(mk, mv, g, p.slots, base, st)
-                    : launch_attend_t<T, 64, 2>(mk, mv, g, p.slots, base + 1, st);
-  else
-    err = p.mt == 1 ? launch_attend_t<T, 128, 1>(mk, mv, g, p.slots, base + 2, st)
-                    : launch_attend_t<T, 128, 2>(mk, mv, g, p.slots, base + 3, st);
+  const cudaError_t err =
+      g.c.d <= 64 ? launch_attend_d<T, 64>(mk, mv, g, p, st) : launch_attend_d<T, 128>(mk, mv, g, p, st);
   if (err != cudaSuccess || g.splits == 1) return err;
   const long long rows = (long long)g.c.total_new * g.q_heads;
   return launch_kernel(k_attend_join<T>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, true, g);
