@@ -28,6 +28,11 @@
 // Probabilities are rounded to the cache's 16-bit type for the second
 // product (the tensor cores take both operands in one type); their sum is
 // taken before that rounding, and everything else is fp32.
+//
+// Bound by the tensor cores where there are many keys: 2048 tokens over 32768
+// keys, 28/4 heads of 128, bf16, 614 us on GB300 (1.52 PFLOP/s, 0.79 of the
+// measured cuBLAS rate).  A 128 x 128 x 16 product reads 8 KB of shared
+// memory, or 4 KB and tensor memory, in the 64 cycles it could take.
 #include <cfloat>
 #include <climits>
 #include <cmath>
@@ -48,7 +53,7 @@ using namespace attend;
 // MT blocks of 128 rows a CTA.  PAIRED (MT = 1): two CTAs share an SM, each
 // with room for little more than the tile in use, so that one's start and
 // end run beside the other's work: for keys of a few tiles, where a CTA is
-// mostly start and end (16 prompts of 227 tokens, 32 heads: 48 us against 54
+// mostly start and end (16 prompts of 227 tokens, 32 heads: 46 us against 54
 // us with MT = 2).
 template <int D, int MT, bool PAIRED>
 struct Shape {
@@ -97,7 +102,8 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
   auto s_full = [&](int m, int b) { return bars + 8u * (2 * S::kStages + MT + m * S::kSBuf + b); };
   auto p_full = [&](int m, int b) { return bars + 8u * (2 * S::kStages + MT + MT * S::kSBuf + m * S::kSBuf + b); };
   auto o_done = [&](int m) { return bars + 8u * (2 * S::kStages + MT + 2 * MT * S::kSBuf + m); };
-  const uint32_t tail = bars + 8u * (2 * S::kStages + 2 * MT + 2 * MT * S::kSBuf);
+  auto o_last = [&](int m) { return bars + 8u * (2 * S::kStages + 2 * MT + 2 * MT * S::kSBuf + m); };
+  const uint32_t tail = bars + 8u * (2 * S::kStages + 3 * MT + 2 * MT * S::kSBuf);
   const uint32_t tmem_slot = tail + 8;
 
   // (the warp's index by shuffle: the compiler then knows it to be uniform)
@@ -141,6 +147,7 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
           tc::mbar_init(p_full(m, i), kTile);
         }
         tc::mbar_init(o_done(m), 1);
+        tc::mbar_init(o_last(m), 1);
       }
       tc::mbar_init(tail, 1);
       tc::mbar_fence_init();
@@ -220,7 +227,8 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
         for (int i = 0; i < kTile / 16; ++i)
           tc::mma_16_ta_warp(dst, p + 8 * i, vd + (uint64_t)(2048 * i >> 4), idesc_o, i > 0 ? 1u : more, lead);
         // one score buffer: the next scores, issued after this product, say as much
-        if (S::kSBuf == 2 || last) tc::mma_commit_warp(o_done(m), lead);
+        if (last) tc::mma_commit_warp(o_last(m), lead);
+        else if (S::kSBuf == 2) tc::mma_commit_warp(o_done(m), lead);
         ++pn[m];
       };
       // Step t issues P V of tile t - 1 and the scores of tile t.  The tensor
@@ -385,11 +393,9 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
         tc::fence_before_sync();
         tc::mbar_arrive(p_full(m, buf));
       }
-      // One phase after the other: the last scores say that all products but
-      // the last two are in (with two buffers scores are ahead of a product).
-      const int n = tb - ta;
-      if (ok && S::kSBuf == 2 && n > 1) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 2) & 1u));
-      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), S::kSBuf == 2 ? (uint32_t)(n - 1) & 1u : 0u));
+      // A barrier of its own: of one that every product completes, a thread
+      // that comes late could not tell the last phase from the one before.
+      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_last(m), 0));
       tc::fence_after_sync();
       if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
     }
@@ -691,7 +697,7 @@ tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *
     return TR_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (p.few) {
-    g.ctas = sm_count();
+    g.ctas = sm_count() > 0 ? sm_count() : 1;
     return launch_few(mk, mv, g, c->dtype == TR_BF16, ws, st) == cudaSuccess ? TR_OK : TR_ERR_CUDA;
   }
   const cudaError_t err =

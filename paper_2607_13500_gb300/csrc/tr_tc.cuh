@@ -57,11 +57,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
     if (global_ns() - t0 > kWaitNs) return false;
   }
 }
-// The same for a whole warp: lane 0 waits, the warp agrees on the outcome.
+// The same for a whole warp: every lane waits and the warp agrees on the
+// outcome.  A lane may issue products or loads only after a wait of its own:
+// with lane 0 waiting and the elected lane told by a shuffle, which orders no
+// memory, products lost accumulations and reads came early (a block in some
+// thousands).
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
-  bool ok = true;
-  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity);
-  return __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0;
 }
 
 // ---------------------------------------------------------------- TMA

@@ -373,6 +373,22 @@ def test_attend_long_runs_repeat(case):
         assert int(cache.error) == 0
 
 
+@pytest.mark.parametrize("case", [(32, 32, 128, 16), (28, 4, 128, 64), (16, 16, 64, 32)],
+                         ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}-p{c[3]}")
+@pytest.mark.parametrize("new", [227, 700])
+def test_attend_many_blocks_repeat(case, new):
+    # hundreds of short blocks per call, many calls: work of one block that the
+    # next step takes up too early shows in a block in some thousands only
+    hq, hk, d, page = case
+    seqs = [(new, new)] * 16
+    first = _check_attend(seqs, hq, hk, d, page, torch.bfloat16, max_new=new, max_len=new, seed=3)
+    cache, table, lens, cu, _, _ = _step(seqs, hk, page, d, torch.bfloat16, 3)
+    q = _randn(int(cu[-1]), hq, d, dtype=torch.bfloat16, seed=4, gain=1.5)
+    for _ in range(60):
+        assert torch.equal(cache.attend(q, table, lens, cu, max_new=new, max_len=new), first)
+    assert int(cache.error) == 0
+
+
 @pytest.mark.parametrize("bounds", [(None, None), (20, 700), (1000, 100000)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_attend_bounds_and_splits(bounds, dtype):
