@@ -475,9 +475,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
           m = fmaxf(m, top[j][r]);
         }
+        // A maximum passes over NaN scores, so a warp that saw no other has the
+        // maximum of one that saw nothing: its sum, 0 or NaN, enters as it is.
 #pragma unroll
-        for (int j = 0; j < kWarps; ++j)
-          if (top[j][r] != -INFINITY) l += tot[j][r] * exp2_fast(top[j][r] - m);
+        for (int j = 0; j < kWarps; ++j) l += top[j][r] == -INFINITY ? tot[j][r] : tot[j][r] * exp2_fast(top[j][r] - m);
         if (!finite4(v)) atomicOr(&bad_rows, 1u << r);
         put_row<T>(g, w, part, block0, hk, r, ch, v, m, l);
       }

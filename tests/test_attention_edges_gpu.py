@@ -1,0 +1,76 @@
+"""Rows and keys at the edges of tr_cache_attend: values that are not finite,
+rows that no sequence owns, pages that no row sees.  The plain implementation,
+the steps and the tolerances are those of test_attention_gpu."""
+import math
+
+import pytest
+import torch
+
+from test_attention_gpu import DEV, U, _alt, _attend_ref, _randn, _step, _within
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+    from paper_2607_13500_gb300 import _build
+    _build.build()
+
+
+def _check_rows(got, lse, q, keys, vals, seqs, cu, spoilt, causal=True, window=0, scale=None):
+    """Rows [token, head] of `spoilt` are NaN in out and lse, the others as the plain form has them."""
+    d, dtype = q.shape[2], q.dtype
+    assert torch.isnan(got[spoilt]).all() and torch.isnan(lse[spoilt]).all()
+    for b, (n, length) in enumerate(seqs):
+        if n == 0:
+            continue
+        sl = slice(int(cu[b]), int(cu[b + 1]))
+        keep = ~spoilt[sl]
+        o, z, pv, e = _attend_ref(q[sl].nan_to_num(0, 0, 0), keys[b], vals[b], n, causal, window,
+                                  1 / math.sqrt(d) if scale is None else scale)
+        tol = U[dtype] * o.abs() + (U[dtype] + 2 * e + 2.0 ** -17)[..., None] * pv + 2.0 ** -24
+        if dtype == torch.float16:
+            tol = tol + length * 2.0 ** -25 * vals[b].double().nan_to_num(0, 0, 0).abs().max()
+        _within(got[sl][keep], o[keep], tol[keep], ("o", b))
+        _within(lse[sl][keep], z[keep], (e + 2.0 ** -17 * (1 + z.abs()))[keep], ("lse", b))
+
+
+# Single tokens: items cut into shares (a tile or two each), and whole ones (one tile).
+FEW = [
+    ([(1, 609), (1, 40)], 32, 32, 128, 16),
+    ([(1, 513)], 32, 32, 128, 64),
+    ([(1, 33), (1, 17), (1, 100)], 4, 2, 64, 16),
+    ([(2, 1025), (1, 300)], 7, 1, 64, 32),
+]
+
+
+@pytest.mark.parametrize("case", FEW, ids=lambda c: f"{c[0][0][1]}-{c[1]}-{c[2]}-{c[3]}")
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_few_rows_nan_query(case, value):
+    # one head's query of one token: its row and no other
+    seqs, hq, hk, d, page = case
+    cache, table, lens, cu, keys, vals = _step(seqs, hk, page, d, torch.bfloat16, 5)
+    q = _randn(int(cu[-1]), hq, d, dtype=torch.bfloat16, seed=6, gain=1.5)
+    q[0, 1, 5] = value
+    spoilt = torch.zeros(q.shape[:2], dtype=torch.bool, device=DEV)
+    spoilt[0, 1] = True
+    got, lse = cache.attend(q, table, lens, cu, max_new=2, return_lse=True)
+    _check_rows(got, lse, q, keys, vals, seqs, cu, spoilt)
+
+
+@pytest.mark.parametrize("case", FEW, ids=lambda c: f"{c[0][0][1]}-{c[1]}-{c[2]}-{c[3]}")
+def test_few_rows_nan_key(case):
+    # a visible key of NaN, alone in the last 16 keys of its tile: every row that sees it
+    seqs, hq, hk, d, page = case
+    cache, table, lens, cu, keys, vals = _step(seqs, hk, page, d, torch.bfloat16, 5)
+    q = _randn(int(cu[-1]), hq, d, dtype=torch.bfloat16, seed=6, gain=1.5)
+    n, length = seqs[0]
+    j = length - 1
+    assert j % 16 == 0
+    cache.k[table[0, j // page], 0, j % page, 3] = float("nan")
+    spoilt = torch.zeros(q.shape[:2], dtype=torch.bool, device=DEV)
+    spoilt[n - 1, :hq // hk] = True  # the last token of the first sequence, the first key head's rows
+    got, lse = cache.attend(q, table, lens, cu, max_new=2, return_lse=True)
+    _check_rows(got, lse, q, keys, vals, seqs, cu, spoilt)
