@@ -465,7 +465,9 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
       // A non-finite value of a key hidden from a row reaches it all the same
       // as 0 * inf in the product over the tile.  Such rows are taken again
       // without it: only when a row came out non-finite and a value hidden
-      // from it inside its tiles is.
+      // from it inside its tiles is.  The lanes that do write over what the
+      // row's own lane has just written, so its stores come first.
+      __syncwarp();
       unsigned bad = __ballot_sync(0xffffffffu, valid && !finite);
       while (bad) {
         const int src = __ffs(bad) - 1;

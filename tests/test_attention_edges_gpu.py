@@ -74,3 +74,43 @@ def test_few_rows_nan_key(case):
     spoilt[n - 1, :hq // hk] = True  # the last token of the first sequence, the first key head's rows
     got, lse = cache.attend(q, table, lens, cu, max_new=2, return_lse=True)
     _check_rows(got, lse, q, keys, vals, seqs, cu, spoilt)
+
+
+def _check_bad_keys(seqs, hq, hk, d, page, dtype, bad, window=0, scale=None, repeats=1, **kw):
+    """Keys `bad` (counted back from each sequence's end, 1 = the last) are NaN, their values infinite: rows that see
+    one are NaN, the others as if it did not exist, and the same bits on every call."""
+    cache, table, lens, cu, keys, vals = _step(seqs, hk, page, d, dtype, 5)
+    q = _randn(int(cu[-1]), hq, d, dtype=dtype, seed=6, gain=1.5)
+    spoilt = torch.zeros(q.shape[:2], dtype=torch.bool, device=DEV)
+    for b, (n, length) in enumerate(seqs):
+        own = length - n + torch.arange(n, device=DEV)
+        for j in (length - back for back in bad if back <= length):
+            cache.k[table[b, j // page], :, j % page] = float("nan")
+            cache.v[table[b, j // page], :, j % page] = float("inf") if j % 2 else float("-inf")
+            keys[b][j] = vals[b][j] = 0
+            spoilt[int(cu[b]):int(cu[b + 1])] |= ((own >= j) & ((own < j + window) if window else own >= 0))[:, None]
+    assert not spoilt.all()
+    got, lse = cache.attend(q, table, lens, cu, window=window, scale=scale, return_lse=True, **kw)
+    _check_rows(got, lse, q, keys, vals, seqs, cu, spoilt, window=window, scale=scale)
+    for _ in range(repeats - 1):
+        again, lse2 = cache.attend(q, table, lens, cu, window=window, scale=scale, return_lse=True, **kw)
+        assert torch.equal(again.nan_to_num(9), got.nan_to_num(9)) and torch.equal(lse2.nan_to_num(9), lse.nan_to_num(9))
+    assert int(cache.error) == 0
+
+
+CHUNKS = [  # sequences, q heads, k heads, d, page, dtype, window, scale, max_len
+    ([(40, 1000), (90, 1111)], 4, 2, 64, 32, torch.bfloat16, 0, None, 1111),     # the keys in parts, joined
+    ([(300, 2000)], 7, 1, 128, 64, torch.float16, 0, -0.2, 2000),
+    ([(200, 1500)], 4, 2, 80, 16, torch.bfloat16, 100, None, 1500),
+    ([(150, 150), (33, 500)], 4, 2, 64, 32, torch.bfloat16, 0, None, 500),       # in one part
+    ([(300, 700)] * 16, 7, 1, 128, 64, torch.bfloat16, 0, 0.1, 700),
+    ([(100, 700)] * 40, 8, 4, 64, 64, torch.float16, 90, None, 700),
+]
+
+
+@pytest.mark.parametrize("case", CHUNKS, ids=lambda c: f"{len(c[0])}x{c[0][0][0]}of{c[0][0][1]}-{c[3]}-w{c[6]}")
+def test_chunk_rows_without_hidden_bad_keys(case):
+    # rows taken again: their partial results and statistics are the second ones, on every call
+    seqs, hq, hk, d, page, dtype, window, scale, max_len = case
+    _check_bad_keys(seqs, hq, hk, d, page, dtype, (2, 9, 30), window=window, scale=scale, repeats=10,
+                    max_new=max(n for n, _ in seqs), max_len=max_len)
