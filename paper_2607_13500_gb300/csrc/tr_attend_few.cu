@@ -224,6 +224,22 @@ __device__ __forceinline__ void put_row(const AttendArgs &g, const Walk &w, int 
   }
 }
 
+// Whether what put_row wrote for row r of the piece is finite, by a warp.
+template <typename T>
+__device__ __forceinline__ bool row_finite(const AttendArgs &g, const Walk &w, int part, int block0, int hk, int r) {
+  const int ch = 4 * (threadIdx.x & 31);
+  bool ok = true;
+  if (ch < g.c.d) {
+    if (w.whole) {
+      const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
+      ok = finite4(load4<T>(g.o + 2 * ((long long)(w.s.tok0 + tok) * g.o_tok + (long long)head * g.o_head + ch)));
+    } else {
+      ok = finite4(*reinterpret_cast<const float4 *>(g.part + ((long long)part * kFewRows + r) * g.c.d + ch));
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attend_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -232,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ unsigned char smem_raw[];
   __shared__ int runs[kFewMaxBatch / 32];  // units of 32 sequences each
   __shared__ float top[kWarps][kFewRows], tot[kWarps][kFewRows];
-  __shared__ unsigned bad_rows;
+  __shared__ int bad, share0, share_units;
   const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
   float *join = reinterpret_cast<float *>(smem_raw + (base - tc::smem_u32(smem_raw)) + F::kStages * F::kTileBytes);
   const uint32_t bars = tc::smem_u32(join) + F::kJoinBytes;
@@ -248,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc::mbar_fence_init();
     tc::tma_prefetch_map(&map_k);
     tc::tma_prefetch_map(&map_v);
-    bad_rows = 0;
+    bad = 0;
   }
   pdl_wait();  // q and the cache come from the kernels before
   pdl_trigger();
@@ -258,6 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const Shares shares(count_units(g, runs, kWarps + 2, run0), g.ctas);
   const int share = shares.start(blockIdx.x), share_end = shares.start(blockIdx.x + 1);
   if (share >= share_end) return;
+  if (threadIdx.x == 0) share0 = share, share_units = share_end - share;  // for the consumers' second walk
   w.seek(g, runs, run0, share, share_end);
 
   if (warp >= kWarps) {
@@ -479,32 +496,35 @@ __global__ void __launch_bounds__(kThreads, 1)
         // maximum of one that saw nothing: its sum, 0 or NaN, enters as it is.
 #pragma unroll
         for (int j = 0; j < kWarps; ++j) l += top[j][r] == -INFINITY ? tot[j][r] : tot[j][r] * exp2_fast(top[j][r] - m);
-        if (!finite4(v)) atomicOr(&bad_rows, 1u << r);
+        if (!finite4(v)) bad = 1;  // (any thread's word will do)
         put_row<T>(g, w, part, block0, hk, r, ch, v, m, l);
       }
       named_sync(32 * kWarps);
     }
-    // Rows that came out non-finite because of a value they do not see (see
-    // k_attend) are taken again without it.
-    const unsigned bad = bad_rows;
-    if (bad) {
-      named_sync(32 * kWarps);
-      if (threadIdx.x == 0) bad_rows = 0;
-      for (int r = warp; r < rows; r += kWarps) {
-        if (!(bad >> r & 1u)) continue;
-        const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
-        const int own = w.s.base + tok, from = w.tile * kTile, end = min((w.tile + w.count) * kTile, w.s.len);
-        const int rlo = max(g.window > 0 ? window_start(own, g.window) : 0, from);
-        const int rhi = min(g.causal ? min(w.s.len, own + 1) : w.s.len, end);
-        if (hidden_values_finite<T>(g, w.seq(), hk, from, min(rlo, end)) &&
-            hidden_values_finite<T>(g, w.seq(), hk, max(rhi, from), end))
-          continue;
-        const char *qr = g.q + 2 * ((long long)(w.s.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
-        float m, l;
-        float4 v = row_by_warp<T>(g, w.seq(), hk, qr, rlo, rhi, m, l);
-        if (4 * lane < g.c.d) put_row<T>(g, w, part, block0, hk, r, 4 * lane, v, m, l);
-      }
-      named_sync(32 * kWarps);
+  }
+
+  // Rows that came out non-finite because of a value they do not see (see
+  // k_attend) are taken again without it, when the share's tiles are all used
+  // up: this may take far longer than a producer would wait for its ring.
+  named_sync(32 * kWarps);  // the rows written by other warps
+  if (!ok || !bad) return;
+  w.seek(g, runs, seq_of(g, lane), share0, share0 + share_units);
+  while (w.next(g)) {
+    const int hk = w.item % g.c.heads, block0 = w.item / g.c.heads * kFewRows;
+    const int rows = min(kFewRows, w.s.rows - block0), part = 2 * blockIdx.x + (w.starts ? 1 : 0);
+    for (int r = warp; r < rows; r += kWarps) {
+      if (row_finite<T>(g, w, part, block0, hk, r)) continue;
+      const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
+      const int own = w.s.base + tok, from = w.tile * kTile, end = min((w.tile + w.count) * kTile, w.s.len);
+      const int rlo = max(g.window > 0 ? window_start(own, g.window) : 0, from);
+      const int rhi = min(g.causal ? min(w.s.len, own + 1) : w.s.len, end);
+      if (hidden_values_finite<T>(g, w.seq(), hk, from, min(rlo, end)) &&
+          hidden_values_finite<T>(g, w.seq(), hk, max(rhi, from), end))
+        continue;
+      const char *qr = g.q + 2 * ((long long)(w.s.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
+      float m, l;
+      float4 v = row_by_warp<T>(g, w.seq(), hk, qr, rlo, rhi, m, l);
+      if (4 * lane < g.c.d) put_row<T>(g, w, part, block0, hk, r, 4 * lane, v, m, l);
     }
   }
 }

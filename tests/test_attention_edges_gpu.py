@@ -114,3 +114,48 @@ def test_chunk_rows_without_hidden_bad_keys(case):
     seqs, hq, hk, d, page, dtype, window, scale, max_len = case
     _check_bad_keys(seqs, hq, hk, d, page, dtype, (2, 9, 30), window=window, scale=scale, repeats=10,
                     max_new=max(n for n, _ in seqs), max_len=max_len)
+
+
+FEW_BAD = [  # sequences, q heads, k heads, d, page, dtype, window, scale
+    ([(3, 40), (2, 100), (1, 33)], 4, 2, 64, 16, torch.bfloat16, 0, None),           # whole items
+    ([(4, 3000)], 4, 1, 128, 64, torch.bfloat16, 0, -0.15),                          # one item in many shares
+    ([(2, 700), (2, 1300), (0, 9), (2, 64)], 28, 4, 128, 16, torch.float16, 0, None),
+    ([(4, 400), (3, 130)] * 120, 4, 1, 64, 32, torch.bfloat16, 0, None),             # several items in a share
+    ([(1, 333), (1, 1000), (1, 5000)], 8, 2, 80, 16, torch.bfloat16, 7, None),       # below the window
+    ([(1, 250), (2, 900)] * 90, 8, 2, 64, 64, torch.float16, 20, -0.3),
+]
+
+
+@pytest.mark.parametrize("case", FEW_BAD, ids=lambda c: f"{len(c[0])}x{c[0][0][0]}of{c[0][0][1]}-{c[3]}-w{c[6]}")
+def test_few_rows_without_hidden_bad_keys(case):
+    seqs, hq, hk, d, page, dtype, window, scale = case
+    most = max(n for n, _ in seqs)
+    bad = (window + 4, window + 9) if window else (1, 2)[:most - 1]  # a draft's first token sees none of them
+    _check_bad_keys(seqs, hq, hk, d, page, dtype, bad, window=window, scale=scale, repeats=5, max_new=most)
+
+
+def test_few_rows_taken_again_over_a_long_history():
+    # 160 requests over the same pages, drafts of four tokens, an infinity in the last value: three tokens of each
+    # are taken again over 800 000 keys while the rest of the step goes on.  The rows' sums are chains of at most
+    # `length` additions in 32 bits.
+    batch, length, page, d, hq = 160, 800000, 256, 64, 4
+    g = torch.Generator(device=DEV).manual_seed(1)
+    pages = length // page + 1
+    k, v = (torch.randn(pages, 1, page, d, device=DEV, generator=g).to(torch.bfloat16) for _ in range(2))
+    v[(length - 1) // page, 0, (length - 1) % page] = float("inf")
+    cache = _alt().PagedCache(k, v)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV).repeat(batch, 1)
+    lens = torch.full((batch,), length, dtype=torch.int32, device=DEV)
+    cu = 4 * torch.arange(batch + 1, dtype=torch.int32, device=DEV)
+    q = _randn(4, hq, d, dtype=torch.bfloat16, seed=6)
+    got, lse = cache.attend(q.repeat(batch, 1, 1), table, lens, cu, max_new=4, return_lse=True)
+    assert int(cache.error) == 0
+    got, lse = got.view(batch, 4, hq, d), lse.view(batch, 4, hq)
+    keys, vals = k.reshape(-1, 1, d)[:length], v.reshape(-1, 1, d)[:length]
+    o, z, pv, e = _attend_ref(q, keys, vals, 4, True, 0, 1 / math.sqrt(d))
+    sums = 2.0 ** -17 + length * 2.0 ** -24
+    tol = U[torch.bfloat16] * o.abs() + (U[torch.bfloat16] + 2 * e + sums)[..., None] * pv + 2.0 ** -24
+    for b in range(batch):
+        _within(got[b, :3], o[:3], tol[:3], ("o", b))
+        _within(lse[b], z, e + sums * (1 + z.abs()), ("lse", b))
+        assert not torch.isfinite(got[b, 3]).any()  # the token that sees the infinity
