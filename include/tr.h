@@ -477,8 +477,10 @@ tr_status tr_rotary_backward(const tr_rotary *r, int32_t dtype, int32_t tokens, 
  * counts the keys of sequence b with the step's new tokens, which are its
  * last: new token t, cu_new[b] <= t < cu_new[b+1], is key
  * lens[b] - cu_new[b+1] + t.  All of this may change on the device between
- * replays of a captured graph.  page is a power of two from 16 to 256,
- * head_dim a multiple of 16 up to 128.  Nothing outside the cache is
+ * replays of a captured graph; rows from cu_new[batch] on, if total_new is
+ * larger, belong to no sequence (a graph captured for more tokens than a
+ * replay has): they append nothing and attend to nothing.  page is a power
+ * of two from 16 to 256, head_dim a multiple of 16 up to 128.  Nothing outside the cache is
  * touched whatever the device arrays hold: keys beyond max_pages * page do
  * not exist, a page id outside [0, pages) takes no append and reads as
  * zeros.  d_error (optional device int32, zero it first) then gets
@@ -495,7 +497,7 @@ typedef struct {
   int32_t batch, max_pages;
   const int32_t *lens;     /* device [batch]                       */
   const int32_t *cu_new;   /* device [batch + 1], cu_new[0] = 0    */
-  int32_t total_new;       /* host: cu_new[batch]                  */
+  int32_t total_new;       /* host: rows; cu_new[batch] at most    */
 } tr_cache;
 
 /*
@@ -514,7 +516,8 @@ tr_status tr_cache_append(const tr_cache *c, const tr_heads *k, const tr_heads *
  * the visible keys j of key head h / (q heads / key heads).  With
  * i = lens[b] - cu_new[b+1] + t the token's own key, key j is visible when
  *   0 <= j < lens[b],  j <= i if causal,  j > i - window if window > 0.
- * A row that sees no key (or only scores of -inf) gives zeros (lse = -inf).
+ * A row that sees no key (or only scores of -inf, or of no sequence) gives
+ * zeros (lse = -inf).
  * A key that a row does not see takes no part in it, whatever it holds (a
  * row whose tiles hold a hidden non-finite value is computed again without
  * it, slowly).  Probabilities are rounded to the cache's type for their

@@ -86,6 +86,22 @@ __device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
   return v;
 }
 
+// The block of tokens that belong to no sequence (first: their first) in this
+// slot: zeros, lse -inf.
+__device__ __noinline__ void clear_block(const AttendArgs &g, int first, int slot, int rows_per_block, int hk) {
+  const int rows = (g.c.total_new - first) * g.group;
+  const int block = slot - ((int)((long long)first * g.group / rows_per_block) + g.c.batch);
+  if (block < 0) return;  // an empty slot of the last sequence
+  const int r0 = block * rows_per_block, chunks = g.c.d / 8;
+  for (int i = threadIdx.x; i < min(rows - r0, rows_per_block) * chunks; i += blockDim.x) {
+    const int r = r0 + i / chunks, c = i % chunks;
+    const long long t = first + r / g.group;
+    const int head = hk * g.group + r % g.group;
+    *reinterpret_cast<uint4 *>(g.o + 2 * (t * g.o_tok + (long long)head * g.o_head) + 16 * c) = make_uint4(0u, 0u, 0u, 0u);
+    if (c == 0 && g.lse) g.lse[t * g.q_heads + head] = -INFINITY;
+  }
+}
+
 template <typename T, int D, int MT, bool PAIRED>
 __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1)
     k_attend(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -112,7 +128,10 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
   const int slot = gridDim.x - 1 - blockIdx.x;  // causal chunks: the longest key ranges first
   const int hk = blockIdx.y, split = blockIdx.z;
   const Block k = find_block(g, slot, kRows);
-  if (k.seq < 0) return;
+  if (k.seq < 0) {  // (with parts of the keys the join sees to the tokens of no sequence)
+    if (k.end < g.c.total_new && g.splits == 1) clear_block(g, k.end, slot, kRows, hk);
+    return;
+  }
 
   // tiles of the whole CTA and of each 128-row block, cut to this split
   int t0, t1, a[MT], b[MT];
@@ -573,7 +592,7 @@ Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_le
   p.paired = tiles <= kPairedTiles;
   p.mt = most <= kTile || p.paired ? 1 : 2;
   const int rows = kTile * p.mt;
-  p.slots = (int)((long long)c->total_new * group / rows) + c->batch;
+  p.slots = (int)((long long)c->total_new * group / rows) + c->batch + 1;  // (tokens of no sequence: one more)
   if (p.paired) {
     p.splits = 1;
     p.split_tiles = tiles;
@@ -584,7 +603,7 @@ Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_le
   // writing and reading a row's fp32 sums once per part (kJoinRows rows in
   // the time of one tile).
   constexpr double kCtaTiles = 4.0, kJoinRows = 8192.0;
-  const double blocks = (double)p.slots * c->heads;
+  const double blocks = (double)(p.slots - 1) * c->heads;
   double best = 0;
   for (int s = 1; s <= 64 && s <= (tiles > 1 ? tiles : 1); ++s) {
     const double waves = std::ceil(blocks * s / sms);
@@ -666,7 +685,7 @@ tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *
   if (reinterpret_cast<uintptr_t>(lse) & 3u) return TR_ERR_ALIGN;
   if ((long long)c->total_new * q->heads > INT_MAX - 65536) return TR_ERR_UNSUPPORTED;
   if (c->heads > 65535) return TR_ERR_UNSUPPORTED;
-  if (c->total_new == 0 || c->batch == 0) return TR_OK;
+  if (c->total_new == 0) return TR_OK;
   const Plan p = plan_of(c, q->heads, window, max_new, max_len);
   if (p.total && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < p.total)) return TR_ERR_WORKSPACE;
   AttendArgs g{};

@@ -66,13 +66,15 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // ---------------------------------------------------------------- where a CTA works
 // Sequence b's row blocks occupy the slots from floor(cu_new[b] group / R) + b
 // on (R rows a block), which leaves room for all of them whatever cu_new
-// holds; the last slot of a sequence may stay empty.
+// holds; the last slot of a sequence may stay empty.  The tokens behind the
+// last sequence's, which belong to none, have the slots behind its own.
 struct Block {
   int seq, first;     // sequence, first row (token * group + head) of the block
   int rows;           // rows of the sequence: new tokens * group
   int tok0;           // first new token of the sequence
   int base;           // key of new token 0
   int len;            // keys of the sequence
+  int end;            // the last sequence's slots and those behind: first token of no sequence (others: total_new)
 };
 
 // All lanes of a warp together; seq = -1 for an empty slot.
@@ -92,10 +94,12 @@ __device__ __forceinline__ Block find_block(const AttendArgs &g, int slot, int r
   Block k;
   k.seq = -1;
   k.rows = k.first = k.tok0 = k.base = k.len = 0;
+  k.end = c.batch ? c.total_new : 0;
   if (b < 0) return k;
   const int t0 = __ldg(c.cu_new + b), t1 = min(__ldg(c.cu_new + b + 1), c.total_new);
   const int n = t1 > t0 ? t1 - t0 : 0;
   const long long start = ((long long)t0 * g.group) / rows_per_block + b;
+  if (b + 1 == c.batch) k.end = max(t1, 0);
   k.first = (int)((slot - start) * rows_per_block);
   k.rows = n * g.group;
   if (t0 < 0 || k.first < 0 || k.first >= k.rows) return k;

@@ -33,6 +33,7 @@ struct NewToken {
   int key;  // its own key; negative or past the table when lens and cu_new disagree
 };
 __device__ __forceinline__ NewToken find_token(const CacheView &c, int t) {
+  if (c.batch == 0) return NewToken{-1, -1};
   int lo = 0, hi = c.batch;  // the last b with cu_new[b] <= t
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;

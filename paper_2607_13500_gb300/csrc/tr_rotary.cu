@@ -777,7 +777,7 @@ tr_status tr_cache_append(const tr_cache *c, const tr_heads *k, const tr_heads *
   if ((rc = check_heads(k, 2)) != TR_OK || (rc = check_heads(v, 2)) != TR_OK) return rc;
   if (misaligned16(k_weight) || (reinterpret_cast<uintptr_t>(pos) & 3u)) return TR_ERR_ALIGN;
   if ((rc = check_pair(q, q_out, q_weight, 2, false)) != TR_OK) return rc;
-  if (c->total_new == 0 || c->batch == 0) return TR_OK;
+  if (c->total_new == 0) return TR_OK;
   const int rot = r ? r->rot_dim : 0;
   RotArgs g{};
   shape(g, c->dtype, c->head_dim, rot, c->total_new);

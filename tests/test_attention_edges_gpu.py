@@ -159,3 +159,77 @@ def test_few_rows_taken_again_over_a_long_history():
         _within(got[b, :3], o[:3], tol[:3], ("o", b))
         _within(lse[b], z, e + sums * (1 + z.abs()), ("lse", b))
         assert not torch.isfinite(got[b, 3]).any()  # the token that sees the infinity
+
+
+UNOWNED = [  # sequences (new, length), rows of the call, q heads, k heads, d, page, max_new, max_len
+    ([(1, 50), (1, 300), (1, 17)], 5, 4, 2, 64, 16, 1, 300),      # few rows
+    ([(1, 3000)], 2, 7, 1, 128, 64, 1, 3000),
+    ([(40, 300), (1, 100)], 45, 14, 2, 128, 16, 40, 400),         # chunks, the keys in one part
+    ([(3, 300)], 700, 7, 1, 64, 32, 700, 400),
+    ([(127, 200)], 128, 4, 4, 80, 16, 128, 400),
+    ([(128, 200)], 129, 4, 4, 80, 16, 128, 400),
+    ([(300, 700)] * 16, 5000, 7, 1, 128, 64, 300, 700),
+    ([(200, 4000)], 257, 4, 2, 64, 32, 200, 4000),                # in parts
+    ([(0, 100), (0, 0)], 150, 4, 2, 64, 32, 100, 100),            # no new token at all
+    ([], 3, 4, 2, 64, 16, 1, 100),                                # no sequence
+    ([], 300, 4, 2, 64, 16, 300, 100),
+]
+
+
+@pytest.mark.parametrize("case", UNOWNED, ids=lambda c: f"{len(c[0])}seqs-{c[1]}rows-{c[2]}-{c[3]}-{c[4]}")
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_rows_of_no_sequence_come_out_as_zeros(case, dtype):
+    # more rows than cu_new hands out: the same zeros whichever kernel takes the call
+    seqs, rows, hq, hk, d, page, max_new, max_len = case
+    cache, table, lens, cu, keys, vals = _step(seqs, hk, page, d, dtype, 5)
+    q = _randn(rows, hq, d, dtype=dtype, seed=6, gain=1.5)
+    wide = torch.full((rows, hq + 1, d), 7.0, dtype=dtype, device=DEV)
+    got, lse = cache.attend(q, table, lens, cu, max_new=max_new, max_len=max_len, return_lse=True, out=wide[:, :hq])
+    owned = int(cu[-1])
+    assert (got[owned:] == 0).all() and (lse[owned:] == -math.inf).all()
+    assert (wide[:, hq] == 7).all()
+    spoilt = torch.zeros(rows, hq, dtype=torch.bool, device=DEV)
+    _check_rows(got, lse, q, keys, vals, seqs, cu, spoilt)
+    assert int(cache.error) == 0
+
+
+def test_graph_with_fewer_rows_than_captured():
+    # a graph captured for 300 rows serves 300, 40 and none
+    cache, table, lens, cu, keys, vals = _step([(300, 900)], 2, 32, 64, torch.bfloat16, 5)
+    q = _randn(300, 8, 64, dtype=torch.bfloat16, seed=6, gain=1.5)
+    out = torch.empty_like(q)
+    cache.attend(q, table, lens, cu, max_new=300, max_len=600, out=out)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cache.attend(q, table, lens, cu, max_new=300, max_len=600, out=out)
+    for n in (300, 40, 0):
+        cu[1] = n
+        g.replay()
+        assert (out[n:] == 0).all()
+        if n:
+            o, _, pv, e = _attend_ref(q[:n], keys[0], vals[0], n, True, 0, 1 / 8)
+            _within(out[:n], o, U[torch.bfloat16] * o.abs() + (U[torch.bfloat16] + 2 * e + 2.0 ** -17)[..., None] * pv
+                    + 2.0 ** -24, n)
+
+
+@pytest.mark.parametrize("seqs", [[(20, 100), (3, 40)], []])
+def test_append_rows_of_no_sequence(seqs):
+    # their keys and values go nowhere, their queries are turned all the same
+    altr = _alt()
+    cache, table, lens, cu, _, _ = _step(seqs, 2, 16, 64, torch.bfloat16, 5, stale=3.0)
+    rows = _randn(40, 8, 64, dtype=torch.bfloat16, seed=6)
+    q, k, v = rows[:, :4], rows[:, 4:6], rows[:, 6:]
+    pos = torch.arange(40, dtype=torch.int32, device=DEV)
+    r = altr.Rotary(64, DEV)
+    want_k, want_v = cache.k.clone(), cache.v.clone()
+    rq, rk = r.apply(q, k, pos)
+    for b, (n, length) in enumerate(seqs):
+        for i in range(n):
+            j = length - n + i
+            want_k[table[b, j // 16], :, j % 16] = rk[int(cu[b]) + i]
+            want_v[table[b, j // 16], :, j % 16] = v[int(cu[b]) + i]
+    out = torch.full_like(q, 7.0)
+    got = cache.append(k, v, table, lens, cu, rotary=r, pos=pos, q=q, q_out=out)
+    assert torch.equal(got, rq)
+    assert torch.equal(cache.k, want_k) and torch.equal(cache.v, want_v)
+    assert int(cache.error) == 0
