@@ -13,6 +13,9 @@
  *    device memory, frees it or synchronises.  Every call enqueues work on
  *    `stream` (a cudaStream_t; NULL is the legacy default stream) and returns
  *    at once.  (A tr_pipeline owns host-side CUDA events, see below.)
+ *  - The device of `stream` and of the pointers is the current one (a NULL
+ *    stream names no device, and launch shapes follow the current device's
+ *    SM count); the Python binding makes its tensors' device current itself.
  *  - Host-detectable errors (null or misaligned pointers, bad sizes, too small
  *    a workspace) are returned before anything is launched; outputs are left
  *    untouched.  A launch failure returns TR_ERR_CUDA.

@@ -12,6 +12,7 @@ from dataclasses import dataclass
 import torch
 
 from . import _lib
+from ._device import on_device_of, resolved
 from ._lib import (STRIDE_MODES, TR_ACT, TR_BF16, TR_F16, TR_F32, TR_STATS_WORDS, TR_STATUS_WORDS, TrMlp,
                    TrTokens, check, load)
 
@@ -110,11 +111,13 @@ def budgets(seqlens, k=None, ratio=None, lam=(1, 3)):
     return list(hk)[:b], list(hk1)[:b], list(hcu)
 
 
+@on_device_of("x")
 def workspace_bytes(x, x_pre, x_post, seqlens=None) -> int:
     x, x_pre, x_post, seqlens = _flatten(x, x_pre, x_post, seqlens)
     return load().tr_workspace_bytes(_Tokens(x, x_pre, x_post, seqlens).ref())
 
 
+@on_device_of("x")
 def score(x, x_pre, x_post, seqlens=None):
     """tr_score: returns (stats [T, 8] fp32, h2 [T] fp32, s [T] fp32)."""
     lib = load()
@@ -135,6 +138,7 @@ def _workspace(lib, tok, device):
     return ws, nbytes
 
 
+@on_device_of("x")
 def select(x, x_pre, x_post, stats, k=None, ratio=None, lam=(1, 3), seqlens=None, h2=None, s=None, budget=None,
            stride="alg1"):
     """tr_select: returns (idx int32 [sum K], role uint8 [T], cu_k list, status int32 [4]).
@@ -185,7 +189,7 @@ class Reducer:
                  budget=None, stride="alg1"):
         self.lib = load()
         self.seqlens = [int(v) for v in seqlens]
-        self.device = torch.device(device)
+        self.device = resolved(device)
         self.d, self.dtype, self.alias_pre, self.stride = d, dtype, alias_pre, stride
         self.ks, self.k1s, self.cu_k = budget if budget is not None else budgets(self.seqlens, k, ratio, lam)
         self.total_k = self.cu_k[-1]
@@ -205,6 +209,8 @@ class Reducer:
 
     def _bind(self, x, x_pre, x_post):
         x, x_pre, x_post, _ = _flatten(x, x_pre, x_post, self.seqlens)
+        if x.device != self.device:
+            raise ValueError(f"the token tensors must be on {self.device}, not {x.device}")
         key = (x.data_ptr(), None if x_pre is None else x_pre.data_ptr(), x_post.data_ptr())
         if self._tok is None or self._in != key:
             self._tok = _Tokens(x, x_pre, x_post, self.seqlens, self.stride)
@@ -213,6 +219,7 @@ class Reducer:
                 self._ws, self._ws_bytes = _workspace(self.lib, self._tok, self.device)
         return self._tok
 
+    @on_device_of("self")
     def run(self, x, x_pre, x_post) -> ReduceResult:
         tok = self._bind(x, x_pre, x_post)
         check("tr_reduce", self.lib.tr_reduce(
@@ -222,6 +229,7 @@ class Reducer:
         return ReduceResult(self.y[:self.total_k], self.idx[:self.total_k], self.cu_k, self.h2, self.s,
                             self.status)
 
+    @on_device_of("self")
     def graph(self, x, x_pre, x_post) -> "torch.cuda.CUDAGraph":
         """``run`` (with the status words zeroed first) captured into a CUDA
         graph for these input tensors; ``replay()`` repeats it with one
@@ -234,6 +242,7 @@ class Reducer:
             self.run(x, x_pre, x_post)
         return g
 
+    @on_device_of("self")
     def run_split(self, x, x_pre, x_post, events=None):
         """The same two kernels as ``run`` through the entry points tr_score
         and tr_select_gather, with ``events`` (three torch.cuda.Event, or
@@ -256,6 +265,7 @@ class Reducer:
         return ReduceResult(self.y[:self.total_k], self.idx[:self.total_k], self.cu_k, self.h2, self.s,
                             self.status)
 
+    @on_device_of("self")
     def run_select_gather(self, x, x_pre, x_post, stats, events=None):
         """tr_select then tr_gather on statistics records made elsewhere (e.g.
         by Mlp's fused scoring), on the current stream; ``events`` (three
@@ -278,6 +288,7 @@ class Reducer:
         return ReduceResult(self.y[:self.total_k], self.idx[:self.total_k], self.cu_k, self.h2, self.s,
                             self.status)
 
+    @on_device_of("self")
     def run_separate(self, x, x_pre, x_post, events=None):
         """The three kernels the pipeline launches, tr_score, tr_select and
         tr_gather, on the current stream, with ``events`` (four
@@ -313,6 +324,7 @@ class Reducer:
         mk = lambda: torch.empty(t, self.d, dtype=self.dtype, device=self.device)
         return mk(), (None if self.alias_pre else mk()), mk()
 
+    @on_device_of("self")
     def run_host(self, x_h, x_pre_h, x_post_h, dev_in, y_h, idx_h) -> ReduceResult:
         """End-to-end: pinned host inputs -> device -> reduce -> pinned host y, idx."""
         dx, dp, dq = dev_in
@@ -341,7 +353,7 @@ class Pipeline:
                  budget=None, slots=2, stride="alg1", score_streams=None):
         self.lib = load()
         self.seqlens = [int(v) for v in seqlens]
-        self.device = torch.device(device)
+        self.device = resolved(device)
         self.d, self.dtype, self.alias_pre, self.slots, self.stride = d, dtype, alias_pre, int(slots), stride
         self.ks, self.k1s, self.cu_k = budget if budget is not None else budgets(self.seqlens, k, ratio, lam)
         self.total_k = self.cu_k[-1]
@@ -369,6 +381,8 @@ class Pipeline:
 
     def _bind(self, x, x_pre, x_post):
         x, x_pre, x_post, _ = _flatten(x, x_pre, x_post, self.seqlens)
+        if x.device != self.device:
+            raise ValueError(f"the token tensors must be on {self.device}, not {x.device}")
         key = (x.data_ptr(), None if x_pre is None else x_pre.data_ptr(), x_post.data_ptr())
         if self._tok is None or self._in != key:
             self._tok = _Tokens(x, x_pre, x_post, self.seqlens, self.stride)
@@ -390,6 +404,7 @@ class Pipeline:
             self._handle = handle
         return self._tok
 
+    @on_device_of("self")
     def submit(self, x, x_pre, x_post, score_events=None, after_current=True) -> ReduceResult:
         """Enqueues one batch; ``score_events`` (two torch.cuda.Event, or
         None) are recorded on the slot's score stream around the score
@@ -416,6 +431,7 @@ class Pipeline:
         self.submitted += 1
         return ReduceResult(o["y"][:self.total_k], o["idx"][:self.total_k], self.cu_k, o["h2"], o["s"], o["status"])
 
+    @on_device_of("self")
     def submit_host(self, x_h, x_pre_h, x_post_h, y_h, idx_h) -> ReduceResult:
         """End to end from pinned host memory: copies this batch's inputs into
         the slot's device buffers on a copy-in stream, submits it, and copies
@@ -454,6 +470,7 @@ class Pipeline:
         h["out_free"][slot] = out
         return r
 
+    @on_device_of("self")
     def graph(self, x, x_pre, x_post, steps=16, score_events=None, inputs=None) -> "torch.cuda.CUDAGraph":
         """``steps`` pipelined submissions of these input tensors captured into
         one CUDA graph: ``replay()`` runs them (each step's selection and
@@ -493,6 +510,7 @@ class Pipeline:
         self._graphed = True
         return g
 
+    @on_device_of("self")
     def graph_host(self, x_h, x_pre_h, x_post_h, y_h, idx_h, steps=16) -> "torch.cuda.CUDAGraph":
         """``steps`` end-to-end steps (``submit_host``: pinned host inputs
         copied in, reduced, y and idx copied back to the pinned ``y_h`` /
@@ -532,6 +550,7 @@ class Pipeline:
         captured graph launches per replay)."""
         return int(self.lib.tr_pipeline_kernels(self._handle)) if self._handle is not None else 0
 
+    @on_device_of("self")
     def wait(self, stream=None):
         """Makes ``stream`` (default: the current stream) wait for every submission."""
         st = stream if stream is not None else torch.cuda.current_stream(self.device)
@@ -559,6 +578,7 @@ class Pipeline:
             pass
 
 
+@on_device_of("x")
 def reduce(x, x_pre, x_post, k=None, ratio=None, lam=(1, 3), seqlens=None, scores=False, budget=None,
            stride="alg1"):
     """tr_reduce in one call: returns a ReduceResult (device tensors).
@@ -631,6 +651,7 @@ class Mlp:
                      b2=None if self.b2 is None else self.b2.data_ptr(),
                      t=self.t, d=self.d, d_hidden=self.dh, act=TR_ACT[self.act])
 
+    @on_device_of("self")
     def run(self, x_pre, resid=None, events=None) -> MlpResult:
         """Both GEMMs on the current stream; ``events`` (three torch.cuda.Event
         or None) are recorded before, between and after them."""
@@ -657,12 +678,14 @@ class Mlp:
                          self.error)
 
 
+@on_device_of("x_pre")
 def mlp(x_pre, w1, w2, b1=None, b2=None, resid=None, act="gelu", scores=False) -> MlpResult:
     """The encoder's final-layer MLP with the scoring fused in, in one call
     (Eq. 5; see Mlp)."""
     return Mlp(x_pre.shape[0], w1, w2, b1, b2, act, scores).run(x_pre, resid)
 
 
+@on_device_of("x")
 def project_kept(x, idx, cu_k, w, bias=None, act="gelu", seqlens=None, error=None):
     """tr_project_kept: z = sigma(X* W^T + bias) for the kept tokens X*, their
     rows read from ``x`` by the selection's ``idx`` (local per image, image b
@@ -690,6 +713,7 @@ def project_kept(x, idx, cu_k, w, bias=None, act="gelu", seqlens=None, error=Non
     return z[:total_k], err
 
 
+@on_device_of("y")
 def project(y, w, bias=None, act="gelu", error=None, out=None):
     """tr_project: z = sigma(y W^T + bias) for rows already gathered (tr_gather's
     y, bf16 [rows, D]); ``w`` bf16 [d_out, D], ``bias`` fp32 [d_out] or None;

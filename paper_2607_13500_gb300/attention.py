@@ -3,8 +3,9 @@ several axes (``Rotary``) and the paged key/value cache (``PagedCache``).
 
 As in api.py the kernels run in libtr on the current stream and nothing here
 computes on the host: the binding checks what the C side cannot (types,
-shapes, the device), supplies outputs and workspaces, and raises when libtr.so
-is missing or a tensor is not on the CUDA device.  No call synchronises.
+shapes, the device), supplies outputs and workspaces, makes the tensors' device
+current around the call, and raises when libtr.so is missing or a tensor is not
+on the CUDA device.  No call synchronises.
 """
 from __future__ import annotations
 
@@ -16,6 +17,7 @@ from dataclasses import dataclass
 import torch
 
 from . import _lib
+from ._device import at, resolved
 from ._lib import TR_BF16, TR_F16, TR_F32, TR_ROTARY_LAYOUT, check, load
 
 _CODES = {torch.bfloat16: TR_BF16, torch.float16: TR_F16, torch.float32: TR_F32}
@@ -58,10 +60,9 @@ def _library():
 
 
 def _device(device):
-    dev = torch.device(device)
-    if dev.type != "cuda":
+    if torch.device(device).type != "cuda":
         raise ValueError("a CUDA device is needed (libtr has no CPU path)")
-    return torch.device("cuda", torch.cuda.current_device()) if dev.index is None else dev
+    return resolved(device)
 
 
 try:  # the raw handle without a Stream object around it
@@ -176,7 +177,7 @@ class Rotary:
             k_out, hko = _output(k_out, k, "k_out", i)
         wq, wk = _vector(q_weight, "q_weight", d, i), _vector(k_weight, "k_weight", d, i)
         if t:
-            rc = self.calls.rotary_apply(self._struct, code, t, p, hq, wq, hqo, hk, wk, hko, eps, _stream(i))
+            rc = at(i, self.calls.rotary_apply)(self._struct, code, t, p, hq, wq, hqo, hk, wk, hko, eps, _stream(i))
             if rc:
                 check("tr_rotary_apply", rc)
         return q_out, k_out
@@ -211,11 +212,11 @@ class Rotary:
             return RotaryGrads(gq, gk, None if wq is None else wq.zero_(), None if wk is None else wk.zero_())
         nbytes = 0
         if wq is not None or wk is not None:
-            nbytes = self.calls.rotary_backward_workspace_bytes(self._struct, t)
+            nbytes = at(i, self.calls.rotary_backward_workspace_bytes)(self._struct, t)
             ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         ptr = lambda x: None if x is None else x.data_ptr()
-        rc = self.calls.rotary_backward(self._struct, code, t, p, hdq, hq, pq, hgq, ptr(wq), hdk, hk, pk, hgk, ptr(wk),
-                                        eps, ptr(ws), nbytes, _stream(i))
+        rc = at(i, self.calls.rotary_backward)(self._struct, code, t, p, hdq, hq, pq, hgq, ptr(wq), hdk, hk, pk, hgk,
+                                               ptr(wk), eps, ptr(ws), nbytes, _stream(i))
         if rc:
             check("tr_rotary_backward", rc)
         return RotaryGrads(gq, gk, wq, wk)
@@ -280,7 +281,8 @@ class PagedCache:
             q_out, hqo = _output(q_out, q, "q_out", i)
         wq, wk = _vector(q_weight, "q_weight", d, i), _vector(k_weight, "k_weight", d, i)
         if t:
-            rc = self.calls.cache_append(c, hk, hv, r, p, wk, hq, wq, hqo, eps, self.error.data_ptr(), _stream(i))
+            rc = at(i, self.calls.cache_append)(c, hk, hv, r, p, wk, hq, wq, hqo, eps, self.error.data_ptr(),
+                                                _stream(i))
             if rc:
                 check("tr_cache_append", rc)
         return None if q is None else q_out
@@ -310,13 +312,13 @@ class PagedCache:
             if nbytes is None:
                 if len(self._sizes) >= 4096:
                     self._sizes.clear()
-                nbytes = self.calls.cache_attend_workspace_bytes(c, heads, window, max_new, max_len)
+                nbytes = at(i, self.calls.cache_attend_workspace_bytes)(c, heads, window, max_new, max_len)
                 self._sizes[key] = nbytes
             ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
-            rc = self.calls.cache_attend(
-                c, hq, ho, None if lse is None else lse.data_ptr(), 1.0 / math.sqrt(d) if scale is None else scale,
-                1 if causal else 0, window, max_new, max_len, None if ws is None else ws.data_ptr(), nbytes,
-                self.error.data_ptr(), _stream(i))
+            rc = at(i, self.calls.cache_attend)(
+                c, hq, ho, None if lse is None else lse.data_ptr(),
+                1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0, window, max_new, max_len,
+                None if ws is None else ws.data_ptr(), nbytes, self.error.data_ptr(), _stream(i))
             if rc:
                 check("tr_cache_attend", rc)
         return (out, lse) if return_lse else out
