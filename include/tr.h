@@ -487,7 +487,8 @@ tr_status tr_rotary_backward(const tr_rotary *r, int32_t dtype, int32_t tokens, 
  * touched whatever the device arrays hold: keys beyond max_pages * page do
  * not exist, a page id outside [0, pages) takes no append and reads as
  * zeros.  d_error (optional device int32, zero it first) then gets
- * TR_CACHE_ERR_PAGE, or TR_CACHE_ERR_WAIT when a pipeline wait inside the
+ * TR_CACHE_ERR_PAGE (for the attention: if some row sees a key there; pages
+ * before every window may be given away), or TR_CACHE_ERR_WAIT when a pipeline wait inside the
  * attention timed out (not expected in a correct run; outputs incomplete).
  */
 #define TR_CACHE_ERR_PAGE 1

@@ -194,6 +194,7 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
     TileRing<D, S::kStages, true> tiles;
     tiles.base = ring, tiles.full0 = full(0), tiles.empty0 = empty(0), tiles.tail = tail;
     tiles.take(warp == 4 * MT ? 0 : 1);
+    tiles.seen = keys_of_rows(g, k, k.first, min(k.first + kRows, k.rows));
     const CUtensorMap *map = warp == 4 * MT ? &map_k : &map_v;
     bool ok = true;
     int id = t0 < t1 ? tiles.page_id(g, k.seq, k.len, t0) : -1;

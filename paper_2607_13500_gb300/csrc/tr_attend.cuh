@@ -206,6 +206,7 @@ struct TileRing {
   static constexpr int kK = (STAGES + 1) / 2;
   uint32_t base, full0, empty0, tail;
   int kv = 0, stage = 0;  // 0: K, 1: V; position of the next tile
+  Range seen;             // keys that some row sees: a bad page is only an error there
   uint32_t phase = 0, tails = 0, filled = 0, parity = 0;
 
   __device__ __forceinline__ void take(int kind) {
@@ -242,7 +243,7 @@ struct TileRing {
     int row = max(1, g.c.pages * g.c.heads * page);  // a row past the cache: reads as zeros
     if (mine) {
       if ((unsigned)id < (unsigned)g.c.pages) row = (id * g.c.heads + hk) * page + ((key0 + pc * piece) & (page - 1));
-      else flag(g, TR_CACHE_ERR_PAGE);
+      else if (key0 + pc * piece < seen.hi && key0 + (pc + 1) * piece > seen.lo) flag(g, TR_CACHE_ERR_PAGE);
     }
     const uint32_t bytes = (uint32_t)pieces * piece * 128u * kHalves;
     if (!tc::mbar_wait_warp(empty(stage), phase ^ 1u)) return false;

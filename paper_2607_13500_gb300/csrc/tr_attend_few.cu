@@ -53,19 +53,22 @@ struct Seq {
   int tile0, tiles;  // first tile, tiles
   int items;         // blocks of rows x key heads
 };
+__device__ __forceinline__ Range keys_of_seq(const AttendArgs &g, const Seq &s) {
+  Block k;
+  k.len = s.len;
+  k.base = s.base;
+  return keys_of_rows(g, k, 0, s.rows);
+}
 __device__ __forceinline__ Seq seq_of(const AttendArgs &g, int b) {
   Seq s{0, 0, 0, 0, 0, 0, 0};
   if (b >= g.c.batch) return s;
   const int t0 = __ldg(g.c.cu_new + b), t1 = min(__ldg(g.c.cu_new + b + 1), g.c.total_new);
   if (t0 < 0 || t1 <= t0) return s;
-  Block k;
-  k.len = cache_len(g.c, b);
-  k.base = max(__ldg(g.c.lens + b), 0) - (t1 - t0);
   s.tok0 = t0;
   s.rows = (t1 - t0) * g.group;
-  s.len = k.len;
-  s.base = k.base;
-  const Range r = keys_of_rows(g, k, 0, s.rows);
+  s.len = cache_len(g.c, b);
+  s.base = max(__ldg(g.c.lens + b), 0) - (t1 - t0);
+  const Range r = keys_of_seq(g, s);
   s.tile0 = r.lo / kTile;
   s.tiles = (r.hi + kTile - 1) / kTile - s.tile0;
   s.items = (s.rows + kFewRows - 1) / kFewRows * g.c.heads;
@@ -283,6 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     while (ok && w.next(g)) {
       const int hk = w.item % g.c.heads, end = w.tile + w.count;
+      ring.seen = keys_of_seq(g, w.s);
       int id = ring.page_id(g, w.seq(), w.s.len, w.tile);
       for (int t = w.tile; t < end && ok; ++t) {
         const int next = t + 1 < end ? ring.page_id(g, w.seq(), w.s.len, t + 1) : -1;

@@ -233,3 +233,37 @@ def test_append_rows_of_no_sequence(seqs):
     assert torch.equal(got, rq)
     assert torch.equal(cache.k, want_k) and torch.equal(cache.v, want_v)
     assert int(cache.error) == 0
+
+
+GIVEN_AWAY = [  # sequences, q heads, k heads, page, window
+    ([(1, 300), (1, 1000), (1, 40)], 4, 2, 16, 50),       # few rows
+    ([(3, 2000)], 4, 1, 32, 129),
+    ([(1, 70)], 8, 8, 16, 1),
+    ([(40, 300), (90, 1500)], 4, 2, 16, 50),              # chunks
+    ([(300, 2000)], 7, 1, 64, 500),
+    ([(33, 200)] * 30, 4, 4, 128, 20),
+]
+
+
+@pytest.mark.parametrize("case", GIVEN_AWAY, ids=lambda c: f"{len(c[0])}x{c[0][0][0]}of{c[0][0][1]}-p{c[3]}-w{c[4]}")
+@pytest.mark.parametrize("gone", [-1, 2 ** 31 - 1])
+def test_pages_before_the_window_may_be_given_away(case, gone):
+    # table entries that no row's window reaches are no error; the first one that a window reaches is
+    seqs, hq, hk, page, window = case
+    cache, table, lens, cu, keys, vals = _step(seqs, hk, page, 64, torch.bfloat16, 5)
+    q = _randn(int(cu[-1]), hq, 64, dtype=torch.bfloat16, seed=6, gain=1.5)
+    most = dict(max_new=max(n for n, _ in seqs), max_len=max(n for _, n in seqs))
+    first = [max(0, length - n - window + 1) // page for n, length in seqs]  # the page of the first key in a window
+    for b, p in enumerate(first):
+        table[b, :p] = gone
+    got, lse = cache.attend(q, table, lens, cu, window=window, return_lse=True, **most)
+    assert int(cache.error) == 0
+    spoilt = torch.zeros(q.shape[:2], dtype=torch.bool, device=DEV)
+    _check_rows(got, lse, q, keys, vals, seqs, cu, spoilt, window=window)
+    for b, p in enumerate(first):
+        cache.error.zero_()
+        kept = int(table[b, p])
+        table[b, p] = gone
+        cache.attend(q, table, lens, cu, window=window, **most)
+        assert int(cache.error) == 1, b
+        table[b, p] = kept
