@@ -483,13 +483,14 @@ tr_status tr_rotary_backward(const tr_rotary *r, int32_t dtype, int32_t tokens, 
  * replays of a captured graph; rows from cu_new[batch] on, if total_new is
  * larger, belong to no sequence (a graph captured for more tokens than a
  * replay has): they append nothing and attend to nothing.  page is a power
- * of two from 16 to 256, head_dim a multiple of 16 up to 128.  Nothing outside the cache is
- * touched whatever the device arrays hold: keys beyond max_pages * page do
- * not exist, a page id outside [0, pages) takes no append and reads as
- * zeros.  d_error (optional device int32, zero it first) then gets
- * TR_CACHE_ERR_PAGE (for the attention: if some row sees a key there; pages
- * before every window may be given away), or TR_CACHE_ERR_WAIT when a pipeline wait inside the
- * attention timed out (not expected in a correct run; outputs incomplete).
+ * of two from 16 to 256, head_dim a multiple of 16 up to 128.  Nothing
+ * outside the cache is touched whatever the device arrays hold: keys beyond
+ * max_pages * page do not exist, a page id outside [0, pages) takes no append
+ * and reads as zeros.  d_error (optional device int32, zero it first) then
+ * gets TR_CACHE_ERR_PAGE (for the attention: if some row sees a key there;
+ * pages before every window may be given away), or TR_CACHE_ERR_WAIT when a
+ * pipeline wait inside the attention timed out (not expected in a correct
+ * run; outputs incomplete).
  */
 #define TR_CACHE_ERR_PAGE 1
 #define TR_CACHE_ERR_WAIT 2
@@ -521,11 +522,12 @@ tr_status tr_cache_append(const tr_cache *c, const tr_heads *k, const tr_heads *
  * i = lens[b] - cu_new[b+1] + t the token's own key, key j is visible when
  *   0 <= j < lens[b],  j <= i if causal,  j > i - window if window > 0.
  * A row that sees no key (or only scores of -inf, or of no sequence) gives
- * zeros (lse = -inf).
- * A key that a row does not see takes no part in it, whatever it holds (a
- * row whose tiles hold a hidden non-finite value is computed again without
- * it, slowly).  Probabilities are rounded to the cache's type for their
- * product with V; their sum and everything else is fp32.
+ * zeros (lse = -inf).  A key that a row does not see takes no part in it,
+ * whatever it holds.  (Values that are not finite cost a step little, however
+ * long its sequences; only where max_len promises 512 keys at most are the
+ * rows that one would spoil computed again, one by one, in 0.1 us a key.)
+ * Probabilities are rounded to the cache's type for their product with V;
+ * their sum and everything else is fp32.
  *   q, o:     tr_heads of total_new rows, the same number of heads, a
  *             multiple of the cache's
  *   lse:      device fp32 [total_new, q heads] or NULL: log sum exp of the

@@ -13,9 +13,11 @@
 //                   probabilities go back to tensor memory as the A operand
 //                   of the second product, in the place of the scores;
 //   producer warps  TMA loads of K (one warp) and V (another) tiles, page by
-//                   page, into a ring of 128-byte-swizzled tiles; the value
-//                   rows past the sequence's end are zeroed (stale memory
-//                   there may hold NaN);
+//                   page, into a ring of 128-byte-swizzled tiles;
+//   checking warp   value rows past the sequence's end become zeros (stale
+//                   memory there may hold NaN), and values that are not finite
+//                   leave the tiles that some row does not see all of (Edges
+//                   in tr_attend.cuh);
 //   MMA warp        S = Q K^T and O += P V from one thread.  The products of
 //                   the two 128-row blocks alternate, so one block's softmax
 //                   runs while the tensor cores work on the other.
@@ -80,11 +82,6 @@ __device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
   return r;
 }
-__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-  return v;
-}
 
 // The block of tokens that belong to no sequence (first: their first) in this
 // slot: zeros, lse -inf.
@@ -101,6 +98,26 @@ __device__ __noinline__ void clear_block(const AttendArgs &g, int first, int slo
     if (c == 0 && g.lse) g.lse[t * g.q_heads + head] = -INFINITY;
   }
 }
+
+// The values taken out of open tiles among [t0, t1) to those rows of the warp
+// that see them.  (Not inline: it would cost the softmax registers.)
+template <typename T>
+__device__ __noinline__ void put_back(const AttendArgs &g, int seq, int tok0, int base, int len, int rows, int first, int block,
+                                      int hk, int split, int warp, int t0, int t1) {
+  const Edges e = edges_of_rows(g, base, len, first, min(first + block, rows));
+  for_bad_values<T>(g, e, seq, hk, t0, t1, [&](int j, const float4 &v) {
+    for (int r = first + 32 * warp; r < min(first + 32 * warp + 32, rows); ++r) {
+      const int tok = r / g.group, head = hk * g.group + r % g.group, own = base + tok;
+      if ((g.causal && j > own) || (g.window > 0 && j < window_start(own, g.window))) continue;
+      const long long t = tok0 + tok;
+      add_to_row<T>(g.o + 2 * (t * g.o_tok + (long long)head * g.o_head),
+                    g.splits > 1 ? g.part + (((long long)split * g.c.total_new + t) * g.q_heads + head) * g.c.d : nullptr, v);
+    }
+  });
+}
+
+__device__ __forceinline__ void named_sync(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+__device__ __forceinline__ void named_arrive(int threads) { asm volatile("bar.arrive 1, %0;" ::"r"(threads) : "memory"); }
 
 template <typename T, int D, int MT, bool PAIRED>
 __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1)
@@ -119,8 +136,10 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
   auto p_full = [&](int m, int b) { return bars + 8u * (2 * S::kStages + MT + MT * S::kSBuf + m * S::kSBuf + b); };
   auto o_done = [&](int m) { return bars + 8u * (2 * S::kStages + MT + 2 * MT * S::kSBuf + m); };
   auto o_last = [&](int m) { return bars + 8u * (2 * S::kStages + 2 * MT + 2 * MT * S::kSBuf + m); };
-  const uint32_t tail = bars + 8u * (2 * S::kStages + 3 * MT + 2 * MT * S::kSBuf);
-  const uint32_t tmem_slot = tail + 8;
+  using Ring = TileRing<D, S::kStages, true>;
+  const uint32_t raw0 = bars + 8u * (2 * S::kStages + 3 * MT + 2 * MT * S::kSBuf);
+  const uint32_t tmem_slot = raw0 + 8u * (S::kStages - Ring::kK);
+  __shared__ int bad_values;  // some were taken out of the tiles
 
   // (the warp's index by shuffle: the compiler then knows it to be uniform)
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -168,7 +187,8 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
         tc::mbar_init(o_done(m), 1);
         tc::mbar_init(o_last(m), 1);
       }
-      tc::mbar_init(tail, 1);
+      for (int s = 0; s < S::kStages - Ring::kK; ++s) tc::mbar_init(raw0 + 8u * s, 1);
+      bad_values = 0;
       tc::mbar_fence_init();
       tc::tma_prefetch_map(&map_k);
       tc::tma_prefetch_map(&map_v);
@@ -181,6 +201,9 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
     __syncthreads();
     tc::fence_after_sync();
   }
+  // (PAIRED: no tile counts as open, see the rows' results)
+  const Edges edges = PAIRED ? Edges{0, k.len, k.len} : edges_of_rows(g, k.base, k.len, k.first, min(k.first + kRows, k.rows));
+  const bool opens = !PAIRED && t0 < t1 && (edges.open(t0) || edges.open(t1 - 1));  // (those between are open only if one of these is)
   uint32_t tmem = 0;
   if (t0 < t1) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
 
@@ -189,10 +212,11 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
     if (PAIRED) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   }
+  Ring tiles;
+  tiles.base = ring, tiles.full0 = full(0), tiles.empty0 = empty(0), tiles.raw0 = raw0;
+  tiles.edges = edges;
   if (warp == 4 * MT || warp == 4 * MT + 2) {
     // ---------------------------------------------------------------- TMA producers
-    TileRing<D, S::kStages, true> tiles;
-    tiles.base = ring, tiles.full0 = full(0), tiles.empty0 = empty(0), tiles.tail = tail;
     tiles.take(warp == 4 * MT ? 0 : 1);
     tiles.seen = keys_of_rows(g, k, k.first, min(k.first + kRows, k.rows));
     const CUtensorMap *map = warp == 4 * MT ? &map_k : &map_v;
@@ -205,6 +229,10 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
     }
     if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
     tiles.drain();
+  } else if (warp == 4 * MT + 3) {
+    // ---------------------------------------------------------------- values that not every row sees
+    if (!tiles.template check_values<T>(t0, t1, &bad_values) && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+    if (opens) named_arrive(kTile * MT + 32);
   } else if (warp == 4 * MT + 1) {
     // ---------------------------------------------------------------- MMA issuer
     {
@@ -256,7 +284,6 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
       // probabilities that the product issued before them reads.  One block
       // with two score buffers issues the scores first: its softmax of tile t
       // runs during the products of tile t - 1.
-      using Ring = TileRing<D, S::kStages, true>;
       int kst = Ring::first(0), vst = Ring::first(1);
       uint32_t kph = 0, vph = 0;
       for (int t = t0; t <= t1; ++t) {
@@ -449,7 +476,7 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               v[j] = __uint_as_float(o[i + j]) * inv;
-              finite &= fabsf(v[j]) <= FLT_MAX;
+              if (PAIRED) finite &= finite1(v[j]);
             }
             if (parts) {
               *reinterpret_cast<float4 *>(prow + c + i) = make_float4(v[0], v[1], v[2], v[3]);
@@ -474,7 +501,7 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
           const long long off = __shfl_sync(0xffffffffu, ooff, r1);
           const uint32_t src = sbase + m * S::kTileBytes + (32 * quarter + r1) * 128 + (c >> 3) * (kTile * 128) +
                                (((c & 7) ^ (r1 & 7)) << 4);
-          if (off >= 0 && 8 * c < g.c.d) *reinterpret_cast<uint4 *>(g.o + off + 16 * c) = ld_shared_v4(src);
+          if (off >= 0 && 8 * c < g.c.d) *reinterpret_cast<uint4 *>(g.o + off + 16 * c) = tc::ld_shared_v4(src);
         }
         __syncwarp();
       }
@@ -482,40 +509,38 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
         if (parts) g.part_ml[(long long)split * all_rows + out_row] = make_float2(mx, sum);
         else if (g.lse) g.lse[out_row] = sum > 0.f || sum != sum ? mx * 0.693147180559945309f + logf(sum) : -INFINITY;
       }
-      // A non-finite value of a key hidden from a row reaches it all the same
-      // as 0 * inf in the product over the tile.  Such rows are taken again
-      // without it: only when a row came out non-finite and a value hidden
-      // from it inside its tiles is.  The lanes that do write over what the
-      // row's own lane has just written, so its stores come first.
-      __syncwarp();
-      unsigned bad = __ballot_sync(0xffffffffu, valid && !finite);
-      while (bad) {
-        const int src = __ffs(bad) - 1;
-        bad &= bad - 1;
-        const int rlo = max(__shfl_sync(0xffffffffu, lo, src), ta * kTile);
-        const int rhi = min(__shfl_sync(0xffffffffu, hi, src), tb * kTile);
-        const int end = min(tb * kTile, k.len);
-        if (hidden_values_finite<T>(g, k.seq, hk, ta * kTile, min(rlo, end)) &&
-            hidden_values_finite<T>(g, k.seq, hk, max(rhi, ta * kTile), end))
-          continue;
-        const unsigned long long qp = __shfl_sync(0xffffffffu, (unsigned long long)qrow, src);
-        const unsigned long long op = __shfl_sync(0xffffffffu, (unsigned long long)orow, src);
-        const unsigned long long pp = __shfl_sync(0xffffffffu, (unsigned long long)prow, src);
-        const long long orow_id = __shfl_sync(0xffffffffu, out_row, src);
-        float m1, l1;
-        float4 v = row_by_warp<T>(g, k.seq, hk, reinterpret_cast<const char *>(qp), rlo, rhi, m1, l1);
-        const float f = parts ? 1.f : l1 > 0.f || l1 != l1 ? 1.f / l1 : 0.f;
-        v.x *= f, v.y *= f, v.z *= f, v.w *= f;
-        if (4 * lane < g.c.d) {
-          if (parts) reinterpret_cast<float4 *>(pp)[lane] = v;
-          else
-            reinterpret_cast<uint2 *>(op)[lane] = make_uint2(Bits<T>::pack(v.x, v.y), Bits<T>::pack(v.z, v.w));
-        }
-        if (lane == 0) {
-          if (parts) g.part_ml[(long long)split * all_rows + orow_id] = make_float2(m1, l1);
-          else if (g.lse) g.lse[orow_id] = l1 > 0.f || l1 != l1 ? m1 * 0.693147180559945309f + logf(l1) : -INFINITY;
+      // PAIRED: a check of the values would stand in the way of a CTA's one or
+      // two tiles (16 prompts of 227 tokens 51 us against 48).  Instead a row
+      // that came out not finite, and not because of what it sees, is taken
+      // again by itself: the keys are few.  The lanes that do write over what
+      // the row's own lane has just written, so its stores come first.
+      if (PAIRED) {
+        __syncwarp();
+        unsigned bad = __ballot_sync(0xffffffffu, valid && !finite);
+        while (bad) {
+          const int src = __ffs(bad) - 1;
+          bad &= bad - 1;
+          const int rlo = max(__shfl_sync(0xffffffffu, lo, src), ta * kTile);
+          const int rhi = min(__shfl_sync(0xffffffffu, hi, src), tb * kTile);
+          const int end = min(tb * kTile, k.len);
+          if (hidden_values_finite<T>(g, k.seq, hk, ta * kTile, min(rlo, end)) &&
+              hidden_values_finite<T>(g, k.seq, hk, max(rhi, ta * kTile), end))
+            continue;
+          const unsigned long long qp = __shfl_sync(0xffffffffu, (unsigned long long)qrow, src);
+          const unsigned long long op = __shfl_sync(0xffffffffu, (unsigned long long)orow, src);
+          const long long orow_id = __shfl_sync(0xffffffffu, out_row, src);
+          float m1, l1;
+          float4 v = row_by_warp<T>(g, k.seq, hk, reinterpret_cast<const char *>(qp), rlo, rhi, m1, l1);
+          const float f = l1 > 0.f || l1 != l1 ? 1.f / l1 : 0.f;
+          if (4 * lane < g.c.d)
+            reinterpret_cast<uint2 *>(op)[lane] = make_uint2(Bits<T>::pack(v.x * f, v.y * f), Bits<T>::pack(v.z * f, v.w * f));
+          if (lane == 0 && g.lse) g.lse[orow_id] = l1 > 0.f || l1 != l1 ? m1 * 0.693147180559945309f + logf(l1) : -INFINITY;
         }
       }
+    }
+    if (opens) {
+      named_sync(kTile * MT + 32);  // the check is over, and the rows' results are in
+      if (bad_values && ok) put_back<T>(g, k.seq, k.tok0, k.base, k.len, k.rows, k.first, kRows, hk, split, warp, ta, tb);
     }
   }
 

@@ -1,5 +1,6 @@
 // What the attention kernels share: their arguments, the rows and keys of a
-// block, the loads of K and V tiles, and the slow exact path of one row.
+// block, the loads of K and V tiles, and what becomes of values that are not
+// finite and not seen by every row.
 #pragma once
 
 #include <cfloat>
@@ -47,6 +48,12 @@ struct Bits<__nv_bfloat16> {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
   }
+  // a * 0 + b of a pair: b, or NaN where a is not finite
+  static __device__ __forceinline__ uint32_t fma0(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(0u), "r"(b));
+    return r;
+  }
 };
 template <>
 struct Bits<__half> {
@@ -54,6 +61,11 @@ struct Bits<__half> {
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  }
+  static __device__ __forceinline__ uint32_t fma0(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(0u), "r"(b));
     return r;
   }
 };
@@ -126,59 +138,172 @@ __device__ __forceinline__ Range keys_of_rows(const AttendArgs &g, const Block &
   return r;
 }
 
-// One row by one warp on the plain cores, four channels a lane: the running
-// maximum (powers of two), sum and weighted values over the keys [lo, hi).
+// Keys [lo, hi) are seen by every row of [r0, r1).  A tile with others is
+// open: in the product over it, a row gets 0 * v of a value v that it does not
+// see, which is NaN where v is not finite.  So values that are not finite are
+// taken out of open tiles before the product and added to the results of the
+// rows that do see them after it.  A block has a few open tiles at most (at
+// its own tokens and where its windows begin), however long the sequence is.
+struct Edges {
+  int lo, hi, len;
+  __device__ __forceinline__ bool open(int t) const {
+    return t * kTile < lo || min(t * kTile + kTile, len) > hi;
+  }
+};
+__device__ __forceinline__ Edges edges_of_rows(const AttendArgs &g, int base, int len, int r0, int r1) {
+  Edges e;
+  e.lo = g.window > 0 ? window_start(base + (r1 - 1) / g.group, g.window) : 0;
+  e.hi = g.causal ? min(len, base + r0 / g.group + 1) : len;
+  e.len = len;
+  return e;
+}
+
 template <typename T>
 __device__ __forceinline__ float4 load4(const char *p) {
   const uint2 v = *reinterpret_cast<const uint2 *>(p);
   const T *h = reinterpret_cast<const T *>(&v);
   return make_float4((float)h[0], (float)h[1], (float)h[2], (float)h[3]);
 }
+__device__ __forceinline__ bool finite1(float v) { return fabsf(v) <= FLT_MAX; }
 __device__ __forceinline__ bool finite4(const float4 &v) {
-  return fabsf(v.x) <= FLT_MAX && fabsf(v.y) <= FLT_MAX && fabsf(v.z) <= FLT_MAX && fabsf(v.w) <= FLT_MAX;
+  return finite1(v.x) && finite1(v.y) && finite1(v.z) && finite1(v.w);
 }
+// Zeros in the place of what is not finite in a pair; whether there was any.
+template <typename T>
+__device__ __forceinline__ bool clean_pair(uint32_t &v) {
+  constexpr uint32_t kExp = Bits<T>::kBf16 ? 0x7f80u : 0x7c00u;
+  const bool lo = (v & kExp) == kExp, hi = (v >> 16 & kExp) == kExp;
+  if (lo) v &= 0xffff0000u;
+  if (hi) v &= 0x0000ffffu;
+  return lo || hi;
+}
+// Offset in bytes of key j's row in the cache, -1 when its page is bad (then
+// it reads as zeros).
+__device__ __forceinline__ long long key_offset(const AttendArgs &g, int seq, int hk, int j) {
+  const int page = page_of(g.c, seq, j);
+  return page < 0 ? -1 : 2 * ((((long long)page * g.c.heads + hk) * g.c.page + (j & (g.c.page - 1))) * g.c.d);
+}
+// Whether the values there (-1: none) are finite.
+template <typename T>
+__device__ __forceinline__ bool values_finite(const AttendArgs &g, long long off) {
+  bool ok = true;
+  if (off >= 0)
+    for (int ch = 0; ch < g.c.d; ch += 4) ok &= finite4(load4<T>(static_cast<const char *>(g.c.v) + off + 2 * ch));
+  return ok;
+}
+// The values of the open tiles among [t0, t1) that are not finite, by a warp:
+// add(j, bad) for every key j that has any, with zeros for the finite ones
+// (four channels a lane, for all lanes together).  Those of keys that every
+// row sees are in the results already; once more makes no difference.
+template <typename T, typename F>
+__device__ __forceinline__ void for_bad_values(const AttendArgs &g, const Edges &e, int seq, int hk, int t0, int t1, F add) {
+  const int lane = threadIdx.x & 31;
+  for (int t = t0; t < t1; ++t) {
+    if (!e.open(t)) continue;
+    for (int j0 = t * kTile; j0 < min((t + 1) * kTile, e.len); j0 += 32) {
+      const long long off = j0 + lane < e.len ? key_offset(g, seq, hk, j0 + lane) : -1;
+      unsigned keys = __ballot_sync(0xffffffffu, !values_finite<T>(g, off));
+      while (keys) {
+        const int i = __ffs(keys) - 1;
+        keys &= keys - 1;
+        const long long from = __shfl_sync(0xffffffffu, off, i);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (4 * lane < g.c.d) v = load4<T>(static_cast<const char *>(g.c.v) + from + 8 * lane);
+        if (finite1(v.x)) v.x = 0.f;
+        if (finite1(v.y)) v.y = 0.f;
+        if (finite1(v.z)) v.z = 0.f;
+        if (finite1(v.w)) v.w = 0.f;
+        add(j0 + i, v);
+      }
+    }
+  }
+}
+// Adds to four channels of a row of 16-bit or of fp32 results.
+template <typename T>
+__device__ __forceinline__ void add_to_row(char *row16, float *row32, const float4 &v) {
+  const int ch = 4 * (threadIdx.x & 31);
+  if (finite4(v)) return;  // zeros
+  if (row32) {
+    float4 *p = reinterpret_cast<float4 *>(row32 + ch);
+    const float4 x = *p;
+    *p = make_float4(x.x + v.x, x.y + v.y, x.z + v.z, x.w + v.w);
+  } else {
+    const float4 x = load4<T>(row16 + 2 * ch);
+    *reinterpret_cast<uint2 *>(row16 + 2 * ch) = make_uint2(Bits<T>::pack(x.x + v.x, x.y + v.y), Bits<T>::pack(x.z + v.z, x.w + v.w));
+  }
+}
+
+// Whether the values of keys [lo, hi) are finite, by a warp.
 template <typename T>
 __device__ __forceinline__ bool hidden_values_finite(const AttendArgs &g, int seq, int hk, int lo, int hi) {
-  const int ch = 4 * (threadIdx.x & 31);
   bool ok = true;
-  for (int j = lo; j < hi; ++j) {
-    const int page = page_of(g.c, seq, j);
-    if (page >= 0 && ch < g.c.d)
-      ok &= finite4(load4<T>(static_cast<const char *>(g.c.v) +
-                             2 * ((((long long)page * g.c.heads + hk) * g.c.page + (j & (g.c.page - 1))) * g.c.d + ch)));
-  }
+  for (int j = lo + (int)(threadIdx.x & 31); j < hi; j += 32) ok &= values_finite<T>(g, key_offset(g, seq, hk, j));
   return __all_sync(0xffffffffu, ok);
 }
+// The product of two pairs, summed.
+template <typename T>
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b) {
+  const T *x = reinterpret_cast<const T *>(&a), *y = reinterpret_cast<const T *>(&b);
+  return (float)x[0] * (float)y[0] + (float)x[1] * (float)y[1];
+}
+// One row by one warp on the plain cores: the running maximum (powers of two),
+// sum and weighted values (four channels a lane) over the keys [lo, hi), 32 at
+// a time.  A lane takes the whole score of one key, so that a run of keys
+// costs one wait for its pages, keys and values each and one exchange.
 template <typename T>
 __device__ __forceinline__ float4 row_by_warp(const AttendArgs &g, int seq, int hk, const char *q, int lo, int hi, float &m,
                                            float &l) {
-  const int d = g.c.d, ch = 4 * (threadIdx.x & 31);
-  const bool holds = ch < d;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f), acc = x;
-  if (holds) x = load4<T>(q + 2 * ch);
+  const int d = g.c.d, lane = threadIdx.x & 31;
+  const bool holds = 4 * lane < d;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   const float sc = g.negate ? -g.scale : g.scale;
   m = -INFINITY;
   l = 0.f;
-  for (int j = lo; j < hi; ++j) {
-    const int page = page_of(g.c, seq, j);
-    float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-    if (page >= 0 && holds) {
-      const long long off = 2 * ((((long long)page * g.c.heads + hk) * g.c.page + (j & (g.c.page - 1))) * d + ch);
-      k = load4<T>(static_cast<const char *>(g.c.k) + off);
-      v = load4<T>(static_cast<const char *>(g.c.v) + off);
-    }
-    float s = x.x * k.x + x.y * k.y + x.z * k.z + x.w * k.w;
+  for (int j0 = lo; j0 < hi; j0 += 32) {
+    const int n = min(hi - j0, 32);
+    const long long off = lane < n ? key_offset(g, seq, hk, j0 + lane) : -1;
+    float s = 0.f;
+    for (int c0 = 0; c0 < d; c0 += 64) {
+      uint4 k[8];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    s *= sc;
-    const float mn = fmaxf(m, s);
+      for (int i = 0; i < 8; ++i) {
+        k[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (off >= 0 && c0 + 8 * i < d)
+          k[i] = *reinterpret_cast<const uint4 *>(static_cast<const char *>(g.c.k) + off + 2 * c0 + 16 * i);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c0 + 8 * i < d) {
+          const uint4 x = *reinterpret_cast<const uint4 *>(q + 2 * c0 + 16 * i);
+          s += dot2<T>(x.x, k[i].x) + dot2<T>(x.y, k[i].y) + (dot2<T>(x.z, k[i].z) + dot2<T>(x.w, k[i].w));
+        }
+    }
+    s = lane < n ? s * sc : -INFINITY;
+    float mn = fmaxf(m, s);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
     const float f = m == mn ? 1.f : exp2_fast(m - mn), p = s == -INFINITY ? 0.f : exp2_fast(s - mn);
+    float sum = p;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     m = mn;
-    l = l * f + p;
-    acc.x = acc.x * f + p * v.x;
-    acc.y = acc.y * f + p * v.y;
-    acc.z = acc.z * f + p * v.z;
-    acc.w = acc.w * f + p * v.w;
+    l = l * f + sum;
+    float4 run = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < n; i0 += 16) {
+      float4 v[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const long long oi = __shfl_sync(0xffffffffu, off, i0 + i);
+        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (oi >= 0 && holds) v[i] = load4<T>(static_cast<const char *>(g.c.v) + oi + 8 * lane);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float pi = __shfl_sync(0xffffffffu, p, i0 + i);
+        run.x += pi * v[i].x, run.y += pi * v[i].y, run.z += pi * v[i].z, run.w += pi * v[i].w;
+      }
+    }
+    acc.x = acc.x * f + run.x, acc.y = acc.y * f + run.y, acc.z = acc.z * f + run.z, acc.w = acc.w * f + run.w;
   }
   return acc;
 }
@@ -194,20 +319,21 @@ __device__ __forceinline__ void flag(const AttendArgs &g, int bit) {
 // to follow the other's laps: a barrier tells only two phases apart).  A tile
 // is loaded page by page, the halves apart; the lanes of the warp issue its
 // loads (one warp for both kinds took 3 us a tile of 16-key pages).
-// ZERO_TAIL: value rows past the sequence's end are zeroed before the tile is
-// handed on -- stale memory may hold NaN there, and 0 * NaN would reach every
-// row of a product that reads the tile from shared memory.  That waits for
-// the tile, so it suits a CTA that ends with it; consumers that read the
-// tile into registers drop those rows themselves.
-template <int D, int STAGES, bool ZERO_TAIL>
+// CHECKED: value tiles that are open or hold the sequence's end pass through
+// check_values before they are handed on -- values there that are not finite
+// (stale memory behind the end may hold NaN) would reach every row of a
+// product that reads the tile from shared memory.  Consumers that read the
+// tile into registers see to those values themselves.
+template <int D, int STAGES, bool CHECKED>
 struct TileRing {
   static constexpr int kHalves = D / 64;
   static constexpr uint32_t kBytes = kTile * D * 2;
   static constexpr int kK = (STAGES + 1) / 2;
-  uint32_t base, full0, empty0, tail;
+  uint32_t base, full0, empty0, raw0;
   int kv = 0, stage = 0;  // 0: K, 1: V; position of the next tile
   Range seen;             // keys that some row sees: a bad page is only an error there
-  uint32_t phase = 0, tails = 0, filled = 0, parity = 0;
+  Edges edges;            // CHECKED
+  uint32_t phase = 0, filled = 0, parity = 0;
 
   __device__ __forceinline__ void take(int kind) {
     kv = kind;
@@ -223,6 +349,8 @@ struct TileRing {
   }
   __device__ __forceinline__ uint32_t full(int s) const { return full0 + 8u * s; }
   __device__ __forceinline__ uint32_t empty(int s) const { return empty0 + 8u * s; }
+  __device__ __forceinline__ uint32_t raw(int s) const { return raw0 + 8u * (s - kK); }  // value tiles, before the check
+  __device__ __forceinline__ bool checked(int t) const { return edges.open(t) || (t + 1) * kTile > edges.len; }
 
   // The page id that this lane's part of tile t needs (part: one half of
   // the rows of one page).  Asked for one tile ahead of its load, so that
@@ -248,26 +376,68 @@ struct TileRing {
     const uint32_t bytes = (uint32_t)pieces * piece * 128u * kHalves;
     if (!tc::mbar_wait_warp(empty(stage), phase ^ 1u)) return false;
     const uint32_t dst = base + stage * kBytes;
-    const bool cut = ZERO_TAIL && kv == 1 && left < kTile;  // the sequence ends inside this value tile
-    const uint32_t bar = cut ? tail : full(stage);
+    const uint32_t bar = CHECKED && kv == 1 && checked(t) ? raw(stage) : full(stage);
     if (lane == 0) tc::mbar_expect_tx(bar, bytes);
     __syncwarp();
     if (mine) tc::tma_load_2d(dst + half * (kTile * 128) + pc * piece * 128, map, half * 64, row, bar);
-    bool ok = true;
-    if (cut) {
-      ok = __all_sync(0xffffffffu, tc::mbar_wait(tail, tails));
-      tails ^= 1u;
+    filled |= 1u << stage;
+    parity = (parity & ~(1u << stage)) | (phase << stage);
+    on(kv, stage, phase);
+    return true;
+  }
+  // The value tiles [t0, t1) that need it, checked by a warp of its own (so
+  // that loads go on meanwhile) before their consumers get them: rows past the
+  // sequence's end become zeros, and so does, in an open tile, what is not
+  // finite of the keys that some row does not see; then *bad is set.  A product
+  // with zero tells, the places are looked for only where there are any.  False when
+  // a wait timed out.
+  template <typename T>
+  __device__ __forceinline__ bool check_values(int t0, int t1, int *bad) {
+    const int lane = threadIdx.x & 31;
+    uint32_t raw_parity = 0;
+    take(1);
+    for (int t = t0; t < t1; ++t, on(1, stage, phase)) {
+      if (!checked(t)) continue;
+      if (!tc::mbar_wait_warp(raw(stage), raw_parity >> stage & 1u)) return false;
+      raw_parity ^= 1u << stage;
+      const uint32_t tile = base + stage * kBytes;
+      const int left = min(edges.len - t * kTile, kTile);
+      // keys [0, below) are before some row's window, keys [above, left) after some row's own
+      const int below = min(max(edges.lo - t * kTile, 0), left), above = max(min(edges.hi - t * kTile, left), below);
+#pragma unroll 1
+      for (int part = 0; part < 2; ++part) clean_rows<T>(tile, part ? above : 0, part ? left : below, bad);
       for (int i = lane + left * 8; i < kTile * 8; i += 32)
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h) tc::st_shared_v4(dst + h * (kTile * 128) + i * 16, 0, 0, 0, 0);
+        for (int h = 0; h < kHalves; ++h) tc::st_shared_v4(tile + h * (kTile * 128) + i * 16, 0, 0, 0, 0);
       tc::fence_async_shared();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(full(stage));
     }
-    filled |= 1u << stage;
-    parity = (parity & ~(1u << stage)) | (phase << stage);
-    on(kv, stage, phase);
-    return ok;
+    return true;
+  }
+  template <typename T>
+  __device__ __forceinline__ void clean_rows(uint32_t tile, int r0, int r1, int *bad) {
+    if (r0 >= r1) return;
+    const int lane = threadIdx.x & 31;
+    uint32_t s0 = 0u, s1 = 0u;
+#pragma unroll 2
+    for (int i = r0 * 8 + lane; i < r1 * 8; i += 32)
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        const uint4 v = tc::ld_shared_v4(tile + h * (kTile * 128) + i * 16);
+        s0 = Bits<T>::fma0(v.y, Bits<T>::fma0(v.x, s0)), s1 = Bits<T>::fma0(v.w, Bits<T>::fma0(v.z, s1));
+      }
+    if (!__any_sync(0xffffffffu, ((s0 | s1) & 0x7fff7fffu) != 0u)) return;
+#pragma unroll 1
+    for (int h = 0; h < kHalves; ++h)
+#pragma unroll 1
+      for (int i = r0 * 8 + lane; i < r1 * 8; i += 32) {
+        const uint32_t at = tile + h * (kTile * 128) + i * 16;
+        uint4 v = tc::ld_shared_v4(at);
+        clean_pair<T>(v.x), clean_pair<T>(v.y), clean_pair<T>(v.z), clean_pair<T>(v.w);
+        tc::st_shared_v4(at, v.x, v.y, v.z, v.w);
+      }
+    if (lane == 0) *bad = 1;
   }
   // The loads already issued land before the CTA may exit.
   __device__ __forceinline__ void drain() const {

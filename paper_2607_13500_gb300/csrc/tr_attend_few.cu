@@ -227,22 +227,6 @@ __device__ __forceinline__ void put_row(const AttendArgs &g, const Walk &w, int 
   }
 }
 
-// Whether what put_row wrote for row r of the piece is finite, by a warp.
-template <typename T>
-__device__ __forceinline__ bool row_finite(const AttendArgs &g, const Walk &w, int part, int block0, int hk, int r) {
-  const int ch = 4 * (threadIdx.x & 31);
-  bool ok = true;
-  if (ch < g.c.d) {
-    if (w.whole) {
-      const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
-      ok = finite4(load4<T>(g.o + 2 * ((long long)(w.s.tok0 + tok) * g.o_tok + (long long)head * g.o_head + ch)));
-    } else {
-      ok = finite4(*reinterpret_cast<const float4 *>(g.part + ((long long)part * kFewRows + r) * g.c.d + ch));
-    }
-  }
-  return __all_sync(0xffffffffu, ok);
-}
-
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attend_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -251,14 +235,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ unsigned char smem_raw[];
   __shared__ int runs[kFewMaxBatch / 32];  // units of 32 sequences each
   __shared__ float top[kWarps][kFewRows], tot[kWarps][kFewRows];
-  __shared__ int bad, share0, share_units;
+  __shared__ int bad, share0, share_units;  // bad: values were taken out of a tile
   const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
   float *join = reinterpret_cast<float *>(smem_raw + (base - tc::smem_u32(smem_raw)) + F::kStages * F::kTileBytes);
   const uint32_t bars = tc::smem_u32(join) + F::kJoinBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   TileRing<D, F::kStages, false> ring;
-  ring.base = base, ring.full0 = bars, ring.empty0 = bars + 8u * F::kStages, ring.tail = 0;
+  ring.base = base, ring.full0 = bars, ring.empty0 = bars + 8u * F::kStages, ring.raw0 = 0;
   if (threadIdx.x == 0) {
     for (int s = 0; s < F::kStages; ++s) {
       tc::mbar_init(ring.full(s), 1);
@@ -370,8 +354,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 
       // ---- softmax: s[n][0..1] row g, s[n][2..3] row g + 8, keys 8 n + 2 c and + 1
       const int key0 = t * kTile + 16 * warp;
-      const bool cut = lo[0] > key0 || hi[0] < key0 + 16 || lo[1] > key0 || hi[1] < key0 + 16;
-      if (__any_sync(0xffffffffu, cut)) {
+      const bool ends = key0 + 16 > w.s.len;
+      const int most = min(key0 + 16, w.s.len);  // open: some row does not see some of the sequence's keys here
+      const bool open = __any_sync(0xffffffffu, lo[0] > key0 || hi[0] < most || lo[1] > key0 || hi[1] < most);
+      if (open || ends) {
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -420,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
         break;
       }
-      const bool ends = key0 + 16 > w.s.len;
+      bool found = false;
       const uint32_t vt = base + vst * F::kTileBytes + (uint32_t)(16 * warp) * 128u;
 #pragma unroll
       for (int h = 0; h < F::kHalves; ++h) {
@@ -435,6 +421,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int j = 0; j < 4; ++j)
             if (key0 + 2 * c + (j & 1) + 8 * (j >> 1) >= w.s.len) v[j] = make_uint4(0u, 0u, 0u, 0u);
         }
+        if (open) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            found |= clean_pair<T>(v[j].x) | clean_pair<T>(v[j].y) | clean_pair<T>(v[j].z) | clean_pair<T>(v[j].w);
+          }
+        }
         const uint32_t *v0 = &v[0].x, *v1 = &v[1].x, *v2 = &v[2].x, *v3 = &v[3].x;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -443,6 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                       __byte_perm(v2[i >> 1], v3[i >> 1], sel));
         }
       }
+      if (found) bad = 1;  // (any thread's word will do)
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(ring.empty(vst));
       Ring::on(1, vst, vph);
@@ -500,36 +493,30 @@ __global__ void __launch_bounds__(kThreads, 1)
         // maximum of one that saw nothing: its sum, 0 or NaN, enters as it is.
 #pragma unroll
         for (int j = 0; j < kWarps; ++j) l += top[j][r] == -INFINITY ? tot[j][r] : tot[j][r] * exp2_fast(top[j][r] - m);
-        if (!finite4(v)) bad = 1;  // (any thread's word will do)
         put_row<T>(g, w, part, block0, hk, r, ch, v, m, l);
       }
       named_sync(32 * kWarps);
     }
   }
 
-  // Rows that came out non-finite because of a value they do not see (see
-  // k_attend) are taken again without it, when the share's tiles are all used
-  // up: this may take far longer than a producer would wait for its ring.
+  // What was taken out of open tiles goes to the rows that see it, when the
+  // share's tiles are all used up.
   named_sync(32 * kWarps);  // the rows written by other warps
   if (!ok || !bad) return;
   w.seek(g, runs, seq_of(g, lane), share0, share0 + share_units);
   while (w.next(g)) {
     const int hk = w.item % g.c.heads, block0 = w.item / g.c.heads * kFewRows;
     const int rows = min(kFewRows, w.s.rows - block0), part = 2 * blockIdx.x + (w.starts ? 1 : 0);
-    for (int r = warp; r < rows; r += kWarps) {
-      if (row_finite<T>(g, w, part, block0, hk, r)) continue;
-      const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
-      const int own = w.s.base + tok, from = w.tile * kTile, end = min((w.tile + w.count) * kTile, w.s.len);
-      const int rlo = max(g.window > 0 ? window_start(own, g.window) : 0, from);
-      const int rhi = min(g.causal ? min(w.s.len, own + 1) : w.s.len, end);
-      if (hidden_values_finite<T>(g, w.seq(), hk, from, min(rlo, end)) &&
-          hidden_values_finite<T>(g, w.seq(), hk, max(rhi, from), end))
-        continue;
-      const char *qr = g.q + 2 * ((long long)(w.s.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
-      float m, l;
-      float4 v = row_by_warp<T>(g, w.seq(), hk, qr, rlo, rhi, m, l);
-      if (4 * lane < g.c.d) put_row<T>(g, w, part, block0, hk, r, 4 * lane, v, m, l);
-    }
+    for_bad_values<T>(g, edges_of_rows(g, w.s.base, w.s.len, block0, block0 + rows), w.seq(), hk, w.tile, w.tile + w.count,
+                      [&](int j, const float4 &v) {
+                        for (int r = warp; r < rows; r += kWarps) {
+                          const int tok = (block0 + r) / g.group, head = hk * g.group + (block0 + r) % g.group;
+                          const int own = w.s.base + tok;
+                          if ((g.causal && j > own) || (g.window > 0 && j < window_start(own, g.window))) continue;
+                          add_to_row<T>(g.o + 2 * ((long long)(w.s.tok0 + tok) * g.o_tok + (long long)head * g.o_head),
+                                        w.whole ? nullptr : g.part + ((long long)part * kFewRows + r) * g.c.d, v);
+                        }
+                      });
   }
 }
 

@@ -19,8 +19,8 @@ def _built():
     _build.build()
 
 
-def _check_rows(got, lse, q, keys, vals, seqs, cu, spoilt, causal=True, window=0, scale=None):
-    """Rows [token, head] of `spoilt` are NaN in out and lse, the others as the plain form has them."""
+def _check_rows(got, lse, q, keys, vals, seqs, cu, spoilt, causal=True, window=0, scale=None, channels=None):
+    """Rows [token, head] of `spoilt` are NaN in out and lse, the others as the plain form has them (in `channels`)."""
     d, dtype = q.shape[2], q.dtype
     assert torch.isnan(got[spoilt]).all() and torch.isnan(lse[spoilt]).all()
     for b, (n, length) in enumerate(seqs):
@@ -33,6 +33,8 @@ def _check_rows(got, lse, q, keys, vals, seqs, cu, spoilt, causal=True, window=0
         tol = U[dtype] * o.abs() + (U[dtype] + 2 * e + 2.0 ** -17)[..., None] * pv + 2.0 ** -24
         if dtype == torch.float16:
             tol = tol + length * 2.0 ** -25 * vals[b].double().nan_to_num(0, 0, 0).abs().max()
+        if channels is not None:
+            o = torch.where(channels[sl], o, 0.0)
         _within(got[sl][keep], o[keep], tol[keep], ("o", b))
         _within(lse[sl][keep], z[keep], (e + 2.0 ** -17 * (1 + z.abs()))[keep], ("lse", b))
 
@@ -267,3 +269,82 @@ def test_pages_before_the_window_may_be_given_away(case, gone):
         cache.attend(q, table, lens, cu, window=window, **most)
         assert int(cache.error) == 1, b
         table[b, p] = kept
+
+
+VALUES = [  # sequences, q heads, k heads, d, page, dtype, window, max_len
+    ([(1, 33), (1, 128), (1, 700)], 4, 2, 64, 16, torch.bfloat16, 0, 700),               # few rows, all see it
+    ([(4, 3000)], 4, 1, 128, 64, torch.bfloat16, 0, 3000),
+    ([(4, 400), (3, 130), (1, 20)] * 80, 4, 1, 64, 32, torch.float16, 0, 400),
+    ([(1, 250), (2, 900)] * 90, 8, 2, 80, 64, torch.float16, 40, 900),
+    ([(150, 150), (33, 500)], 4, 2, 64, 32, torch.bfloat16, 0, 500),                     # chunks, two CTAs an SM
+    ([(227, 227)] * 20, 8, 8, 128, 16, torch.float16, 0, 227),
+    ([(100, 700)] * 40, 8, 4, 64, 64, torch.float16, 90, 700),
+    ([(40, 1000), (90, 1111)], 4, 2, 64, 32, torch.bfloat16, 0, 1111),                   # the keys in parts
+    ([(300, 2000)], 7, 1, 128, 64, torch.float16, 33, 2000),
+    ([(300, 700)] * 16, 7, 1, 128, 64, torch.bfloat16, 0, 700),                          # in one part, 256 rows a CTA
+    ([(130, 2000)] * 20, 8, 8, 112, 128, torch.bfloat16, 0, 2000),
+    ([(40, 2000)], 4, 1, 128, 64, torch.bfloat16, 0, 100),                               # a bound that is off
+]
+
+
+@pytest.mark.parametrize("case", VALUES, ids=lambda c: f"{len(c[0])}x{c[0][0][0]}of{c[0][0][1]}-{c[3]}-w{c[6]}")
+def test_values_that_are_not_finite(case):
+    # single channels of a value: infinite or NaN for the rows that see them, in that channel and no other
+    seqs, hq, hk, d, page, dtype, window, max_len = case
+    cache, table, lens, cu, keys, vals = _step(seqs, hk, page, d, dtype, 5)
+    q = _randn(int(cu[-1]), hq, d, dtype=dtype, seed=6, gain=1.5)
+    inf, nan = float("inf"), float("nan")
+    add = torch.zeros(q.shape, dtype=torch.float64, device=DEV)  # what they make of each channel
+    for b, (n, length) in enumerate(seqs):
+        own = length - n + torch.arange(n, device=DEV)
+        rows = slice(int(cu[b]), int(cu[b + 1]))
+        for back, ch, bad in ((1, 3, inf), (2, 3, -inf), (3, d - 1, nan), (7, 8, -inf), (16, 9, inf), (60, 10, inf),
+                              (window + n // 2, 11, -inf)):
+            if back > length or back < 1:
+                continue
+            j, head = length - back, back % hk
+            cache.v[table[b, j // page], head, j % page, ch] = bad
+            vals[b][j, head, ch] = 0
+            see = (own >= j) & ((own < j + window) if window else own >= 0)
+            group = slice(head * (hq // hk), (head + 1) * (hq // hk))
+            add[rows, group, ch] += torch.where(see, bad, 0.0)[:, None]
+    got, lse = cache.attend(q, table, lens, cu, window=window, max_new=max(n for n, _ in seqs), max_len=max_len,
+                            return_lse=True)
+    assert int(cache.error) == 0
+    fine = add == 0
+    assert torch.equal(got.double()[~fine].nan_to_num(7), add[~fine].nan_to_num(7))
+    _check_rows(torch.where(fine, got, got.new_zeros(())), lse, q, keys, vals, seqs, cu,
+                torch.zeros(q.shape[:2], dtype=torch.bool, device=DEV), window=window, channels=fine)
+
+
+@pytest.mark.parametrize("case", [([(4, 50000)] * 160, 4, 1), ([(2048, 8192)], 28, 4)], ids=["drafts", "chunk"])
+def test_values_that_are_not_finite_cost_little(case):
+    # an infinity that some rows do not see, against the same step without it: a few times as long at most, however
+    # long the sequence
+    seqs, hq, hk = case
+    n, length = seqs[0]
+    page, d = 64, 64
+    pages = (length + page - 1) // page
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, v = (torch.randn(pages, hk, page, d, device=DEV, generator=g).to(torch.bfloat16) for _ in range(2))
+    cache = _alt().PagedCache(k, v)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV).repeat(len(seqs), 1)  # the same pages for all
+    lens = torch.full((len(seqs),), length, dtype=torch.int32, device=DEV)
+    cu = n * torch.arange(len(seqs) + 1, dtype=torch.int32, device=DEV)
+    q = _randn(n * len(seqs), hq, d, dtype=torch.bfloat16, seed=6)
+
+    def took():
+        times = []
+        for _ in range(5):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            cache.attend(q, table, lens, cu, max_new=n, max_len=length)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+
+    good = took()
+    v[pages - 1, :, (length - 1) % page, 5] = float("inf")
+    bad = took()
+    assert bad <= 4 * good, (good, bad)
