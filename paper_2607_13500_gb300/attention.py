@@ -118,6 +118,34 @@ class RotaryGrads:
     k_weight: torch.Tensor | None
 
 
+def _readable(t):
+    """A gradient as the kernels can read it: autograd hands on whatever strides it has."""
+    es = t.element_size()
+    s0, s1, s2 = t.stride()
+    if s2 == 1 and s0 * es % 16 == 0 and s1 * es % 16 == 0 and t.data_ptr() % 16 == 0:
+        return t
+    # (contiguous() would keep the odd strides of a single row, or of none)
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device).copy_(t)
+
+
+class _Turned(torch.autograd.Function):
+    """Rotary.apply as a node of the graph."""
+
+    @staticmethod
+    def forward(ctx, rotary, eps, pos, q, k, q_weight, k_weight):
+        ctx.rotary, ctx.eps = rotary, eps
+        ctx.save_for_backward(pos, None if q_weight is None else q, None if k_weight is None else k, q_weight, k_weight)
+        return rotary._apply(q, k, pos, q_weight, k_weight, eps)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq, dk):
+        pos, q, k, q_weight, k_weight = ctx.saved_tensors
+        g = ctx.rotary.backward(_readable(dq), None if dk is None else _readable(dk), pos, q=q, k=k, q_weight=q_weight,
+                                k_weight=k_weight, eps=ctx.eps)
+        return None, None, None, g.q, g.k, g.q_weight, g.k_weight
+
+
 class Rotary:
     """Rotary positions of heads of ``head_dim`` channels, several axes, with
     an optional RMS norm of each head in the same pass (tr_rotary_apply).
@@ -162,7 +190,17 @@ class Rotary:
         [T, k heads, head_dim] (or None), any strides with contiguous
         channels; ``pos`` int32 [axes, T].  A head is normed where its fp32
         [head_dim] weight is given.  ``q_out`` / ``k_out`` may be q / k
-        themselves.  Returns (q_out, k_out)."""
+        themselves.  Returns (q_out, k_out), part of the graph where autograd
+        records an input that requires a gradient (then without q_out and
+        k_out)."""
+        if (q.requires_grad or (k is not None and k.requires_grad) or (q_weight is not None and q_weight.requires_grad)
+                or (k_weight is not None and k_weight.requires_grad)) and torch.is_grad_enabled():
+            if q_out is not None or k_out is not None:
+                raise ValueError("no gradient goes through q_out and k_out: leave them out or use torch.no_grad()")
+            return _Turned.apply(self, eps, pos, q, k, q_weight, k_weight)
+        return self._apply(q, k, pos, q_weight, k_weight, eps, q_out, k_out)
+
+    def _apply(self, q, k, pos, q_weight, k_weight, eps, q_out=None, k_out=None):
         dt, i, d = q.dtype, self.index, self.head_dim
         code = _CODES.get(dt)
         if code is None:
@@ -232,7 +270,8 @@ class PagedCache:
     graph): ``table`` [batch, max_pages] page ids, ``lens`` [batch] the keys
     of each sequence with the new ones, ``cu_new`` [batch + 1] prefix sums of
     the new tokens, which are each sequence's last.  ``error`` (int32[1])
-    collects TR_CACHE_ERR_PAGE / TR_CACHE_ERR_WAIT."""
+    collects TR_CACHE_ERR_PAGE / TR_CACHE_ERR_WAIT.  No gradient goes through
+    a cache: what ``append`` and ``attend`` return is no part of a graph."""
 
     def __init__(self, k, v):
         self.calls = _library()
