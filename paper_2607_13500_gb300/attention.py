@@ -20,6 +20,7 @@ from . import _lib
 from ._device import at, resolved
 from ._lib import TR_BF16, TR_F16, TR_F32, TR_ROTARY_LAYOUT, check, load
 
+_MOST = 2 ** 31 - 1
 _CODES = {torch.bfloat16: TR_BF16, torch.float16: TR_F16, torch.float32: TR_F32}
 
 # The C structs are packed with struct.Struct and passed as bytes through
@@ -345,7 +346,9 @@ class PagedCache:
             if max_new is None:
                 max_new = t
             if max_len is None:
-                max_len = min(table.shape[1] * self.page, 2 ** 31 - 1)
+                max_len = table.shape[1] * self.page
+            if window > _MOST or max_new > _MOST or max_len > _MOST:  # (ctypes would take them modulo 2^32)
+                window, max_new, max_len = min(window, _MOST), min(max_new, _MOST), min(max_len, _MOST)
             key = (t, lens.shape[0], table.shape[1], heads, window, max_new, max_len)
             nbytes = self._sizes.get(key)
             if nbytes is None:

@@ -349,3 +349,12 @@ def test_values_that_are_not_finite_cost_little(case):
     v[pages - 1, :, (length - 1) % page, 5] = float("inf")
     bad = took()
     assert bad <= 4 * good, (good, bad)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 32 + 5])
+def test_window_wider_than_any_sequence(window):
+    for seqs, new in (([(1, 900), (1, 30)], 1), ([(200, 900), (33, 40)], 200)):
+        cache, table, lens, cu, _, _ = _step(seqs, 2, 32, 64, torch.bfloat16, 5)
+        q = _randn(int(cu[-1]), 4, 64, dtype=torch.bfloat16, seed=6, gain=1.5)
+        assert torch.equal(cache.attend(q, table, lens, cu, max_new=new, window=window),
+                           cache.attend(q, table, lens, cu, max_new=new))
