@@ -358,3 +358,53 @@ def test_window_wider_than_any_sequence(window):
         q = _randn(int(cu[-1]), 4, 64, dtype=torch.bfloat16, seed=6, gain=1.5)
         assert torch.equal(cache.attend(q, table, lens, cu, max_new=new, window=window),
                            cache.attend(q, table, lens, cu, max_new=new))
+
+
+def _check_single_tokens(cache, table, lens, q, **kw):
+    """One new token of each sequence, all keys short enough for one padded computation."""
+    got, lse = cache.attend(q, table, lens, torch.arange(len(lens) + 1, dtype=torch.int32, device=DEV), max_new=1,
+                            return_lse=True, **kw)
+    assert int(cache.error) == 0
+    d, group, n = q.shape[2], q.shape[1] // cache.heads, int(lens.max())
+    pages = (n + cache.page - 1) // cache.page
+    k, v = (t[table[:, :pages].long()].transpose(1, 2).flatten(2, 3)[:, :, :n].double() for t in (cache.k, cache.v))
+    x = q.double().view(len(lens), cache.heads, group, d)
+    seen = (torch.arange(n, device=DEV) < lens[:, None])[:, None, None]
+    s = (x @ k.transpose(2, 3) / math.sqrt(d)).masked_fill(~seen, -math.inf)
+    z = torch.logsumexp(s, -1)
+    p = torch.where(seen, torch.exp(s - torch.where(z.isinf(), 0.0, z)[..., None]), 0.0)
+    e = torch.where(seen, x.abs() @ k.abs().transpose(2, 3), 0.0).amax(-1) / math.sqrt(d) * d * 2.0 ** -23
+    o, pv = p @ v, p @ v.abs()
+    u = U[q.dtype]
+    _within(got.view(o.shape), o, u * o.abs() + (u + 2 * e + 2.0 ** -17)[..., None] * pv + 2.0 ** -24, "o")
+    lse = lse.view(z.shape)
+    assert torch.equal(lse.isinf(), z.isinf())
+    some = ~z.isinf()
+    _within(lse[some], z[some], (e + 2.0 ** -17 * (1 + z.abs()))[some], "lse")
+
+
+def test_more_sequences_than_shares_are_counted_for():
+    # past 8192 sequences single tokens go to the kernel of chunks
+    g = torch.Generator(device=DEV).manual_seed(7)
+    batch, page, d = 8300, 16, 64
+    k, v = (torch.randn(500, 1, page, d, device=DEV, generator=g).to(torch.bfloat16) for _ in range(2))
+    table = torch.randint(0, 500, (batch, 13), device=DEV, generator=g, dtype=torch.int32)
+    lens = torch.randint(0, 13 * page + 1, (batch,), device=DEV, generator=g, dtype=torch.int32)
+    q = _randn(batch, 2, d, dtype=torch.bfloat16, seed=6, gain=1.5)
+    cache = _alt().PagedCache(k, v)
+    _check_single_tokens(cache, table, lens, q)
+    _check_single_tokens(cache, table[:8192], lens[:8192], q[:8192])  # the most that are
+
+
+def test_tables_whose_tiles_pass_31_bits():
+    # 2 sequences x 80 key heads x 16.8 million tiles that the table could hold: the kernel of chunks again
+    g = torch.Generator(device=DEV).manual_seed(7)
+    heads, page, d, most = 80, 256, 64, 2 ** 23 - 257
+    k, v = (torch.randn(5, heads, page, d, device=DEV, generator=g).to(torch.bfloat16) for _ in range(2))
+    table = torch.full((2, most), -1, dtype=torch.int32, device=DEV)
+    table[0, :2], table[1, :3] = torch.tensor([4, 0], device=DEV), torch.tensor([1, 3, 2], device=DEV)
+    lens = torch.tensor([300, 517], dtype=torch.int32, device=DEV)
+    q = _randn(2, heads, d, dtype=torch.bfloat16, seed=6, gain=1.5)
+    cache = _alt().PagedCache(k, v)
+    _check_single_tokens(cache, table, lens, q)
+    _check_single_tokens(cache, table, lens, q, max_len=517)
