@@ -529,7 +529,7 @@ tr_status tr_cache_append(const tr_cache *c, const tr_heads *k, const tr_heads *
  * Probabilities are rounded to the cache's type for their product with V;
  * their sum and everything else is fp32.
  *   q, o:     tr_heads of total_new rows, the same number of heads, a
- *             multiple of the cache's
+ *             multiple of the cache's; o does not overlap q
  *   lse:      device fp32 [total_new, q heads] or NULL: log sum exp of the
  *             scaled scores
  *   max_new, max_len: what the host knows of a sequence's new tokens and of

@@ -334,7 +334,8 @@ class PagedCache:
         ``causal`` a token sees the keys up to its own, with ``window`` > 0 only
         the last ``window`` of those.  ``max_new`` and ``max_len``, what the
         host knows of a sequence's new tokens and length at most, only choose
-        the launch (defaults: all T, and what the table can hold).  Returns
+        the launch (defaults: all T, and what the table can hold).  Rows from
+        cu_new[batch] on are zeros.  ``out`` does not overlap q.  Returns
         out, or (out, lse fp32 [T, q heads])."""
         t, d, i = q.shape[0], self.head_dim, self.index
         c = self._struct(table, lens, cu_new, t)

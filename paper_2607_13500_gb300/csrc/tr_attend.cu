@@ -32,7 +32,7 @@
 // taken before that rounding, and everything else is fp32.
 //
 // Bound by the tensor cores where there are many keys: 2048 tokens over 32768
-// keys, 28/4 heads of 128, bf16, 614 us on GB300 (1.52 PFLOP/s, 0.79 of the
+// keys, 28/4 heads of 128, bf16, 615 us on GB300 (1.52 PFLOP/s, 0.79 of the
 // measured cuBLAS rate).  A 128 x 128 x 16 product reads 8 KB of shared
 // memory, or 4 KB and tensor memory, in the 64 cycles it could take.
 #include <cfloat>
@@ -55,8 +55,8 @@ using namespace attend;
 // MT blocks of 128 rows a CTA.  PAIRED (MT = 1): two CTAs share an SM, each
 // with room for little more than the tile in use, so that one's start and
 // end run beside the other's work: for keys of a few tiles, where a CTA is
-// mostly start and end (16 prompts of 227 tokens, 32 heads: 46 us against 54
-// us with MT = 2).
+// mostly start and end (16 prompts of 227 tokens, 32 heads: 49 us; MT = 2 took
+// 54 us when it was left).
 template <int D, int MT, bool PAIRED>
 struct Shape {
   static_assert(MT == 2 || MT == 1, "");
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(Shape<D, MT, PAIRED>::kThreads, PAIRED ? 2 : 1
         else if (g.lse) g.lse[out_row] = sum > 0.f || sum != sum ? mx * 0.693147180559945309f + logf(sum) : -INFINITY;
       }
       // PAIRED: a check of the values would stand in the way of a CTA's one or
-      // two tiles (16 prompts of 227 tokens 51 us against 48).  Instead a row
+      // two tiles (16 prompts of 227 tokens 51 us against 49).  Instead a row
       // that came out not finite, and not because of what it sees, is taken
       // again by itself: the keys are few.  The lanes that do write over what
       // the row's own lane has just written, so its stores come first.

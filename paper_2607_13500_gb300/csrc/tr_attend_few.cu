@@ -19,10 +19,11 @@
 // over all banks) and the queries are laid out to match; for V a lane takes
 // 8 channels of four keys and pairs keys with byte permutes.
 //
-// Measured on GB300, bf16, heads of 128: one token of 64 requests over 256 to
-// 16384 keys, 28/4 heads, 86 us with the join (480 MB: 5.6 TB/s of the
-// measured 6.77 copy); one token of one request over 611 keys, 32 heads, 9.5
-// us (latency: launch, lengths, page ids, one tile, join).
+// Measured on GB300, bf16, heads of 128, both kernels: one token of 64 requests
+// over 256 to 16384 keys, 28/4 heads, 88 us (480 MB: 5.5 TB/s of the measured
+// 6.77 copy); one token of one request over 611 keys, 32 heads, 10.8 us in a
+// graph (latency: launch, lengths, page ids, one tile, join).  With heads of 128
+// the 168 registers of a thread spill 16 bytes.
 #include <atomic>
 
 #include "tr_attend.cuh"

@@ -8,12 +8,13 @@
 // Backward, with g = the gradient dy turned by the opposite angle:
 //   dw = sum g x r,  dx = r (w g) - x r^3 mean(x w g).
 //
-// All of it is bound by memory, or nearly: each row is read once and written
-// once.  Measured on GB300: 12288 tokens x 64 heads of 128, bf16, 65 us (6.2
-// TB/s of the measured 6.77 copy); with the norm the instructions weigh in
-// (issue slots 60 % busy): 6272 tokens x 32 heads 20.0 us (5.1 TB/s), their
-// gradients 39.5 us (3.9 TB/s), 29.6k tokens appended 107 us (5.0 TB/s).  A
-// row belongs to a group of lanes, each of which holds both halves of V
+// Each row is read once and written once.  Measured on GB300, bf16, graphs of
+// calls over inputs larger than L2: 12288 tokens x 64 heads of 128 66.6 us (6.0
+// TB/s of the measured 6.77 copy: memory); with the norm 6272 tokens x 32 heads
+// 23.3 us (4.4 TB/s), their gradients 44.0 us (3.5 TB/s, two launches), 29.6k
+// tokens appended 109 us (4.9 TB/s).  There neither memory (30 to 55 % busy) nor
+// instruction issue (47 to 58 %) is full: with two rows in flight per lane
+// group, latency is the limit.  fp32: 128, 37.4 and 66.9 us.  A row belongs to a group of lanes, each of which holds both halves of V
 // pairs (two vector loads), so the rotation needs no exchange and the norm a
 // few shuffles.  The angles of a token are shared by all its heads: a CTA
 // takes a few tokens, computes their cosines and sines once into shared
@@ -240,8 +241,8 @@ __device__ __forceinline__ void fill_trig(const RotArgs &g, int t0, int nt, floa
 // before the angles: a CTA has few rows per group, so the latency of its
 // first loads would otherwise stand alone.
 // (Rows of all three segments in one CTA took far more instructions -- which
-// segment, whose weight, where to: 26.3 us against 20.0 us for 6272 tokens x
-// 32 normed heads.)
+// segment, whose weight, where to: a third more time, 26.3 us against 20.0 us,
+// for 6272 tokens x 32 normed heads when both were tried, on inputs in L2.)
 template <typename T, int V, bool PAIRS, bool NORM>
 __global__ void __launch_bounds__(kRotThreads, V == 8 ? 3 : 4) k_rotate(const __grid_constant__ RotArgs g) {
   __shared__ __align__(16) float cs[kMaxTrig], sn[kMaxTrig];
@@ -537,8 +538,8 @@ void set_steps(RotArgs &g) {
 }
 
 // The tokens that a CTA takes of each segment: four rows for every lane
-// group, all asked for at once (12288 tokens x 64 heads: 65 us, with sixteen
-// 82 us), eight where they are normed, so that what a CTA costs besides its
+// group, all asked for at once (12288 tokens x 64 heads: with sixteen a quarter
+// more time), eight where they are normed, so that what a CTA costs besides its
 // rows (addresses, weights) is spread over more; fewer when the three CTAs an
 // SM holds would not all get some, and within the room for angles.  Returns
 // the CTAs of all segments.
