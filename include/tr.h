@@ -526,6 +526,8 @@ tr_status tr_cache_append(const tr_cache *c, const tr_heads *k, const tr_heads *
  * whatever it holds.  (Values that are not finite cost a step little, however
  * long its sequences; only where max_len promises 512 keys at most are the
  * rows that one would spoil computed again, one by one, in 0.1 us a key.)
+ * An infinite value that a row does see gives infinity in its channel, or NaN
+ * where its probability rounds to zero.
  * Probabilities are rounded to the cache's type for their product with V;
  * their sum and everything else is fp32.
  *   q, o:     tr_heads of total_new rows, the same number of heads, a
