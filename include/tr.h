@@ -546,6 +546,93 @@ tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *
                           int32_t causal, int32_t window, int32_t max_new, int32_t max_len, void *ws,
                           size_t ws_bytes, int32_t *d_error, void *stream);
 
+/*
+ * ---- The paged cache held in 8 bits ----
+ *
+ * The same cache in half the bytes: c.k and c.v hold e4m3 codes (one byte,
+ * [pages, heads, page, head_dim]), and every 16 keys of a head (a block)
+ * share one scale 2^(e - 127), a byte e in k_scale / v_scale [pages, heads,
+ * page / 16]: key j's channel c stands for code * scale.  c.dtype is the type
+ * of the rows (queries, new keys and values, outputs: TR_BF16 or TR_F16);
+ * everything else is as in tr_cache.
+ *
+ * tr_cache8_append: a block's scale is the least one that holds the finite
+ * magnitudes of the rows it gets by the call (magnitude <= 448 * scale, 10 <=
+ * e <= 246), and not below the block's old one if it has keys
+ * before the call's; those keys are then coded anew by the scales' quotient,
+ * a power of two, which rounds nothing but what falls under the codes'
+ * smallest step.  Codes are the nearest (ties to even, 448 at most); a value
+ * that is not finite is held as NaN.  k_weight, r, pos, q as in
+ * tr_cache_append: norm and rotation in fp32, rounded once into the codes.
+ * Two sequences of a call may not share a page that it writes.
+ */
+#define TR_CACHE8_BLOCK 16
+typedef struct {
+  tr_cache c;
+  uint8_t *k_scale, *v_scale; /* device [pages, heads, page / 16] */
+} tr_cache8;
+tr_status tr_cache8_append(const tr_cache8 *c, const tr_heads *k, const tr_heads *v, const tr_rotary *r,
+                           const int32_t *pos, const float *k_weight, const tr_heads *q, const float *q_weight,
+                           const tr_heads *q_out, float eps, int32_t *d_error, void *stream);
+
+/*
+ * Attention over it: tr_cache_attend, with the keys and values that the codes
+ * stand for.
+ */
+size_t tr_cache8_attend_workspace_bytes(const tr_cache8 *c, int32_t q_heads, int32_t window, int32_t max_new,
+                                        int32_t max_len);
+tr_status tr_cache8_attend(const tr_cache8 *c, const tr_heads *q, const tr_heads *o, float *lse, float scale,
+                           int32_t causal, int32_t window, int32_t max_new, int32_t max_len, void *ws,
+                           size_t ws_bytes, int32_t *d_error, void *stream);
+
+/*
+ * ---- Block tables kept on the device ----
+ *
+ * What a step of the paged caches goes by -- table, lens, cu_new -- built from
+ * the tokens that each sequence gets, without the host: a stack of free pages
+ * (free[0 .. *free_count), the next one to be taken last) and two calls.
+ *
+ * tr_pages_extend: sequence b gets d_new[b] tokens (negative: none).  cu_new
+ * [batch + 1] becomes their prefix sums; the pages that the sequences grow
+ * into are taken from the stack, sequence by sequence, and entered into the
+ * table; lens grows; and each of the total_new rows gets the slot of its key
+ * in the cache (page id * page + place in the page), its position in its
+ * sequence and the sequence's number.  Rows behind the last token get -1 in
+ * all three.
+ *   A step that cannot be taken changes neither table, lens nor stack: cu_new
+ * is zeros, all rows belong to no sequence, and d_error (optional device
+ * int32, zero it first) gets TR_PAGES_ERR_FULL (not enough free pages),
+ * TR_PAGES_ERR_LONG (a sequence would outgrow its row of the table),
+ * TR_PAGES_ERR_ROWS (more tokens than total_new) or TR_PAGES_ERR_STATE (lens
+ * or free_count are out of range).
+ *
+ * tr_pages_truncate: sequence b keeps its first d_keep[b] tokens at most
+ * (negative: none); pages that hold none of these go back to the stack in the
+ * opposite of the order in which they were taken, and their entries become -1.
+ * Directly after an extend, to the lengths before it, everything is as it was.  Refused as above
+ * (TR_PAGES_ERR_STATE).
+ *
+ * Calls on one table come one after another (a stream, or events between
+ * streams); all of it may be captured and replayed.  ticket is one int32 of
+ * the calls' own, zero before the first.
+ */
+#define TR_PAGES_ERR_FULL 1
+#define TR_PAGES_ERR_LONG 2
+#define TR_PAGES_ERR_ROWS 4
+#define TR_PAGES_ERR_STATE 8
+typedef struct {
+  int32_t *table;       /* device [batch, max_pages]  */
+  int32_t *lens;        /* device [batch]             */
+  int32_t *free;        /* device [pages]             */
+  int32_t *free_count;  /* device [1]                 */
+  int32_t *ticket;      /* device [1]                 */
+  int32_t batch, max_pages;
+  int32_t pages, page;  /* of the cache               */
+} tr_pages;
+tr_status tr_pages_extend(const tr_pages *p, const int32_t *d_new, int32_t total_new, int32_t *cu_new, int32_t *slots,
+                          int32_t *pos, int32_t *seq, int32_t *d_error, void *stream);
+tr_status tr_pages_truncate(const tr_pages *p, const int32_t *d_keep, int32_t *d_error, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,11 +14,15 @@ projector's first layer on the kept tokens, reading them from x by index, and
 ``project`` the same layer on the gathered rows y (the faster route).
 ``Rotary`` and ``PagedCache`` take the kept tokens on through an attention
 layer of the language model: rotary positions with several axes, the append of
-keys and values to a paged cache, and the attention over it.
+keys and values to a paged cache, and the attention over it.  ``PagedCache8``
+is that cache in 8 bits, and ``PageTable`` keeps the block tables of either on
+the GPU.
 """
 from .api import (Mlp, MlpResult, Pipeline, Reducer, ReduceResult, budgets, mlp, project, project_kept, reduce,
                   score, select, workspace_bytes)
-from .attention import PagedCache, Rotary, RotaryGrads
+from .attention import PagedCache, PagedCache8, Rotary, RotaryGrads
+from .pages import PageTable, Step
 
-__all__ = ["Mlp", "MlpResult", "PagedCache", "Pipeline", "Reducer", "ReduceResult", "Rotary", "RotaryGrads", "budgets",
-           "mlp", "project", "project_kept", "reduce", "score", "select", "workspace_bytes"]
+__all__ = ["Mlp", "MlpResult", "PageTable", "PagedCache", "PagedCache8", "Pipeline", "Reducer", "ReduceResult", "Rotary",
+           "RotaryGrads", "Step", "budgets", "mlp", "project", "project_kept", "reduce", "score", "select",
+           "workspace_bytes"]

@@ -96,6 +96,28 @@ class TrCache(ctypes.Structure):
     ]
 
 
+class TrCache8(ctypes.Structure):
+    _fields_ = [
+        ("c", TrCache),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+    ]
+
+
+class TrPages(ctypes.Structure):
+    _fields_ = [
+        ("table", ctypes.c_void_p),
+        ("lens", ctypes.c_void_p),
+        ("free", ctypes.c_void_p),
+        ("free_count", ctypes.c_void_p),
+        ("ticket", ctypes.c_void_p),
+        ("batch", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("pages", ctypes.c_int32),
+        ("page", ctypes.c_int32),
+    ]
+
+
 class TrError(RuntimeError):
     def __init__(self, fn, code, lib):
         self.code = code
@@ -160,6 +182,13 @@ def load() -> ctypes.CDLL:
     lib.tr_cache_attend_workspace_bytes.restype = SZ
     lib.tr_cache_attend.argtypes = [cache, heads, heads, VP, F32, I32, I32, I32, I32, VP, SZ, VP, VP]
     lib.tr_cache_attend.restype = I32
+    cache8, pages = P(TrCache8), P(TrPages)
+    lib.tr_cache8_append.argtypes, lib.tr_cache8_append.restype = [cache8, *lib.tr_cache_append.argtypes[1:]], I32
+    lib.tr_cache8_attend_workspace_bytes.argtypes = [cache8, I32, I32, I32, I32]
+    lib.tr_cache8_attend_workspace_bytes.restype = SZ
+    lib.tr_cache8_attend.argtypes, lib.tr_cache8_attend.restype = [cache8, *lib.tr_cache_attend.argtypes[1:]], I32
+    lib.tr_pages_extend.argtypes, lib.tr_pages_extend.restype = [pages, VP, I32, VP, VP, VP, VP, VP, VP], I32
+    lib.tr_pages_truncate.argtypes, lib.tr_pages_truncate.restype = [pages, VP, VP, VP], I32
     _lib = lib
     return lib
 

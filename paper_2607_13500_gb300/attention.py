@@ -1,5 +1,6 @@
 """Python binding of libtr's attention-layer operators: rotary positions with
-several axes (``Rotary``) and the paged key/value cache (``PagedCache``).
+several axes (``Rotary``) and the paged key/value cache, in 16 bits
+(``PagedCache``) and in 8 (``PagedCache8``).
 
 As in api.py the kernels run in libtr on the current stream and nothing here
 computes on the host: the binding checks what the C side cannot (types,
@@ -30,9 +31,20 @@ _CODES = {torch.bfloat16: TR_BF16, torch.float16: TR_F16, torch.float32: TR_F32}
 _pack_heads = struct.Struct("@Pqqi0q").pack           # tr_heads
 _pack_rotary = struct.Struct("@PPiiii").pack          # tr_rotary
 _pack_cache = struct.Struct("@PPiiiiiPiiPPi0q").pack  # tr_cache
+_pack_scales = struct.Struct("@PP").pack              # what follows it in tr_cache8
 assert len(_pack_heads(0, 0, 0, 0)) == ctypes.sizeof(_lib.TrHeads)
 assert len(_pack_rotary(0, 0, 0, 0, 0, 0)) == ctypes.sizeof(_lib.TrRotary)
 assert len(_pack_cache(*([0] * 13))) == ctypes.sizeof(_lib.TrCache)
+assert len(_pack_cache(*([0] * 13)) + _pack_scales(0, 0)) == ctypes.sizeof(_lib.TrCache8)
+
+
+def _raw(lib, name):
+    """A function of the library with raw argument types."""
+    known, fn = getattr(lib, name), lib[name]  # indexing gives a function object of our own
+    fn.argtypes = [a if a in (ctypes.c_int32, ctypes.c_float, ctypes.c_size_t) else ctypes.c_void_p
+                   for a in known.argtypes]
+    fn.restype = known.restype
+    return fn
 
 
 class _Calls:
@@ -41,11 +53,16 @@ class _Calls:
     def __init__(self, lib):
         for name in ("tr_rotary_apply", "tr_rotary_backward", "tr_rotary_backward_workspace_bytes", "tr_cache_append",
                      "tr_cache_attend", "tr_cache_attend_workspace_bytes"):
-            known, fn = getattr(lib, name), lib[name]  # indexing gives a function object of our own
-            fn.argtypes = [a if a in (ctypes.c_int32, ctypes.c_float, ctypes.c_size_t) else ctypes.c_void_p
-                           for a in known.argtypes]
-            fn.restype = known.restype
-            setattr(self, name[3:], fn)
+            setattr(self, name[3:], _raw(lib, name))
+        self.cache8 = _Calls8(lib)
+
+
+class _Calls8:
+    """The same of the cache held in 8 bits, by the same names."""
+
+    def __init__(self, lib):
+        for name in ("cache_append", "cache_attend", "cache_attend_workspace_bytes"):
+            setattr(self, name, _raw(lib, name.replace("cache", "tr_cache8")))
 
 
 _calls = None
@@ -294,11 +311,18 @@ class PagedCache:
         mk = lambda: torch.empty(pages, heads, page, head_dim, dtype=dtype, device=device)
         return cls(mk(), mk())
 
-    def _struct(self, table, lens, cu_new, tokens):
+    def _rows_type(self, rows, name):
+        """The type of a step's rows."""
+        return self.dtype
+
+    def _struct(self, table, lens, cu_new, tokens, dtype):
+        return self._pack(self._fixed, table, lens, cu_new, tokens)
+
+    def _pack(self, fixed, table, lens, cu_new, tokens):
         i, batch, shape = self.index, lens.shape[0], table.shape
         if len(shape) != 2 or shape[0] != batch:
             raise ValueError("table must be [batch, max_pages], lens [batch]")
-        return _pack_cache(*self._fixed, _ints(table, "table", shape, i), batch, shape[1],
+        return _pack_cache(*fixed, _ints(table, "table", shape, i), batch, shape[1],
                            _ints(lens, "lens", (batch,), i), _ints(cu_new, "cu_new", (batch + 1,), i), tokens)
 
     def append(self, k, v, table, lens, cu_new, rotary=None, pos=None, k_weight=None, q=None, q_weight=None,
@@ -308,8 +332,8 @@ class PagedCache:
         Rotary, with ``pos``) and ``k_weight`` are optional.  ``q`` [T, q
         heads, head_dim], when given, is normed and rotated in the same
         launch; returns it (``q_out``, which may be q), else None."""
-        t, d, i, dt = k.shape[0], self.head_dim, self.index, self.dtype
-        c = self._struct(table, lens, cu_new, t)
+        t, d, i, dt = k.shape[0], self.head_dim, self.index, self._rows_type(k, "k")
+        c = self._struct(table, lens, cu_new, t, dt)
         hk, hv = _heads(k, "k", t, self.heads, d, dt, i), _heads(v, "v", t, self.heads, d, dt, i)
         r = p = hq = hqo = None
         if rotary is not None:
@@ -337,9 +361,9 @@ class PagedCache:
         the launch (defaults: all T, and what the table can hold).  Rows from
         cu_new[batch] on are zeros.  ``out`` does not overlap q.  Returns
         out, or (out, lse fp32 [T, q heads])."""
-        t, d, i = q.shape[0], self.head_dim, self.index
-        c = self._struct(table, lens, cu_new, t)
-        hq = _heads(q, "q", t, None, d, self.dtype, i)
+        t, d, i, dt = q.shape[0], self.head_dim, self.index, self._rows_type(q, "q")
+        c = self._struct(table, lens, cu_new, t, dt)
+        hq = _heads(q, "q", t, None, d, dt, i)
         out, ho = _output(out, q, "out", i)
         heads = q.shape[1]
         lse = torch.empty((t, heads), dtype=torch.float32, device=self.device) if return_lse else None
@@ -365,3 +389,55 @@ class PagedCache:
             if rc:
                 check("tr_cache_attend", rc)
         return (out, lse) if return_lse else out
+
+
+class PagedCache8(PagedCache):
+    """A paged key/value cache of one layer in 8 bits: ``k`` and ``v``
+    (float8_e4m3fn [pages, heads, page, head_dim]) hold codes, and every 16
+    keys of a head share a power-of-two scale, ``k_scale`` and ``v_scale``
+    (float8_e8m0fnu [pages, heads, page // 16]): a key's channel stands for
+    code * scale.  A page is a power of two from 16 to 256.
+
+    ``append`` and ``attend`` are PagedCache's, with rows (queries, new keys
+    and values, outputs) in bf16 or fp16, whichever a call brings.  A block's
+    scale is the least that holds what was appended to it, and grows with it:
+    its older keys are then coded anew, by a power of two.  What is not finite
+    is held as NaN."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        self.calls = _library().cache8
+        if k.device.type != "cuda" or any(t.device != k.device for t in (v, k_scale, v_scale)):
+            raise ValueError("the cache must live on one CUDA device (libtr has no CPU path)")
+        if k.dtype != torch.float8_e4m3fn or v.dtype != k.dtype:
+            raise TypeError("k and v must be float8_e4m3fn")
+        if k_scale.dtype != torch.float8_e8m0fnu or v_scale.dtype != k_scale.dtype:
+            raise TypeError("k_scale and v_scale must be float8_e8m0fnu")
+        if k.dim() != 4 or v.shape != k.shape or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("k and v must be contiguous [pages, heads, page, head_dim]")
+        scales = (k.shape[0], k.shape[1], k.shape[2] // 16)
+        for t in (k_scale, v_scale):
+            if t.shape != scales or not t.is_contiguous():
+                raise ValueError(f"k_scale and v_scale must be contiguous {list(scales)}")
+        self.k, self.v, self.device, self.dtype, self.index = k, v, k.device, k.dtype, k.get_device()
+        self.k_scale, self.v_scale = k_scale, v_scale
+        self.pages, self.heads, self.page, self.head_dim = k.shape
+        self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._fixed = {t: (k.data_ptr(), v.data_ptr(), _CODES[t], *k.shape) for t in (torch.bfloat16, torch.float16)}
+        self._scales = _pack_scales(k_scale.data_ptr(), v_scale.data_ptr())
+        self._sizes = {}
+
+    @classmethod
+    def empty(cls, pages, heads, page, head_dim, device="cuda"):
+        """An uninitialised cache."""
+        mk = lambda d, t: torch.empty(pages, heads, *d, dtype=torch.uint8, device=device).view(t)
+        codes, scales = (page, head_dim), (page // 16,)
+        return cls(mk(codes, torch.float8_e4m3fn), mk(codes, torch.float8_e4m3fn), mk(scales, torch.float8_e8m0fnu),
+                   mk(scales, torch.float8_e8m0fnu))
+
+    def _rows_type(self, rows, name):
+        if rows.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError(f"{name} must be bf16 or fp16")
+        return rows.dtype
+
+    def _struct(self, table, lens, cu_new, tokens, dtype):
+        return self._pack(self._fixed[dtype], table, lens, cu_new, tokens) + self._scales

@@ -1,0 +1,114 @@
+"""Python binding of libtr's block tables (``PageTable``): which pages of a paged
+cache the keys of each sequence lie in, kept on the GPU.
+
+As in attention.py the kernels run in libtr on the current stream and no call
+synchronises.
+"""
+from __future__ import annotations
+
+import ctypes
+import struct
+from dataclasses import dataclass
+
+import torch
+
+from . import _lib, attention
+from ._device import at
+from ._lib import check, load
+
+_pack_pages = struct.Struct("@PPPPPiiii").pack  # tr_pages
+assert len(_pack_pages(*([0] * 9))) == ctypes.sizeof(_lib.TrPages)
+
+_calls = None
+
+
+class _Calls:
+    def __init__(self, lib):
+        self.lib = lib
+        self.extend, self.truncate = (attention._raw(lib, n) for n in ("tr_pages_extend", "tr_pages_truncate"))
+
+
+def _library():
+    global _calls
+    lib = load()
+    if _calls is None or _calls.lib is not lib:
+        _calls = _Calls(lib)
+    return _calls
+
+
+@dataclass
+class Step:
+    cu_new: torch.Tensor  # int32 [batch + 1], prefix sums of the new tokens
+    slots: torch.Tensor   # int32 [rows], place of the row's key in the cache (page id * page + place in the page), or -1
+    pos: torch.Tensor     # int32 [rows], its position in its sequence, or -1
+    seq: torch.Tensor     # int32 [rows], its sequence, or -1
+
+
+class PageTable:
+    """The block tables of ``batch`` sequences in a paged cache of ``pages``
+    pages of ``page`` keys, at most ``max_pages`` of them a sequence: ``table``
+    int32 [batch, max_pages] and ``lens`` int32 [batch] as PagedCache and
+    PagedCache8 read them, and a stack of free pages, ``free`` int32 [pages]
+    with ``free_count`` int32 [1] of them in use, the last the next to be
+    taken.  New: no sequence has a token, and page 0 is the next.
+
+    ``extend`` and ``truncate`` change them on the GPU from device tensors, so
+    a captured step follows its requests.  Calls on one table come one after
+    another (one stream, or events between streams).  A call that cannot be
+    carried out changes nothing, and ``error`` (int32[1]) collects
+    TR_PAGES_ERR_FULL, _LONG, _ROWS or _STATE."""
+
+    def __init__(self, batch, max_pages, pages, page, device="cuda"):
+        self.calls = _library()
+        self.device = attention._device(device)
+        self.index = self.device.index
+        self.batch, self.max_pages, self.pages, self.page = int(batch), int(max_pages), int(pages), int(page)
+        if min(self.batch, self.max_pages, self.pages) < 0:
+            raise ValueError("batch, max_pages and pages cannot be negative")
+        if not 16 <= self.page <= 256 or self.page & (self.page - 1):
+            raise ValueError("page must be a power of two from 16 to 256")
+        if self.pages * self.page > attention._MOST or self.max_pages * self.page > attention._MOST - 65536:
+            raise ValueError("slots and positions are 32-bit numbers: fewer pages")
+        mk = lambda *s: torch.zeros(s, dtype=torch.int32, device=self.device)
+        self.table, self.lens = mk(self.batch, self.max_pages).fill_(-1), mk(self.batch)
+        self.free = torch.arange(self.pages - 1, -1, -1, dtype=torch.int32, device=self.device)
+        self.free_count = mk(1).fill_(self.pages)
+        self.error, self._ticket = mk(1), mk(1)
+
+    def _struct(self):
+        i = self.index
+        ints = attention._ints
+        return _pack_pages(ints(self.table, "table", (self.batch, self.max_pages), i),
+                           ints(self.lens, "lens", (self.batch,), i), ints(self.free, "free", (self.pages,), i),
+                           ints(self.free_count, "free_count", (1,), i), self._ticket.data_ptr(), self.batch,
+                           self.max_pages, self.pages, self.page)
+
+    def extend(self, new, rows) -> Step:
+        """``new`` int32 [batch] more tokens for each sequence (negative:
+        none), ``rows`` of them at most in all: their pages are taken from the
+        free ones and ``lens`` grows (tr_pages_extend).  Returns what the rows
+        need, rows behind the last token with -1.  If a step cannot be taken,
+        cu_new is zeros and every row has -1."""
+        i, b = self.index, self.batch
+        rows = int(rows)
+        if not 0 <= rows <= attention._MOST:
+            raise ValueError("rows must be a 32-bit number that is not negative")
+        c, p = self._struct(), attention._ints(new, "new", (b,), i)
+        buf = torch.empty(b + 1 + 3 * rows, dtype=torch.int32, device=self.device)
+        cu, slots, pos, seq = buf.split((b + 1, rows, rows, rows))
+        rc = at(i, self.calls.extend)(c, p, rows, cu.data_ptr(), slots.data_ptr(), pos.data_ptr(), seq.data_ptr(),
+                                      self.error.data_ptr(), attention._stream(i))
+        if rc:
+            check("tr_pages_extend", rc)
+        return Step(cu, slots, pos, seq)
+
+    def truncate(self, keep):
+        """Every sequence keeps its first ``keep`` int32 [batch] tokens at
+        most (0 or less: none), and the pages behind them are free again
+        (tr_pages_truncate).  Directly after an extend, to the lengths before
+        it, everything is as it was."""
+        i = self.index
+        c, p = self._struct(), attention._ints(keep, "keep", (self.batch,), i)
+        rc = at(i, self.calls.truncate)(c, p, self.error.data_ptr(), attention._stream(i))
+        if rc:
+            check("tr_pages_truncate", rc)
