@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libtr.so")
 SOURCES = ["tr_api.cu", "tr_score.cu", "tr_select.cu", "tr_gather.cu", "tr_noalloc.cu", "tr_mlp.cu",
-           "tr_rotary.cu", "tr_attend.cu", "tr_attend_few.cu", "tr_append8.cu", "tr_attend8.cu", "tr_pages.cu"]
+           "tr_rotary.cu", "tr_attend.cu", "tr_attend_few.cu", "tr_append8.cu", "tr_attend8.cu",
+           "tr_attend8_few.cu", "tr_pages.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-O2", "-I", INCLUDE, "-I", CSRC]
 

@@ -603,10 +603,7 @@ Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_le
   const int group = q_heads / c->heads;
   const long long most = (long long)(max_new < c->total_new ? max_new : c->total_new) * group;
   const int sms = sm_count() > 0 ? sm_count() : 1;
-  // (its units, tiles of all blocks and key heads, are counted in 31 bits)
-  const long long blocks16 = (long long)c->total_new * group / kFewRows + c->batch;
-  const long long table_tiles = ((long long)c->max_pages * c->page + kTile - 1) / kTile + kFewItemCost;
-  if (most <= kFewRows && c->batch <= kFewMaxBatch && blocks16 * c->heads <= INT_MAX / table_tiles) {
+  if (few_takes(c, q_heads, max_new)) {
     p.few = true;
     p.total = few_workspace_bytes(c->head_dim, sms);
     return p;

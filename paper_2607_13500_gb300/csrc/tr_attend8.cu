@@ -6,14 +6,12 @@
 // scores at a time, one after another, then their values.
 #include <cmath>
 
-#include "tr_attend.cuh"
-#include "tr_cache8.cuh"
+#include "tr_attend8.cuh"
 
 namespace tr {
 namespace {
 
-using namespace attend;
-using namespace cache8;
+using namespace attend8;
 
 __device__ __forceinline__ float4 values4(const uint8_t *codes, float scale) {
   const uint32_t w = *reinterpret_cast<const uint32_t *>(codes);
@@ -81,7 +79,7 @@ size_t tr_cache8_attend_workspace_bytes(const tr_cache8 *c, int32_t q_heads, int
                                         int32_t max_len) {
   if (check_cache8(c) != TR_OK || q_heads <= 0 || q_heads % c->c.heads || window < 0 || max_new < 0 || max_len < 0)
     return 0;
-  return 0;
+  return few_takes(&c->c, q_heads, max_new) ? few_workspace_bytes(c->c.head_dim, sm_count() > 0 ? sm_count() : 1) : 0;
 }
 
 tr_status tr_cache8_attend(const tr_cache8 *c8, const tr_heads *q, const tr_heads *o, float *lse, float scale,
@@ -113,6 +111,21 @@ tr_status tr_cache8_attend(const tr_cache8 *c8, const tr_heads *q, const tr_head
   const Scales sc{c8->k_scale, c8->v_scale};
   const long long rows = (long long)c->total_new * q->heads;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  while ((1 << g.page_log2) < c->page) ++g.page_log2;
+  if (few_takes(c, q->heads, max_new)) {
+    g.ctas = sm_count() > 0 ? sm_count() : 1;
+    const size_t need = few_workspace_bytes(c->head_dim, g.ctas);
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < need) return TR_ERR_WORKSPACE;
+    CUtensorMap mk{}, mv{};
+    const long long keys = (long long)c->pages * c->heads * c->page;
+    const int box = c->page < kTile ? c->page : kTile, wide = c->head_dim <= 64 ? 64 : 128;
+    // an empty cache keeps one row in the maps' extents: no page id is valid, so nothing reads it
+    if (!make_map_bytes(&mk, c->k, keys > 0 ? keys : 1, c->head_dim, box, wide) ||
+        !make_map_bytes(&mv, c->v, keys > 0 ? keys : 1, c->head_dim, box, wide))
+      return TR_ERR_CUDA;
+    Attend8Args p{g, sc};
+    return launch_few8(mk, mv, p, c->dtype == TR_BF16, ws, st) == cudaSuccess ? TR_OK : TR_ERR_CUDA;
+  }
   const dim3 grid((unsigned)((rows + 3) / 4));
   const cudaError_t err = c->dtype == TR_BF16 ? launch_kernel(k_attend8_rows<__nv_bfloat16>, grid, dim3(128), 0, st, false, g, sc)
                                               : launch_kernel(k_attend8_rows<__half>, grid, dim3(128), 0, st, false, g, sc);

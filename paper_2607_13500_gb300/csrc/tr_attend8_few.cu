@@ -1,0 +1,440 @@
+// Attention of few rows per key head over the paged cache held in 8 bits:
+// bound, like its 16-bit counterpart (tr_attend_few.cu, whose shares, walk and
+// join it uses), by reading K and V once, and they are half as long.
+//
+// Codes become halves in registers, two at a time and exactly, on their way
+// into warp-level products (m16n8k16).  A warp's 16 keys of a tile are one
+// block, so scales cost next to nothing:
+//   K   one factor for the 16 keys' scores;
+//   V   2^(e - R) with R the largest exponent of the warp's blocks so far, like
+//       the running maximum of the softmax: when R grows, the sums move with
+//       it (by a power of two, exactly).  Values keep all their bits down to
+//       2^-22 of the largest block's scale.
+// bf16 queries enter as halves as well, each row divided by a power of two.
+// Probabilities are kept below 2^14 and rounded to halves, so that they keep
+// their bits down to 2^-20 of the row's largest.
+#include <atomic>
+
+#include "tr_attend8.cuh"
+#include "tr_attend_few.cuh"
+
+namespace tr {
+namespace {
+
+using namespace attend8;
+using namespace attend::few;
+
+template <int D>
+struct Few8 {
+  static constexpr int kTileBytes = kTile * D;
+  static constexpr int kJoinRow = D + 4;  // floats
+  static constexpr int kJoinBytes = kWarps * kPass * kJoinRow * 4;
+  static constexpr int kFit = (227 * 1024 - 4096 - 1024 - kJoinBytes) / kTileBytes;
+  static constexpr int kStages = kFit < 16 ? kFit : 16;
+  static constexpr size_t kSmem = (size_t)kStages * kTileBytes + kJoinBytes + 1024 + 4096;
+};
+
+constexpr float kLift = 6.f;   // probabilities are taken times 2^6 (and grow by 2^8 at most)
+constexpr int kValueLift = 7;  // and values times 2^7: 448 becomes 57344
+constexpr int kNoExp = -1000;  // R before the first block
+
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
+  return v;
+}
+// 2^e as a pair of halves, e <= 15; 0 below 2^-24.
+__device__ __forceinline__ uint32_t half_pow2(int e) {
+  const uint32_t h = e >= -14 ? (uint32_t)(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u;
+  return h | h << 16;
+}
+__device__ __forceinline__ uint32_t mul_halves(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_attend8_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                  const __grid_constant__ Attend8Args p) {
+  using F = Few8<D>;
+  using Ring = CodeRing<D, F::kStages>;
+  const AttendArgs &g = p.a;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ int runs[kFewMaxBatch / 32];  // units of 32 sequences each
+  __shared__ float top[kWarps][kFewRows], tot[kWarps][kFewRows];
+  __shared__ int bad, share0, share_units;  // bad: values were taken out of a tile
+  const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
+  float *join = reinterpret_cast<float *>(smem_raw + (base - tc::smem_u32(smem_raw)) + F::kStages * F::kTileBytes);
+  const uint32_t bars = tc::smem_u32(join) + F::kJoinBytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  Ring ring;
+  ring.base = base, ring.full0 = bars, ring.empty0 = bars + 8u * F::kStages;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < F::kStages; ++s) {
+      tc::mbar_init(ring.full(s), 1);
+      tc::mbar_init(ring.empty(s), kWarps);
+    }
+    tc::mbar_fence_init();
+    tc::tma_prefetch_map(&map_k);
+    tc::tma_prefetch_map(&map_v);
+    bad = 0;
+  }
+  pdl_wait();  // q and the cache come from the kernels before
+  pdl_trigger();
+  __syncthreads();  // the barriers are ready
+  Walk w;
+  Seq run0;
+  const Shares shares(count_units(g, runs, kWarps + 2, run0), g.ctas);
+  const int share = shares.start(blockIdx.x), share_end = shares.start(blockIdx.x + 1);
+  if (share >= share_end) return;
+  if (threadIdx.x == 0) share0 = share, share_units = share_end - share;  // for the consumers' second walk
+  w.seek(g, runs, run0, share, share_end);
+
+  if (warp >= kWarps) {
+    ring.take(warp - kWarps);
+    const CUtensorMap *map = warp == kWarps ? &map_k : &map_v;
+    bool ok = true;
+    while (ok && w.next(g)) {
+      const int hk = w.item % g.c.heads, end = w.tile + w.count;
+      ring.seen = keys_of_seq(g, w.s);
+      int id = ring.page_id(g, w.seq(), w.s.len, w.tile);
+      for (int t = w.tile; t < end && ok; ++t) {
+        const int next = t + 1 < end ? ring.page_id(g, w.seq(), w.s.len, t + 1) : -1;
+        ok = ring.load(g, map, id, w.s.len, hk, t);
+        id = next;
+      }
+    }
+    if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+    ring.drain();
+    return;
+  }
+
+  // ------------------------------------------------------------------ consumers
+  constexpr int kPieces = D / 64;          // 16-byte pieces of a key's row a lane takes
+  constexpr int kTiles = D / 8;            // n-tiles of the second product
+  const int gq = lane >> 2, c = lane & 3;  // quad (row or key of a fragment), lane of the quad
+  int kst = Ring::first(0), vst = Ring::first(1);
+  uint32_t kph = 0, vph = 0;
+  bool ok = true;  // once a wait has timed out the warp only keeps up with the others' barriers
+  while (w.next(g)) {
+    const int hk = w.item % g.c.heads, block0 = w.item / g.c.heads * kFewRows;
+    const int rows = min(kFewRows, w.s.rows - block0);
+    // scales of this warp's blocks of the piece's first tiles, a tile each lane
+    uint32_t held = block_scales(p, w.seq(), hk, lane < w.count ? w.s.len : 0, (w.tile + lane) * kTile + 16 * warp);
+    uint32_t ahead = kNoScales;
+    // this lane's two rows of a fragment, and the keys they see
+    int lo[2], hi[2];
+    float fr[2];                 // what a score of the row is multiplied by, K's scale apart
+    uint32_t q[kPieces * 4][4];  // fragments of the first product: channels 4 m .. 4 m + 3 of a piece
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = gq + 8 * i, row = block0 + r;
+      const bool valid = r < rows;
+      const int tok = valid ? row / g.group : 0, head = hk * g.group + (valid ? row - tok * g.group : 0);
+      const int own = w.s.base + tok;
+      hi[i] = !valid ? INT_MAX : g.causal ? min(w.s.len, own + 1) : w.s.len;
+      lo[i] = valid && g.window > 0 ? window_start(own, g.window) : 0;
+      const char *qrow = g.q + 2 * ((long long)(w.s.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
+      uint32_t x[kPieces][8], most = 0u;
+#pragma unroll
+      for (int s = 0; s < kPieces; ++s) {
+        const int ch = (kPieces * c + s) * 16;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (valid && ch < g.c.d) v = *reinterpret_cast<const uint4 *>(qrow + 2 * ch + 16 * h);
+          x[s][4 * h] = v.x, x[s][4 * h + 1] = v.y, x[s][4 * h + 2] = v.z, x[s][4 * h + 3] = v.w;
+        }
+        if (Bits<T>::kBf16)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) most = max(most, top_of_pair(x[s][k]));
+      }
+      fr[i] = g.scale;
+      float down = 1.f;
+      if (Bits<T>::kBf16) {
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        const int e = query_exp(most);
+        down = pow2(-e);
+        fr[i] *= pow2(e);
+      }
+      const uint32_t flip = g.negate ? 0x80008000u : 0u;
+#pragma unroll
+      for (int s = 0; s < kPieces; ++s)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          // a0, a2: the row g's first and second pair; a1, a3: row g + 8's
+          q[4 * s + m][i] = (Bits<T>::kBf16 ? query_pair(x[s][2 * m], down) : x[s][2 * m]) ^ flip;
+          q[4 * s + m][2 + i] = (Bits<T>::kBf16 ? query_pair(x[s][2 * m + 1], down) : x[s][2 * m + 1]) ^ flip;
+        }
+    }
+    float o[kTiles][4];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+    float mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+    int big = kNoExp;  // R
+
+    for (int n0 = 0; ok && n0 < w.count; ++n0) {
+      const int t = w.tile + n0;
+      if ((n0 & 31) == 0) {  // the next 32 tiles' scales, long before they are needed
+        if (n0) held = ahead;
+        ahead = block_scales(p, w.seq(), hk, n0 + 32 + lane < w.count ? w.s.len : 0, (t + 32 + lane) * kTile + 16 * warp);
+      }
+      const uint32_t sc = __shfl_sync(0xffffffffu, held, n0 & 31);
+      const int ek = (int)(sc & 0xffu) - 127, ev = (int)(sc >> 8) - 127;
+      // ---- scores of 16 keys: two products of 8 keys
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(kst), kph));
+      if (!ok) {
+        if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+        break;
+      }
+      const uint32_t kt = base + kst * F::kTileBytes;
+      float s[2][4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        // two chains of products, so that one's latency hides the other's
+        float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+          const uint4 v = lds128(kt + Ring::piece(16 * warp + 8 * n + gq, kPieces * c + j));
+          const uint32_t *word = &v.x;
+#pragma unroll
+          for (int m = 0; m < 4; ++m)
+            mma16816<__half>(m & 1 ? y : x, q[4 * j + m][0], q[4 * j + m][1], q[4 * j + m][2], q[4 * j + m][3],
+                             halves((uint16_t)word[m]), halves((uint16_t)(word[m] >> 16)));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] = x[i] + y[i];
+      }
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(ring.empty(kst));
+      Ring::on(0, kst, kph);
+
+      // ---- softmax: s[n][0..1] row g, s[n][2..3] row g + 8, keys 8 n + 2 c and + 1
+      const int key0 = t * kTile + 16 * warp;
+      const bool ends = key0 + 16 > w.s.len;
+      const int most = min(key0 + 16, w.s.len);  // open: some row does not see some of the sequence's keys here
+      const bool open = __any_sync(0xffffffffu, lo[0] > key0 || hi[0] < most || lo[1] > key0 || hi[1] < most);
+      if (open || ends) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int key = key0 + 8 * n + 2 * c + (j & 1);
+            if (key < lo[j >> 1] || key >= hi[j >> 1]) s[n][j] = -INFINITY;
+          }
+      }
+      float now[2], fs[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fs[i] = fminf(fmaxf(fr[i] * pow2(ek), 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
+        now[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1])) * fs[i];
+        now[i] = fmaxf(now[i], __shfl_xor_sync(0xffffffffu, now[i], 1));
+        now[i] = fmaxf(now[i], __shfl_xor_sync(0xffffffffu, now[i], 2));
+      }
+      if (__any_sync(0xffffffffu, now[0] > mx[0] + 8.f || now[1] > mx[1] + 8.f)) {
+        float f[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const bool up = now[i] > mx[i] + 8.f;
+          f[i] = up ? exp2_fast(mx[i] - now[i]) : 1.f;
+          if (up) mx[i] = now[i];
+          sum[i] *= f[i];
+        }
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          o[i][0] *= f[0], o[i][1] *= f[0];
+          o[i][2] *= f[1], o[i][3] *= f[1];
+        }
+      }
+      uint32_t pr[4];  // the A fragment of the second product
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float neg = mx[i] == -INFINITY ? 0.f : kLift - mx[i];
+          const float p0 = exp2_fast(fmaf(s[n][2 * i], fs[i], neg)), p1 = exp2_fast(fmaf(s[n][2 * i + 1], fs[i], neg));
+          sum[i] += p0 + p1;
+          pr[2 * n + i] = Bits<__half>::pack(p0, p1);
+        }
+      if (ev > big && ev <= 127) {  // a larger block of values (128: none)
+        const float f = big - ev < -126 ? 0.f : pow2(big - ev);
+        big = ev;
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[i][j] *= f;
+      }
+      const uint32_t lift = half_pow2(kValueLift + min(ev - big, 0));
+
+      // ---- o += p V: n-tile i holds channels D / 8 g + i
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(vst), vph));
+      if (!ok) {
+        if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+        break;
+      }
+      bool found = false;
+      const uint32_t vt = base + vst * F::kTileBytes;
+      uint32_t v[4][D / 32];  // of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = 2 * c + (j & 1) + 8 * (j >> 1);
+        if (D == 128) {
+          const uint4 x = lds128(vt + Ring::piece(16 * warp + key, gq));
+          v[j][0] = x.x, v[j][1] = x.y, v[j][D / 32 - 2] = x.z, v[j][D / 32 - 1] = x.w;
+        } else {
+          const uint2 x = lds64(vt + Ring::piece(16 * warp + key, gq >> 1) + 8 * (gq & 1));
+          v[j][0] = x.x, v[j][1] = x.y;
+        }
+        if (ends && key0 + key >= w.s.len) {  // what lies behind the sequence's end may be NaN
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) v[j][i] = 0u;
+        }
+        if (open) {
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) found |= clean_codes(v[j][i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          // channels 4 i + 2 h and + 1 of a pair of keys: one after the other
+          const uint32_t a = __byte_perm(v[0][i], v[1][i], h ? 0x7362u : 0x5140u);
+          const uint32_t b = __byte_perm(v[2][i], v[3][i], h ? 0x7362u : 0x5140u);
+          mma16816<__half>(o[4 * i + 2 * h], pr[0], pr[1], pr[2], pr[3], mul_halves(halves((uint16_t)a), lift),
+                           mul_halves(halves((uint16_t)b), lift));
+          mma16816<__half>(o[4 * i + 2 * h + 1], pr[0], pr[1], pr[2], pr[3], mul_halves(halves((uint16_t)(a >> 16)), lift),
+                           mul_halves(halves((uint16_t)(b >> 16)), lift));
+        }
+      if (found) bad = 1;  // (any thread's word will do)
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(ring.empty(vst));
+      Ring::on(1, vst, vph);
+    }
+
+    // ------------------------------------------------------------------ the piece's result
+    // (mx - kLift: what the probabilities were taken against)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
+      sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+      mx[i] -= kLift;
+      if (c == 0) top[warp][gq + 8 * i] = mx[i], tot[warp][gq + 8 * i] = sum[i];
+    }
+    named_sync(32 * kWarps);
+    // The row's maximum and sum over the warps.  (A maximum passes over NaN
+    // scores, so a warp that saw no other has the maximum of one that saw
+    // nothing: its sum, 0 or NaN, enters as it is.)
+    auto row_total = [&](int r, float &m, float &l) {
+      m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int j = 0; j < kWarps; ++j) m = fmaxf(m, top[j][r]);
+#pragma unroll
+      for (int j = 0; j < kWarps; ++j) l += top[j][r] == -INFINITY ? tot[j][r] : tot[j][r] * exp2_fast(top[j][r] - m);
+    };
+    // Sums are divided by the row's total before V's scale, up to 2^127, enters.
+    float f[2];
+    const float up = big == kNoExp ? 0.f : pow2(big);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float m, l;
+      row_total(gq + 8 * i, m, l);
+      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+      f[i] = (mx[i] == -INFINITY ? 0.f : exp2_fast(mx[i] - m)) * inv * (1.f / (1 << kValueLift));
+    }
+    const int part = 2 * blockIdx.x + (w.starts ? 1 : 0);
+    for (int r0 = 0; r0 < rows; r0 += kPass) {
+      // accumulator column 2 c + (j & 1) of n-tile i is channel D / 8 (2 c + (j & 1)) + i
+      const int mine = gq - (r0 & 7);  // row of the pass that this quad holds (of its rows g or g + 8)
+      if (mine >= 0 && mine < kPass) {
+        float *dst = join + (warp * kPass + mine) * F::kJoinRow + 2 * kTiles * c;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < kTiles; i += 4) {
+            float4 v;
+            if (r0 < 8)
+              v = make_float4(o[i][b] * f[0] * up, o[i + 1][b] * f[0] * up, o[i + 2][b] * f[0] * up, o[i + 3][b] * f[0] * up);
+            else
+              v = make_float4(o[i][2 + b] * f[1] * up, o[i + 1][2 + b] * f[1] * up, o[i + 2][2 + b] * f[1] * up,
+                              o[i + 3][2 + b] * f[1] * up);
+            *reinterpret_cast<float4 *>(dst + kTiles * b + i) = v;
+          }
+      }
+      named_sync(32 * kWarps);
+      const int r = r0 + (int)threadIdx.x / (D / 4), ch = (int)threadIdx.x % (D / 4) * 4;
+      if ((int)threadIdx.x < kPass * (D / 4) && r < rows && ch < g.c.d) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < kWarps; ++j) {
+          const float4 x = *reinterpret_cast<const float4 *>(join + (j * kPass + r - r0) * F::kJoinRow + ch);
+          v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+        }
+        float m, l;
+        row_total(r, m, l);
+        put_row<T, true>(g, w, part, block0, hk, r, ch, v, m, l);
+      }
+      named_sync(32 * kWarps);
+    }
+  }
+
+  // What was taken out of open tiles goes to the rows that see it, when the
+  // share's tiles are all used up.
+  named_sync(32 * kWarps);  // the rows written by other warps
+  if (!ok || !bad) return;
+  w.seek(g, runs, seq_of(g, lane), share0, share0 + share_units);
+  while (w.next(g)) {
+    const int hk = w.item % g.c.heads, block0 = w.item / g.c.heads * kFewRows;
+    const int rows = min(kFewRows, w.s.rows - block0), part = 2 * blockIdx.x + (w.starts ? 1 : 0);
+    for_bad_codes(g, edges_of_rows(g, w.s.base, w.s.len, block0, block0 + rows), w.seq(), hk, w.tile, w.tile + w.count,
+                  [&](int j, const float4 &v) {
+                    for (int r = warp; r < rows; r += kWarps) {
+                      const int tok = (block0 + r) / g.group, head = hk * g.group + (block0 + r) % g.group;
+                      const int own = w.s.base + tok;
+                      if ((g.causal && j > own) || (g.window > 0 && j < window_start(own, g.window))) continue;
+                      add_to_row<T>(g.o + 2 * ((long long)(w.s.tok0 + tok) * g.o_tok + (long long)head * g.o_head),
+                                    w.whole ? nullptr : g.part + ((long long)part * kFewRows + r) * g.c.d, v);
+                    }
+                  });
+  }
+}
+
+std::atomic<int> g_few8_smem_set[64];
+
+template <typename T, int D>
+cudaError_t launch_few8_t(const CUtensorMap &mk, const CUtensorMap &mv, const Attend8Args &p, int variant, cudaStream_t st) {
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  if (!(g_few8_smem_set[dev & 63].load() & (1 << variant))) {
+    err = cudaFuncSetAttribute(k_attend8_few<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Few8<D>::kSmem);
+    if (err != cudaSuccess) return err;
+    g_few8_smem_set[dev & 63].fetch_or(1 << variant);
+  }
+  err = launch_kernel(k_attend8_few<T, D>, dim3(p.a.ctas), dim3(kThreads), Few8<D>::kSmem, st, false, mk, mv, p);
+  if (err != cudaSuccess) return err;
+  const long long rows = (long long)p.a.c.total_new * p.a.q_heads;
+  return launch_kernel(k_few_join<T, true>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, true, p.a);
+}
+
+}  // namespace
+
+namespace attend8 {
+
+cudaError_t launch_few8(const CUtensorMap &mk, const CUtensorMap &mv, Attend8Args p, bool bf16, void *ws, cudaStream_t st) {
+  p.a.part = static_cast<float *>(ws);
+  p.a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + few::part_bytes(p.a.c.d, p.a.ctas));
+  if (bf16)
+    return p.a.c.d <= 64 ? launch_few8_t<__nv_bfloat16, 64>(mk, mv, p, 0, st)
+                         : launch_few8_t<__nv_bfloat16, 128>(mk, mv, p, 1, st);
+  return p.a.c.d <= 64 ? launch_few8_t<__half, 64>(mk, mv, p, 2, st) : launch_few8_t<__half, 128>(mk, mv, p, 3, st);
+}
+
+}  // namespace attend8
+}  // namespace tr
