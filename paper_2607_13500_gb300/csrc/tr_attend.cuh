@@ -446,6 +446,83 @@ struct TileRing {
   }
 };
 
+// ---------------------------------------------------------------- chunks (tr_attend.cu, tr_attend8.cu)
+__device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+  return r;
+}
+
+// The block of tokens that belong to no sequence (first: their first) in this
+// slot: zeros, lse -inf.
+inline __device__ __noinline__ void clear_block(const AttendArgs &g, int first, int slot, int rows_per_block, int hk) {
+  const int rows = (g.c.total_new - first) * g.group;
+  const int block = slot - ((int)((long long)first * g.group / rows_per_block) + g.c.batch);
+  if (block < 0) return;  // an empty slot of the last sequence
+  const int r0 = block * rows_per_block, chunks = g.c.d / 8;
+  for (int i = threadIdx.x; i < min(rows - r0, rows_per_block) * chunks; i += blockDim.x) {
+    const int r = r0 + i / chunks, c = i % chunks;
+    const long long t = first + r / g.group;
+    const int head = hk * g.group + r % g.group;
+    *reinterpret_cast<uint4 *>(g.o + 2 * (t * g.o_tok + (long long)head * g.o_head) + 16 * c) = make_uint4(0u, 0u, 0u, 0u);
+    if (c == 0 && g.lse) g.lse[t * g.q_heads + head] = -INFINITY;
+  }
+}
+
+// Joins the splits of each row: one warp per row, in the splits' order.
+// NORMED: the splits' values are divided by their sums.
+template <typename T, bool NORMED>
+__global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ AttendArgs g) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const long long rows = (long long)g.c.total_new * g.q_heads;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const int t = (int)(row / g.q_heads), h = (int)(row - (long long)t * g.q_heads);
+  char *orow = g.o + 2 * ((long long)t * g.o_tok + (long long)h * g.o_head);
+  const bool holds = 4 * lane < g.c.d;
+  float m = -INFINITY, l = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (find_token(g.c, t).seq >= 0) {
+    for (int s = 0; s < g.splits; ++s) m = fmaxf(m, g.part_ml[s * rows + row].x);
+    for (int s = 0; s < g.splits; ++s) {
+      const float2 ml = g.part_ml[s * rows + row];
+      if (ml.y == 0.f) continue;  // saw no key
+      const float f = exp2_fast(ml.x - m);
+      l += ml.y * f;
+      if (holds) {
+        const float4 v = reinterpret_cast<const float4 *>(g.part + (s * rows + row) * g.c.d)[lane];
+        const float w = NORMED ? ml.y * f : f;
+        acc.x += v.x * w, acc.y += v.y * w, acc.z += v.z * w, acc.w += v.w * w;
+      }
+    }
+  }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  if (holds)
+    reinterpret_cast<uint2 *>(orow)[lane] =
+        make_uint2(Bits<T>::pack(acc.x * inv, acc.y * inv), Bits<T>::pack(acc.z * inv, acc.w * inv));
+  if (g.lse && lane == 0) g.lse[row] = l > 0.f || l != l ? m * 0.693147180559945309f + logf(l) : -INFINITY;
+}
+
+// Parts of the keys: as many as finish earliest when `sms` CTAs run at a
+// time, one costing its tiles and about kCtaTiles more, and the join
+// writing and reading a row's fp32 sums once per part (kJoinRows rows in
+// the time of one tile).
+inline int choose_parts(double blocks, int tiles, int sms, double rows) {
+  constexpr double kCtaTiles = 4.0, kJoinRows = 8192.0;
+  double best = 0;
+  int parts = 1;
+  for (int s = 1; s <= 64 && s <= (tiles > 1 ? tiles : 1); ++s) {
+    const double waves = std::ceil(blocks * s / sms);
+    const double t = waves * ((tiles + s - 1) / s + kCtaTiles) + (s > 1 ? kCtaTiles + rows * s / kJoinRows : 0.0);
+    if (s == 1 || t < best) {
+      best = t;
+      parts = s;
+    }
+  }
+  return parts;
+}
+
 // ---------------------------------------------------------------- few rows (tr_attend_few.cu)
 constexpr int kFewRows = 16;         // rows of a block there
 constexpr int kFewItemCost = 2;      // units that an item counts besides its tiles

@@ -43,17 +43,6 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
   return v;
 }
-// 2^e as a pair of halves, e <= 15; 0 below 2^-24.
-__device__ __forceinline__ uint32_t half_pow2(int e) {
-  const uint32_t h = e >= -14 ? (uint32_t)(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u;
-  return h | h << 16;
-}
-__device__ __forceinline__ uint32_t mul_halves(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attend8_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
