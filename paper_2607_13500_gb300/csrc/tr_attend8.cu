@@ -611,7 +611,7 @@ Plan8 plan8_of(const tr_cache *c, int q_heads, int window, int max_new, int max_
   const int group = q_heads / c->heads;
   const long long most = (long long)(max_new < c->total_new ? max_new : c->total_new) * group;
   const int sms = sm_count() > 0 ? sm_count() : 1;
-  if (few_takes(c, q_heads, max_new)) {
+  if (few_takes(c, q_heads, max_new, kItemCost)) {
     p.few = true;
     p.total = few_workspace_bytes(c->head_dim, sms);
     return p;

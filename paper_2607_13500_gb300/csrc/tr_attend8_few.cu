@@ -3,16 +3,16 @@
 // join it uses), by reading K and V once, and they are half as long.
 //
 // Codes become halves in registers, two at a time and exactly, on their way
-// into warp-level products (m16n8k16).  A warp's 16 keys of a tile are one
-// block, so scales cost next to nothing:
+// into warp-level products (m16n8k16), whose 16 keys are one block, so scales
+// cost next to nothing:
 //   K   one factor for the 16 keys' scores;
-//   V   2^(e - R) with R the largest exponent of the warp's blocks so far, like
-//       the running maximum of the softmax: when R grows, the sums move with
-//       it (by a power of two, exactly).  Values keep all their bits down to
-//       2^-22 of the largest block's scale.
+//   V   2^(e - R), R the largest exponent of the warp's blocks so far, enters
+//       the block's probabilities: like the running maximum of the softmax,
+//       and when R grows, the sums move with it (by a power of two, exactly).
 // bf16 queries enter as halves as well, each row divided by a power of two.
-// Probabilities are kept below 2^14 and rounded to halves, so that they keep
-// their bits down to 2^-20 of the row's largest.
+// Probabilities are taken times 2^6 (2^14 at most) and rounded to halves: they
+// and the scales that they carry keep their bits down to 2^-20 of the largest,
+// and what is lost below is 2^-31 of it.
 #include <atomic>
 
 #include "tr_attend8.cuh"
@@ -23,6 +23,8 @@ namespace {
 
 using namespace attend8;
 using namespace attend::few;
+
+constexpr int kAllThreads = 32 * (kWarps + 4);  // consumers, the producers of K and of V, two more for whole warpgroups
 
 template <int D>
 struct Few8 {
@@ -35,7 +37,6 @@ struct Few8 {
 };
 
 constexpr float kLift = 6.f;   // probabilities are taken times 2^6 (and grow by 2^8 at most)
-constexpr int kValueLift = 7;  // and values times 2^7: 448 becomes 57344
 constexpr int kNoExp = -1000;  // R before the first block
 
 __device__ __forceinline__ uint2 lds64(uint32_t addr) {
@@ -43,8 +44,9 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
   return v;
 }
+
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kAllThreads, 1)
     k_attend8_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ Attend8Args p) {
   using F = Few8<D>;
@@ -64,7 +66,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < F::kStages; ++s) {
       tc::mbar_init(ring.full(s), 1);
-      tc::mbar_init(ring.empty(s), kWarps);
+      tc::mbar_init(ring.empty(s), kWarps / 2);
     }
     tc::mbar_fence_init();
     tc::tma_prefetch_map(&map_k);
@@ -74,15 +76,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   pdl_wait();  // q and the cache come from the kernels before
   pdl_trigger();
   __syncthreads();  // the barriers are ready
-  Walk w;
+  Walk<kItemCost> w;
   Seq run0;
-  const Shares shares(count_units(g, runs, kWarps + 2, run0), g.ctas);
+  const Shares shares(count_units<kItemCost>(g, runs, kWarps + 4, run0), g.ctas);
   const int share = shares.start(blockIdx.x), share_end = shares.start(blockIdx.x + 1);
   if (share >= share_end) return;
   if (threadIdx.x == 0) share0 = share, share_units = share_end - share;  // for the consumers' second walk
   w.seek(g, runs, run0, share, share_end);
 
   if (warp >= kWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp >= kWarps + 2) return;
     ring.take(warp - kWarps);
     const CUtensorMap *map = warp == kWarps ? &map_k : &map_v;
     bool ok = true;
@@ -102,18 +106,27 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 
   // ------------------------------------------------------------------ consumers
+  // Of the share's tiles warps 0 to 3 take the even ones and 4 to 7 the odd
+  // ones, a quarter each: 32 keys, two blocks.
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");  // (with 56 what 168 at launch give)
+  const int odd = warp >> 2, quarter = warp & 3;
   constexpr int kPieces = D / 64;          // 16-byte pieces of a key's row a lane takes
   constexpr int kTiles = D / 8;            // n-tiles of the second product
   const int gq = lane >> 2, c = lane & 3;  // quad (row or key of a fragment), lane of the quad
   int kst = Ring::first(0), vst = Ring::first(1);
   uint32_t kph = 0, vph = 0;
+  int tiles = 0;   // of the share so far
   bool ok = true;  // once a wait has timed out the warp only keeps up with the others' barriers
   while (w.next(g)) {
     const int hk = w.item % g.c.heads, block0 = w.item / g.c.heads * kFewRows;
     const int rows = min(kFewRows, w.s.rows - block0);
-    // scales of this warp's blocks of the piece's first tiles, a tile each lane
-    uint32_t held = block_scales(p, w.seq(), hk, lane < w.count ? w.s.len : 0, (w.tile + lane) * kTile + 16 * warp);
-    uint32_t ahead = kNoScales;
+    // scales of this warp's two blocks of the first 16 of its tiles, in two lanes each
+    const int first = (tiles ^ odd) & 1;
+    auto scales = [&](int nth) {
+      const int n = first + 2 * (nth + (lane >> 1));
+      return block_scales(p, w.seq(), hk, n < w.count ? w.s.len : 0, (w.tile + n) * kTile + 32 * quarter + 16 * (lane & 1));
+    };
+    uint32_t held = scales(0), ahead = kNoScales;
     // this lane's two rows of a fragment, and the keys they see
     int lo[2], hi[2];
     float fr[2];                 // what a score of the row is multiplied by, K's scale apart
@@ -168,34 +181,47 @@ __global__ void __launch_bounds__(kThreads, 1)
     float mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
     int big = kNoExp;  // R
 
+    int nth = 0;  // of this warp's tiles
     for (int n0 = 0; ok && n0 < w.count; ++n0) {
-      const int t = w.tile + n0;
-      if ((n0 & 31) == 0) {  // the next 32 tiles' scales, long before they are needed
-        if (n0) held = ahead;
-        ahead = block_scales(p, w.seq(), hk, n0 + 32 + lane < w.count ? w.s.len : 0, (t + 32 + lane) * kTile + 16 * warp);
+      if (((tiles + n0) & 1) != odd) {
+        Ring::on(0, kst, kph);
+        Ring::on(1, vst, vph);
+        continue;
       }
-      const uint32_t sc = __shfl_sync(0xffffffffu, held, n0 & 31);
-      const int ek = (int)(sc & 0xffu) - 127, ev = (int)(sc >> 8) - 127;
-      // ---- scores of 16 keys: two products of 8 keys
+      const int t = w.tile + n0;
+      if ((nth & 15) == 0) {  // the next 16 tiles' scales, long before they are needed
+        if (nth) held = ahead;
+        ahead = scales(nth + 16);
+      }
+      int ek[2], ev[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t sc = __shfl_sync(0xffffffffu, held, 2 * (nth & 15) + h);
+        ek[h] = (int)(sc & 0xffu) - 127, ev[h] = (int)(sc >> 8) - 127;
+      }
+      ++nth;
+      // ---- scores of 32 keys: four products of 8 keys
       ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(kst), kph));
       if (!ok) {
         if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
         break;
       }
-      const uint32_t kt = base + kst * F::kTileBytes;
-      float s[2][4];
+      const uint32_t kt = base + kst * F::kTileBytes + 32 * quarter * D;
+      float s[4][4];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
+      for (int n = 0; n < 4; ++n) {
         // two chains of products, so that one's latency hides the other's
         float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-          const uint4 v = lds128(kt + Ring::piece(16 * warp + 8 * n + gq, kPieces * c + j));
+          const uint4 v = lds128(kt + Ring::piece(8 * n + gq, kPieces * c + j));
           const uint32_t *word = &v.x;
 #pragma unroll
-          for (int m = 0; m < 4; ++m)
-            mma16816<__half>(m & 1 ? y : x, q[4 * j + m][0], q[4 * j + m][1], q[4 * j + m][2], q[4 * j + m][3],
-                             halves((uint16_t)word[m]), halves((uint16_t)(word[m] >> 16)));
+          for (int m = 0; m < 4; ++m) {
+            uint32_t b0, b1;
+            halves4(word[m], b0, b1);
+            mma16816<__half>(m & 1 ? y : x, q[4 * j + m][0], q[4 * j + m][1], q[4 * j + m][2], q[4 * j + m][3], b0, b1);
+          }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[n][i] = x[i] + y[i];
@@ -205,24 +231,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       Ring::on(0, kst, kph);
 
       // ---- softmax: s[n][0..1] row g, s[n][2..3] row g + 8, keys 8 n + 2 c and + 1
-      const int key0 = t * kTile + 16 * warp;
-      const bool ends = key0 + 16 > w.s.len;
-      const int most = min(key0 + 16, w.s.len);  // open: some row does not see some of the sequence's keys here
+      const int key0 = t * kTile + 32 * quarter;
+      const bool ends = key0 + 32 > w.s.len;
+      const int most = min(key0 + 32, w.s.len);  // open: some row does not see some of the sequence's keys here
       const bool open = __any_sync(0xffffffffu, lo[0] > key0 || hi[0] < most || lo[1] > key0 || hi[1] < most);
       if (open || ends) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < 4; ++n)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int key = key0 + 8 * n + 2 * c + (j & 1);
             if (key < lo[j >> 1] || key >= hi[j >> 1]) s[n][j] = -INFINITY;
           }
       }
-      float now[2], fs[2];
+      float now[2], fs[2][2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        fs[i] = fminf(fmaxf(fr[i] * pow2(ek), 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
-        now[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1])) * fs[i];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) fs[i][h] = fminf(fmaxf(fr[i] * pow2(ek[h]), 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
+        now[i] = fmaxf(fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1])) * fs[i][0],
+                       fmaxf(fmaxf(s[2][2 * i], s[2][2 * i + 1]), fmaxf(s[3][2 * i], s[3][2 * i + 1])) * fs[i][1]);
         now[i] = fmaxf(now[i], __shfl_xor_sync(0xffffffffu, now[i], 1));
         now[i] = fmaxf(now[i], __shfl_xor_sync(0xffffffffu, now[i], 2));
       }
@@ -241,25 +269,27 @@ __global__ void __launch_bounds__(kThreads, 1)
           o[i][2] *= f[1], o[i][3] *= f[1];
         }
       }
-      uint32_t pr[4];  // the A fragment of the second product
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float neg = mx[i] == -INFINITY ? 0.f : kLift - mx[i];
-          const float p0 = exp2_fast(fmaf(s[n][2 * i], fs[i], neg)), p1 = exp2_fast(fmaf(s[n][2 * i + 1], fs[i], neg));
-          sum[i] += p0 + p1;
-          pr[2 * n + i] = Bits<__half>::pack(p0, p1);
-        }
-      if (ev > big && ev <= 127) {  // a larger block of values (128: none)
-        const float f = big - ev < -126 ? 0.f : pow2(big - ev);
-        big = ev;
+      const int top_v = max(ev[0] <= 127 ? ev[0] : kNoExp, ev[1] <= 127 ? ev[1] : kNoExp);  // (128: no block)
+      if (top_v > big) {  // a larger block of values
+        const float f = big - top_v < -126 ? 0.f : pow2(big - top_v);
+        big = top_v;
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j) o[i][j] *= f;
       }
-      const uint32_t lift = half_pow2(kValueLift + min(ev - big, 0));
+      uint32_t pr[2][4];  // the A fragments of the second product, times their block's scale
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float neg = mx[i] == -INFINITY ? 0.f : kLift - mx[i];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const float f = fs[i][n >> 1];
+          const float p0 = exp2_fast(fmaf(s[n][2 * i], f, neg)), p1 = exp2_fast(fmaf(s[n][2 * i + 1], f, neg));
+          sum[i] += p0 + p1;
+          pr[n >> 1][2 * (n & 1) + i] = mul_halves(Bits<__half>::pack(p0, p1), half_pow2(min(ev[n >> 1] - big, 0)));
+        }
+      }
 
       // ---- o += p V: n-tile i holds channels D / 8 g + i
       ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(vst), vph));
@@ -268,44 +298,47 @@ __global__ void __launch_bounds__(kThreads, 1)
         break;
       }
       bool found = false;
-      const uint32_t vt = base + vst * F::kTileBytes;
-      uint32_t v[4][D / 32];  // of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+      const uint32_t vt = base + vst * F::kTileBytes + 32 * quarter * D;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int key = 2 * c + (j & 1) + 8 * (j >> 1);
-        if (D == 128) {
-          const uint4 x = lds128(vt + Ring::piece(16 * warp + key, gq));
-          v[j][0] = x.x, v[j][1] = x.y, v[j][D / 32 - 2] = x.z, v[j][D / 32 - 1] = x.w;
-        } else {
-          const uint2 x = lds64(vt + Ring::piece(16 * warp + key, gq >> 1) + 8 * (gq & 1));
-          v[j][0] = x.x, v[j][1] = x.y;
-        }
-        if (ends && key0 + key >= w.s.len) {  // what lies behind the sequence's end may be NaN
+      for (int h2 = 0; h2 < 2; ++h2) {
+        uint32_t v[4][D / 32];  // of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of the block
 #pragma unroll
-          for (int i = 0; i < D / 32; ++i) v[j][i] = 0u;
-        }
-        if (open) {
+        for (int j = 0; j < 4; ++j) {
+          const int key = 16 * h2 + 2 * c + (j & 1) + 8 * (j >> 1);
+          if (D == 128) {
+            const uint4 x = lds128(vt + Ring::piece(key, gq));
+            v[j][0] = x.x, v[j][1] = x.y, v[j][D / 32 - 2] = x.z, v[j][D / 32 - 1] = x.w;
+          } else {
+            const uint2 x = lds64(vt + Ring::piece(key, gq >> 1) + 8 * (gq & 1));
+            v[j][0] = x.x, v[j][1] = x.y;
+          }
+          if (ends && key0 + key >= w.s.len) {  // what lies behind the sequence's end may be NaN
 #pragma unroll
-          for (int i = 0; i < D / 32; ++i) found |= clean_codes(v[j][i]);
+            for (int i = 0; i < D / 32; ++i) v[j][i] = 0u;
+          }
+          if (open) {
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) found |= clean_codes(v[j][i]);
+          }
         }
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            // channels 4 i + 2 h and + 1 of a pair of keys: one after the other
+            uint32_t a0, a1, b0, b1;
+            halves4(__byte_perm(v[0][i], v[1][i], h ? 0x7362u : 0x5140u), a0, a1);
+            halves4(__byte_perm(v[2][i], v[3][i], h ? 0x7362u : 0x5140u), b0, b1);
+            mma16816<__half>(o[4 * i + 2 * h], pr[h2][0], pr[h2][1], pr[h2][2], pr[h2][3], a0, b0);
+            mma16816<__half>(o[4 * i + 2 * h + 1], pr[h2][0], pr[h2][1], pr[h2][2], pr[h2][3], a1, b1);
+          }
       }
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          // channels 4 i + 2 h and + 1 of a pair of keys: one after the other
-          const uint32_t a = __byte_perm(v[0][i], v[1][i], h ? 0x7362u : 0x5140u);
-          const uint32_t b = __byte_perm(v[2][i], v[3][i], h ? 0x7362u : 0x5140u);
-          mma16816<__half>(o[4 * i + 2 * h], pr[0], pr[1], pr[2], pr[3], mul_halves(halves((uint16_t)a), lift),
-                           mul_halves(halves((uint16_t)b), lift));
-          mma16816<__half>(o[4 * i + 2 * h + 1], pr[0], pr[1], pr[2], pr[3], mul_halves(halves((uint16_t)(a >> 16)), lift),
-                           mul_halves(halves((uint16_t)(b >> 16)), lift));
-        }
       if (found) bad = 1;  // (any thread's word will do)
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(ring.empty(vst));
       Ring::on(1, vst, vph);
     }
+    tiles += w.count;
 
     // ------------------------------------------------------------------ the piece's result
     // (mx - kLift: what the probabilities were taken against)
@@ -335,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float m, l;
       row_total(gq + 8 * i, m, l);
       const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-      f[i] = (mx[i] == -INFINITY ? 0.f : exp2_fast(mx[i] - m)) * inv * (1.f / (1 << kValueLift));
+      f[i] = (mx[i] == -INFINITY ? 0.f : exp2_fast(mx[i] - m)) * inv;
     }
     const int part = 2 * blockIdx.x + (w.starts ? 1 : 0);
     for (int r0 = 0; r0 < rows; r0 += kPass) {
@@ -406,10 +439,10 @@ cudaError_t launch_few8_t(const CUtensorMap &mk, const CUtensorMap &mv, const At
     if (err != cudaSuccess) return err;
     g_few8_smem_set[dev & 63].fetch_or(1 << variant);
   }
-  err = launch_kernel(k_attend8_few<T, D>, dim3(p.a.ctas), dim3(kThreads), Few8<D>::kSmem, st, false, mk, mv, p);
+  err = launch_kernel(k_attend8_few<T, D>, dim3(p.a.ctas), dim3(kAllThreads), Few8<D>::kSmem, st, false, mk, mv, p);
   if (err != cudaSuccess) return err;
   const long long rows = (long long)p.a.c.total_new * p.a.q_heads;
-  return launch_kernel(k_few_join<T, true>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, true, p.a);
+  return launch_kernel(k_few_join<T, true, kItemCost>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, true, p.a);
 }
 
 }  // namespace

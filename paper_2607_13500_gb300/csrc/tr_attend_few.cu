@@ -74,9 +74,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   pdl_wait();  // q and the cache come from the kernels before
   pdl_trigger();
   __syncthreads();  // the barriers are ready
-  Walk w;
+  Walk<kFewItemCost> w;
   Seq run0;
-  const Shares shares(count_units(g, runs, kWarps + 2, run0), g.ctas);
+  const Shares shares(count_units<kFewItemCost>(g, runs, kWarps + 2, run0), g.ctas);
   const int share = shares.start(blockIdx.x), share_end = shares.start(blockIdx.x + 1);
   if (share >= share_end) return;
   if (threadIdx.x == 0) share0 = share, share_units = share_end - share;  // for the consumers' second walk
@@ -354,7 +354,7 @@ cudaError_t launch_few_t(const CUtensorMap &mk, const CUtensorMap &mv, const Att
   err = launch_kernel(k_attend_few<T, D>, dim3(g.ctas), dim3(kThreads), Few<D>::kSmem, st, false, mk, mv, g);
   if (err != cudaSuccess) return err;
   const long long rows = (long long)g.c.total_new * g.q_heads;
-  return launch_kernel(k_few_join<T, false>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, true, g);
+  return launch_kernel(k_few_join<T, false, kFewItemCost>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, true, g);
 }
 
 }  // namespace

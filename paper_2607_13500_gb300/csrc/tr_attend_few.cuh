@@ -41,10 +41,12 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs &g, int b) {
   return s;
 }
 // An item counts kExtra units before its tiles', the time that taking it up
-// and finishing it cost (about 3 us against 1.3 us a tile): without them the
-// shares that hold many short items end last.
-constexpr int kExtra = kFewItemCost;
-__device__ __forceinline__ int units_of(const Seq &s) { return s.tiles > 0 ? s.items * (s.tiles + kExtra) : 0; }
+// and finishing it cost (in 16 bits about 3 us against 1.3 us a tile): without
+// them the shares that hold many short items end last.
+template <int kExtra>
+__device__ __forceinline__ int units_of(const Seq &s) {
+  return s.tiles > 0 ? s.items * (s.tiles + kExtra) : 0;
+}
 
 // Share c of `all` units over `ctas` CTAs: the first all % ctas shares are
 // one unit longer.
@@ -73,13 +75,14 @@ __device__ __forceinline__ Seq seq_from(const Seq &mine, int lane) {
 
 // Total units, and `mine` = this lane's sequence of the first run.  With more
 // than one run their units are left in shared memory by all warps together.
+template <int kExtra>
 __device__ __forceinline__ int count_units(const AttendArgs &g, int *runs, int warps, Seq &mine) {
   const int lane = threadIdx.x & 31;
   const int n = (g.c.batch + 31) / 32;
   mine = seq_of(g, lane);
-  if (n <= 1) return (int)__reduce_add_sync(0xffffffffu, (unsigned)units_of(mine));
+  if (n <= 1) return (int)__reduce_add_sync(0xffffffffu, (unsigned)units_of<kExtra>(mine));
   for (int i = threadIdx.x >> 5; i < n; i += warps) {
-    const int u = (int)__reduce_add_sync(0xffffffffu, (unsigned)units_of(seq_of(g, 32 * i + lane)));
+    const int u = (int)__reduce_add_sync(0xffffffffu, (unsigned)units_of<kExtra>(seq_of(g, 32 * i + lane)));
     if (lane == 0) runs[i] = u;
   }
   __syncthreads();
@@ -90,6 +93,7 @@ __device__ __forceinline__ int count_units(const AttendArgs &g, int *runs, int w
 
 // A walk over the units of a share, item by item; the same in all lanes
 // (but `mine`).
+template <int kExtra>
 struct Walk {
   int u, end;  // next unit, end of the share
   int first;   // first unit of the sequence
@@ -113,7 +117,7 @@ struct Walk {
       while (run + 1 < n && u >= first + runs[run]) first += runs[run++];
       if (run) mine = seq_of(g, 32 * run + lane);
     }
-    const int own = units_of(mine);
+    const int own = units_of<kExtra>(mine);
     int before = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -127,12 +131,12 @@ struct Walk {
   // The next piece; false at the end of the share.
   __device__ __forceinline__ bool next(const AttendArgs &g) {
     while (u < end) {
-      if (u >= first + units_of(s)) {  // on to the next sequence that has units
-        first += units_of(s);
-        unsigned any = __ballot_sync(0xffffffffu, units_of(mine) > 0) & ~(at == 31 ? 0xffffffffu : (2u << at) - 1u);
+      if (u >= first + units_of<kExtra>(s)) {  // on to the next sequence that has units
+        first += units_of<kExtra>(s);
+        unsigned any = __ballot_sync(0xffffffffu, units_of<kExtra>(mine) > 0) & ~(at == 31 ? 0xffffffffu : (2u << at) - 1u);
         while (!any && 32 * (run + 1) < g.c.batch) {
           mine = seq_of(g, 32 * ++run + (threadIdx.x & 31));
-          any = __ballot_sync(0xffffffffu, units_of(mine) > 0);
+          any = __ballot_sync(0xffffffffu, units_of<kExtra>(mine) > 0);
         }
         if (!any) return false;
         at = __ffs(any) - 1;
@@ -177,8 +181,8 @@ __device__ __forceinline__ void named_sync(int threads) { asm volatile("bar.sync
 
 // Four channels of row r of the piece: into the output, or into its share's
 // partial result.  NORMED: v is divided by l already.
-template <typename T, bool NORMED = false>
-__device__ __forceinline__ void put_row(const AttendArgs &g, const Walk &w, int part, int block0, int hk, int r, int ch,
+template <typename T, bool NORMED = false, int kExtra>
+__device__ __forceinline__ void put_row(const AttendArgs &g, const Walk<kExtra> &w, int part, int block0, int hk, int r, int ch,
                                         const float4 &v, float m, float l) {
   if (w.whole) {
     const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
@@ -196,12 +200,12 @@ __device__ __forceinline__ void put_row(const AttendArgs &g, const Walk &w, int 
 // Joins the pieces of the items that several shares cover, one warp per row,
 // in the shares' order; rows of sequences without a visible tile get zeros.
 // NORMED: the pieces' values are divided by their sums.
-template <typename T, bool NORMED>
+template <typename T, bool NORMED, int kExtra>
 __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ AttendArgs g) {
   __shared__ int runs[kFewMaxBatch / 32];
   const int lane = threadIdx.x & 31;
   Seq run0;
-  const Shares shares(count_units(g, runs, 8, run0), g.ctas);  // reads nothing that k_attend_few writes
+  const Shares shares(count_units<kExtra>(g, runs, 8, run0), g.ctas);  // reads nothing that k_attend_few writes
   const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= (long long)g.c.total_new * g.q_heads) {
     pdl_wait();
@@ -216,7 +220,7 @@ __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ Attend
   Seq s = seq_from(mine, b & 31);
   if (b < 0) s.tiles = 0;
   if (s.tiles > 0) {
-    unsigned x = lane < b % 32 ? units_of(mine) : 0;
+    unsigned x = lane < b % 32 ? units_of<kExtra>(mine) : 0;
     for (int i = lane; i < b / 32; i += 32) x += runs[i];
     const int local = (t - s.tok0) * g.group + h % g.group, r = local % kFewRows;
     const int u0 = (int)__reduce_add_sync(0xffffffffu, x) + (local / kFewRows * g.c.heads + h / g.group) * (s.tiles + kExtra) + kExtra;

@@ -32,6 +32,12 @@ __device__ __forceinline__ uint32_t halves(uint16_t codes) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(codes));
   return r;
 }
+// The same of four.
+__device__ __forceinline__ void halves4(uint32_t codes, uint32_t &lo, uint32_t &hi) {
+  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(codes));
+}
 // Two values to their nearest codes, the low byte first.
 __device__ __forceinline__ uint16_t codes_of(float lo, float hi) {
   uint16_t r;
