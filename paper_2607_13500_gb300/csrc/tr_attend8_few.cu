@@ -126,7 +126,9 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       const int n = first + 2 * (nth + (lane >> 1));
       return block_scales(p, w.seq(), hk, n < w.count ? w.s.len : 0, (w.tile + n) * kTile + 32 * quarter + 16 * (lane & 1));
     };
-    uint32_t held = scales(0), ahead = kNoScales;
+    uint32_t ahead = scales(0);
+    float held_k = 1.f;   // 2^e of keys
+    int held_v = kNoExp;  // e of values
     // this lane's two rows of a fragment, and the keys they see
     int lo[2], hi[2];
     float fr[2];                 // what a score of the row is multiplied by, K's scale apart
@@ -190,14 +192,16 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       }
       const int t = w.tile + n0;
       if ((nth & 15) == 0) {  // the next 16 tiles' scales, long before they are needed
-        if (nth) held = ahead;
+        held_k = pow2((int)(ahead & 0xffu) - 127);
+        held_v = ahead >> 8 < 255u ? (int)(ahead >> 8) - 127 : kNoExp;
         ahead = scales(nth + 16);
       }
-      int ek[2], ev[2];
+      float fk[2];
+      int ev[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t sc = __shfl_sync(0xffffffffu, held, 2 * (nth & 15) + h);
-        ek[h] = (int)(sc & 0xffu) - 127, ev[h] = (int)(sc >> 8) - 127;
+        fk[h] = __shfl_sync(0xffffffffu, held_k, 2 * (nth & 15) + h);
+        ev[h] = __shfl_sync(0xffffffffu, held_v, 2 * (nth & 15) + h);
       }
       ++nth;
       // ---- scores of 32 keys: four products of 8 keys
@@ -230,6 +234,31 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       if (lane == 0) tc::mbar_arrive(ring.empty(kst));
       Ring::on(0, kst, kph);
 
+      // ---- the values' codes: of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of each block
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(vst), vph));
+      if (!ok) {
+        if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+        break;
+      }
+      const uint32_t vt = base + vst * F::kTileBytes + 32 * quarter * D;
+      uint32_t v[2][4][D / 32];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = 16 * h + 2 * c + (j & 1) + 8 * (j >> 1);
+          if (D == 128) {
+            const uint4 x = lds128(vt + Ring::piece(key, gq));
+            v[h][j][0] = x.x, v[h][j][1] = x.y, v[h][j][D / 32 - 2] = x.z, v[h][j][D / 32 - 1] = x.w;
+          } else {
+            const uint2 x = lds64(vt + Ring::piece(key, gq >> 1) + 8 * (gq & 1));
+            v[h][j][0] = x.x, v[h][j][1] = x.y;
+          }
+        }
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(ring.empty(vst));
+      Ring::on(1, vst, vph);
+
       // ---- softmax: s[n][0..1] row g, s[n][2..3] row g + 8, keys 8 n + 2 c and + 1
       const int key0 = t * kTile + 32 * quarter;
       const bool ends = key0 + 32 > w.s.len;
@@ -243,12 +272,25 @@ __global__ void __launch_bounds__(kAllThreads, 1)
             const int key = key0 + 8 * n + 2 * c + (j & 1);
             if (key < lo[j >> 1] || key >= hi[j >> 1]) s[n][j] = -INFINITY;
           }
+        bool found = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const bool behind = key0 + 16 * h + 2 * c + (j & 1) + 8 * (j >> 1) >= w.s.len;  // it may be NaN there
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+              if (behind) v[h][j][i] = 0u;
+              if (open) found |= clean_codes(v[h][j][i]);
+            }
+          }
+        if (found) bad = 1;  // (any thread's word will do)
       }
       float now[2], fs[2][2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) fs[i][h] = fminf(fmaxf(fr[i] * pow2(ek[h]), 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
+        for (int h = 0; h < 2; ++h) fs[i][h] = fminf(fmaxf(fr[i] * fk[h], 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
         now[i] = fmaxf(fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1])) * fs[i][0],
                        fmaxf(fmaxf(s[2][2 * i], s[2][2 * i + 1]), fmaxf(s[3][2 * i], s[3][2 * i + 1])) * fs[i][1]);
         now[i] = fmaxf(now[i], __shfl_xor_sync(0xffffffffu, now[i], 1));
@@ -269,7 +311,7 @@ __global__ void __launch_bounds__(kAllThreads, 1)
           o[i][2] *= f[1], o[i][3] *= f[1];
         }
       }
-      const int top_v = max(ev[0] <= 127 ? ev[0] : kNoExp, ev[1] <= 127 ? ev[1] : kNoExp);  // (128: no block)
+      const int top_v = max(ev[0], ev[1]);
       if (top_v > big) {  // a larger block of values
         const float f = big - top_v < -126 ? 0.f : pow2(big - top_v);
         big = top_v;
@@ -292,51 +334,19 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       }
 
       // ---- o += p V: n-tile i holds channels D / 8 g + i
-      ok = __all_sync(0xffffffffu, tc::mbar_wait(ring.full(vst), vph));
-      if (!ok) {
-        if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
-        break;
-      }
-      bool found = false;
-      const uint32_t vt = base + vst * F::kTileBytes + 32 * quarter * D;
 #pragma unroll
-      for (int h2 = 0; h2 < 2; ++h2) {
-        uint32_t v[4][D / 32];  // of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of the block
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int key = 16 * h2 + 2 * c + (j & 1) + 8 * (j >> 1);
-          if (D == 128) {
-            const uint4 x = lds128(vt + Ring::piece(key, gq));
-            v[j][0] = x.x, v[j][1] = x.y, v[j][D / 32 - 2] = x.z, v[j][D / 32 - 1] = x.w;
-          } else {
-            const uint2 x = lds64(vt + Ring::piece(key, gq >> 1) + 8 * (gq & 1));
-            v[j][0] = x.x, v[j][1] = x.y;
-          }
-          if (ends && key0 + key >= w.s.len) {  // what lies behind the sequence's end may be NaN
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) v[j][i] = 0u;
-          }
-          if (open) {
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) found |= clean_codes(v[j][i]);
-          }
-        }
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            // channels 4 i + 2 h and + 1 of a pair of keys: one after the other
+          for (int j = 0; j < 2; ++j) {
+            // channels 4 i + 2 j and + 1 of a pair of keys: one after the other
             uint32_t a0, a1, b0, b1;
-            halves4(__byte_perm(v[0][i], v[1][i], h ? 0x7362u : 0x5140u), a0, a1);
-            halves4(__byte_perm(v[2][i], v[3][i], h ? 0x7362u : 0x5140u), b0, b1);
-            mma16816<__half>(o[4 * i + 2 * h], pr[h2][0], pr[h2][1], pr[h2][2], pr[h2][3], a0, b0);
-            mma16816<__half>(o[4 * i + 2 * h + 1], pr[h2][0], pr[h2][1], pr[h2][2], pr[h2][3], a1, b1);
+            halves4(__byte_perm(v[h][0][i], v[h][1][i], j ? 0x7362u : 0x5140u), a0, a1);
+            halves4(__byte_perm(v[h][2][i], v[h][3][i], j ? 0x7362u : 0x5140u), b0, b1);
+            mma16816<__half>(o[4 * i + 2 * j], pr[h][0], pr[h][1], pr[h][2], pr[h][3], a0, b0);
+            mma16816<__half>(o[4 * i + 2 * j + 1], pr[h][0], pr[h][1], pr[h][2], pr[h][3], a1, b1);
           }
-      }
-      if (found) bad = 1;  // (any thread's word will do)
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(ring.empty(vst));
-      Ring::on(1, vst, vph);
     }
     tiles += w.count;
 
