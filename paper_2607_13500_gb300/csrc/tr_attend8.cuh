@@ -142,12 +142,14 @@ struct CodeRing {
 // The scales of key block j / 16 of the sequence, as held: keys' (low byte) and
 // values'; kNoScales where there is no such block (its keys read as zeros).
 constexpr uint32_t kNoScales = 0xff7fu;
+__device__ __forceinline__ uint32_t scales_at(const Attend8Args &p, long long i) {
+  return (uint32_t)min((int)__ldg(p.scale.k + i), 254) | (uint32_t)min((int)__ldg(p.scale.v + i), 254) << 8;
+}
 __device__ __forceinline__ uint32_t block_scales(const Attend8Args &p, int seq, int hk, int len, int j) {
   const AttendArgs &g = p.a;
-  const int page = j < len ? page_of(g.c, seq, j) : -1;
-  if (page < 0) return kNoScales;
-  const long long i = scale_at(g.c, page, hk, j & (g.c.page - 1));
-  return (uint32_t)min((int)__ldg(p.scale.k + i), 254) | (uint32_t)min((int)__ldg(p.scale.v + i), 254) << 8;
+  const int i = j >> g.page_log2;
+  const int page = j < len && i < g.c.max_pages ? __ldg(g.c.table + (long long)seq * g.c.max_pages + i) : -1;
+  return (unsigned)page < (unsigned)g.c.pages ? scales_at(p, scale_at(g.c, page, hk, j & (g.c.page - 1))) : kNoScales;
 }
 
 // A query's numbers as halves: fp16 as they are; bf16 times a power of two
@@ -164,7 +166,7 @@ __device__ __forceinline__ uint32_t top_of_pair(uint32_t bf16x2) {
   return max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u);
 }
 
-constexpr int kItemCost = 3;  // few rows: an item's own cost in tiles (see units_of)
+constexpr int kItemCost = 5;  // few rows: an item's own cost in tiles (see units_of)
 // Few rows (tr_attend8_few.cu): the launch (work and join kernels).
 cudaError_t launch_few8(const CUtensorMap &mk, const CUtensorMap &mv, Attend8Args p, bool bf16, void *ws, cudaStream_t st);
 

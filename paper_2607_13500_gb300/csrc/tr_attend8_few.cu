@@ -29,8 +29,9 @@ constexpr int kAllThreads = 32 * (kWarps + 4);  // consumers, the producers of K
 template <int D>
 struct Few8 {
   static constexpr int kTileBytes = kTile * D;
-  static constexpr int kJoinRow = D + 4;  // floats
-  static constexpr int kJoinBytes = kWarps * kPass * kJoinRow * 4;
+  // Rows joined at a time, each quarter of a row 4 floats on, so that a phase's stores lie in different banks.
+  static constexpr int kRows = 8, kJoinRow = D + 16;
+  static constexpr int kJoinBytes = kWarps * kRows * kJoinRow * 4;
   static constexpr int kFit = (227 * 1024 - 4096 - 1024 - kJoinBytes) / kTileBytes;
   static constexpr int kStages = kFit < 16 ? kFit : 16;
   static constexpr size_t kSmem = (size_t)kStages * kTileBytes + kJoinBytes + 1024 + 4096;
@@ -54,12 +55,13 @@ __global__ void __launch_bounds__(kAllThreads, 1)
   const AttendArgs &g = p.a;
   extern __shared__ unsigned char smem_raw[];
   __shared__ int runs[kFewMaxBatch / 32];  // units of 32 sequences each
-  __shared__ float top[kWarps][kFewRows], tot[kWarps][kFewRows];
+  __shared__ float tops[2][kWarps][kFewRows], tots[2][kWarps][kFewRows];  // (two: of a piece and the next one)
   __shared__ int bad, share0, share_units;  // bad: values were taken out of a tile
   const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
   float *join = reinterpret_cast<float *>(smem_raw + (base - tc::smem_u32(smem_raw)) + F::kStages * F::kTileBytes);
   const uint32_t bars = tc::smem_u32(join) + F::kJoinBytes;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // (the warp's index by shuffle: the compiler then knows it to be uniform)
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
   Ring ring;
   ring.base = base, ring.full0 = bars, ring.empty0 = bars + 8u * F::kStages;
@@ -117,16 +119,49 @@ __global__ void __launch_bounds__(kAllThreads, 1)
   uint32_t kph = 0, vph = 0;
   int tiles = 0;   // of the share so far
   bool ok = true;  // once a wait has timed out the warp only keeps up with the others' barriers
-  while (w.next(g)) {
-    const int hk = w.item % g.c.heads, block0 = w.item / g.c.heads * kFewRows;
-    const int rows = min(kFewRows, w.s.rows - block0);
+  // What the present piece is, and what the next one needs from memory, asked
+  // for before the present one's results are joined.
+  struct Piece {
+    int hk, block0, rows, tok0, base, len, seq, tile, count;
+    bool whole, starts;
+  } now;
+  uint32_t raw[2][kPieces * 8];  // this lane's channels of its two rows
+  int page0;                     // page of the first block that it holds the scales of
+  auto key_of = [&](const Piece &x, int nth) {  // the block of this warp's nth tile (and the 15 on) that the lane holds
+    const int n = ((tiles ^ odd) & 1) + 2 * (nth + (lane >> 1));
+    return n < x.count ? (x.tile + n) * kTile + 32 * quarter + 16 * (lane & 1) : x.len;
+  };
+  auto ask = [&](Piece &x) {
+    if (!w.next(g)) return false;
+    x.hk = w.item % g.c.heads, x.block0 = w.item / g.c.heads * kFewRows;
+    x.rows = min(kFewRows, w.s.rows - x.block0);
+    x.tok0 = w.s.tok0, x.base = w.s.base, x.len = w.s.len, x.seq = w.seq();
+    x.tile = w.tile, x.count = w.count, x.whole = w.whole, x.starts = w.starts;
+    const int j = key_of(x, 0);
+    page0 = j < x.len && (j >> g.page_log2) < g.c.max_pages ? __ldg(g.c.table + (long long)x.seq * g.c.max_pages + (j >> g.page_log2)) : -1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = gq + 8 * i, row = x.block0 + r;
+      const bool valid = r < x.rows;
+      const int tok = valid ? row / g.group : 0, head = x.hk * g.group + (valid ? row - tok * g.group : 0);
+      const char *qrow = g.q + 2 * ((long long)(x.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
+#pragma unroll
+      for (int s = 0; s < 2 * kPieces; ++s) {
+        const int ch = kPieces * c * 16 + 8 * s;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (valid && ch < g.c.d) v = *reinterpret_cast<const uint4 *>(qrow + 2 * ch);
+        raw[i][4 * s] = v.x, raw[i][4 * s + 1] = v.y, raw[i][4 * s + 2] = v.z, raw[i][4 * s + 3] = v.w;
+      }
+    }
+    return true;
+  };
+  int turn = 0;  // of the pieces
+  for (bool more = ask(now); more; turn ^= 1) {
     // scales of this warp's two blocks of the first 16 of its tiles, in two lanes each
-    const int first = (tiles ^ odd) & 1;
-    auto scales = [&](int nth) {
-      const int n = first + 2 * (nth + (lane >> 1));
-      return block_scales(p, w.seq(), hk, n < w.count ? w.s.len : 0, (w.tile + n) * kTile + 32 * quarter + 16 * (lane & 1));
-    };
-    uint32_t ahead = scales(0);
+    auto scales = [&](int nth) { return block_scales(p, now.seq, now.hk, now.len, key_of(now, nth)); };
+    uint32_t ahead = kNoScales;
+    if ((unsigned)page0 < (unsigned)g.c.pages)
+      ahead = scales_at(p, scale_at(g.c, page0, now.hk, key_of(now, 0) & (g.c.page - 1)));
     float held_k = 1.f;   // 2^e of keys
     int held_v = kNoExp;  // e of values
     // this lane's two rows of a fragment, and the keys they see
@@ -135,30 +170,17 @@ __global__ void __launch_bounds__(kAllThreads, 1)
     uint32_t q[kPieces * 4][4];  // fragments of the first product: channels 4 m .. 4 m + 3 of a piece
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int r = gq + 8 * i, row = block0 + r;
-      const bool valid = r < rows;
-      const int tok = valid ? row / g.group : 0, head = hk * g.group + (valid ? row - tok * g.group : 0);
-      const int own = w.s.base + tok;
-      hi[i] = !valid ? INT_MAX : g.causal ? min(w.s.len, own + 1) : w.s.len;
+      const int r = gq + 8 * i;
+      const bool valid = r < now.rows;
+      const int own = now.base + (valid ? (now.block0 + r) / g.group : 0);
+      hi[i] = !valid ? INT_MAX : g.causal ? min(now.len, own + 1) : now.len;
       lo[i] = valid && g.window > 0 ? window_start(own, g.window) : 0;
-      const char *qrow = g.q + 2 * ((long long)(w.s.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
-      uint32_t x[kPieces][8], most = 0u;
-#pragma unroll
-      for (int s = 0; s < kPieces; ++s) {
-        const int ch = (kPieces * c + s) * 16;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (valid && ch < g.c.d) v = *reinterpret_cast<const uint4 *>(qrow + 2 * ch + 16 * h);
-          x[s][4 * h] = v.x, x[s][4 * h + 1] = v.y, x[s][4 * h + 2] = v.z, x[s][4 * h + 3] = v.w;
-        }
-        if (Bits<T>::kBf16)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) most = max(most, top_of_pair(x[s][k]));
-      }
       fr[i] = g.scale;
       float down = 1.f;
       if (Bits<T>::kBf16) {
+        uint32_t most = 0u;
+#pragma unroll
+        for (int k = 0; k < 8 * kPieces; ++k) most = max(most, top_of_pair(raw[i][k]));
         most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
         most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
         const int e = query_exp(most);
@@ -167,13 +189,11 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       }
       const uint32_t flip = g.negate ? 0x80008000u : 0u;
 #pragma unroll
-      for (int s = 0; s < kPieces; ++s)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          // a0, a2: the row g's first and second pair; a1, a3: row g + 8's
-          q[4 * s + m][i] = (Bits<T>::kBf16 ? query_pair(x[s][2 * m], down) : x[s][2 * m]) ^ flip;
-          q[4 * s + m][2 + i] = (Bits<T>::kBf16 ? query_pair(x[s][2 * m + 1], down) : x[s][2 * m + 1]) ^ flip;
-        }
+      for (int m = 0; m < 4 * kPieces; ++m) {
+        // a0, a2: the row g's first and second pair; a1, a3: row g + 8's
+        q[m][i] = (Bits<T>::kBf16 ? query_pair(raw[i][2 * m], down) : raw[i][2 * m]) ^ flip;
+        q[m][2 + i] = (Bits<T>::kBf16 ? query_pair(raw[i][2 * m + 1], down) : raw[i][2 * m + 1]) ^ flip;
+      }
     }
     float o[kTiles][4];
 #pragma unroll
@@ -184,13 +204,13 @@ __global__ void __launch_bounds__(kAllThreads, 1)
     int big = kNoExp;  // R
 
     int nth = 0;  // of this warp's tiles
-    for (int n0 = 0; ok && n0 < w.count; ++n0) {
+    for (int n0 = 0; ok && n0 < now.count; ++n0) {
       if (((tiles + n0) & 1) != odd) {
         Ring::on(0, kst, kph);
         Ring::on(1, vst, vph);
         continue;
       }
-      const int t = w.tile + n0;
+      const int t = now.tile + n0;
       if ((nth & 15) == 0) {  // the next 16 tiles' scales, long before they are needed
         held_k = pow2((int)(ahead & 0xffu) - 127);
         held_v = ahead >> 8 < 255u ? (int)(ahead >> 8) - 127 : kNoExp;
@@ -214,8 +234,8 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       float s[4][4];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
-        // two chains of products, so that one's latency hides the other's
-        float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
           const uint4 v = lds128(kt + Ring::piece(8 * n + gq, kPieces * c + j));
@@ -224,11 +244,9 @@ __global__ void __launch_bounds__(kAllThreads, 1)
           for (int m = 0; m < 4; ++m) {
             uint32_t b0, b1;
             halves4(word[m], b0, b1);
-            mma16816<__half>(m & 1 ? y : x, q[4 * j + m][0], q[4 * j + m][1], q[4 * j + m][2], q[4 * j + m][3], b0, b1);
+            mma16816<__half>(s[n], q[4 * j + m][0], q[4 * j + m][1], q[4 * j + m][2], q[4 * j + m][3], b0, b1);
           }
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[n][i] = x[i] + y[i];
       }
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(ring.empty(kst));
@@ -261,8 +279,8 @@ __global__ void __launch_bounds__(kAllThreads, 1)
 
       // ---- softmax: s[n][0..1] row g, s[n][2..3] row g + 8, keys 8 n + 2 c and + 1
       const int key0 = t * kTile + 32 * quarter;
-      const bool ends = key0 + 32 > w.s.len;
-      const int most = min(key0 + 32, w.s.len);  // open: some row does not see some of the sequence's keys here
+      const bool ends = key0 + 32 > now.len;
+      const int most = min(key0 + 32, now.len);  // open: some row does not see some of the sequence's keys here
       const bool open = __any_sync(0xffffffffu, lo[0] > key0 || hi[0] < most || lo[1] > key0 || hi[1] < most);
       if (open || ends) {
 #pragma unroll
@@ -277,7 +295,7 @@ __global__ void __launch_bounds__(kAllThreads, 1)
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const bool behind = key0 + 16 * h + 2 * c + (j & 1) + 8 * (j >> 1) >= w.s.len;  // it may be NaN there
+            const bool behind = key0 + 16 * h + 2 * c + (j & 1) + 8 * (j >> 1) >= now.len;  // it may be NaN there
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
               if (behind) v[h][j][i] = 0u;
@@ -286,23 +304,23 @@ __global__ void __launch_bounds__(kAllThreads, 1)
           }
         if (found) bad = 1;  // (any thread's word will do)
       }
-      float now[2], fs[2][2];
+      float most_s[2], fs[2][2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) fs[i][h] = fminf(fmaxf(fr[i] * fk[h], 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
-        now[i] = fmaxf(fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1])) * fs[i][0],
+        most_s[i] = fmaxf(fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1])) * fs[i][0],
                        fmaxf(fmaxf(s[2][2 * i], s[2][2 * i + 1]), fmaxf(s[3][2 * i], s[3][2 * i + 1])) * fs[i][1]);
-        now[i] = fmaxf(now[i], __shfl_xor_sync(0xffffffffu, now[i], 1));
-        now[i] = fmaxf(now[i], __shfl_xor_sync(0xffffffffu, now[i], 2));
+        most_s[i] = fmaxf(most_s[i], __shfl_xor_sync(0xffffffffu, most_s[i], 1));
+        most_s[i] = fmaxf(most_s[i], __shfl_xor_sync(0xffffffffu, most_s[i], 2));
       }
-      if (__any_sync(0xffffffffu, now[0] > mx[0] + 8.f || now[1] > mx[1] + 8.f)) {
+      if (__any_sync(0xffffffffu, most_s[0] > mx[0] + 8.f || most_s[1] > mx[1] + 8.f)) {
         float f[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const bool up = now[i] > mx[i] + 8.f;
-          f[i] = up ? exp2_fast(mx[i] - now[i]) : 1.f;
-          if (up) mx[i] = now[i];
+          const bool up = most_s[i] > mx[i] + 8.f;
+          f[i] = up ? exp2_fast(mx[i] - most_s[i]) : 1.f;
+          if (up) mx[i] = most_s[i];
           sum[i] *= f[i];
         }
 #pragma unroll
@@ -348,10 +366,12 @@ __global__ void __launch_bounds__(kAllThreads, 1)
             mma16816<__half>(o[4 * i + 2 * j + 1], pr[h][0], pr[h][1], pr[h][2], pr[h][3], a1, b1);
           }
     }
-    tiles += w.count;
-
     // ------------------------------------------------------------------ the piece's result
+    const Piece done = now;
+    tiles += done.count;
+    more = ask(now);
     // (mx - kLift: what the probabilities were taken against)
+    float(&top)[kWarps][kFewRows] = tops[turn], (&tot)[kWarps][kFewRows] = tots[turn];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
@@ -359,7 +379,7 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       mx[i] -= kLift;
       if (c == 0) top[warp][gq + 8 * i] = mx[i], tot[warp][gq + 8 * i] = sum[i];
     }
-    named_sync(32 * kWarps);
+    named_sync(32 * kWarps);  // (and the last piece's results are read)
     // The row's maximum and sum over the warps.  (A maximum passes over NaN
     // scores, so a warp that saw no other has the maximum of one that saw
     // nothing: its sum, 0 or NaN, enters as it is.)
@@ -370,49 +390,38 @@ __global__ void __launch_bounds__(kAllThreads, 1)
 #pragma unroll
       for (int j = 0; j < kWarps; ++j) l += top[j][r] == -INFINITY ? tot[j][r] : tot[j][r] * exp2_fast(top[j][r] - m);
     };
-    // Sums are divided by the row's total before V's scale, up to 2^127, enters.
-    float f[2];
     const float up = big == kNoExp ? 0.f : pow2(big);
+    const int part = 2 * blockIdx.x + (done.starts ? 1 : 0);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+      const int r0 = 8 * i;
+      if (r0 >= done.rows) break;
+      if (i) named_sync(32 * kWarps);
+      // Sums are divided by the row's total before V's scale, up to 2^127, enters.
       float m, l;
-      row_total(gq + 8 * i, m, l);
-      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-      f[i] = (mx[i] == -INFINITY ? 0.f : exp2_fast(mx[i] - m)) * inv;
-    }
-    const int part = 2 * blockIdx.x + (w.starts ? 1 : 0);
-    for (int r0 = 0; r0 < rows; r0 += kPass) {
-      // accumulator column 2 c + (j & 1) of n-tile i is channel D / 8 (2 c + (j & 1)) + i
-      const int mine = gq - (r0 & 7);  // row of the pass that this quad holds (of its rows g or g + 8)
-      if (mine >= 0 && mine < kPass) {
-        float *dst = join + (warp * kPass + mine) * F::kJoinRow + 2 * kTiles * c;
+      row_total(gq + r0, m, l);
+      const float f = (mx[i] == -INFINITY ? 0.f : exp2_fast(mx[i] - m)) * (l > 0.f || l != l ? 1.f / l : 0.f);
+      // accumulator column 2 c + (j & 1) of n-tile k is channel D / 8 (2 c + (j & 1)) + k
+      float *dst = join + (warp * F::kRows + gq) * F::kJoinRow + (2 * kTiles + 4) * c;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int i = 0; i < kTiles; i += 4) {
-            float4 v;
-            if (r0 < 8)
-              v = make_float4(o[i][b] * f[0] * up, o[i + 1][b] * f[0] * up, o[i + 2][b] * f[0] * up, o[i + 3][b] * f[0] * up);
-            else
-              v = make_float4(o[i][2 + b] * f[1] * up, o[i + 1][2 + b] * f[1] * up, o[i + 2][2 + b] * f[1] * up,
-                              o[i + 3][2 + b] * f[1] * up);
-            *reinterpret_cast<float4 *>(dst + kTiles * b + i) = v;
-          }
-      }
+        for (int k = 0; k < kTiles; k += 4)
+          *reinterpret_cast<float4 *>(dst + kTiles * b + k) =
+              make_float4(o[k][2 * i + b] * f * up, o[k + 1][2 * i + b] * f * up, o[k + 2][2 * i + b] * f * up,
+                          o[k + 3][2 * i + b] * f * up);
       named_sync(32 * kWarps);
       const int r = r0 + (int)threadIdx.x / (D / 4), ch = (int)threadIdx.x % (D / 4) * 4;
-      if ((int)threadIdx.x < kPass * (D / 4) && r < rows && ch < g.c.d) {
+      if ((int)threadIdx.x < F::kRows * (D / 4) && r < done.rows && ch < g.c.d) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int j = 0; j < kWarps; ++j) {
-          const float4 x = *reinterpret_cast<const float4 *>(join + (j * kPass + r - r0) * F::kJoinRow + ch);
+          const float4 x = *reinterpret_cast<const float4 *>(join + (j * F::kRows + r - r0) * F::kJoinRow + ch + ch / (D / 4) * 4);
           v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
         }
-        float m, l;
         row_total(r, m, l);
-        put_row<T, true>(g, w, part, block0, hk, r, ch, v, m, l);
+        put_row<T, true>(g, done.whole, done.tok0, part, done.block0, done.hk, r, ch, v, m, l);
       }
-      named_sync(32 * kWarps);
     }
   }
 

@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // maximum of one that saw nothing: its sum, 0 or NaN, enters as it is.
 #pragma unroll
         for (int j = 0; j < kWarps; ++j) l += top[j][r] == -INFINITY ? tot[j][r] : tot[j][r] * exp2_fast(top[j][r] - m);
-        put_row<T>(g, w, part, block0, hk, r, ch, v, m, l);
+        put_row<T>(g, w.whole, w.s.tok0, part, block0, hk, r, ch, v, m, l);
       }
       named_sync(32 * kWarps);
     }

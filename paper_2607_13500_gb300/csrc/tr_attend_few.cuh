@@ -181,12 +181,12 @@ __device__ __forceinline__ void named_sync(int threads) { asm volatile("bar.sync
 
 // Four channels of row r of the piece: into the output, or into its share's
 // partial result.  NORMED: v is divided by l already.
-template <typename T, bool NORMED = false, int kExtra>
-__device__ __forceinline__ void put_row(const AttendArgs &g, const Walk<kExtra> &w, int part, int block0, int hk, int r, int ch,
+template <typename T, bool NORMED = false>
+__device__ __forceinline__ void put_row(const AttendArgs &g, bool whole, int tok0, int part, int block0, int hk, int r, int ch,
                                         const float4 &v, float m, float l) {
-  if (w.whole) {
+  if (whole) {
     const int row = block0 + r, tok = row / g.group, head = hk * g.group + row - tok * g.group;
-    const long long t = w.s.tok0 + tok;
+    const long long t = tok0 + tok;
     const float inv = NORMED ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;
     *reinterpret_cast<uint2 *>(g.o + 2 * (t * g.o_tok + (long long)head * g.o_head + ch)) =
         make_uint2(Bits<T>::pack(v.x * inv, v.y * inv), Bits<T>::pack(v.z * inv, v.w * inv));
