@@ -82,14 +82,14 @@ __device__ __forceinline__ void codes_sync() { asm volatile("bar.sync 2, 128;" :
 // were any.
 // The eight lanes of a phase of shared memory take the same half of rows r and
 // r ^ 5: their 16-byte pieces lie in different banks on both sides.
-template <int D, bool CLEAN>
+// AT_ONCE pieces are loaded before any is turned.
+template <int D, bool CLEAN, int AT_ONCE>
 __device__ __forceinline__ bool to_halves(uint32_t codes, uint32_t tile, int row0, int left, const uint32_t (&up)[2]) {
   const int lane = threadIdx.x & 31;
   bool found = false;
   constexpr int kSteps = D / 16;  // of 4 (D = 128) or 8 rows
-#pragma unroll 2
-  for (int i = 0; i < kSteps; ++i) {
-    int r, c;
+  static_assert(kSteps % AT_ONCE == 0, "");
+  auto place = [&](int i, int &r, int &c) {
     if (D == 128) {
       const int x = 2 * (i & 1) + (lane >> 3 & 1);
       r = row0 + 8 * (i >> 1) + (lane & 4 ? x ^ 5 : x);
@@ -98,21 +98,41 @@ __device__ __forceinline__ bool to_halves(uint32_t codes, uint32_t tile, int row
       r = row0 + 8 * i + (lane >> 2);
       c = lane & 3;
     }
-    uint4 v = tc::ld_shared_v4(codes + CodeRing<D, 2>::piece(r, c));
-    if (r >= left) v = make_uint4(0u, 0u, 0u, 0u);
-    if (CLEAN) found |= clean_codes(v.x) | clean_codes(v.y) | clean_codes(v.z) | clean_codes(v.w);
-    const uint32_t f = up[i / (kSteps / 2)];
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    uint32_t h[8];
+  };
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      h[2 * k] = mul_halves(halves((uint16_t)w[k]), f);
-      h[2 * k + 1] = mul_halves(halves((uint16_t)(w[k] >> 16)), f);
+  for (int i0 = 0; i0 < kSteps; i0 += AT_ONCE) {
+    uint4 v[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      int r, c;
+      place(i0 + i, r, c);
+      v[i] = tc::ld_shared_v4(codes + CodeRing<D, 2>::piece(r, c));
     }
-    const uint32_t at = tile + (c >> 2) * (kTile * 128) + r * 128;
-    const int chunk = 2 * (c & 3), flip = r & 7;
-    tc::st_shared_v4(at + ((chunk ^ flip) << 4), h[0], h[1], h[2], h[3]);
-    tc::st_shared_v4(at + (((chunk + 1) ^ flip) << 4), h[4], h[5], h[6], h[7]);
+    if (row0 + 32 > left)
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        int r, c;
+        place(i0 + i, r, c);
+        if (r >= left) v[i] = make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      int r, c;
+      place(i0 + i, r, c);
+      if (CLEAN) found |= clean_codes(v[i].x) | clean_codes(v[i].y) | clean_codes(v[i].z) | clean_codes(v[i].w);
+      const uint32_t f = up[(i0 + i) / (kSteps / 2)];
+      const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+      uint32_t h[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        halves4(w[k], h[2 * k], h[2 * k + 1]);
+        h[2 * k] = mul_halves(h[2 * k], f), h[2 * k + 1] = mul_halves(h[2 * k + 1], f);
+      }
+      const uint32_t at = tile + (c >> 2) * (kTile * 128) + r * 128;
+      const int chunk = 2 * (c & 3), flip = r & 7;
+      tc::st_shared_v4(at + ((chunk ^ flip) << 4), h[0], h[1], h[2], h[3]);
+      tc::st_shared_v4(at + (((chunk + 1) ^ flip) << 4), h[4], h[5], h[6], h[7]);
+    }
   }
   return found;
 }
@@ -278,8 +298,9 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
         if (!tc::mbar_wait_warp(code_full(kst), kind ? ph[1] : ph[0])) return false;
         if (!tc::mbar_wait_warp(half_empty(kind, buf), (n >> 1 & 1) ^ 1)) return false;
         const uint32_t from = ring + kst * S::kCodeBytes, to = (kind ? v16 : k16) + buf * S::kTileBytes;
-        if (kind && edges.open(t)) found |= to_halves<D, true>(from, to, 32 * w, k.len - t * kTile, up);
-        else to_halves<D, false>(from, to, 32 * w, k.len - t * kTile, up);
+        constexpr int kAtOnce = MT == 2 ? 4 : D / 16;
+        if (kind && edges.open(t)) found |= to_halves<D, true, kAtOnce>(from, to, 32 * w, k.len - t * kTile, up);
+        else to_halves<D, false, kAtOnce>(from, to, 32 * w, k.len - t * kTile, up);
         tc::fence_async_shared();
         __syncwarp();
         if (lane == 0) {
