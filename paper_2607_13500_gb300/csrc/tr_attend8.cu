@@ -8,17 +8,22 @@
 // too few for queries and probabilities, so codes become halves on their way:
 // rows, products and softmax are those of tr_attend.cu, and between the TMA
 // loads and the products stand four warps that turn a tile of codes in shared
-// memory into a tile of halves,
-//   k' = c 2^(7 + e - R),  R the largest exponent of all keys of the CTA,
-// exactly down to 2^-22 of R's scale (two instructions for two values: the
-// conversion and the product with 2^(7 + e - R)).  R - 7 goes into the factor
-// of the scores, and for values into the results.  They also put zeros in the
-// place of the keys past the sequence's end and of codes that are no numbers in
-// tiles that some row does not see all of (Edges in tr_attend.cuh).
-// bf16 queries enter as halves, each row divided by a power of two.
+// memory into a tile of halves, exactly, an instruction for two values.  They
+// also put zeros in the place of the keys past the sequence's end and of codes
+// that are no numbers in tiles that some row does not see all of (Edges in
+// tr_attend.cuh).  bf16 queries enter as halves, each row divided by a power of
+// two.
 //
-// Probabilities are at most 2^14 and rounded to halves for the second product;
-// their sum is taken before that rounding, and everything else is fp32.
+// The scales enter in the softmax, where they cost eight numbers a row and
+// tile (a product of halves for each pair of codes took a fifth of the time:
+// 2048 tokens over 32768 keys 758 us against 617):
+//   keys    a factor of the block's 16 scores;
+//   values  with R the largest exponent of the CTA's keys, d = e - R is added
+//           to the exponents of the block's 16 probabilities, and R enters the
+//           results.  Their sum is taken block by block, times 2^-d.
+// So what enters the second product is p 2^d, 2^14 at most, rounded to halves:
+// it keeps its bits down to 2^-20 of the largest, and what is lost below is
+// 2^-31 of it.  Sums and everything else are fp32.
 #include <atomic>
 #include <cmath>
 
@@ -51,8 +56,15 @@ struct Shape8 {
 };
 
 constexpr float kLift8 = 6.f;   // probabilities are taken times 2^6 (and grow by 2^8 at most)
-constexpr int kUp = 7;          // codes' halves times 2^7: 448 becomes 57344
 constexpr int kNone = -1000;    // R without a block
+constexpr int kLeast = -60;     // of d: a block below adds nothing to the product, but to the sum
+
+// What the softmax needs of a tile's blocks.
+struct TileScales {
+  float k[8];     // 2^e of keys
+  float v[8];     // d of values
+  float undo[8];  // 2^-d
+};
 
 // The values taken out of open tiles among [t0, t1) to those rows of the warp
 // that see them.  (Not inline: it would cost the softmax registers.)
@@ -77,14 +89,13 @@ __device__ __forceinline__ void rows_arrive(int threads) { asm volatile("bar.arr
 __device__ __forceinline__ void codes_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
 
 // Codes to halves: 32 rows (from row0, a multiple of 32) of a tile by a warp;
-// up: 2^(7 + e - R) of each 16 of them as a pair of halves; rows from `left` on
-// become zeros; CLEAN: so do codes that are no numbers.  Returns whether there
+// rows from `left` on become zeros; CLEAN: so do codes that are no numbers.  Returns whether there
 // were any.
 // The eight lanes of a phase of shared memory take the same half of rows r and
 // r ^ 5: their 16-byte pieces lie in different banks on both sides.
 // AT_ONCE pieces are loaded before any is turned.
 template <int D, bool CLEAN, int AT_ONCE>
-__device__ __forceinline__ bool to_halves(uint32_t codes, uint32_t tile, int row0, int left, const uint32_t (&up)[2]) {
+__device__ __forceinline__ bool to_halves(uint32_t codes, uint32_t tile, int row0, int left) {
   const int lane = threadIdx.x & 31;
   bool found = false;
   constexpr int kSteps = D / 16;  // of 4 (D = 128) or 8 rows
@@ -120,14 +131,10 @@ __device__ __forceinline__ bool to_halves(uint32_t codes, uint32_t tile, int row
       int r, c;
       place(i0 + i, r, c);
       if (CLEAN) found |= clean_codes(v[i].x) | clean_codes(v[i].y) | clean_codes(v[i].z) | clean_codes(v[i].w);
-      const uint32_t f = up[(i0 + i) / (kSteps / 2)];
       const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
       uint32_t h[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        halves4(w[k], h[2 * k], h[2 * k + 1]);
-        h[2 * k] = mul_halves(h[2 * k], f), h[2 * k + 1] = mul_halves(h[2 * k + 1], f);
-      }
+      for (int k = 0; k < 4; ++k) halves4(w[k], h[2 * k], h[2 * k + 1]);
       const uint32_t at = tile + (c >> 2) * (kTile * 128) + r * 128;
       const int chunk = 2 * (c & 3), flip = r & 7;
       tc::st_shared_v4(at + ((chunk ^ flip) << 4), h[0], h[1], h[2], h[3]);
@@ -160,10 +167,14 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
   auto p_full = [&](int m, int b) { return row_bars + 8u * (MT + MT * S::kSBuf + m * S::kSBuf + b); };
   auto o_done = [&](int m) { return row_bars + 8u * (MT + 2 * MT * S::kSBuf + m); };
   auto o_last = [&](int m) { return row_bars + 8u * (2 * MT + 2 * MT * S::kSBuf + m); };
-  const uint32_t ref_full = row_bars + 8u * (3 * MT + 2 * MT * S::kSBuf);
-  const uint32_t tmem_slot = ref_full + 8u;
-  __shared__ int bad_values;        // some were taken out of the tiles
-  __shared__ int ref_of[4], ref[2]; // R of K and of V
+  const uint32_t scale_bars = row_bars + 8u * (3 * MT + 2 * MT * S::kSBuf);
+  auto scale_full = [&](int s) { return scale_bars + 8u * s; };
+  const uint32_t tmem_slot = scale_bars + 32u;
+  __shared__ int bad_values;     // some were taken out of the tiles
+  __shared__ int ref_of[4], ref; // R
+  // Of tile t in slot t % 4: when the codes of tile t + 4 are turned, the
+  // scores of tile t + 2 are done, and with them the softmax of tile t.
+  __shared__ __align__(16) TileScales tile_scales[4];
 
   // (the warp's index by shuffle: the compiler then knows it to be uniform)
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -215,7 +226,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
         tc::mbar_init(o_done(m), 1);
         tc::mbar_init(o_last(m), 1);
       }
-      tc::mbar_init(ref_full, 128);
+      for (int s = 0; s < 4; ++s) tc::mbar_init(scale_full(s), 4);
       bad_values = 0;
       tc::mbar_fence_init();
       tc::tma_prefetch_map(&map_k);
@@ -256,23 +267,21 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
     } else if (warp >= 4 * MT + 4) {
       // ---------------------------------------------------------------- codes to halves
       const int w = warp - 4 * MT - 4;  // its rows: 32 w to 32 w + 31 of each tile
-      int rk = kNone, rv = kNone;
+      int most = kNone;
       const int blocks = min(8 * t1, (k.len + kBlock - 1) / kBlock);
 #pragma unroll 4
       for (int i = 8 * t0 + 32 * w + lane; i < blocks; i += 128) {
         const uint32_t s = block_scales(p, k.seq, hk, k.len, kBlock * i);
-        if (s != kNoScales) rk = max(rk, (int)(s & 0xffu) - 127), rv = max(rv, (int)(s >> 8) - 127);
+        if (s != kNoScales) most = max(most, (int)(s >> 8) - 127);
       }
-      rk = __reduce_max_sync(0xffffffffu, rk);
-      rv = __reduce_max_sync(0xffffffffu, rv);
+      most = __reduce_max_sync(0xffffffffu, most);
       if (t0 < t1) {
-        if (lane == 0) ref_of[w] = (rk & 0xffff) | rv << 16;
+        if (lane == 0) ref_of[w] = most;
         codes_sync();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) rk = max(rk, (int)(short)(ref_of[i] & 0xffff)), rv = max(rv, ref_of[i] >> 16);
-        if (rk == kNone) rk = rv = 0;
-        if (w == 0 && lane == 0) ref[0] = rk, ref[1] = rv;
-        tc::mbar_arrive(ref_full);
+        for (int i = 0; i < 4; ++i) most = max(most, ref_of[i]);
+        if (most == kNone) most = 0;
+        if (w == 0 && lane == 0) ref = most;
       }
       // scales of 16 tiles at a time, this warp's two blocks of one tile in two lanes
       auto scales = [&](int t) {
@@ -285,22 +294,27 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
       bool found = false;
       auto turn = [&](int kind, int t) {
         const int n = t - t0, buf = n & 1;
-        uint32_t up[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int at = 2 * (t - held0 & 15) + i;
-          const uint32_t s0 = __shfl_sync(0xffffffffu, held, at), s1 = __shfl_sync(0xffffffffu, ahead, at);
-          const uint32_t s = t - held0 < 16 ? s0 : s1;
-          const int e = kind ? (int)(s >> 8) - 127 - rv : (int)(s & 0xffu) - 127 - rk;
-          up[i] = half_pow2(kUp + min(e, 0));
-        }
         const int kst = kind ? st[1] : st[0];
         if (!tc::mbar_wait_warp(code_full(kst), kind ? ph[1] : ph[0])) return false;
         if (!tc::mbar_wait_warp(half_empty(kind, buf), (n >> 1 & 1) ^ 1)) return false;
         const uint32_t from = ring + kst * S::kCodeBytes, to = (kind ? v16 : k16) + buf * S::kTileBytes;
+        if (!kind) {  // the tile's scales, for the softmax
+          const int at = 2 * (t - held0 & 15) + (lane & 1);
+          const uint32_t s0 = __shfl_sync(0xffffffffu, held, at), s1 = __shfl_sync(0xffffffffu, ahead, at);
+          const uint32_t s = t - held0 < 16 ? s0 : s1;
+          if (lane < 2) {
+            TileScales &out = tile_scales[n & 3];
+            const int d = s >> 8 < 255u ? max((int)(s >> 8) - 127 - most, kLeast) : 0;
+            out.k[2 * w + lane] = pow2((int)(s & 0xffu) - 127);
+            out.v[2 * w + lane] = (float)d;
+            out.undo[2 * w + lane] = pow2(-d);
+          }
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(scale_full(n & 3));
+        }
         constexpr int kAtOnce = MT == 2 ? 4 : D / 16;
-        if (kind && edges.open(t)) found |= to_halves<D, true, kAtOnce>(from, to, 32 * w, k.len - t * kTile, up);
-        else to_halves<D, false, kAtOnce>(from, to, 32 * w, k.len - t * kTile, up);
+        if (kind && edges.open(t)) found |= to_halves<D, true, kAtOnce>(from, to, 32 * w, k.len - t * kTile);
+        else to_halves<D, false, kAtOnce>(from, to, 32 * w, k.len - t * kTile);
         tc::fence_async_shared();
         __syncwarp();
         if (lane == 0) {
@@ -458,16 +472,15 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
       }
       tc::fence_async_shared();
       tc::mbar_arrive(q_full(m));
-      ok = __all_sync(0xffffffffu, tc::mbar_wait(ref_full, 0));
-      // (from 1e-30 to 1e30: -inf and 0 times it stay what they are)
-      const int up = eq + (ok ? ref[0] : 0) - kUp;
-      const float scale = fminf(fmaxf(g.scale * pow2(up >> 1) * pow2(up - (up >> 1)), 1e-30f), 1e30f);
+      // what a score of the row is multiplied by, its key's scale apart
+      const float row_scale = g.scale * pow2(eq);
 
       for (int t = ta; t < tb && ok; ++t) {
         const int n = t - ta;
         const int buf = S::kSBuf == 2 ? n & 1 : 0;
         const uint32_t s_par = S::kSBuf == 2 ? (uint32_t)(n >> 1) & 1u : (uint32_t)n & 1u;
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(s_full(m, buf), s_par));
+        const int ts = t - t0;
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(s_full(m, buf), s_par) && tc::mbar_wait(scale_full(ts & 3), (uint32_t)(ts >> 2) & 1u));
         if (!ok) break;
         tc::fence_after_sync();
         if (live) {
@@ -484,18 +497,23 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
             for (int i = 0; i < kTile; ++i)
               if (i < c0 || i >= c1) s[i] = 0xff800000u;  // -inf
           }
-          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          // (factors from 1e-30 to 1e30: -inf and 0 times them stay what they are)
+          const TileScales &sc = tile_scales[ts & 3];
+          float f[8], now = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < kTile; i += 8)
+          for (int b = 0; b < 8; ++b) {
+            f[b] = fminf(fmaxf(row_scale * sc.k[b], 1e-30f), 1e30f);
+            float top0 = max3(__uint_as_float(s[16 * b]), s[16 * b + 1], s[16 * b + 2]), top1 = __uint_as_float(s[16 * b + 3]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top[j] = max3(top[j], s[i + 2 * j], s[i + 2 * j + 1]);
-          const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale;
+            for (int i = 4; i < 16; i += 4) top0 = max3(top0, s[16 * b + i], s[16 * b + i + 1]), top1 = max3(top1, s[16 * b + i + 2], s[16 * b + i + 3]);
+            now = fmaxf(now, fmaxf(top0, top1) * f[b]);
+          }
           if (n == 0) {
             mx = now;
           } else if (__any_sync(0xffffffffu, now > mx + 8.f)) {
             // the sums so far (all products up to the last tile's are in) move to the new maximum
             const bool more = now > mx + 8.f;
-            const float f = more ? exp2_fast(mx - now) : 1.f;
+            const float down = more ? exp2_fast(mx - now) : 1.f;
             if (S::kSBuf == 2) {  // (one buffer: these scores came after the last tile's product)
               ok = __all_sync(0xffffffffu, tc::mbar_wait(o_done(m), (uint32_t)(n - 1) & 1u));
               if (!ok) break;
@@ -507,25 +525,29 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
               tc::tmem_ld32_issue(o_col + c1, o);
               tc::tmem_ld32_wait(o);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * down);
               tc::tmem_st32(o_col + c1, o);
             }
             tc::tmem_st_wait();
             if (more) mx = now;
-            sum *= f;
+            sum *= down;
           }
           const float neg = mx == -INFINITY ? 0.f : kLift8 - mx;  // a row that has seen nothing: exp2(-inf) = 0
-          const pack::f2 sc2 = pack::make(scale, scale), neg2 = pack::make(neg, neg);
-          pack::f2 acc[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
-          for (int i = 0; i < kTile; i += 2) {
-            const float2 e = pack::split(pack::fma(pack::make(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), sc2, neg2));
-            const float p0 = exp2_fast(e.x), p1 = exp2_fast(e.y);
-            acc[(i >> 1) & 3] = pack::add(acc[(i >> 1) & 3], pack::make(p0, p1));
-            s[i >> 1] = Bits<__half>::pack(p0, p1);
+          for (int b = 0; b < 8; ++b) {
+            const float d = neg + sc.v[b];
+            const pack::f2 f2b = pack::make(f[b], f[b]), d2 = pack::make(d, d);
+            pack::f2 acc[2] = {0ull, 0ull};
+#pragma unroll
+            for (int i = 16 * b; i < 16 * b + 16; i += 2) {
+              const float2 e = pack::split(pack::fma(pack::make(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), f2b, d2));
+              const float p0 = exp2_fast(e.x), p1 = exp2_fast(e.y);
+              acc[(i >> 1) & 1] = pack::add(acc[(i >> 1) & 1], pack::make(p0, p1));
+              s[i >> 1] = Bits<__half>::pack(p0, p1);
+            }
+            const float2 x = pack::split(pack::add(acc[0], acc[1]));
+            sum += (x.x + x.y) * sc.undo[b];
           }
-          const float2 x = pack::split(pack::add(pack::add(acc[0], acc[1]), pack::add(acc[2], acc[3])));
-          sum += x.x + x.y;
           tc::tmem_st32(s_col, s);
           tc::tmem_st32(s_col + 32, s + 32);
           tc::tmem_st_wait();
@@ -548,8 +570,8 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
       const long long all_rows = (long long)g.c.total_new * g.q_heads;
       float *prow = g.part + ((long long)split * all_rows + out_row) * g.c.d;
       // divided by the sum before V's scale, up to 2^127, enters
-      const float inv = (sum > 0.f || sum != sum ? 1.f / sum : 0.f) * (1.f / (1 << kUp));
-      const float up = ta < tb ? pow2(ref[1]) : 0.f;
+      const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+      const float up = ta < tb ? pow2(ref) : 0.f;
       // staged in the place of this row's queries, whose products are done
       const uint32_t stage_row = sbase + m * S::kTileBytes + row * 128;
 #pragma unroll 1

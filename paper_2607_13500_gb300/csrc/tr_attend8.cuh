@@ -16,17 +16,6 @@ struct Attend8Args {
   Scales scale;
 };
 
-// 2^e as a pair of halves, e <= 15; 0 below 2^-24.
-__device__ __forceinline__ uint32_t half_pow2(int e) {
-  const uint32_t h = e >= -14 ? (uint32_t)(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u;
-  return h | h << 16;
-}
-__device__ __forceinline__ uint32_t mul_halves(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-
 // ---------------------------------------------------------------- codes that stand for no number
 // Zeros in the place of NaN among four codes; whether there was any.
 __device__ __forceinline__ bool clean_codes(uint32_t &w) {

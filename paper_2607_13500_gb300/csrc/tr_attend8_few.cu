@@ -6,9 +6,9 @@
 // into warp-level products (m16n8k16), whose 16 keys are one block, so scales
 // cost next to nothing:
 //   K   one factor for the 16 keys' scores;
-//   V   2^(e - R), R the largest exponent of the warp's blocks so far, enters
-//       the block's probabilities: like the running maximum of the softmax,
-//       and when R grows, the sums move with it (by a power of two, exactly).
+//   V   e - R, R the largest exponent of the warp's blocks so far, is added to
+//       the exponents of the block's probabilities and taken out of their sum;
+//       when R grows, the results so far move with it, exactly.
 // bf16 queries enter as halves as well, each row divided by a power of two.
 // Probabilities are taken times 2^6 (2^14 at most) and rounded to halves: they
 // and the scales that they carry keep their bits down to 2^-20 of the largest,
@@ -39,6 +39,7 @@ struct Few8 {
 
 constexpr float kLift = 6.f;   // probabilities are taken times 2^6 (and grow by 2^8 at most)
 constexpr int kNoExp = -1000;  // R before the first block
+constexpr int kLeast = -60;    // of e - R: a block below adds nothing to the product, but to the sum
 
 __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   uint2 v;
@@ -338,16 +339,22 @@ __global__ void __launch_bounds__(kAllThreads, 1)
 #pragma unroll
           for (int j = 0; j < 4; ++j) o[i][j] *= f;
       }
-      uint32_t pr[2][4];  // the A fragments of the second product, times their block's scale
+      uint32_t pr[2][4];  // the A fragments of the second product
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float neg = mx[i] == -INFINITY ? 0.f : kLift - mx[i];
+      for (int h = 0; h < 2; ++h) {
+        // the values' scale, 2^d, is in the exponents, and out of the sum
+        const int d = max(ev[h] - big, kLeast);
+        const float undo = pow2(-d);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          const float f = fs[i][n >> 1];
-          const float p0 = exp2_fast(fmaf(s[n][2 * i], f, neg)), p1 = exp2_fast(fmaf(s[n][2 * i + 1], f, neg));
-          sum[i] += p0 + p1;
-          pr[n >> 1][2 * (n & 1) + i] = mul_halves(Bits<__half>::pack(p0, p1), half_pow2(min(ev[n >> 1] - big, 0)));
+        for (int i = 0; i < 2; ++i) {
+          const float neg = (mx[i] == -INFINITY ? 0.f : kLift - mx[i]) + (float)d, f = fs[i][h];
+          float p0[2], p1[2];
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            p0[n] = exp2_fast(fmaf(s[2 * h + n][2 * i], f, neg)), p1[n] = exp2_fast(fmaf(s[2 * h + n][2 * i + 1], f, neg));
+            pr[h][2 * n + i] = Bits<__half>::pack(p0[n], p1[n]);
+          }
+          sum[i] = fmaf((p0[0] + p1[0]) + (p0[1] + p1[1]), undo, sum[i]);
         }
       }
 
