@@ -488,6 +488,20 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
           uint32_t s[kTile];
 #pragma unroll
           for (int i = 0; i < kTile; i += 32) tc::tmem_ld32_issue(s_col + i, s + i);
+          // (the scales while the scores are on their way)
+          float f[8], dv[8], undo[8];
+          {
+            const uint32_t at = tc::smem_u32(&tile_scales[ts & 3]);
+#pragma unroll
+            for (int b = 0; b < 8; b += 4) {
+              const uint4 x = tc::ld_shared_v4(at + 4 * b), y = tc::ld_shared_v4(at + 32 + 4 * b), z = tc::ld_shared_v4(at + 64 + 4 * b);
+              f[b] = __uint_as_float(x.x), f[b + 1] = __uint_as_float(x.y), f[b + 2] = __uint_as_float(x.z), f[b + 3] = __uint_as_float(x.w);
+              dv[b] = __uint_as_float(y.x), dv[b + 1] = __uint_as_float(y.y), dv[b + 2] = __uint_as_float(y.z), dv[b + 3] = __uint_as_float(y.w);
+              undo[b] = __uint_as_float(z.x), undo[b + 1] = __uint_as_float(z.y), undo[b + 2] = __uint_as_float(z.z), undo[b + 3] = __uint_as_float(z.w);
+            }
+#pragma unroll
+            for (int b = 0; b < 8; ++b) f[b] = fmaxf(row_scale * f[b], 1e-30f);  // (not zero: masked scores are -inf)
+          }
 #pragma unroll
           for (int i = 0; i < kTile; i += 32) tc::tmem_ld32_wait(s + i);
           const int key0 = t * kTile;
@@ -497,17 +511,15 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
             for (int i = 0; i < kTile; ++i)
               if (i < c0 || i >= c1) s[i] = 0xff800000u;  // -inf
           }
-          // (factors from 1e-30 to 1e30: -inf and 0 times them stay what they are)
-          const TileScales &sc = tile_scales[ts & 3];
-          float f[8], now = -INFINITY;
+          float tops[8];
 #pragma unroll
           for (int b = 0; b < 8; ++b) {
-            f[b] = fminf(fmaxf(row_scale * sc.k[b], 1e-30f), 1e30f);
             float top0 = max3(__uint_as_float(s[16 * b]), s[16 * b + 1], s[16 * b + 2]), top1 = __uint_as_float(s[16 * b + 3]);
 #pragma unroll
             for (int i = 4; i < 16; i += 4) top0 = max3(top0, s[16 * b + i], s[16 * b + i + 1]), top1 = max3(top1, s[16 * b + i + 2], s[16 * b + i + 3]);
-            now = fmaxf(now, fmaxf(top0, top1) * f[b]);
+            tops[b] = fmaxf(top0, top1) * f[b];
           }
+          const float now = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
           if (n == 0) {
             mx = now;
           } else if (__any_sync(0xffffffffu, now > mx + 8.f)) {
@@ -535,7 +547,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
           const float neg = mx == -INFINITY ? 0.f : kLift8 - mx;  // a row that has seen nothing: exp2(-inf) = 0
 #pragma unroll
           for (int b = 0; b < 8; ++b) {
-            const float d = neg + sc.v[b];
+            const float d = neg + dv[b];
             const pack::f2 f2b = pack::make(f[b], f[b]), d2 = pack::make(d, d);
             pack::f2 acc[2] = {0ull, 0ull};
 #pragma unroll
@@ -546,7 +558,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
               s[i >> 1] = Bits<__half>::pack(p0, p1);
             }
             const float2 x = pack::split(pack::add(acc[0], acc[1]));
-            sum += (x.x + x.y) * sc.undo[b];
+            sum = fmaf(x.x + x.y, undo[b], sum);
           }
           tc::tmem_st32(s_col, s);
           tc::tmem_st32(s_col + 32, s + 32);
