@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import struct
-from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -36,8 +36,7 @@ def _library():
     return _calls
 
 
-@dataclass
-class Step:
+class Step(NamedTuple):
     cu_new: torch.Tensor  # int32 [batch + 1], prefix sums of the new tokens
     slots: torch.Tensor   # int32 [rows], place of the row's key in the cache (page id * page + place in the page), or -1
     pos: torch.Tensor     # int32 [rows], its position in its sequence, or -1
@@ -70,18 +69,20 @@ class PageTable:
         if self.pages * self.page > attention._MOST or self.max_pages * self.page > attention._MOST - 65536:
             raise ValueError("slots and positions are 32-bit numbers: fewer pages")
         mk = lambda *s: torch.zeros(s, dtype=torch.int32, device=self.device)
-        self.table, self.lens = mk(self.batch, self.max_pages).fill_(-1), mk(self.batch)
-        self.free = torch.arange(self.pages - 1, -1, -1, dtype=torch.int32, device=self.device)
-        self.free_count = mk(1).fill_(self.pages)
-        self.error, self._ticket = mk(1), mk(1)
+        self._table, self._lens = mk(self.batch, self.max_pages).fill_(-1), mk(self.batch)
+        self._free = torch.arange(self.pages - 1, -1, -1, dtype=torch.int32, device=self.device)
+        self._free_count = mk(1).fill_(self.pages)
+        self._errors, self._ticket = mk(1), mk(1)
+        self._error = self._errors.data_ptr()
+        self._struct = _pack_pages(*(x.data_ptr() for x in (self._table, self._lens, self._free, self._free_count, self._ticket)),
+                                   self.batch, self.max_pages, self.pages, self.page)
 
-    def _struct(self):
-        i = self.index
-        ints = attention._ints
-        return _pack_pages(ints(self.table, "table", (self.batch, self.max_pages), i),
-                           ints(self.lens, "lens", (self.batch,), i), ints(self.free, "free", (self.pages,), i),
-                           ints(self.free_count, "free_count", (1,), i), self._ticket.data_ptr(), self.batch,
-                           self.max_pages, self.pages, self.page)
+    # (written in place, never replaced: the calls go by their addresses)
+    table = property(lambda self: self._table)
+    lens = property(lambda self: self._lens)
+    free = property(lambda self: self._free)
+    free_count = property(lambda self: self._free_count)
+    error = property(lambda self: self._errors)
 
     def extend(self, new, rows) -> Step:
         """``new`` int32 [batch] more tokens for each sequence (negative:
@@ -93,14 +94,16 @@ class PageTable:
         rows = int(rows)
         if not 0 <= rows <= attention._MOST:
             raise ValueError("rows must be a 32-bit number that is not negative")
-        c, p = self._struct(), attention._ints(new, "new", (b,), i)
-        buf = torch.empty(b + 1 + 3 * rows, dtype=torch.int32, device=self.device)
-        cu, slots, pos, seq = buf.split((b + 1, rows, rows, rows))
-        rc = at(i, self.calls.extend)(c, p, rows, cu.data_ptr(), slots.data_ptr(), pos.data_ptr(), seq.data_ptr(),
-                                      self.error.data_ptr(), attention._stream(i))
+        p = attention._ints(new, "new", (b,), i)
+        mk, dt, dev = torch.empty, torch.int32, self.device
+        # (each by itself: views of one buffer take the host longer)
+        s = Step(mk(b + 1, dtype=dt, device=dev), mk(rows, dtype=dt, device=dev), mk(rows, dtype=dt, device=dev),
+                 mk(rows, dtype=dt, device=dev))
+        rc = at(i, self.calls.extend)(self._struct, p, rows, s[0].data_ptr(), s[1].data_ptr(), s[2].data_ptr(),
+                                      s[3].data_ptr(), self._error, attention._stream(i))
         if rc:
             check("tr_pages_extend", rc)
-        return Step(cu, slots, pos, seq)
+        return s
 
     def truncate(self, keep):
         """Every sequence keeps its first ``keep`` int32 [batch] tokens at
@@ -108,7 +111,7 @@ class PageTable:
         (tr_pages_truncate).  Directly after an extend, to the lengths before
         it, everything is as it was."""
         i = self.index
-        c, p = self._struct(), attention._ints(keep, "keep", (self.batch,), i)
-        rc = at(i, self.calls.truncate)(c, p, self.error.data_ptr(), attention._stream(i))
+        p = attention._ints(keep, "keep", (self.batch,), i)
+        rc = at(i, self.calls.truncate)(self._struct, p, self._error, attention._stream(i))
         if rc:
             check("tr_pages_truncate", rc)
