@@ -21,8 +21,8 @@
 namespace tr {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kPerCta = 4096;  // pages or rows that are worth a CTA of their own
+constexpr int kThreads = 1024;  // at most (a few sequences and rows: fewer, for cheaper barriers)
+constexpr int kPerCta = 1024;  // pages or rows that are worth a CTA of their own
 
 struct PagesArgs {
   int32_t *table, *lens, *free, *free_count, *ticket;
@@ -55,17 +55,27 @@ __device__ __forceinline__ Change change_of(const PagesArgs &g, int b) {
   return c;
 }
 
-// Sums over the CTA.
-__device__ __forceinline__ long long cta_sum(long long v, long long *part) {
+// Sums over the CTA of two numbers, and the OR of a third.
+struct Sums {
+  long long a, b;
+  int bits;
+};
+__device__ __forceinline__ Sums warp_sums(Sums s) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  for (int o = 16; o; o >>= 1) {
+    s.a += __shfl_xor_sync(0xffffffffu, s.a, o);
+    s.b += __shfl_xor_sync(0xffffffffu, s.b, o);
+  }
+  s.bits = (int)__reduce_or_sync(0xffffffffu, (unsigned)s.bits);
+  return s;
+}
+__device__ __forceinline__ Sums cta_sums(Sums s, Sums *part) {
+  const int lane = threadIdx.x & 31;
+  s = warp_sums(s);
+  if (lane == 0) part[threadIdx.x >> 5] = s;
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = part[threadIdx.x & 31];
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
+  s = lane < (int)blockDim.x >> 5 ? part[lane] : Sums{0, 0, 0};
+  return warp_sums(s);
 }
 // Exclusive prefix sums over the CTA of two numbers, and their totals.
 __device__ __forceinline__ int2 cta_scan(int2 v, int2 *part, int2 &all) {
@@ -76,10 +86,10 @@ __device__ __forceinline__ int2 cta_scan(int2 v, int2 *part, int2 &all) {
     const int a = __shfl_up_sync(0xffffffffu, x.x, o), b = __shfl_up_sync(0xffffffffu, x.y, o);
     if (lane >= o) x.x += a, x.y += b;
   }
-  __syncthreads();
   if (lane == 31) part[warp] = x;
   __syncthreads();
-  int2 w = part[lane], s = w;
+  const int2 w = lane < (int)blockDim.x >> 5 ? part[lane] : make_int2(0, 0);
+  int2 s = w;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int a = __shfl_up_sync(0xffffffffu, s.x, o), b = __shfl_up_sync(0xffffffffu, s.y, o);
@@ -101,49 +111,45 @@ __device__ __forceinline__ int last_at(const int *at, int n, int u) {
 
 template <bool EXTEND>
 __global__ void __launch_bounds__(kThreads) k_pages(const __grid_constant__ PagesArgs g) {
-  __shared__ long long sums[32];
+  __shared__ Sums sums[32];
   __shared__ int2 part[32];
-  __shared__ int rows_at[kThreads], pages_at[kThreads];  // of 1024 sequences: first row, first page moved
+  __shared__ int rows_at[kThreads], pages_at[kThreads];  // of a run of sequences: first row, first page moved
   __shared__ int len_at[kThreads], first_at[kThreads];
   __shared__ bool last;
-  __shared__ int refused;
-  if (threadIdx.x == 0) refused = 0;
-  pdl_wait();  // the counts come from the kernels before
-  const int tid = threadIdx.x, stride = kThreads * gridDim.x, me = blockIdx.x * kThreads + tid;
-  const int runs = (g.batch + kThreads - 1) / kThreads;
+  pdl_trigger();
+  pdl_wait();  // the counts and the tables come from the kernels before
+  const int threads = blockDim.x, tid = threadIdx.x, stride = threads * gridDim.x, me = blockIdx.x * threads + tid;
+  const int runs = (g.batch + threads - 1) / threads;
   const int have = *g.free_count;
   // ---- whether the step can be taken
   Change mine = change_of<EXTEND>(g, tid);
-  long long rows = 0, moved = 0;
-  int bits = (unsigned)have > (unsigned)g.pages ? TR_PAGES_ERR_STATE : 0;
+  Sums s{0, 0, (unsigned)have > (unsigned)g.pages ? TR_PAGES_ERR_STATE : 0};
   for (int r = 0; r < runs; ++r) {
-    const Change c = r ? change_of<EXTEND>(g, r * kThreads + tid) : mine;
-    rows += c.to - c.len;
-    moved += c.pages;
-    if (c.bad) bits |= TR_PAGES_ERR_STATE;
-    if (EXTEND && c.to > (long long)g.max_pages << g.page_log2) bits |= TR_PAGES_ERR_LONG;
+    const Change c = r ? change_of<EXTEND>(g, r * threads + tid) : mine;
+    s.a += c.to - c.len;
+    s.b += c.pages;
+    if (c.bad) s.bits |= TR_PAGES_ERR_STATE;
+    if (EXTEND && c.to > (long long)g.max_pages << g.page_log2) s.bits |= TR_PAGES_ERR_LONG;
   }
-  rows = cta_sum(rows, sums);
-  moved = cta_sum(moved, sums);
+  s = cta_sums(s, sums);
+  const long long rows = s.a, moved = s.b;
+  int bits = s.bits;
   if (EXTEND) {
     if (moved > have) bits |= TR_PAGES_ERR_FULL;
     if (rows > g.total_new) bits |= TR_PAGES_ERR_ROWS;
   } else if (have + moved > g.pages) {
     bits |= TR_PAGES_ERR_STATE;
   }
-  if (bits) atomicOr(&refused, bits);
-  __syncthreads();
-  bits = refused;
   const bool take = bits == 0;
 
-  // ---- pages and rows, 1024 sequences at a time
+  // ---- pages and rows, a run of sequences at a time
   int2 before = make_int2(0, 0);
   for (int r = 0; take && r < runs; ++r) {
-    const int b0 = r * kThreads, n = min(g.batch - b0, kThreads);
+    const int b0 = r * threads, n = min(g.batch - b0, threads);
     if (r) mine = change_of<EXTEND>(g, b0 + tid);
     int2 all;
     const int2 at = cta_scan(make_int2(EXTEND ? (int)(mine.to - mine.len) : 0, mine.pages), part, all);
-    __syncthreads();  // the last sequences' are used up
+    if (r) __syncthreads();  // the last sequences' are used up
     rows_at[tid] = before.x + at.x;
     pages_at[tid] = before.y + at.y;
     len_at[tid] = (int)mine.len;
@@ -178,7 +184,7 @@ __global__ void __launch_bounds__(kThreads) k_pages(const __grid_constant__ Page
     for (int t = (take ? (int)rows : 0) + me; t < g.total_new; t += stride) g.slots[t] = g.pos[t] = g.seq[t] = -1;
     if (blockIdx.x == 0) {
       if (!take)
-        for (int b = tid; b < g.batch; b += kThreads) g.cu_new[b] = 0;
+        for (int b = tid; b < g.batch; b += threads) g.cu_new[b] = 0;
       if (tid == 0) g.cu_new[g.batch] = take ? (int)rows : 0;
     }
   }
@@ -195,7 +201,7 @@ __global__ void __launch_bounds__(kThreads) k_pages(const __grid_constant__ Page
   }
   if (take) {
     for (int r = 0; r < runs; ++r) {
-      const int b = r * kThreads + tid;
+      const int b = r * threads + tid;
       if (b >= g.batch) break;
       if (runs > 1) mine = change_of<EXTEND>(g, b);
       g.lens[b] = (int)mine.to;
@@ -232,9 +238,14 @@ PagesArgs pages_args(const tr_pages *p, const int32_t *in, int32_t *err) {
   return g;
 }
 
-int ctas_of(long long n) {
-  const long long sms = sm_count() > 0 ? sm_count() : 1, want = (n + kPerCta - 1) / kPerCta;
-  return (int)(want < 1 ? 1 : want > sms ? sms : want);
+// work: pages or rows at most.
+template <bool EXTEND>
+cudaError_t launch_pages(const PagesArgs &g, long long work, cudaStream_t st) {
+  const long long sms = sm_count() > 0 ? sm_count() : 1, want = (work + kPerCta - 1) / kPerCta;
+  const int ctas = (int)(want < 1 ? 1 : want > sms ? sms : want);
+  int threads = 128;
+  while (threads < kThreads && (threads < g.batch || 4ll * threads < work)) threads *= 2;
+  return launch_kernel(k_pages<EXTEND>, dim3(ctas), dim3(threads), 0, st, true, g);
 }
 
 }  // namespace
@@ -255,10 +266,7 @@ tr_status tr_pages_extend(const tr_pages *p, const int32_t *d_new, int32_t total
   PagesArgs g = pages_args(p, d_new, d_error);
   g.total_new = total_new;
   g.cu_new = cu_new, g.slots = slots, g.pos = pos, g.seq = seq;
-  return launch_kernel(k_pages<true>, dim3(ctas_of(total_new)), dim3(kThreads), 0, static_cast<cudaStream_t>(stream),
-                       false, g) == cudaSuccess
-             ? TR_OK
-             : TR_ERR_CUDA;
+  return launch_pages<true>(g, total_new, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TR_OK : TR_ERR_CUDA;
 }
 
 tr_status tr_pages_truncate(const tr_pages *p, const int32_t *d_keep, int32_t *d_error, void *stream) {
@@ -269,10 +277,9 @@ tr_status tr_pages_truncate(const tr_pages *p, const int32_t *d_keep, int32_t *d
   if (p->batch == 0) return TR_OK;
   const PagesArgs g = pages_args(p, d_keep, d_error);
   const long long most = (long long)p->batch * p->max_pages;
-  return launch_kernel(k_pages<false>, dim3(ctas_of(most < p->pages ? most : p->pages)), dim3(kThreads), 0,
-                       static_cast<cudaStream_t>(stream), false, g) == cudaSuccess
-             ? TR_OK
-             : TR_ERR_CUDA;
+  // few of the pages that could come back do as a rule: the last steps' of each sequence, or some sequences whole
+  const long long work = 4ll * p->batch + (most < p->pages ? most : p->pages) / 16;
+  return launch_pages<false>(g, work, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TR_OK : TR_ERR_CUDA;
 }
 
 }  // extern "C"
