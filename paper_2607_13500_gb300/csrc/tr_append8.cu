@@ -25,7 +25,9 @@ using namespace cache8;
 struct Append8Args {
   RotArgs g;      // seg[0]: queries; seg[1], seg[2]: the rows of keys and values
   Scales scale;
-  int blocks;     // slots of blocks; CTAs behind them take the queries
+  int blocks;     // slots of blocks
+  int parts;      // CTAs of one: its heads' keys and values in turn
+  int every;      // one CTA in so many is a block's, while there are any; the others take the queries
 };
 
 // Sequence b's blocks have the slots from cu_new[b] / 16 + 2 b on: n new keys
@@ -67,136 +69,172 @@ __device__ __forceinline__ NewBlock find_new_block(const CacheView &c, int slot)
 
 __device__ __forceinline__ bool finite1(float v) { return fabsf(v) <= 3.402823466e38f; }
 
-// One head's new rows of a block: loaded, normed and rotated, coded, stored.
+// One head's new rows of a block, by a warp: d / (2 V) <= 8 or 16 lanes a row.
+// They stay in registers as they came, from the load to the codes; the norm's
+// factors are kept and the rotation is done twice, for the scale and for the
+// codes (held in fp32 instead, rows took 128 registers and two CTAs filled an
+// SM: 29.6k tokens 43 us without queries).
 template <typename T, int V, bool PAIRS>
-__device__ __forceinline__ void put_block(const Append8Args &a, const Rows &s, const NewBlock &k, int page, int head,
-                                          uint8_t *codes, uint8_t *scales, const float *cs, const float *sn) {
-  const RotArgs &g = a.g;
-  constexpr int kPasses = V == 8 ? 4 : 8;  // 16 rows, d / (2 V) <= 8 or 16 lanes a row
-  const int lane = threadIdx.x & 31, slot = lane & ((1 << g.lanes_log2) - 1);
-  const int at_once = 32 >> g.lanes_log2, row0 = lane >> g.lanes_log2;
-  const bool holds = slot < g.slots;
-  const SlotPlace at = slot_place<V, PAIRS>(slot, g.half);
+struct BlockRows {
+  static constexpr int kPasses = V == 8 ? 4 : 8;
   Chunk<T, V> ra[kPasses], rb[kPasses];
-#pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
-    const int r = p * at_once + row0;
-    if (holds && r >= k.r0 && r < k.r1) {
-      const char *src = s.in + row_bytes<T>(k.tok0 + r, s.in_tok, head, s.in_head);
-      ra[p].load(src + sizeof(T) * at.a);
-      rb[p].load(src + sizeof(T) * at.b);
-    }
+  int slot, at_once, row0;
+  bool holds;
+  SlotPlace at;
+
+  __device__ __forceinline__ BlockRows(const RotArgs &g) {
+    const int lane = threadIdx.x & 31;
+    slot = lane & ((1 << g.lanes_log2) - 1);
+    at_once = 32 >> g.lanes_log2, row0 = lane >> g.lanes_log2;
+    holds = slot < g.slots;
+    at = slot_place<V, PAIRS>(slot, g.half);
   }
-  const long long sc = scale_at(g.cache, page, head, k.key & (g.cache.page - 1));
-  const int before = exp_of(scales[sc]);
-  f2 wa[V / 2] = {}, wb[V / 2] = {};
-  if (s.w && holds) get_weights<V>(s.w, at.a, at.b, wa, wb);
-  f2 x[kPasses][V / 2], y[kPasses][V / 2];
-  float most = 0.f;
-#pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
+  __device__ __forceinline__ bool live(const NewBlock &k, int p) const {
     const int r = p * at_once + row0;
-    const bool live = holds && r >= k.r0 && r < k.r1;
-    ra[p].get(x[p]);
-    rb[p].get(y[p]);
+    return holds && r >= k.r0 && r < k.r1;
+  }
+  __device__ __forceinline__ void load(const Rows &s, const NewBlock &k, int head) {
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p)
+      if (live(k, p)) {
+        const char *src = s.in + row_bytes<T>(k.tok0 + p * at_once + row0, s.in_tok, head, s.in_head);
+        ra[p].load(src + sizeof(T) * at.a);
+        rb[p].load(src + sizeof(T) * at.b);
+      }
+  }
+  // Row of pass p as it enters the cache; f: its norm's factor.
+  __device__ __forceinline__ void values(const RotArgs &g, const Rows &s, const NewBlock &k, int p, float f, const float *cs,
+                                         const float *sn, f2 (&x)[V / 2], f2 (&y)[V / 2]) const {
+    ra[p].get(x);
+    rb[p].get(y);
     if (s.w) {
-      f2 s2 = 0ull;
-#pragma unroll
-      for (int i = 0; i < V / 2; ++i) s2 = pack::fma(x[p][i], x[p][i], pack::fma(y[p][i], y[p][i], s2));
-      const float2 t = pack::split(s2);
-      const float ss = group_sum(live ? t.x + t.y : 0.f, g.lanes_log2);
-      const float f = rsqrtf(ss * g.inv_d + g.eps);
       const f2 ff = pack::make(f, f);
+      f2 wa[V / 2], wb[V / 2];
+      get_weights<V>(s.w, at.a, at.b, wa, wb);
 #pragma unroll
-      for (int i = 0; i < V / 2; ++i) {
-        x[p][i] = pack::mul(x[p][i], pack::mul(ff, wa[i]));
-        y[p][i] = pack::mul(y[p][i], pack::mul(ff, wb[i]));
+      for (int i = 0; i < V / 2; ++i) x[i] = pack::mul(x[i], pack::mul(ff, wa[i])), y[i] = pack::mul(y[i], pack::mul(ff, wb[i]));
+    }
+    if (s.turn && at.turns) {
+      const int t = (p * at_once + row0 - k.r0) * g.half + slot * V;
+      turn<V, PAIRS>(x, y, cs + t, sn + t);
+    }
+  }
+
+  // Codes and scale of one head's keys or values.
+  __device__ __forceinline__ void put(const RotArgs &g, const Rows &s, const NewBlock &k, int page, int head, uint8_t *codes,
+                                      uint8_t *scales, const float *cs, const float *sn) const {
+    const int lane = threadIdx.x & 31;
+    const long long sc = scale_at(g.cache, page, head, k.key & (g.cache.page - 1));
+    const int before = exp_of(scales[sc]);
+    float norm[kPasses], most = 0.f;
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      f2 x[V / 2], y[V / 2];
+      norm[p] = 1.f;
+      if (s.w) {
+        ra[p].get(x);
+        rb[p].get(y);
+        f2 s2 = 0ull;
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) s2 = pack::fma(x[i], x[i], pack::fma(y[i], y[i], s2));
+        const float2 t = pack::split(s2);
+        norm[p] = rsqrtf(group_sum(live(k, p) ? t.x + t.y : 0.f, g.lanes_log2) * g.inv_d + g.eps);
+      }
+      if (live(k, p)) {
+        values(g, s, k, p, norm[p], cs, sn, x, y);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+          const float2 u = pack::split(x[i]), w = pack::split(y[i]);
+          const float v[4] = {u.x, u.y, w.x, w.y};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (finite1(v[j])) most = fmaxf(most, fabsf(v[j]));
+        }
       }
     }
-    if (live && s.turn && at.turns) {
-      const int t = (r - k.r0) * g.half + slot * V;
-      turn<V, PAIRS>(x[p], y[p], cs + t, sn + t);
+    // a <= 448 2^e = 1.75 2^(8 + e)
+    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(most));
+    const bool older = k.r0 > 0;
+    int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+    e = min(max(e, kMinExp), kMaxExp);
+    if (older) e = max(e, before);
+    uint8_t *rows =
+        codes + (((long long)page * g.cache.heads + head) * g.cache.page + (k.key & (g.cache.page - 1))) * g.d;
+    if (older && e > before) {  // the older keys' codes, by 2^(before - e)
+      const int down = min(e - before, 24);  // (beyond, all codes become zero)
+      const uint32_t f = down <= 14 ? (uint32_t)(15 - down) << 10 : 1u << (24 - down);  // in half precision
+      const uint32_t f2x = down == 24 ? 0u : f | f << 16;
+      for (int i = lane; i < k.r0 * g.d / 16; i += 32) {
+        uint4 *at16 = reinterpret_cast<uint4 *>(rows) + i;
+        uint4 v = *at16;
+        uint32_t *w = &v.x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t lo, hi;
+          halves4(w[j], lo, hi);
+          asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(lo) : "r"(f2x));
+          asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(hi) : "r"(f2x));
+          w[j] = (uint32_t)codes_of_halves(lo) | (uint32_t)codes_of_halves(hi) << 16;
+        }
+        *at16 = v;
+      }
     }
-    if (live) {
+    if (lane == 0) scales[sc] = (uint8_t)(e + 127);
+    const float f = pow2(-e);
 #pragma unroll
-      for (int i = 0; i < V / 2; ++i) {
-        const float2 u = pack::split(x[p][i]), w = pack::split(y[p][i]);
-        const float v[4] = {u.x, u.y, w.x, w.y};
+    for (int p = 0; p < kPasses; ++p) {
+      if (!live(k, p)) continue;
+      f2 x[V / 2], y[V / 2];
+      values(g, s, k, p, norm[p], cs, sn, x, y);
+      uint32_t ca[V / 4], cb[V / 4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (finite1(v[j])) most = fmaxf(most, fabsf(v[j]));
+      for (int h = 0; h < 2; ++h) {
+        const f2 *z = h ? y : x;
+        uint32_t *out = h ? cb : ca;
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) {
+          const float2 u = pack::split(z[2 * i]), w = pack::split(z[2 * i + 1]);
+          float v[4] = {u.x, u.y, w.x, w.y};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = finite1(v[j]) ? v[j] * f : __int_as_float(0x7fc00000);  // held as NaN
+          out[i] = (uint32_t)codes_of(v[0], v[1]) | (uint32_t)codes_of(v[2], v[3]) << 16;
+        }
+      }
+      uint8_t *dst = rows + (p * at_once + row0) * g.d;
+      if constexpr (V == 8) {
+        *reinterpret_cast<uint2 *>(dst + at.a) = make_uint2(ca[0], ca[1]);
+        *reinterpret_cast<uint2 *>(dst + at.b) = make_uint2(cb[0], cb[1]);
+      } else {
+        *reinterpret_cast<uint32_t *>(dst + at.a) = ca[0];
+        *reinterpret_cast<uint32_t *>(dst + at.b) = cb[0];
       }
     }
   }
-  // a <= 448 2^e = 1.75 2^(8 + e)
-  const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(most));
-  const bool older = k.r0 > 0;
-  int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-  e = min(max(e, kMinExp), kMaxExp);
-  if (older) e = max(e, before);
-  const long long row_at = (((long long)page * g.cache.heads + head) * g.cache.page + (k.key & (g.cache.page - 1))) * g.d;
-  uint8_t *rows = codes + row_at;
-  if (older && e > before) {  // the older keys' codes, by 2^(before - e)
-    const int down = min(e - before, 24);  // (beyond, all codes become zero)
-    const uint32_t f = down <= 14 ? (uint32_t)(15 - down) << 10 : 1u << (24 - down);  // in half precision
-    const uint32_t f2x = down == 24 ? 0u : f | f << 16;
-    for (int i = lane; i < k.r0 * g.d / 16; i += 32) {
-      uint4 *p = reinterpret_cast<uint4 *>(rows) + i;
-      uint4 v = *p;
-      uint32_t *w = &v.x;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t lo = halves((uint16_t)w[j]), hi = halves((uint16_t)(w[j] >> 16));
-        asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(lo) : "r"(f2x));
-        asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(hi) : "r"(f2x));
-        w[j] = (uint32_t)codes_of_halves(lo) | (uint32_t)codes_of_halves(hi) << 16;
-      }
-      *p = v;
-    }
-  }
-  if (lane == 0) scales[sc] = (uint8_t)(e + 127);
-  const float f = pow2(-e);
-#pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
-    const int r = p * at_once + row0;
-    if (!(holds && r >= k.r0 && r < k.r1)) continue;
-    uint32_t ca[V / 4], cb[V / 4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f2 *z = h ? y[p] : x[p];
-      uint32_t *out = h ? cb : ca;
-#pragma unroll
-      for (int i = 0; i < V / 4; ++i) {
-        const float2 u = pack::split(z[2 * i]), w = pack::split(z[2 * i + 1]);
-        float v[4] = {u.x, u.y, w.x, w.y};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = finite1(v[j]) ? v[j] * f : __int_as_float(0x7fc00000);  // held as NaN
-        out[i] = (uint32_t)codes_of(v[0], v[1]) | (uint32_t)codes_of(v[2], v[3]) << 16;
-      }
-    }
-    uint8_t *dst = rows + r * g.d;
-    if constexpr (V == 8) {
-      *reinterpret_cast<uint2 *>(dst + at.a) = make_uint2(ca[0], ca[1]);
-      *reinterpret_cast<uint2 *>(dst + at.b) = make_uint2(cb[0], cb[1]);
-    } else {
-      *reinterpret_cast<uint32_t *>(dst + at.a) = ca[0];
-      *reinterpret_cast<uint32_t *>(dst + at.b) = cb[0];
-    }
-  }
-}
+};
 
 template <typename T, int V, bool PAIRS, bool NORM>
-__global__ void __launch_bounds__(kRotThreads, 2) k_append8(const __grid_constant__ Append8Args a) {
+__global__ void __launch_bounds__(kRotThreads, 3) k_append8(const __grid_constant__ Append8Args a) {
   __shared__ __align__(16) float cs[kMaxTrig], sn[kMaxTrig];
   __shared__ long long home[kMaxTokens];
   const RotArgs &g = a.g;
   pdl_wait();  // q, k, v come from the kernel before
-  if ((int)blockIdx.x >= a.blocks) {
-    rotate_rows<T, V, PAIRS, NORM>(g, blockIdx.x - a.blocks, cs, sn, home);
+  const int nth = blockIdx.x / a.every, all = a.blocks * a.parts;
+  if (nth >= all || nth * a.every != (int)blockIdx.x) {
+    rotate_rows<T, V, PAIRS, NORM>(g, blockIdx.x - min(nth + 1, all), cs, sn, home);
     return;
   }
   const CacheView &c = g.cache;
-  const NewBlock k = find_new_block(c, blockIdx.x);
+  const NewBlock k = find_new_block(c, nth / a.parts);
+  // the first head's rows asked for before the page and the angles
+  constexpr int kWarps = kRotThreads / 32;
+  const int warp = threadIdx.x >> 5, step = a.parts * kWarps;
+  int u = nth % a.parts * kWarps + warp;
+  BlockRows<T, V, PAIRS> rows(g);
+  auto load = [&]() {
+    const bool val = u >= c.heads;
+    if (u < 2 * c.heads) rows.load(val ? g.seg[2] : g.seg[1], k, val ? u - c.heads : u);
+  };
+  if (k.seq >= 0) load();
   const int page = k.seq >= 0 ? page_of(c, k.seq, k.key) : -1;
   if (g.err && threadIdx.x == 0 && (k.lost || (k.seq >= 0 && page < 0))) atomicOr(g.err, TR_CACHE_ERR_PAGE);
   if (page < 0) return;
@@ -204,10 +242,12 @@ __global__ void __launch_bounds__(kRotThreads, 2) k_append8(const __grid_constan
     fill_trig(g, k.tok0 + k.r0, k.r1 - k.r0, cs, sn);
     __syncthreads();
   }
-  for (int u = threadIdx.x >> 5; u < 2 * c.heads; u += kRotThreads / 32) {
+  while (u < 2 * c.heads) {
     const bool val = u >= c.heads;
-    put_block<T, V, PAIRS>(a, val ? g.seg[2] : g.seg[1], k, page, val ? u - c.heads : u,
-                           static_cast<uint8_t *>(val ? c.v : c.k), val ? a.scale.v : a.scale.k, cs, sn);
+    rows.put(g, val ? g.seg[2] : g.seg[1], k, page, val ? u - c.heads : u, static_cast<uint8_t *>(val ? c.v : c.k),
+             val ? a.scale.v : a.scale.k, cs, sn);
+    u += step;
+    load();
   }
 }
 
@@ -215,7 +255,12 @@ template <typename T, int V, bool PAIRS>
 cudaError_t launch_append8_t(Append8Args &a, cudaStream_t st) {
   Append8Args q = a;
   q.g.seg[1] = q.g.seg[2] = Rows{};
-  const int ctas = a.blocks + (a.g.seg[0].in ? cut_segments(q.g) : 0);
+  // a block's heads over several CTAs while the SMs (three CTAs each) would not all get some
+  const int sms = sm_count() > 0 ? sm_count() : 1, rounds = (2 * a.g.cache.heads + kRotThreads / 32 - 1) / (kRotThreads / 32);
+  a.parts = a.blocks ? 3 * sms / a.blocks : 1;
+  a.parts = a.parts < 1 ? 1 : a.parts > rounds ? rounds : a.parts;
+  const int all = a.blocks * a.parts, ctas = all + (a.g.seg[0].in ? cut_segments(q.g) : 0);
+  a.every = all ? ctas / all : 1;
   if (ctas == 0) return cudaSuccess;  // no sequence, fewer rows than a block's, no queries
   a.g.seg[0] = q.g.seg[0];
   a.g.seg[1].cta0 = a.g.seg[2].cta0 = INT_MAX;  // (of the queries' CTAs: none is for keys or values)

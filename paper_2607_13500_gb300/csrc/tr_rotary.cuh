@@ -228,7 +228,7 @@ __device__ __forceinline__ void fill_trig(const RotArgs &g, int t0, int nt, floa
 // segment, whose weight, where to: a third more time, 26.3 us against 20.0 us,
 // for 6272 tokens x 32 normed heads when both were tried, on inputs in L2.)
 // (cs, sn: kMaxTrig floats of shared memory each; home: kMaxTokens keys' rows.)
-template <typename T, int V, bool PAIRS, bool NORM>
+template <typename T, int V, bool PAIRS, bool NORM, int kU = NORM ? 2 : 4>
 __device__ __forceinline__ void rotate_rows(const RotArgs &g, int block, float *cs, float *sn, long long *home) {
   const int sg = block < g.seg[1].cta0 ? 0 : block < g.seg[2].cta0 ? 1 : 2;
   const Rows &s = sg == 0 ? g.seg[0] : sg == 1 ? g.seg[1] : g.seg[2];
@@ -240,7 +240,6 @@ __device__ __forceinline__ void rotate_rows(const RotArgs &g, int block, float *
   const SlotPlace at = slot_place<V, PAIRS>(slot, g.half);
   const char *src = s.in + (long long)sizeof(T) * ((long long)t0 * s.in_tok + at.a);
   const int ab = (int)sizeof(T) * (at.b - at.a);
-  constexpr int kU = NORM ? 2 : 4;
   Chunk<T, V> na[kU], nb[kU];
   RowWalk ahead(group, heads);
   auto ask = [&]() {
