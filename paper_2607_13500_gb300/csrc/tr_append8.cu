@@ -41,18 +41,23 @@ struct NewBlock {
 };
 __device__ __forceinline__ NewBlock find_new_block(const CacheView &c, int slot) {
   const int lane = threadIdx.x & 31;
-  int b = -1;
+  int b = -1, t0 = 0, end = 0, len = 0;  // of the last sequence whose slots start at or before this one
   for (int i0 = 0; i0 < c.batch; i0 += 32) {
     const int i = i0 + lane;
-    const bool before = i < c.batch && (long long)(__ldg(c.cu_new + i) / kBlock) + 2ll * i <= slot;
-    const unsigned m = __ballot_sync(0xffffffffu, before);
-    b += __popc(m);
+    int from = 0, to = 0, n = 0;
+    if (i < c.batch) from = __ldg(c.cu_new + i), to = __ldg(c.cu_new + i + 1), n = __ldg(c.lens + i);
+    const unsigned m = __ballot_sync(0xffffffffu, i < c.batch && (long long)(from / kBlock) + 2ll * i <= slot);
+    if (m) {
+      const int src = __popc(m) - 1;
+      b = i0 + src;
+      t0 = __shfl_sync(0xffffffffu, from, src), end = __shfl_sync(0xffffffffu, to, src), len = __shfl_sync(0xffffffffu, n, src);
+    }
     if (m != 0xffffffffu) break;
   }
   NewBlock k{-1, 0, 0, 0, 0, false};
   if (b < 0) return k;
-  const int t0 = __ldg(c.cu_new + b), end = __ldg(c.cu_new + b + 1), t1 = min(end, c.total_new);
-  const long long base = (long long)max(__ldg(c.lens + b), 0) - end + t0;  // key of token t0
+  const int t1 = min(end, c.total_new);
+  const long long base = (long long)max(len, 0) - end + t0;  // key of token t0
   const long long nth = slot - (t0 / kBlock + 2ll * b);
   if (t0 < 0 || t1 <= t0 || nth < 0) return k;
   k.lost = base < 0 && nth == 0;
@@ -126,7 +131,8 @@ struct BlockRows {
     const int lane = threadIdx.x & 31;
     const long long sc = scale_at(g.cache, page, head, k.key & (g.cache.page - 1));
     const int before = exp_of(scales[sc]);
-    float norm[kPasses], most = 0.f;
+    float norm[kPasses];
+    uint32_t most = 0u;  // largest magnitude, as fp32 bits
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
       f2 x[V / 2], y[V / 2];
@@ -145,15 +151,32 @@ struct BlockRows {
 #pragma unroll
         for (int i = 0; i < V / 2; ++i) {
           const float2 u = pack::split(x[i]), w = pack::split(y[i]);
-          const float v[4] = {u.x, u.y, w.x, w.y};
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (finite1(v[j])) most = fmaxf(most, fabsf(v[j]));
+          most = max(max(most, __float_as_uint(u.x) & 0x7fffffffu), __float_as_uint(u.y) & 0x7fffffffu);
+          most = max(max(most, __float_as_uint(w.x) & 0x7fffffffu), __float_as_uint(w.y) & 0x7fffffffu);
         }
       }
     }
     // a <= 448 2^e = 1.75 2^(8 + e)
-    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(most));
+    uint32_t top = __reduce_max_sync(0xffffffffu, most);
+    const bool bad = top >= 0x7f800000u;  // some are not finite: of the others then
+    if (bad) {
+      most = 0u;
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        f2 x[V / 2], y[V / 2];
+        if (!live(k, p)) continue;
+        values(g, s, k, p, norm[p], cs, sn, x, y);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+          const float2 u = pack::split(x[i]), w = pack::split(y[i]);
+          const float v[4] = {u.x, u.y, w.x, w.y};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (finite1(v[j])) most = max(most, __float_as_uint(v[j]) & 0x7fffffffu);
+        }
+      }
+      top = __reduce_max_sync(0xffffffffu, most);
+    }
     const bool older = k.r0 > 0;
     int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
     e = min(max(e, kMinExp), kMaxExp);
@@ -193,11 +216,13 @@ struct BlockRows {
         uint32_t *out = h ? cb : ca;
 #pragma unroll
         for (int i = 0; i < V / 4; ++i) {
-          const float2 u = pack::split(z[2 * i]), w = pack::split(z[2 * i + 1]);
-          float v[4] = {u.x, u.y, w.x, w.y};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = finite1(v[j]) ? v[j] * f : __int_as_float(0x7fc00000);  // held as NaN
-          out[i] = (uint32_t)codes_of(v[0], v[1]) | (uint32_t)codes_of(v[2], v[3]) << 16;
+          const float2 u = pack::split(pack::mul(z[2 * i], pack::make(f, f))), w = pack::split(pack::mul(z[2 * i + 1], pack::make(f, f)));
+          out[i] = (uint32_t)codes_of(u.x, u.y) | (uint32_t)codes_of(w.x, w.y) << 16;
+          if (bad) {  // held as NaN (an infinite one would be the largest code)
+            const float nan = __int_as_float(0x7fc00000);
+            out[i] = (uint32_t)codes_of(finite1(u.x) ? u.x : nan, finite1(u.y) ? u.y : nan) |
+                     (uint32_t)codes_of(finite1(w.x) ? w.x : nan, finite1(w.y) ? w.y : nan) << 16;
+          }
         }
       }
       uint8_t *dst = rows + (p * at_once + row0) * g.d;
