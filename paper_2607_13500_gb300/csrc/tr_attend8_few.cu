@@ -24,17 +24,26 @@ namespace {
 using namespace attend8;
 using namespace attend::few;
 
-constexpr int kAllThreads = 32 * (kWarps + 4);  // consumers, the producers of K and of V, two more for whole warpgroups
+constexpr int kAllThreads = 32 * (kWarps + 4);  // consumers, the producers of K, of V and of queries, one more for whole warpgroups
+
+// What a piece needs besides tiles, as the consumers' lanes take it.
+template <int D>
+struct Queries {
+  uint4 q[D / 16][32];           // fragments of the first product, halves
+  float scale[2][32];            // what a score of the lane's two rows is multiplied by, K's scale apart
+  uint32_t blocks[kWarps][32];   // scales of each warp's two blocks of its first 16 tiles, in two lanes each
+};
 
 template <int D>
 struct Few8 {
   static constexpr int kTileBytes = kTile * D;
+  static constexpr int kQueryBytes = 2 * (int)sizeof(Queries<D>);  // the present piece's and the next one's
   // Rows joined at a time, each quarter of a row 4 floats on, so that a phase's stores lie in different banks.
   static constexpr int kRows = 8, kJoinRow = D + 16;
   static constexpr int kJoinBytes = kWarps * kRows * kJoinRow * 4;
-  static constexpr int kFit = (227 * 1024 - 4096 - 1024 - kJoinBytes) / kTileBytes;
+  static constexpr int kFit = (227 * 1024 - 4096 - 1024 - kJoinBytes - kQueryBytes) / kTileBytes;
   static constexpr int kStages = kFit < 16 ? kFit : 16;
-  static constexpr size_t kSmem = (size_t)kStages * kTileBytes + kJoinBytes + 1024 + 4096;
+  static constexpr size_t kSmem = (size_t)kStages * kTileBytes + kJoinBytes + kQueryBytes + 1024 + 512;
 };
 
 constexpr float kLift = 6.f;   // probabilities are taken times 2^6 (and grow by 2^8 at most)
@@ -60,7 +69,10 @@ __global__ void __launch_bounds__(kAllThreads, 1)
   __shared__ int bad, share0, share_units;  // bad: values were taken out of a tile
   const uint32_t base = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
   float *join = reinterpret_cast<float *>(smem_raw + (base - tc::smem_u32(smem_raw)) + F::kStages * F::kTileBytes);
-  const uint32_t bars = tc::smem_u32(join) + F::kJoinBytes;
+  Queries<D> *queries = reinterpret_cast<Queries<D> *>(reinterpret_cast<unsigned char *>(join) + F::kJoinBytes);
+  const uint32_t bars = tc::smem_u32(join) + F::kJoinBytes + F::kQueryBytes;
+  auto q_full = [&](int i) { return bars + 8u * (2 * F::kStages + i); };
+  auto q_empty = [&](int i) { return bars + 8u * (2 * F::kStages + 2 + i); };
   // (the warp's index by shuffle: the compiler then knows it to be uniform)
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
@@ -70,6 +82,10 @@ __global__ void __launch_bounds__(kAllThreads, 1)
     for (int s = 0; s < F::kStages; ++s) {
       tc::mbar_init(ring.full(s), 1);
       tc::mbar_init(ring.empty(s), kWarps / 2);
+    }
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(q_full(i), 1);
+      tc::mbar_init(q_empty(i), kWarps);
     }
     tc::mbar_fence_init();
     tc::tma_prefetch_map(&map_k);
@@ -87,9 +103,97 @@ __global__ void __launch_bounds__(kAllThreads, 1)
   if (threadIdx.x == 0) share0 = share, share_units = share_end - share;  // for the consumers' second walk
   w.seek(g, runs, run0, share, share_end);
 
+  // Of the share's tiles warps 0 to 3 take the even ones and 4 to 7 the odd
+  // ones, a quarter each: 32 keys, two blocks.  The block of warp x's nth tile
+  // (of a piece that `tiles` came before; nth and the 15 on) that the lane holds
+  // the scales of:
+  constexpr int kPieces = D / 64;          // 16-byte pieces of a key's row a lane takes
+  constexpr int kTiles = D / 8;            // n-tiles of the second product
+  const int gq = lane >> 2, c = lane & 3;  // quad (row or key of a fragment), lane of the quad
+  auto key_of = [&](int x, int tiles, int tile, int count, int len, int nth) {
+    const int n = ((tiles ^ (x >> 2)) & 1) + 2 * (nth + (lane >> 1));
+    return n < count ? (tile + n) * kTile + 32 * (x & 3) + 16 * (lane & 1) : len;
+  };
   if (warp >= kWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp >= kWarps + 2) return;
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == kWarps + 2) {
+      // ---------------------------------------------------------------- queries, and each piece's first scales
+      // By a warp of its own, a piece ahead: what a piece needs takes two waits
+      // for memory one after the other, and a row's largest magnitude.
+      int n = 0, tiles = 0;
+      while (w.next(g)) {
+        const int hk = w.item % g.c.heads, block0 = w.item / g.c.heads * kFewRows;
+        const int rows = min(kFewRows, w.s.rows - block0);
+        int page[kWarps];
+#pragma unroll
+        for (int x = 0; x < kWarps; ++x) {
+          const int j = key_of(x, tiles, w.tile, w.count, w.s.len, 0), i = j >> g.page_log2;
+          page[x] = j < w.s.len && i < g.c.max_pages ? __ldg(g.c.table + (long long)w.seq() * g.c.max_pages + i) : -1;
+        }
+        uint32_t raw[2][kPieces * 8];  // the lane's channels of its two rows
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = gq + 8 * i, row = block0 + r;
+          const bool valid = r < rows;
+          const int tok = valid ? row / g.group : 0, head = hk * g.group + (valid ? row - tok * g.group : 0);
+          const char *qrow = g.q + 2 * ((long long)(w.s.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
+#pragma unroll
+          for (int s = 0; s < 2 * kPieces; ++s) {
+            const int ch = kPieces * c * 16 + 8 * s;
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (valid && ch < g.c.d) v = *reinterpret_cast<const uint4 *>(qrow + 2 * ch);
+            raw[i][4 * s] = v.x, raw[i][4 * s + 1] = v.y, raw[i][4 * s + 2] = v.z, raw[i][4 * s + 3] = v.w;
+          }
+        }
+        uint32_t blocks[kWarps];
+#pragma unroll
+        for (int x = 0; x < kWarps; ++x) {
+          const int j = key_of(x, tiles, w.tile, w.count, w.s.len, 0);
+          blocks[x] = (unsigned)page[x] < (unsigned)g.c.pages ? scales_at(p, scale_at(g.c, page[x], hk, j & (g.c.page - 1))) : kNoScales;
+        }
+        Queries<D> &out = queries[n & 1];
+        if (!tc::mbar_wait_warp(q_empty(n & 1), (n >> 1 & 1) ^ 1)) {
+          if (lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+          break;
+        }
+#pragma unroll
+        for (int x = 0; x < kWarps; ++x) out.blocks[x][lane] = blocks[x];
+        const uint32_t flip = g.negate ? 0x80008000u : 0u;
+        float down[2] = {1.f, 1.f};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float scale = g.scale;
+          if (Bits<T>::kBf16) {
+            uint32_t most = 0u;
+#pragma unroll
+            for (int k = 0; k < 8 * kPieces; ++k) most = max(most, top_of_pair(raw[i][k]));
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const int e = query_exp(most);
+            down[i] = pow2(-e);
+            scale *= pow2(e);
+          }
+          out.scale[i][lane] = scale;
+        }
+#pragma unroll
+        for (int m = 0; m < 4 * kPieces; ++m) {
+          // a0, a2: the row g's first and second pair of channels 4 m .. 4 m + 3 of the lane's; a1, a3: row g + 8's
+          uint32_t a[4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            a[i] = (Bits<T>::kBf16 ? query_pair(raw[i][2 * m], down[i]) : raw[i][2 * m]) ^ flip;
+            a[2 + i] = (Bits<T>::kBf16 ? query_pair(raw[i][2 * m + 1], down[i]) : raw[i][2 * m + 1]) ^ flip;
+          }
+          out.q[m][lane] = make_uint4(a[0], a[1], a[2], a[3]);
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(q_full(n & 1));
+        tiles += w.count;
+        ++n;
+      }
+      return;
+    }
+    if (warp > kWarps + 2) return;
     ring.take(warp - kWarps);
     const CUtensorMap *map = warp == kWarps ? &map_k : &map_v;
     bool ok = true;
@@ -109,66 +213,32 @@ __global__ void __launch_bounds__(kAllThreads, 1)
   }
 
   // ------------------------------------------------------------------ consumers
-  // Of the share's tiles warps 0 to 3 take the even ones and 4 to 7 the odd
-  // ones, a quarter each: 32 keys, two blocks.
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");  // (with 56 what 168 at launch give)
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");  // (with 88 what 168 at launch give)
   const int odd = warp >> 2, quarter = warp & 3;
-  constexpr int kPieces = D / 64;          // 16-byte pieces of a key's row a lane takes
-  constexpr int kTiles = D / 8;            // n-tiles of the second product
-  const int gq = lane >> 2, c = lane & 3;  // quad (row or key of a fragment), lane of the quad
   int kst = Ring::first(0), vst = Ring::first(1);
   uint32_t kph = 0, vph = 0;
   int tiles = 0;   // of the share so far
   bool ok = true;  // once a wait has timed out the warp only keeps up with the others' barriers
-  // What the present piece is, and what the next one needs from memory, asked
-  // for before the present one's results are joined.
   struct Piece {
     int hk, block0, rows, tok0, base, len, seq, tile, count;
     bool whole, starts;
   } now;
-  uint32_t raw[2][kPieces * 8];  // this lane's channels of its two rows
-  int page0;                     // page of the first block that it holds the scales of
-  auto key_of = [&](const Piece &x, int nth) {  // the block of this warp's nth tile (and the 15 on) that the lane holds
-    const int n = ((tiles ^ odd) & 1) + 2 * (nth + (lane >> 1));
-    return n < x.count ? (x.tile + n) * kTile + 32 * quarter + 16 * (lane & 1) : x.len;
-  };
-  auto ask = [&](Piece &x) {
+  auto next_piece = [&](Piece &x) {
     if (!w.next(g)) return false;
     x.hk = w.item % g.c.heads, x.block0 = w.item / g.c.heads * kFewRows;
     x.rows = min(kFewRows, w.s.rows - x.block0);
     x.tok0 = w.s.tok0, x.base = w.s.base, x.len = w.s.len, x.seq = w.seq();
     x.tile = w.tile, x.count = w.count, x.whole = w.whole, x.starts = w.starts;
-    const int j = key_of(x, 0);
-    page0 = j < x.len && (j >> g.page_log2) < g.c.max_pages ? __ldg(g.c.table + (long long)x.seq * g.c.max_pages + (j >> g.page_log2)) : -1;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = gq + 8 * i, row = x.block0 + r;
-      const bool valid = r < x.rows;
-      const int tok = valid ? row / g.group : 0, head = x.hk * g.group + (valid ? row - tok * g.group : 0);
-      const char *qrow = g.q + 2 * ((long long)(x.tok0 + tok) * g.q_tok + (long long)head * g.q_head);
-#pragma unroll
-      for (int s = 0; s < 2 * kPieces; ++s) {
-        const int ch = kPieces * c * 16 + 8 * s;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (valid && ch < g.c.d) v = *reinterpret_cast<const uint4 *>(qrow + 2 * ch);
-        raw[i][4 * s] = v.x, raw[i][4 * s + 1] = v.y, raw[i][4 * s + 2] = v.z, raw[i][4 * s + 3] = v.w;
-      }
-    }
     return true;
   };
-  int turn = 0;  // of the pieces
-  for (bool more = ask(now); more; turn ^= 1) {
-    // scales of this warp's two blocks of the first 16 of its tiles, in two lanes each
-    auto scales = [&](int nth) { return block_scales(p, now.seq, now.hk, now.len, key_of(now, nth)); };
-    uint32_t ahead = kNoScales;
-    if ((unsigned)page0 < (unsigned)g.c.pages)
-      ahead = scales_at(p, scale_at(g.c, page0, now.hk, key_of(now, 0) & (g.c.page - 1)));
-    float held_k = 1.f;   // 2^e of keys
-    int held_v = kNoExp;  // e of values
+  int nth_piece = 0;
+  for (bool more = next_piece(now); more; ++nth_piece) {
+    const int turn = nth_piece & 1;
+    auto scales = [&](int nth) {
+      return block_scales(p, now.seq, now.hk, now.len, key_of(warp, tiles, now.tile, now.count, now.len, nth));
+    };
     // this lane's two rows of a fragment, and the keys they see
     int lo[2], hi[2];
-    float fr[2];                 // what a score of the row is multiplied by, K's scale apart
-    uint32_t q[kPieces * 4][4];  // fragments of the first product: channels 4 m .. 4 m + 3 of a piece
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = gq + 8 * i;
@@ -176,26 +246,24 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       const int own = now.base + (valid ? (now.block0 + r) / g.group : 0);
       hi[i] = !valid ? INT_MAX : g.causal ? min(now.len, own + 1) : now.len;
       lo[i] = valid && g.window > 0 ? window_start(own, g.window) : 0;
-      fr[i] = g.scale;
-      float down = 1.f;
-      if (Bits<T>::kBf16) {
-        uint32_t most = 0u;
-#pragma unroll
-        for (int k = 0; k < 8 * kPieces; ++k) most = max(most, top_of_pair(raw[i][k]));
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        const int e = query_exp(most);
-        down = pow2(-e);
-        fr[i] *= pow2(e);
-      }
-      const uint32_t flip = g.negate ? 0x80008000u : 0u;
-#pragma unroll
-      for (int m = 0; m < 4 * kPieces; ++m) {
-        // a0, a2: the row g's first and second pair; a1, a3: row g + 8's
-        q[m][i] = (Bits<T>::kBf16 ? query_pair(raw[i][2 * m], down) : raw[i][2 * m]) ^ flip;
-        q[m][2 + i] = (Bits<T>::kBf16 ? query_pair(raw[i][2 * m + 1], down) : raw[i][2 * m + 1]) ^ flip;
-      }
     }
+    if (ok) {
+      ok = tc::mbar_wait_warp(q_full(turn), (uint32_t)(nth_piece >> 1) & 1u);
+      if (!ok && lane == 0) flag(g, TR_CACHE_ERR_WAIT);
+    }
+    const Queries<D> &in = queries[turn];
+    uint32_t q[kPieces * 4][4];
+#pragma unroll
+    for (int m = 0; m < 4 * kPieces; ++m) {
+      const uint4 v = in.q[m][lane];
+      q[m][0] = v.x, q[m][1] = v.y, q[m][2] = v.z, q[m][3] = v.w;
+    }
+    const float fr[2] = {in.scale[0][lane], in.scale[1][lane]};
+    uint32_t ahead = in.blocks[warp][lane];
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(q_empty(turn));
+    float held_k = 1.f;   // 2^e of keys
+    int held_v = kNoExp;  // e of values
     float o[kTiles][4];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
@@ -376,7 +444,7 @@ __global__ void __launch_bounds__(kAllThreads, 1)
     // ------------------------------------------------------------------ the piece's result
     const Piece done = now;
     tiles += done.count;
-    more = ask(now);
+    more = next_piece(now);
     // (mx - kLift: what the probabilities were taken against)
     float(&top)[kWarps][kFewRows] = tops[turn], (&tot)[kWarps][kFewRows] = tots[turn];
 #pragma unroll
