@@ -529,12 +529,12 @@ constexpr int kFewItemCost = 2;      // units that an item counts besides its ti
 constexpr int kFewMaxBatch = 8192;   // sequences its unit count handles
 // Whether that kernel takes a call: its units, tiles of all blocks and key
 // heads, are counted in 31 bits.
-inline bool few_takes(const tr_cache *c, int q_heads, int max_new, int item_cost = kFewItemCost) {
+inline bool few_takes(const tr_cache *c, int q_heads, int max_new, int item_cost = kFewItemCost, int rows = kFewRows) {
   const int group = q_heads / c->heads;
   const long long most = (long long)(max_new < c->total_new ? max_new : c->total_new) * group;
   const long long blocks16 = (long long)c->total_new * group / kFewRows + c->batch;
   const long long table_tiles = ((long long)c->max_pages * c->page + kTile - 1) / kTile + item_cost;
-  return most <= kFewRows && c->batch <= kFewMaxBatch && blocks16 * c->heads <= INT_MAX / table_tiles;
+  return most <= rows && c->batch <= kFewMaxBatch && blocks16 * c->heads <= INT_MAX / table_tiles;
 }
 // Workspace bytes, and the launch (work and join kernels); g.part and
 // g.part_ml are carved from ws by the launch.

@@ -666,15 +666,15 @@ Plan8 plan8_of(const tr_cache *c, int q_heads, int window, int max_new, int max_
   const int group = q_heads / c->heads;
   const long long most = (long long)(max_new < c->total_new ? max_new : c->total_new) * group;
   const int sms = sm_count() > 0 ? sm_count() : 1;
-  if (few_takes(c, q_heads, max_new, kItemCost)) {
-    p.few = true;
-    p.total = few_workspace_bytes(c->head_dim, sms);
-    return p;
-  }
   const long long cap = (long long)c->max_pages * c->page;
   long long keys = max_len < cap ? max_len : cap;
   if (window > 0 && keys > (long long)window + max_new) keys = (long long)window + max_new;
   const int tiles = (int)((keys + kTile - 1) / kTile);
+  if (few_takes(c, q_heads, max_new, kItemCost, tiles < kMinTilesFew ? kFewRows : kMostFew)) {
+    p.few = true;
+    p.total = few_workspace_bytes(c->head_dim, sms);
+    return p;
+  }
   p.mt = most <= kTile ? 1 : 2;
   p.slots = (int)((long long)c->total_new * group / (kTile * p.mt)) + c->batch + 1;  // (tokens of no sequence: one more)
   p.splits = choose_parts((double)(p.slots - 1) * c->heads, tiles, sms, (double)c->total_new * q_heads);
