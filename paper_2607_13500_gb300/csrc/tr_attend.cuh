@@ -505,16 +505,16 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
 }
 
 // Parts of the keys: as many as finish earliest when `sms` CTAs run at a
-// time, one costing its tiles and about kCtaTiles more, and the join
+// time, one costing its tiles and about cta_tiles more, and the join
 // writing and reading a row's fp32 sums once per part (kJoinRows rows in
 // the time of one tile).
-inline int choose_parts(double blocks, int tiles, int sms, double rows) {
-  constexpr double kCtaTiles = 4.0, kJoinRows = 8192.0;
+inline int choose_parts(double blocks, int tiles, int sms, double rows, double cta_tiles = 4.0) {
+  constexpr double kJoinRows = 8192.0;
   double best = 0;
   int parts = 1;
   for (int s = 1; s <= 64 && s <= (tiles > 1 ? tiles : 1); ++s) {
     const double waves = std::ceil(blocks * s / sms);
-    const double t = waves * ((tiles + s - 1) / s + kCtaTiles) + (s > 1 ? kCtaTiles + rows * s / kJoinRows : 0.0);
+    const double t = waves * ((tiles + s - 1) / s + cta_tiles) + (s > 1 ? cta_tiles + rows * s / kJoinRows : 0.0);
     if (s == 1 || t < best) {
       best = t;
       parts = s;
