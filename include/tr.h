@@ -558,10 +558,9 @@ tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *
  *
  * tr_cache8_append: a block's scale is the least one that holds the finite
  * magnitudes of the rows it gets by the call (magnitude <= 448 * scale, 10 <=
- * e <= 246), and not below the block's old one if it has keys
- * before the call's; those keys are then coded anew by the scales' quotient,
- * a power of two, which rounds nothing but what falls under the codes'
- * smallest step.  Codes are the nearest (ties to even, 448 at most); a value
+ * e <= 246), and not below the block's old one if it has keys before the
+ * call's; those keys are then coded anew by the scales' quotient, a power of
+ * two, which rounds nothing but what falls under the codes' smallest step.  Codes are the nearest (ties to even, 448 at most); a value
  * that is not finite is held as NaN.  k_weight, r, pos, q as in
  * tr_cache_append: norm and rotation in fp32, rounded once into the codes.
  * Two sequences of a call may not share a page that it writes.
@@ -577,7 +576,12 @@ tr_status tr_cache8_append(const tr_cache8 *c, const tr_heads *k, const tr_heads
 
 /*
  * Attention over it: tr_cache_attend, with the keys and values that the codes
- * stand for.
+ * stand for.  Every e from 0 to 254 is taken as it stands (255 as 254).  The
+ * products take codes, which fit exactly, queries and probabilities as halves:
+ * bf16 queries in units of a power of two of each row's own, probabilities with
+ * the values' scales on them: whole down to 2^-20, and lost below 2^-31, of the
+ * greatest that the row sees.  Scales of values below 2^-100 of the greatest
+ * that it sees may count as that.  Sums are fp32.
  */
 size_t tr_cache8_attend_workspace_bytes(const tr_cache8 *c, int32_t q_heads, int32_t window, int32_t max_new,
                                         int32_t max_len);
@@ -609,8 +613,8 @@ tr_status tr_cache8_attend(const tr_cache8 *c, const tr_heads *q, const tr_heads
  * tr_pages_truncate: sequence b keeps its first d_keep[b] tokens at most
  * (negative: none); pages that hold none of these go back to the stack in the
  * opposite of the order in which they were taken, and their entries become -1.
- * Directly after an extend, to the lengths before it, everything is as it was.  Refused as above
- * (TR_PAGES_ERR_STATE).
+ * Directly after an extend, to the lengths before it, everything is as it was.
+ * Refused as above (TR_PAGES_ERR_STATE).
  *
  * Calls on one table come one after another (a stream, or events between
  * streams); all of it may be captured and replayed.  ticket is one int32 of

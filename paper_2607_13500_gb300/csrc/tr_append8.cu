@@ -78,7 +78,7 @@ __device__ __forceinline__ bool finite1(float v) { return fabsf(v) <= 3.40282346
 // They stay in registers as they came, from the load to the codes; the norm's
 // factors are kept and the rotation is done twice, for the scale and for the
 // codes (held in fp32 instead, rows took 128 registers and two CTAs filled an
-// SM: 29.6k tokens 43 us without queries).
+// SM: 29.6k tokens with their queries 126 us against 114).
 template <typename T, int V, bool PAIRS>
 struct BlockRows {
   static constexpr int kPasses = V == 8 ? 4 : 8;

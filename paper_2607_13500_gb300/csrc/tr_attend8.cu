@@ -15,15 +15,29 @@
 // two.
 //
 // The scales enter in the softmax, where they cost eight numbers a row and
-// tile (a product of halves for each pair of codes took a fifth of the time:
-// 2048 tokens over 32768 keys 758 us against 617):
+// tile (a product of halves for each pair of codes, in the warps that turn
+// them, took longer than the tile's products: 2048 tokens over 32768 keys 758
+// us, here 701):
 //   keys    a factor of the block's 16 scores;
-//   values  with R the largest exponent of the CTA's keys, d = e - R is added
-//           to the exponents of the block's 16 probabilities, and R enters the
-//           results.  Their sum is taken block by block, times 2^-d.
-// So what enters the second product is p 2^d, 2^14 at most, rounded to halves:
-// it keeps its bits down to 2^-20 of the largest, and what is lost below is
-// 2^-31 of it.  Sums and everything else are fp32.
+//   values  d = e - R, R one exponent of the CTA's, is added to the block's 16
+//           scores, and the softmax's maximum is that of these sums: what
+//           enters the second product is p 2^d.  R enters the results, and the
+//           sum of the p is taken block by block, times 2^-d.
+// So what enters the second product, 2^14 at most, is rounded to halves: it
+// keeps its bits down to 2^-20 of what the row's greatest key adds, and what is
+// lost below is 2^-31 of it.  Sums and everything else are fp32.
+//
+// Two blocks of 128 rows share a turned tile (MT = 2); where the rows are few
+// enough for one, a CTA is one block with two score buffers.  Both have the
+// tensor cores wait for shared memory: a tile's codes are read (32 KB), written
+// as halves (64 KB) and read by each block's products (112 KB a block), 320 KB
+// for 256 rows, which at the some 90 B a clock that such a mix gets is the
+// 3700 clocks that a tile takes.
+//
+// 28 heads of 128 over 4: 2048 tokens over 32768 keys 701 us (1.33 PFLOP/s, 0.70
+// of the measured cuBLAS); 5 tokens of 32 sequences over 1000 to 12000 keys (35
+// rows a key head, MT = 1) 86 us; chunks of 784 tokens of 4 sequences over 1000
+// to 6272 keys 104 us, where each CTA's start and end, 11 us, tell.
 #include <atomic>
 #include <cmath>
 
@@ -56,8 +70,13 @@ struct Shape8 {
 };
 
 constexpr float kLift8 = 6.f;   // probabilities are taken times 2^6 (and grow by 2^8 at most)
-constexpr int kNone = -1000;    // R without a block
-constexpr int kLeast = -60;     // of d: a block below adds nothing to the product, but to the sum
+// d is between kLeast and kMost, so that 2^-d and its sums are fp32 numbers: R
+// is the largest exponent of the CTA's blocks, or so much lower that the
+// smallest (but for blocks of zeros) is kLeast above it.  Keys that a row does
+// not see leave its results as they are; keys that it sees are taken to be
+// 2^kLeast of its greatest at least.
+constexpr int kLeast = -100, kMost = 136;
+constexpr int kZeros = -117;  // the exponent of a block of zeros, as the append leaves it
 
 // What the softmax needs of a tile's blocks.
 struct TileScales {
@@ -171,7 +190,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
   auto scale_full = [&](int s) { return scale_bars + 8u * s; };
   const uint32_t tmem_slot = scale_bars + 32u;
   __shared__ int bad_values;     // some were taken out of the tiles
-  __shared__ int ref_of[4], ref; // R
+  __shared__ int top_of[4], low_of[4], ref;  // largest and smallest exponents, R
   // Of tile t in slot t % 4: when the codes of tile t + 4 are turned, the
   // scores of tile t + 2 are done, and with them the softmax of tile t.
   __shared__ __align__(16) TileScales tile_scales[4];
@@ -267,21 +286,24 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
     } else if (warp >= 4 * MT + 4) {
       // ---------------------------------------------------------------- codes to halves
       const int w = warp - 4 * MT - 4;  // its rows: 32 w to 32 w + 31 of each tile
-      int most = kNone;
+      int top = -127, low = 127;
       const int blocks = min(8 * t1, (k.len + kBlock - 1) / kBlock);
 #pragma unroll 4
       for (int i = 8 * t0 + 32 * w + lane; i < blocks; i += 128) {
         const uint32_t s = block_scales(p, k.seq, hk, k.len, kBlock * i);
-        if (s != kNoScales) most = max(most, (int)(s >> 8) - 127);
+        const int e = s != kNoScales ? (int)(s >> 8) - 127 : -127;
+        top = max(top, e);
+        if (e > kZeros) low = min(low, e);
       }
-      most = __reduce_max_sync(0xffffffffu, most);
+      top = __reduce_max_sync(0xffffffffu, top), low = __reduce_min_sync(0xffffffffu, low);
+      int r = 0;  // R
       if (t0 < t1) {
-        if (lane == 0) ref_of[w] = most;
+        if (lane == 0) top_of[w] = top, low_of[w] = low;
         codes_sync();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = max(most, ref_of[i]);
-        if (most == kNone) most = 0;
-        if (w == 0 && lane == 0) ref = most;
+        for (int i = 0; i < 4; ++i) top = max(top, top_of[i]), low = min(low, low_of[i]);
+        r = min(top, low - kLeast);
+        if (w == 0 && lane == 0) ref = r;
       }
       // scales of 16 tiles at a time, this warp's two blocks of one tile in two lanes
       auto scales = [&](int t) {
@@ -304,10 +326,10 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
           const uint32_t s = t - held0 < 16 ? s0 : s1;
           if (lane < 2) {
             TileScales &out = tile_scales[n & 3];
-            const int d = s >> 8 < 255u ? max((int)(s >> 8) - 127 - most, kLeast) : 0;
+            const int d = min(max((s >> 8 < 255u ? (int)(s >> 8) - 127 : -127) - r, kLeast), kMost);
             out.k[2 * w + lane] = pow2((int)(s & 0xffu) - 127);
             out.v[2 * w + lane] = (float)d;
-            out.undo[2 * w + lane] = pow2(-d);
+            out.undo[2 * w + lane] = pow2(-d / 2) * pow2(-d - -d / 2);
           }
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(scale_full(n & 3));
@@ -500,7 +522,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
               undo[b] = __uint_as_float(z.x), undo[b + 1] = __uint_as_float(z.y), undo[b + 2] = __uint_as_float(z.z), undo[b + 3] = __uint_as_float(z.w);
             }
 #pragma unroll
-            for (int b = 0; b < 8; ++b) f[b] = fmaxf(row_scale * f[b], 1e-30f);  // (not zero: masked scores are -inf)
+            for (int b = 0; b < 8; ++b) f[b] = fminf(fmaxf(row_scale * f[b], 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
           }
 #pragma unroll
           for (int i = 0; i < kTile; i += 32) tc::tmem_ld32_wait(s + i);
@@ -517,7 +539,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
             float top0 = max3(__uint_as_float(s[16 * b]), s[16 * b + 1], s[16 * b + 2]), top1 = __uint_as_float(s[16 * b + 3]);
 #pragma unroll
             for (int i = 4; i < 16; i += 4) top0 = max3(top0, s[16 * b + i], s[16 * b + i + 1]), top1 = max3(top1, s[16 * b + i + 2], s[16 * b + i + 3]);
-            tops[b] = fmaxf(top0, top1) * f[b];
+            tops[b] = fmaf(fmaxf(top0, top1), f[b], dv[b]);
           }
           const float now = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
           if (n == 0) {
@@ -585,9 +607,10 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
       const bool parts = g.splits > 1;
       const long long all_rows = (long long)g.c.total_new * g.q_heads;
       float *prow = g.part + ((long long)split * all_rows + out_row) * g.c.d;
-      // divided by the sum before V's scale, up to 2^127, enters
-      const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-      const float up = ta < tb ? pow2(ref) : 0.f;
+      // divided by the sum before V's scale, up to 2^127, enters (a small sum: R is small too)
+      const float more = sum < 0x1p-100f ? 0x1p40f : 1.f;
+      const float inv = sum > 0.f || sum != sum ? 1.f / (sum * more) : 0.f;
+      const float up = ta < tb ? pow2(ref) * more : 0.f;
       // staged in the place of this row's queries, whose products are done
       const uint32_t stage_row = sbase + m * S::kTileBytes + row * 128;
 #pragma unroll 1
@@ -636,9 +659,9 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
       }
       if (valid) {
         const float against = mx - kLift8;  // what the probabilities were taken against
-        if (parts) g.part_ml[(long long)split * all_rows + out_row] = make_float2(against, sum);
-        else if (g.lse)
-          g.lse[out_row] = sum > 0.f || sum != sum ? against * 0.693147180559945309f + logf(sum) : -INFINITY;
+        const bool any = sum > 0.f;         // (the parts' sums, of any size, join as exponents)
+        if (parts) g.part_ml[(long long)split * all_rows + out_row] = any ? make_float2(against + log2f(sum), 1.f) : make_float2(against, sum);
+        else if (g.lse) g.lse[out_row] = any || sum != sum ? against * 0.693147180559945309f + logf(sum) : -INFINITY;
       }
     }
     if (opens) {

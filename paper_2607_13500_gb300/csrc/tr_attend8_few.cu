@@ -6,13 +6,25 @@
 // into warp-level products (m16n8k16), whose 16 keys are one block, so scales
 // cost next to nothing:
 //   K   one factor for the 16 keys' scores;
-//   V   e - R, R the largest exponent of the warp's blocks so far, is added to
-//       the exponents of the block's probabilities and taken out of their sum;
-//       when R grows, the results so far move with it, exactly.
+//   V   a factor of the block's probabilities: with m the row's maximum of the
+//       scores s and L that of s + e, a probability enters the product as
+//       2^(s - m) 2^(e + m - L), and 2^(L - m) enters the result.
 // bf16 queries enter as halves as well, each row divided by a power of two.
-// Probabilities are taken times 2^6 (2^14 at most) and rounded to halves: they
-// and the scales that they carry keep their bits down to 2^-20 of the largest,
-// and what is lost below is 2^-31 of it.
+// What enters the second product is taken times 2^6 (2^14 at most) and rounded
+// to halves: it keeps its bits down to 2^-20 of what the row's greatest key
+// adds, and what is lost below is 2^-31 of it.  (With V's scales relative to
+// the largest of the tiles, keys that a row does not see would take its bits.)
+//
+// A consumer warp takes 32 keys of every second tile of 128, so that two tiles
+// are under way and one's turning and exponentials stand beside the other's
+// products (all eight warps on 16 keys each of every tile: one token of 64
+// requests over 256 to 16384 keys 86 us, so 76).  A piece's queries and first
+// scales come from a warp of their own, a piece ahead (62, so 59).
+//
+// 28 heads of 128 over 4, bf16: those 64 requests 59 us (4.1 TB/s: ragged
+// lengths end in part tiles, and the join takes 3), with 16384 keys each 183 us
+// (5.9 TB/s, 0.88 of a copy).  One token over 611 keys, 32 heads: 12.5 us of
+// latencies in a row, and a second launch.
 #include <atomic>
 
 #include "tr_attend8.cuh"
@@ -46,9 +58,7 @@ struct Few8 {
   static constexpr size_t kSmem = (size_t)kStages * kTileBytes + kJoinBytes + kQueryBytes + 1024 + 512;
 };
 
-constexpr float kLift = 6.f;   // probabilities are taken times 2^6 (and grow by 2^8 at most)
-constexpr int kNoExp = -1000;  // R before the first block
-constexpr int kLeast = -60;    // of e - R: a block below adds nothing to the product, but to the sum
+constexpr int kLift = 6;  // what enters the second product is taken times 2^6 (and grows by 2^8 at most)
 
 __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   uint2 v;
@@ -263,14 +273,14 @@ __global__ void __launch_bounds__(kAllThreads, 1)
     __syncwarp();
     if (lane == 0) tc::mbar_arrive(q_empty(turn));
     float held_k = 1.f;   // 2^e of keys
-    int held_v = kNoExp;  // e of values
+    int held_v = 0;       // e of values
     float o[kTiles][4];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
-    float mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-    int big = kNoExp;  // R
+    // m and L, whole numbers (less than 8 too low: they follow in steps)
+    float mx[2] = {-INFINITY, -INFINITY}, wx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
 
     int nth = 0;  // of this warp's tiles
     for (int n0 = 0; ok && n0 < now.count; ++n0) {
@@ -282,7 +292,7 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       const int t = now.tile + n0;
       if ((nth & 15) == 0) {  // the next 16 tiles' scales, long before they are needed
         held_k = pow2((int)(ahead & 0xffu) - 127);
-        held_v = ahead >> 8 < 255u ? (int)(ahead >> 8) - 127 : kNoExp;
+        held_v = ahead >> 8 < 255u ? (int)(ahead >> 8) - 127 : -127;
         ahead = scales(nth + 16);
       }
       float fk[2];
@@ -373,24 +383,30 @@ __global__ void __launch_bounds__(kAllThreads, 1)
           }
         if (found) bad = 1;  // (any thread's word will do)
       }
-      float most_s[2], fs[2][2];
+      float peak[2][2], fs[2][2];  // of the lane's two rows and the two blocks
+      bool over = false;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) fs[i][h] = fminf(fmaxf(fr[i] * fk[h], 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
-        most_s[i] = fmaxf(fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1])) * fs[i][0],
-                       fmaxf(fmaxf(s[2][2 * i], s[2][2 * i + 1]), fmaxf(s[3][2 * i], s[3][2 * i + 1])) * fs[i][1]);
-        most_s[i] = fmaxf(most_s[i], __shfl_xor_sync(0xffffffffu, most_s[i], 1));
-        most_s[i] = fmaxf(most_s[i], __shfl_xor_sync(0xffffffffu, most_s[i], 2));
-      }
-      if (__any_sync(0xffffffffu, most_s[0] > mx[0] + 8.f || most_s[1] > mx[1] + 8.f)) {
+        for (int h = 0; h < 2; ++h) {
+          fs[i][h] = fminf(fmaxf(fr[i] * fk[h], 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
+          peak[i][h] = fmaxf(fmaxf(s[2 * h][2 * i], s[2 * h][2 * i + 1]), fmaxf(s[2 * h + 1][2 * i], s[2 * h + 1][2 * i + 1])) * fs[i][h];
+          over |= peak[i][h] > mx[i] + 8.f || peak[i][h] + (float)ev[h] > wx[i] + 8.f;
+        }
+      if (__any_sync(0xffffffffu, over)) {
         float f[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const bool up = most_s[i] > mx[i] + 8.f;
-          f[i] = up ? exp2_fast(mx[i] - most_s[i]) : 1.f;
-          if (up) mx[i] = most_s[i];
-          sum[i] *= f[i];
+          float m = fmaxf(peak[i][0], peak[i][1]), x = fmaxf(peak[i][0] + (float)ev[0], peak[i][1] + (float)ev[1]);
+#pragma unroll
+          for (int d = 1; d < 4; d <<= 1) {
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+          }
+          m = ceilf(m), x = ceilf(x);
+          if (m > mx[i]) sum[i] *= exp2_fast(mx[i] - m), mx[i] = m;
+          f[i] = 1.f;
+          if (x > wx[i]) f[i] = exp2_fast(wx[i] - x), wx[i] = x;
         }
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
@@ -398,33 +414,21 @@ __global__ void __launch_bounds__(kAllThreads, 1)
           o[i][2] *= f[1], o[i][3] *= f[1];
         }
       }
-      const int top_v = max(ev[0], ev[1]);
-      if (top_v > big) {  // a larger block of values
-        const float f = big - top_v < -126 ? 0.f : pow2(big - top_v);
-        big = top_v;
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[i][j] *= f;
-      }
       uint32_t pr[2][4];  // the A fragments of the second product
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        // the values' scale, 2^d, is in the exponents, and out of the sum
-        const int d = max(ev[h] - big, kLeast);
-        const float undo = pow2(-d);
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float neg = (mx[i] == -INFINITY ? 0.f : kLift - mx[i]) + (float)d, f = fs[i][h];
+          const float neg = mx[i] == -INFINITY ? 0.f : -mx[i], f = fs[i][h];
+          const float by = pow2((int)fminf(fmaxf((float)(ev[h] + kLift) + (mx[i] - wx[i]), -126.f), 127.f));
           float p0[2], p1[2];
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
             p0[n] = exp2_fast(fmaf(s[2 * h + n][2 * i], f, neg)), p1[n] = exp2_fast(fmaf(s[2 * h + n][2 * i + 1], f, neg));
-            pr[h][2 * n + i] = Bits<__half>::pack(p0[n], p1[n]);
+            pr[h][2 * n + i] = Bits<__half>::pack(p0[n] * by, p1[n] * by);
           }
-          sum[i] = fmaf((p0[0] + p1[0]) + (p0[1] + p1[1]), undo, sum[i]);
+          sum[i] += (p0[0] + p1[0]) + (p0[1] + p1[1]);
         }
-      }
 
       // ---- o += p V: n-tile i holds channels D / 8 g + i
 #pragma unroll
@@ -445,13 +449,11 @@ __global__ void __launch_bounds__(kAllThreads, 1)
     const Piece done = now;
     tiles += done.count;
     more = next_piece(now);
-    // (mx - kLift: what the probabilities were taken against)
     float(&top)[kWarps][kFewRows] = tops[turn], (&tot)[kWarps][kFewRows] = tots[turn];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
       sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
-      mx[i] -= kLift;
       if (c == 0) top[warp][gq + 8 * i] = mx[i], tot[warp][gq + 8 * i] = sum[i];
     }
     named_sync(32 * kWarps);  // (and the last piece's results are read)
@@ -465,7 +467,6 @@ __global__ void __launch_bounds__(kAllThreads, 1)
 #pragma unroll
       for (int j = 0; j < kWarps; ++j) l += top[j][r] == -INFINITY ? tot[j][r] : tot[j][r] * exp2_fast(top[j][r] - m);
     };
-    const float up = big == kNoExp ? 0.f : pow2(big);
     const int part = 2 * blockIdx.x + (done.starts ? 1 : 0);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -475,7 +476,8 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       // Sums are divided by the row's total before V's scale, up to 2^127, enters.
       float m, l;
       row_total(gq + r0, m, l);
-      const float f = (mx[i] == -INFINITY ? 0.f : exp2_fast(mx[i] - m)) * (l > 0.f || l != l ? 1.f / l : 0.f);
+      const float up = mx[i] == -INFINITY ? 0.f : exp2_fast(0.5f * (wx[i] - (float)kLift - m));  // in two steps: it may be 2^-140
+      const float f = (l > 0.f || l != l ? 1.f / l : 0.f) * up;
       // accumulator column 2 c + (j & 1) of n-tile k is channel D / 8 (2 c + (j & 1)) + k
       float *dst = join + (warp * F::kRows + gq) * F::kJoinRow + (2 * kTiles + 4) * c;
 #pragma unroll

@@ -13,6 +13,10 @@
 // and scans all sequences for itself (a few integers each, from L2) and writes
 // its part of the pages and rows; what the scans read is changed by the CTA
 // that finishes last.
+//
+// In a graph of calls: 64 sequences by a token each 4.6 us (a launch that does
+// nothing 2), 32 by 5 and back by 3 9.5 us for the two, 131000 tokens of 64
+// sequences and back 19.5 us for the two.
 #include <climits>
 #include <initializer_list>
 

@@ -213,6 +213,41 @@ def test_scales_of_any_size_side_by_side(new, spread):
     _within(lse, rl, tl, "lse")
 
 
+@pytest.mark.parametrize("new", [2, 5, 40, 300])
+@pytest.mark.parametrize("power", [30, 90])
+def test_values_that_a_row_does_not_see_take_none_of_its_bits(new, power):
+    """Key blocks before every row's window and the last one, which the last rows alone see, 2^power times the others;
+    and a block of zeros.  The tolerance is that of the keys that a row sees."""
+    lens, page, hq, hk, d, window = [640 + new], 16, 8, 2, 128, 600
+    table, pages = _table(lens, page, 61)
+    c = _cache(pages, hk, page, d, 62)
+    n, group = lens[0], hq // hk
+    at = table[0].long()
+    last = (n - 1) // 16
+    _bytes(c.v_scale)[at[0]] += power
+    _bytes(c.v_scale)[at[last]] += power
+    _bytes(c.v)[at[20]], _bytes(c.v_scale)[at[20]] = 0, 10
+    q = _randn(new, hq, d, dtype=BF, seed=63)
+    o, lse = c.attend(q, table, _i32(lens), _i32([0, new]), window=window, return_lse=True)
+    ro, rl, to, tl = _reference(c, q, table, lens, [0, new], window=window)
+    few = n - new + torch.arange(new, device=DEV) < 16 * last  # rows without a large key
+    own = (n - new + torch.arange(new, device=DEV))[few, None]
+    j = torch.arange(n, device=DEV)
+    seen = (j <= own) & (j > own - window)
+    k, v = (_held(x, s, table, 0, n) for x, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+    for h in range(hq):
+        kh, vh, qh = k[:, h // group], v[:, h // group], q[few, h].double()
+        s = (qh @ kh.T / math.sqrt(d)).masked_fill(~seen, -math.inf)
+        p, mag = torch.softmax(s, -1), vh.abs().amax(-1)
+        e = d * 2.0 ** -23 / math.sqrt(d) * ((qh.abs() @ kh.abs().T) * seen).amax(-1)
+        e = e + qh.abs().sum(-1) * 2.0 ** -38 * kh.abs().amax() / math.sqrt(d)
+        most = (p * mag).amax(-1)  # what the greatest key adds (its block's largest code is 448: within 2 of it)
+        to[few, h] = U[BF] * (p @ vh).abs() + ((2.0 ** -11 + 2 * e + 2.0 ** -17)[:, None] * (p @ vh.abs())
+                                               + (n * 2.0 ** -25 * 2 * most)[:, None])
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
+
 @pytest.mark.parametrize("new", [1, 2, 200])
 @pytest.mark.parametrize("power", [-110, -60, 60, 100])
 def test_values_far_from_one(new, power):
