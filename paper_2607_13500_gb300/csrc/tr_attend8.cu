@@ -198,8 +198,9 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
   // (the warp's index by shuffle: the compiler then knows it to be uniform)
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   pdl_wait();  // q and the cache come from the kernels before
-  const int slot = gridDim.x - 1 - blockIdx.x;  // causal chunks: the longest key ranges first
-  const int hk = blockIdx.y, split = blockIdx.z;
+  // Causal chunks: the longest key ranges first, of all heads (head by head, the
+  // last head's longest began last: chunks of 784 tokens 104.7 us).
+  const int hk = blockIdx.x % g.c.heads, slot = (gridDim.x - 1 - blockIdx.x) / g.c.heads, split = blockIdx.y;
   const Block k = find_block(g, slot, kRows);
   if (k.seq < 0) {  // (with parts of the keys the join sees to the tokens of no sequence)
     if (k.end < g.c.total_new && g.splits == 1) clear_block(g, k.end, slot, kRows, hk);
@@ -729,7 +730,7 @@ cudaError_t launch_attend8_t(const CUtensorMap &mk, const CUtensorMap &mv, const
     if (err != cudaSuccess) return err;
     g_attend8_smem_set[dev & 63].fetch_or(bit);
   }
-  return launch_kernel(k_attend8<T, D, MT>, dim3(slots, p.a.c.heads, p.a.splits), dim3(S::kThreads), S::kSmem, st, false, mk,
+  return launch_kernel(k_attend8<T, D, MT>, dim3((unsigned)slots * p.a.c.heads, p.a.splits), dim3(S::kThreads), S::kSmem, st, false, mk,
                        mv, p);
 }
 
@@ -771,9 +772,9 @@ tr_status tr_cache8_attend(const tr_cache8 *c8, const tr_heads *q, const tr_head
   if (q->heads != o->heads || q->heads % c->heads) return TR_ERR_ARG;
   if (reinterpret_cast<uintptr_t>(lse) & 3u) return TR_ERR_ALIGN;
   if ((long long)c->total_new * q->heads > INT_MAX - 65536) return TR_ERR_UNSUPPORTED;
-  if (c->heads > 65535) return TR_ERR_UNSUPPORTED;
   if (c->total_new == 0) return TR_OK;
   const Plan8 plan = plan8_of(c, q->heads, window, max_new, max_len);
+  if ((long long)plan.slots * c->heads > INT_MAX) return TR_ERR_UNSUPPORTED;
   if (plan.total && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < plan.total)) return TR_ERR_WORKSPACE;
   Attend8Args p{};
   AttendArgs &g = p.a;
