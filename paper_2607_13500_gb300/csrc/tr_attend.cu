@@ -566,7 +566,22 @@ Plan plan_of(const tr_cache *c, int q_heads, int window, int max_new, int max_le
     p.split_tiles = tiles;
     return p;
   }
-  p.splits = choose_parts((double)(p.slots - 1) * c->heads, tiles, sms, (double)c->total_new * q_heads);
+  // Parts of the keys: as many as finish earliest when `sms` CTAs run at a
+  // time, one costing its tiles and about kCtaTiles more, and the join
+  // writing and reading a row's fp32 sums once per part (kJoinRows rows in
+  // the time of one tile).
+  constexpr double kCtaTiles = 4.0, kJoinRows = 8192.0;
+  const double blocks = (double)(p.slots - 1) * c->heads;
+  double best = 0;
+  for (int s = 1; s <= 64 && s <= (tiles > 1 ? tiles : 1); ++s) {
+    const double waves = std::ceil(blocks * s / sms);
+    const double t = waves * ((tiles + s - 1) / s + kCtaTiles) +
+                     (s > 1 ? kCtaTiles + (double)c->total_new * q_heads * s / kJoinRows : 0.0);
+    if (s == 1 || t < best) {
+      best = t;
+      p.splits = s;
+    }
+  }
   p.split_tiles = (tiles + p.splits - 1) / p.splits;
   if (p.splits > 1) {
     const size_t r = (size_t)c->total_new * q_heads * p.splits;

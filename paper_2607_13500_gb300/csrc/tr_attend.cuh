@@ -504,25 +504,6 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
   if (g.lse && lane == 0) g.lse[row] = l > 0.f || l != l ? m * 0.693147180559945309f + logf(l) : -INFINITY;
 }
 
-// Parts of the keys: as many as finish earliest when `sms` CTAs run at a
-// time, one costing its tiles and about cta_tiles more, and the join
-// writing and reading a row's fp32 sums once per part (kJoinRows rows in
-// the time of one tile).
-inline int choose_parts(double blocks, int tiles, int sms, double rows, double cta_tiles = 4.0) {
-  constexpr double kJoinRows = 8192.0;
-  double best = 0;
-  int parts = 1;
-  for (int s = 1; s <= 64 && s <= (tiles > 1 ? tiles : 1); ++s) {
-    const double waves = std::ceil(blocks * s / sms);
-    const double t = waves * ((tiles + s - 1) / s + cta_tiles) + (s > 1 ? cta_tiles + rows * s / kJoinRows : 0.0);
-    if (s == 1 || t < best) {
-      best = t;
-      parts = s;
-    }
-  }
-  return parts;
-}
-
 // ---------------------------------------------------------------- few rows (tr_attend_few.cu)
 constexpr int kFewRows = 16;         // rows of a block there
 constexpr int kFewItemCost = 2;      // units that an item counts besides its tiles
