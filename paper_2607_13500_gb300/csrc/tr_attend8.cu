@@ -36,8 +36,8 @@
 //
 // 28 heads of 128 over 4: 2048 tokens over 32768 keys 701 us (1.33 PFLOP/s, 0.70
 // of the measured cuBLAS); 5 tokens of 32 sequences over 1000 to 12000 keys (35
-// rows a key head, MT = 1) 86 us; chunks of 784 tokens of 4 sequences over 1000
-// to 6272 keys 104 us, where each CTA's start and end, 11 us, tell.
+// rows a key head, MT = 1) 65 us; chunks of 784 tokens of 4 sequences over 1000
+// to 6272 keys, in fp16, 83 us, where each CTA's start and end, 11 us, tell.
 #include <atomic>
 #include <cmath>
 

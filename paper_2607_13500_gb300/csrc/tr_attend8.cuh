@@ -156,10 +156,11 @@ __device__ __forceinline__ uint32_t top_of_pair(uint32_t bf16x2) {
 }
 
 constexpr int kItemCost = 5;  // few rows: an item's own cost in tiles (see units_of); 3 and 7: 61.4 and 61.2 us against 59.3 for 64 requests' tokens
-// Rows that go there: 32 in two blocks, the second's keys from L2, where there are
-// more than 8 tiles (28 rows of 32 sequences over 1000 to 12000 keys 63 us, by
-// chunks 94; 32 rows of 64 sequences over 100 to 300 keys 37 and 26).  Three
-// blocks of 16384 keys take longer than a chunk.
+// Rows that go there: 32 in two blocks, the second's keys from L2, where there
+// are more than 8 tiles (21 rows of 64 sequences over 255 to 16000 keys 104 us,
+// by chunks 156; 32 of one over 20000 keys 23 and 30; 28 of 32 over 1000 to
+// 12000 keys 63 and 65, but over 16384 each 188 and 183; 32 of 64 over 100 to
+// 300 keys 37 and 26).
 constexpr int kMostFew = 32, kMinTilesFew = 9;
 // Few rows (tr_attend8_few.cu): the launch (work and join kernels).
 cudaError_t launch_few8(const CUtensorMap &mk, const CUtensorMap &mv, Attend8Args p, bool bf16, void *ws, cudaStream_t st);
