@@ -796,6 +796,7 @@ tr_status tr_cache8_attend(const tr_cache8 *c8, const tr_heads *q, const tr_head
   if (q->heads != o->heads || q->heads % c->heads) return TR_ERR_ARG;
   if (reinterpret_cast<uintptr_t>(lse) & 3u) return TR_ERR_ALIGN;
   if ((long long)c->total_new * q->heads > INT_MAX - 65536) return TR_ERR_UNSUPPORTED;
+  if (c->heads > 65535) return TR_ERR_UNSUPPORTED;  // as tr_cache_attend
   if (c->total_new == 0) return TR_OK;
   const Plan8 plan = plan8_of(c, q->heads, window, max_new, max_len);
   if ((long long)plan.slots * c->heads > INT_MAX) return TR_ERR_UNSUPPORTED;
