@@ -28,11 +28,11 @@
 // lost below is 2^-31 of it.  Sums and everything else are fp32.
 //
 // Two blocks of 128 rows share a turned tile (MT = 2); where the rows are few
-// enough for one, a CTA is one block with two score buffers.  Both have the
-// tensor cores wait for shared memory: a tile's codes are read (32 KB), written
-// as halves (64 KB) and read by each block's products (112 KB a block), 320 KB
-// for 256 rows, which at the some 90 B a clock that such a mix gets is the
-// 3700 clocks that a tile takes.
+// enough for one, a CTA is one block with two score buffers.  A tile of MT = 2
+// takes 3700 clocks: its codes are read (32 KB), written as halves (64 KB) and
+// read by each block's products (112 KB a block), 320 KB at some 90 B a clock,
+// and the chain of a block's scores, softmax and second product has one score
+// buffer (with heads of 64 channels, half the bytes, a tile takes 0.86 of it).
 //
 // 28 heads of 128 over 4: 2048 tokens over 32768 keys 701 us (1.33 PFLOP/s, 0.70
 // of the measured cuBLAS); 5 tokens of 32 sequences over 1000 to 12000 keys (35
