@@ -13,6 +13,10 @@
 // tokens share their angles and the block its page.  A warp takes one head's
 // keys or values at a time, all 16 rows in its registers from the load to the
 // codes, because the scale has to be known before the first code.
+//
+// 29.6k tokens into an empty cache, normed and rotated, 28 heads of 128 over 4,
+// bf16: 108 us with the queries (4.6 TB/s), 39 without; one token of 64
+// sequences 5.0 us.
 #include "tr_cache8.cuh"
 #include "tr_rotary.cuh"
 
@@ -237,23 +241,30 @@ struct BlockRows {
   }
 };
 
-template <typename T, int V, bool PAIRS, bool NORM>
+// PACK: a CTA takes two blocks, each with half of its warps.  A block's
+// CTA waits for one load after the other (its sequence, rows, page), and its
+// keys' warps take longer than its values'; with two blocks, and each warp
+// keys and then values, that is once for both (29.6k tokens 113 us, so 108).
+// It costs registers, so few blocks go without.
+template <typename T, int V, bool PAIRS, bool NORM, bool PACK>
 __global__ void __launch_bounds__(kRotThreads, 3) k_append8(const __grid_constant__ Append8Args a) {
-  __shared__ __align__(16) float cs[kMaxTrig], sn[kMaxTrig];
+  __shared__ __align__(16) float cs[(1 + PACK) * kMaxTrig], sn[(1 + PACK) * kMaxTrig];
   __shared__ long long home[kMaxTokens];
   const RotArgs &g = a.g;
   pdl_wait();  // q, k, v come from the kernel before
-  const int nth = blockIdx.x / a.every, all = a.blocks * a.parts;
+  const int nth = blockIdx.x / a.every, all = PACK ? (a.blocks + 1) / 2 : a.blocks * a.parts;
   if (nth >= all || nth * a.every != (int)blockIdx.x) {
     rotate_rows<T, V, PAIRS, NORM>(g, blockIdx.x - min(nth + 1, all), cs, sn, home);
     return;
   }
   const CacheView &c = g.cache;
-  const NewBlock k = find_new_block(c, nth / a.parts);
-  // the first head's rows asked for before the page and the angles
   constexpr int kWarps = kRotThreads / 32;
-  const int warp = threadIdx.x >> 5, step = a.parts * kWarps;
-  int u = nth % a.parts * kWarps + warp;
+  const int half = PACK ? threadIdx.x / (kRotThreads / 2) : 0, threads = PACK ? kRotThreads / 2 : kRotThreads;
+  const NewBlock k = find_new_block(c, PACK ? 2 * nth + half : nth / a.parts);
+  // the first head's rows asked for before the page and the angles
+  const int warp = (threadIdx.x & (threads - 1)) >> 5, step = PACK ? kWarps / 2 : a.parts * kWarps;
+  int u = PACK ? warp : nth % a.parts * kWarps + warp;
+  const int at = kBlock * g.half;  // the second half's angles
   BlockRows<T, V, PAIRS> rows(g);
   auto load = [&]() {
     const bool val = u >= c.heads;
@@ -261,16 +272,17 @@ __global__ void __launch_bounds__(kRotThreads, 3) k_append8(const __grid_constan
   };
   if (k.seq >= 0) load();
   const int page = k.seq >= 0 ? page_of(c, k.seq, k.key) : -1;
-  if (g.err && threadIdx.x == 0 && (k.lost || (k.seq >= 0 && page < 0))) atomicOr(g.err, TR_CACHE_ERR_PAGE);
+  if (g.err && (threadIdx.x & (threads - 1)) == 0 && (k.lost || (k.seq >= 0 && page < 0))) atomicOr(g.err, TR_CACHE_ERR_PAGE);
   if (page < 0) return;
   if (g.seg[1].turn) {
-    fill_trig(g, k.tok0 + k.r0, k.r1 - k.r0, cs, sn);
-    __syncthreads();
+    fill_trig(g, k.tok0 + k.r0, k.r1 - k.r0, cs + half * at, sn + half * at, threads);
+    if (PACK) asm volatile("bar.sync %0, %1;" ::"r"(1 + half), "r"(threads) : "memory");
+    else __syncthreads();
   }
   while (u < 2 * c.heads) {
     const bool val = u >= c.heads;
     rows.put(g, val ? g.seg[2] : g.seg[1], k, page, val ? u - c.heads : u, static_cast<uint8_t *>(val ? c.v : c.k),
-             val ? a.scale.v : a.scale.k, cs, sn);
+             val ? a.scale.v : a.scale.k, cs + half * at, sn + half * at);
     u += step;
     load();
   }
@@ -284,13 +296,15 @@ cudaError_t launch_append8_t(Append8Args &a, cudaStream_t st) {
   const int sms = sm_count() > 0 ? sm_count() : 1, rounds = (2 * a.g.cache.heads + kRotThreads / 32 - 1) / (kRotThreads / 32);
   a.parts = a.blocks ? 3 * sms / a.blocks : 1;
   a.parts = a.parts < 1 ? 1 : a.parts > rounds ? rounds : a.parts;
-  const int all = a.blocks * a.parts, ctas = all + (a.g.seg[0].in ? cut_segments(q.g) : 0);
+  const bool pack = a.blocks >= 6 * sms;  // every SM gets as many CTAs as it holds all the same
+  const int all = pack ? (a.blocks + 1) / 2 : a.blocks * a.parts, ctas = all + (a.g.seg[0].in ? cut_segments(q.g) : 0);
   a.every = all ? ctas / all : 1;
   if (ctas == 0) return cudaSuccess;  // no sequence, fewer rows than a block's, no queries
   a.g.seg[0] = q.g.seg[0];
   a.g.seg[1].cta0 = a.g.seg[2].cta0 = INT_MAX;  // (of the queries' CTAs: none is for keys or values)
-  return a.g.seg[0].w ? launch_kernel(k_append8<T, V, PAIRS, true>, dim3(ctas), dim3(kRotThreads), 0, st, false, a)
-                      : launch_kernel(k_append8<T, V, PAIRS, false>, dim3(ctas), dim3(kRotThreads), 0, st, false, a);
+  auto kernel = pack ? a.g.seg[0].w ? k_append8<T, V, PAIRS, true, true> : k_append8<T, V, PAIRS, false, true>
+                : a.g.seg[0].w ? k_append8<T, V, PAIRS, true, false> : k_append8<T, V, PAIRS, false, false>;
+  return launch_kernel(kernel, dim3(ctas), dim3(kRotThreads), 0, st, false, a);
 }
 
 template <typename T>

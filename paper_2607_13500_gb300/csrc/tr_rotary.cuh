@@ -206,10 +206,13 @@ struct RowWalk {
 // Cosines and sines of the CTA's tokens into shared memory.  position *
 // turns modulo 2^64 is the angle as a fraction of a turn, exactly; its top 32
 // bits, signed, are the angle in units of pi / 2^31.
-__device__ __forceinline__ void fill_trig(const RotArgs &g, int t0, int nt, float *cs, float *sn) {
+// (threads: a half of the CTA's may take tokens of its own.)
+__device__ __forceinline__ void fill_trig(const RotArgs &g, int t0, int nt, float *cs, float *sn, int threads = kRotThreads) {
   if (!g.half) return;
-  RowWalk w(threadIdx.x, g.half);
-  for (int i = threadIdx.x; i < nt * g.half; i += kRotThreads, w.step(g.trig_toks, g.trig_rest, g.half)) {
+  const int tid = threadIdx.x & (threads - 1);
+  const int toks = threads == kRotThreads ? g.trig_toks : threads / g.half, rest = threads == kRotThreads ? g.trig_rest : threads - toks * g.half;
+  RowWalk w(tid, g.half);
+  for (int i = tid; i < nt * g.half; i += threads, w.step(toks, rest, g.half)) {
     const int lt = w.tok, f = w.head;
     const int ax = __ldg(g.axis + f);
     const long long p = (unsigned)ax < (unsigned)g.axes ? (long long)__ldg(g.pos + (long long)ax * g.tokens + t0 + lt) : 0;

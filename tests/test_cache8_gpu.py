@@ -513,6 +513,34 @@ def test_append_norms_and_rotates(case):
         assert torch.equal(now.double().transpose(1, 2)[~touched], was.transpose(1, 2)[~touched])
 
 
+@pytest.mark.parametrize("hk,d,layout,dtype,norm", [(3, 128, "half", BF, True), (5, 64, "pairs", FP, False), (1, 48, "half", BF, True)])
+def test_append_of_many_sequences_as_of_few(hk, d, layout, dtype, norm):
+    """Bit for bit what calls of 100 sequences each leave (which take other CTAs for it)."""
+    altr, hq, page, batch = _alt(), 3, 32, 701
+    g = torch.Generator().manual_seed(97)
+    new = torch.randint(0, 41, (batch,), generator=g).tolist()
+    lens = [n + int(p) for n, p in zip(new, torch.randint(0, 51, (batch,), generator=g))]
+    cu, t = _cum(new), sum(new)
+    table, pages = _table(lens, page, 98)
+    table[400, 0] = pages  # outside the cache
+    one, few = _cache(pages, hk, page, d, 99), _cache(pages, hk, page, d, 99)
+    rows = _randn(t + 5, hq + 2 * hk, d, dtype=dtype, seed=100)  # five rows of no sequence
+    q, k, v = rows[:, :hq], rows[:, hq:hq + hk], rows[:, hq + hk:]
+    pos = torch.randint(0, 5000, (2, t + 5), generator=g).to(torch.int32).to(DEV)
+    wq, wk = (1 + 0.3 * _randn(d, dtype=torch.float32, seed=x) if norm else None for x in (101, 102))
+    rotary = altr.Rotary(d, DEV, sections=(d // 4, d // 4), layout=layout)
+    got = one.append(k, v, table, _i32(lens), _i32(cu), rotary=rotary, pos=pos, k_weight=wk, q=q, q_weight=wq)
+    for b0 in range(0, batch, 100):
+        b1 = min(b0 + 100, batch)
+        r = slice(cu[b0], cu[b1])
+        part = few.append(k[r], v[r], table[b0:b1], _i32(lens[b0:b1]), _i32([x - cu[b0] for x in cu[b0:b1 + 1]]), rotary=rotary,
+                          pos=pos[:, r].contiguous(), k_weight=wk, q=q[r], q_weight=wq)
+        assert torch.equal(got[r], part)
+    for a, b in zip((one.k, one.v, one.k_scale, one.v_scale), (few.k, few.v, few.k_scale, few.v_scale)):
+        assert torch.equal(_bytes(a), _bytes(b))
+    assert int(one.error) == int(few.error) != 0
+
+
 def test_append_outside_the_cache_writes_nothing_and_is_told():
     c = _cache(3, 2, 16, 64, 101)
     before = [_bytes(x).clone() for x in (c.k, c.v, c.k_scale, c.v_scale)]
