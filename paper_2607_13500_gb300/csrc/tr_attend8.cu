@@ -54,7 +54,7 @@ struct Shape8 {
   static_assert(MT == 2 || MT == 1, "");
   static constexpr int kTileBytes = kTile * D * 2;   // one K or V tile of halves, or one block's Q
   static constexpr int kCodeBytes = kTile * D;       // one tile of codes
-  static constexpr int kBudget = 227 * 1024 - 3072;  // shared memory less barriers and alignment
+  static constexpr int kBudget = 224 * 1024;          // shared memory less barriers and alignment
   static constexpr int kFit = (kBudget - (MT + 4) * kTileBytes) / kCodeBytes;
   static constexpr int kStages = kFit < 12 ? kFit : 12;  // of codes; two tiles of halves of each kind
   static constexpr int kSBuf = MT == 1 ? 2 : 1;      // score buffers of a block
