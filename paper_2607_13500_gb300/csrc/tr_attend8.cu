@@ -608,8 +608,9 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
       const bool parts = g.splits > 1;
       const long long all_rows = (long long)g.c.total_new * g.q_heads;
       float *prow = g.part + ((long long)split * all_rows + out_row) * g.c.d;
-      // divided by the sum before V's scale, up to 2^127, enters (a small sum: R is small too)
-      const float more = sum < 0x1p-100f ? 0x1p40f : 1.f;
+      // divided by the sum before V's scale, up to 2^127, enters (a small sum: R is small too; none, of a row that
+      // sees no key: R may be any)
+      const float more = sum > 0.f && sum < 0x1p-100f ? 0x1p40f : 1.f;
       const float inv = sum > 0.f || sum != sum ? 1.f / (sum * more) : 0.f;
       const float up = ta < tb ? pow2(ref) * more : 0.f;
       // staged in the place of this row's queries, whose products are done

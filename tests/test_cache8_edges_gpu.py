@@ -1,0 +1,82 @@
+"""The attention over the 8-bit cache where its numbers lie far apart, where its
+keys are taken in parts, and past the sizes that its kernels count in 31 bits.
+
+Tolerances are those of test_cache8_gpu.py, except that what a key adds is
+measured by what the row sees: a probability enters its product with the
+value as a half, relative to the greatest probability times scale among the
+keys that the row sees (a block's largest code is 448 at most, and at least
+224 where its rows set the scale; for random codes the largest of 16 keys is
+taken to be within 2 of it), so small ones are off by 2^-25 of twice the
+greatest p_j max |v_j|, n of them at most.
+"""
+import math
+
+import pytest
+import torch
+
+from test_cache8_gpu import BF, DEV, FP, U, _alt, _bytes, _cache, _cum, _held, _i32, _randn, _reference, _spoil, _table, _within
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+    from paper_2607_13500_gb300 import _build
+    _build.build()
+
+
+def _parts(c):
+    """Whether the last calls' plans took the keys in parts (chunks: only then is there a workspace)."""
+    return max(c._sizes.values()) > 0
+
+
+def _seen_reference(c, q, table, n, scale=None, window=0):
+    """o, lse and their tolerances for one sequence, its new tokens the last (causal)."""
+    t, hq, d = q.shape
+    group, scale = hq // c.heads, 1 / math.sqrt(d) if scale is None else scale
+    o, lse = torch.zeros(t, hq, d, dtype=torch.float64, device=DEV), torch.zeros(t, hq, dtype=torch.float64, device=DEV)
+    tol_o, tol_l = torch.zeros_like(o), torch.zeros_like(lse)
+    k, v = (_held(x, s, table, 0, n) for x, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+    own = n - t + torch.arange(t, device=DEV)[:, None]
+    j = torch.arange(n, device=DEV)
+    seen = j <= own
+    if window:
+        seen &= j > own - window
+    for h in range(hq):
+        kh, vh, qh = k[:, h // group], v[:, h // group], q[:, h].double()
+        s = (qh @ kh.T * scale).masked_fill(~seen, -math.inf)
+        z = torch.logsumexp(s, -1)
+        p = (s - z[:, None].nan_to_num(0, 0, 0)).exp()
+        mag = vh.abs().amax(-1)
+        e = d * 2.0 ** -23 * abs(scale) * ((qh.abs() @ kh.abs().T) * seen).amax(-1)
+        e = e + abs(scale) * qh.abs().sum(-1) * 2.0 ** -38 * kh.abs().amax()
+        o[:, h], lse[:, h] = p @ vh, z
+        tol_o[:, h] = U[q.dtype] * (p @ vh).abs() + (2.0 ** -11 + 2 * e + 2.0 ** -17)[:, None] * (p @ vh.abs())
+        tol_o[:, h] += (n * 2.0 ** -25 * 2 * (p * mag).amax(-1))[:, None] + 2.0 ** -133  # (and the types' subnormal numbers)
+        tol_l[:, h] = e + 2.0 ** -17 * (1 + z.nan_to_num(0, 0, 0).abs())
+    return o, lse, tol_o, tol_l
+
+
+def _blocks(table, n, first=0):
+    """The pages of a sequence of n keys (16 a page: a block each), from the first."""
+    return table[0, first:(n + 15) // 16].long()
+
+
+@pytest.mark.parametrize("power", [60, 88, 110, 119])
+@pytest.mark.parametrize("new,group", [(40, 4), (40, 1), (300, 4), (9, 1)])
+def test_rows_without_a_key_are_zeros_whatever_the_scales(new, group, power):
+    """More new tokens than keys: the first see nothing, beside rows that see large values."""
+    n, hk, d = new // 2 + 3, 2, 64
+    table, pages = _table([n], 16, 201)
+    c = _cache(pages, hk, 16, d, 202)
+    _bytes(c.v_scale)[:] = 127 + power
+    q = _randn(new, group * hk, d, dtype=BF, seed=203)
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), return_lse=True)
+    ro, rl, to, tl = _seen_reference(c, q, table, n)
+    none = torch.arange(new, device=DEV) < new - n
+    assert (o[none] == 0).all() and (lse[none] == -math.inf).all()
+    _within(o[~none], ro[~none], to[~none], "o")
+    _within(lse[~none], rl[~none], tl[~none], "lse")
+
