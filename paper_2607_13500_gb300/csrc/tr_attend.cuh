@@ -490,17 +490,27 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
       if (ml.y == 0.f) continue;  // saw no key
       const float f = exp2_fast(ml.x - m);
       l += ml.y * f;
-      if (holds) {
+      if (!NORMED && holds) {
         const float4 v = reinterpret_cast<const float4 *>(g.part + (s * rows + row) * g.c.d)[lane];
-        const float w = NORMED ? ml.y * f : f;
-        acc.x += v.x * w, acc.y += v.y * w, acc.z += v.z * w, acc.w += v.w * w;
+        acc.x += v.x * f, acc.y += v.y * f, acc.z += v.z * f, acc.w += v.w * f;
       }
     }
   }
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  if (NORMED) {  // weighed by their shares of the sum, 1 at most, so that values near the end of fp32 stay below it
+    for (int s = 0; l != 0.f && s < g.splits; ++s) {
+      const float2 ml = g.part_ml[s * rows + row];
+      if (ml.y == 0.f || !holds) continue;
+      const float4 v = reinterpret_cast<const float4 *>(g.part + (s * rows + row) * g.c.d)[lane];
+      const float w = ml.y * exp2_fast(ml.x - m) * inv;
+      acc.x += v.x * w, acc.y += v.y * w, acc.z += v.z * w, acc.w += v.w * w;
+    }
+  } else {
+    acc.x *= inv, acc.y *= inv, acc.z *= inv, acc.w *= inv;
+  }
   if (holds)
     reinterpret_cast<uint2 *>(orow)[lane] =
-        make_uint2(Bits<T>::pack(acc.x * inv, acc.y * inv), Bits<T>::pack(acc.z * inv, acc.w * inv));
+        make_uint2(Bits<T>::pack(acc.x, acc.y), Bits<T>::pack(acc.z, acc.w));
   if (g.lse && lane == 0) g.lse[row] = l > 0.f || l != l ? m * 0.693147180559945309f + logf(l) : -INFINITY;
 }
 

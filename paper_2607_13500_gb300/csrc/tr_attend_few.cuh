@@ -246,8 +246,12 @@ __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ Attend
       float add = add1;
 #pragma unroll
       for (int o = 16; o; o >>= 1) add += __shfl_xor_sync(0xffffffffu, add, o);
-      l = l * f + add;
-      acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
+      const float kept = l * f;
+      l = kept + add;
+      // NORMED: shares of the sum so far, 1 at most, so that values near the end of fp32 stay below it
+      const float inv = NORMED && (l > 0.f || l != l) ? 1.f / l : 0.f;
+      const float keep = NORMED ? kept * inv : f, mine = NORMED ? add1 * inv : e;
+      acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep;
       unsigned left = __ballot_sync(0xffffffffu, seen);
       while (left) {
         constexpr int kU = 4;
@@ -259,7 +263,7 @@ __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ Attend
           const bool have = left != 0;
           left &= left - 1;
           const int from_slot = __shfl_sync(0xffffffffu, slot, src);
-          w[k] = __shfl_sync(0xffffffffu, NORMED ? add1 : e, src);
+          w[k] = __shfl_sync(0xffffffffu, mine, src);
           v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (have && holds)
             v[k] = reinterpret_cast<const float4 *>(g.part + ((long long)from_slot * kFewRows + r) * g.c.d)[lane];
@@ -275,7 +279,7 @@ __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ Attend
     }
   }
   if (s.tiles <= 0) pdl_wait();  // o may still be read by the kernel before last
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  const float inv = NORMED ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;
   if (holds)
     reinterpret_cast<uint2 *>(g.o + 2 * ((long long)t * g.o_tok + (long long)h * g.o_head))[lane] =
         make_uint2(Bits<T>::pack(acc.x * inv, acc.y * inv), Bits<T>::pack(acc.z * inv, acc.w * inv));

@@ -80,3 +80,20 @@ def test_rows_without_a_key_are_zeros_whatever_the_scales(new, group, power):
     _within(o[~none], ro[~none], to[~none], "o")
     _within(lse[~none], rl[~none], tl[~none], "lse")
 
+
+@pytest.mark.parametrize("length", [200, 7000, 40000])
+@pytest.mark.parametrize("new,group", [(1, 4), (8, 4), (40, 1), (40, 4), (300, 4)])
+def test_the_largest_values(new, group, length):
+    """Values up to 448 * 2^119, near the end of fp32: their means are below it, whoever joins them."""
+    n, hk, d = length + new, 2, 64
+    table, pages = _table([n], 16, 205)
+    c = _cache(pages, hk, 16, d, 206)
+    _bytes(c.v_scale)[:] = 127 + 119
+    _bytes(c.v)[:] = 0x7e
+    _bytes(c.v)[:, 1] ^= 0x80
+    q = _randn(new, group * hk, d, dtype=BF, seed=207, gain=0.1)
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), return_lse=True)
+    ro, rl, to, tl = _seen_reference(c, q, table, n)
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
