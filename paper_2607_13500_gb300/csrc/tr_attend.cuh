@@ -469,6 +469,8 @@ inline __device__ __noinline__ void clear_block(const AttendArgs &g, int first, 
   }
 }
 
+constexpr float kFar = 0x1p-126f;
+
 // Joins the splits of each row: one warp per row, in the splits' order.
 // NORMED: the splits' values are divided by their sums.
 template <typename T, bool NORMED>
@@ -497,12 +499,16 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Att
     }
   }
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-  if (NORMED) {  // weighed by their shares of the sum, 1 at most, so that values near the end of fp32 stay below it
+  if (NORMED) {
+    // weighed by their shares of the sum, 1 at most, so that values near the end of fp32 stay below it; shares under
+    // 2^-126 in two factors, of which kFar is one: a value may outweigh its small probability
     for (int s = 0; l != 0.f && s < g.splits; ++s) {
       const float2 ml = g.part_ml[s * rows + row];
       if (ml.y == 0.f || !holds) continue;
-      const float4 v = reinterpret_cast<const float4 *>(g.part + (s * rows + row) * g.c.d)[lane];
-      const float w = ml.y * exp2_fast(ml.x - m) * inv;
+      float4 v = reinterpret_cast<const float4 *>(g.part + (s * rows + row) * g.c.d)[lane];
+      const bool far = ml.x - m < -126.f;
+      if (far) v.x *= kFar, v.y *= kFar, v.z *= kFar, v.w *= kFar;
+      const float w = ml.y * exp2_fast(far ? ml.x - m + 126.f : ml.x - m) * inv;
       acc.x += v.x * w, acc.y += v.y * w, acc.z += v.z * w, acc.w += v.w * w;
     }
   } else {

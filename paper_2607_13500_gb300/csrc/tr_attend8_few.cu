@@ -59,6 +59,10 @@ struct Few8 {
 };
 
 constexpr int kLift = 6;  // what enters the second product is taken times 2^6 (and grows by 2^8 at most)
+// A probability under 2^-126 becomes zero.  Times 2^100 at most, that is what the second product loses anyway (2^-31 of the
+// greatest, which is 2^5 at least); where the factor is larger, what is more enters the exponential (and the sum, where
+// such probabilities, 2^-86 at most, do not count).
+constexpr float kMostLift = 100.f;
 
 __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   uint2 v;
@@ -419,8 +423,9 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float neg = mx[i] == -INFINITY ? 0.f : -mx[i], f = fs[i][h];
-          const float by = pow2((int)fminf(fmaxf((float)(ev[h] + kLift) + (mx[i] - wx[i]), -126.f), 127.f));
+          const float lift = (float)(ev[h] + kLift) + (mx[i] - wx[i]), f = fs[i][h];
+          const float neg = (mx[i] == -INFINITY ? 0.f : -mx[i]) + fmaxf(lift - kMostLift, 0.f);
+          const float by = pow2((int)fmaxf(fminf(lift, kMostLift), -126.f));  // (NaN where the row has seen nothing: times zeros)
           float p0[2], p1[2];
 #pragma unroll
           for (int n = 0; n < 2; ++n) {

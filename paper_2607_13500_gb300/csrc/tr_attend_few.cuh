@@ -246,11 +246,21 @@ __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ Attend
       float add = add1;
 #pragma unroll
       for (int o = 16; o; o >>= 1) add += __shfl_xor_sync(0xffffffffu, add, o);
-      const float kept = l * f;
+      const float was = l, kept = l * f;
       l = kept + add;
-      // NORMED: shares of the sum so far, 1 at most, so that values near the end of fp32 stay below it
+      // NORMED: shares of the sum so far, 1 at most, so that values near the end of fp32 stay below it; those under
+      // 2^-126 in two factors, of which kFar is one: a value may outweigh its small probability
       const float inv = NORMED && (l > 0.f || l != l) ? 1.f / l : 0.f;
-      const float keep = NORMED ? kept * inv : f, mine = NORMED ? add1 * inv : e;
+      float keep = NORMED ? kept * inv : f, mine = NORMED ? add1 * inv : e;
+      unsigned far = 0u;
+      if (NORMED) {
+        far = __ballot_sync(0xffffffffu, seen && ml.x - m < -126.f);
+        if (far >> lane & 1u) mine = ml.y * exp2_fast(ml.x - m + 126.f) * inv;
+        if (before - m < -126.f && before > -INFINITY) {
+          keep = was * exp2_fast(before - m + 126.f) * inv;
+          acc.x *= kFar, acc.y *= kFar, acc.z *= kFar, acc.w *= kFar;
+        }
+      }
       acc.x *= keep, acc.y *= keep, acc.z *= keep, acc.w *= keep;
       unsigned left = __ballot_sync(0xffffffffu, seen);
       while (left) {
@@ -267,6 +277,7 @@ __global__ void __launch_bounds__(256) k_few_join(const __grid_constant__ Attend
           v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (have && holds)
             v[k] = reinterpret_cast<const float4 *>(g.part + ((long long)from_slot * kFewRows + r) * g.c.d)[lane];
+          if (NORMED && (far >> src & 1u)) v[k].x *= kFar, v[k].y *= kFar, v[k].z *= kFar, v[k].w *= kFar;
         }
 #pragma unroll
         for (int k = 0; k < kU; ++k) {

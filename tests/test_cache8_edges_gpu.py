@@ -97,3 +97,26 @@ def test_the_largest_values(new, group, length):
     _within(o, ro, to, "o")
     _within(lse, rl, tl, "lse")
 
+
+@pytest.mark.parametrize("length,width", [(200, 1), (7000, 1), (7000, 180), (40000, 1), (40000, 700)])
+@pytest.mark.parametrize("new,group", [(1, 4), (2, 4), (8, 4), (40, 1), (40, 4), (300, 4)])
+@pytest.mark.parametrize("place", ["first", "middle", "last"])
+def test_values_that_outweigh_their_small_probability(new, group, length, width, place):
+    """Blocks whose scores are 104 below the others' (probabilities of 2^-150) and whose values are 2^179 times theirs:
+    the result is their own, whether other keys are taken with them or apart."""
+    n, hk, d = length + new, 2, 64
+    table, pages = _table([n], 16, 271)
+    c = _cache(pages, hk, 16, d, 272)
+    at = _blocks(table, n)
+    i = {"first": 0, "middle": length // 32, "last": (n - new) // 16 - width}[place]
+    heavy = at[i:i + width]
+    _bytes(c.k)[:], _bytes(c.k_scale)[:] = 0, 127
+    _bytes(c.k)[heavy, :, :, 0] = 0xed  # -104
+    _bytes(c.v_scale)[at], _bytes(c.v_scale)[heavy] = 127 - 60, 127 + 119
+    q = _randn(new, group * hk, d, dtype=BF, seed=273)
+    q[:, :, 0] = 1
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), scale=1.0, return_lse=True)
+    ro, rl, to, tl = _seen_reference(c, q, table, n, scale=1.0)
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
