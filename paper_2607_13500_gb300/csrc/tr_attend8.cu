@@ -40,6 +40,7 @@
 // to 6272 keys, in fp16, 83 us, where each CTA's start and end, 11 us, tell.
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 #include "tr_attend8.cuh"
 #include "tr_pack.cuh"
@@ -70,19 +71,21 @@ struct Shape8 {
 };
 
 constexpr float kLift8 = 6.f;   // probabilities are taken times 2^6 (and grow by 2^8 at most)
-// d is between kLeast and kMost, so that 2^-d and its sums are fp32 numbers: R
-// is the largest exponent of the CTA's blocks, or so much lower that the
-// smallest (but for blocks of zeros) is kLeast above it.  Keys that a row does
-// not see leave its results as they are; keys that it sees are taken to be
-// 2^kLeast of its greatest at least.
-constexpr int kLeast = -100, kMost = 136;
+// R is the largest exponent of the CTA's blocks, and the sum's way through 2^-d
+// holds for kLeast <= d <= 0: a probability that leaves the exponential as zero,
+// because it is 2^-132 of the greatest times its 2^d, is then 2^-52 of another
+// at most, and the sums, up to 2^94 a key, are fp32 numbers.  Where the exponents
+// lie further apart (but for blocks of zeros: a wide CTA) the sum is taken from
+// exponentials of its own, against the maximum of the scores alone
+// (softmax_wide: 2048 tokens over 32768 keys 1800 us, else 692).
+constexpr int kLeast = -80;
 constexpr int kZeros = -117;  // the exponent of a block of zeros, as the append leaves it
 
 // What the softmax needs of a tile's blocks.
 struct TileScales {
   float k[8];     // 2^e of keys
   float v[8];     // d of values
-  float undo[8];  // 2^-d
+  float undo[8];  // 2^-d (wide CTAs: not used)
 };
 
 // The values taken out of open tiles among [t0, t1) to those rows of the warp
@@ -163,6 +166,116 @@ __device__ __forceinline__ bool to_halves(uint32_t codes, uint32_t tile, int row
   return found;
 }
 
+// The softmax of a row's tiles in a wide CTA (see kLeast), by the warps of a
+// block, as in k_attend8 but for the sum and for maxima that are whole numbers,
+// so that their difference is exact.  It stands by itself, 32 scores at a time,
+// because the same in the loop there took registers and order from the others
+// (long 703 -> 757 us; as a second loop beside it drafts 66 -> 70).  False when a
+// wait timed out.
+struct WideRow {
+  uint32_t s_col, o_col;            // tensor memory: scores (the first buffer's) and sums
+  uint32_t s_full, p_full, o_done;  // barriers (the first buffer's)
+  uint32_t scale_full, scales;      // barriers and numbers of the tiles' scales, four slots
+  int t0, ta, tb, lo, hi;           // first tile of the CTA; tiles of the block; keys of the row
+  float row_scale;
+  float mx, top, sum;               // maxima of scores + d and of scores; the sum, against top
+  bool live;
+};
+template <int D, int BUFS>
+__device__ __noinline__ bool softmax_wide(WideRow &row) {
+  WideRow w = row;  // (in registers: 4800 us without)
+  bool ok = true;
+  for (int t = w.ta; t < w.tb; ++t) {
+    const int n = t - w.ta, ts = t - w.t0, buf = BUFS == 2 ? n & 1 : 0;
+    const uint32_t par = BUFS == 2 ? (uint32_t)(n >> 1) & 1u : (uint32_t)n & 1u;
+    if (!__all_sync(0xffffffffu, tc::mbar_wait(w.s_full + 8u * buf, par) &&
+                                     tc::mbar_wait(w.scale_full + 8u * (ts & 3), (uint32_t)(ts >> 2) & 1u))) {
+      ok = false;
+      break;
+    }
+    tc::fence_after_sync();
+    if (w.live) {
+      const uint32_t s_col = w.s_col + buf * kTile, at = w.scales + (ts & 3) * (uint32_t)sizeof(TileScales);
+      // scores 32 c and on, in units of log 2 (-inf: not seen); their blocks' d
+      auto load = [&](int c, float (&s)[32], float (&d)[2]) {
+        uint32_t x[32];
+        tc::tmem_ld32_issue(s_col + 32 * c, x);
+        tc::tmem_ld32_wait(x);
+        float f[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[b]) : "r"(at + 4 * (2 * c + b)));
+          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(d[b]) : "r"(at + 32 + 4 * (2 * c + b)));
+          f[b] = fminf(fmaxf(w.row_scale * f[b], 1e-30f), 1e30f);
+        }
+        const int key0 = t * kTile + 32 * c;
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          s[i] = key0 + i < w.lo || key0 + i >= w.hi ? -INFINITY : __uint_as_float(x[i]) * f[i / 16];
+      };
+      float now = -INFINITY, peak = -INFINITY;
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        float s[32], d[2];
+        load(c, s, d);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) peak = fmaxf(peak, s[i]), now = fmaxf(now, s[i] + d[i / 16]);
+      }
+      now = ceilf(now), peak = ceilf(peak);
+      if (peak > w.top) w.sum *= exp2_fast(w.top - peak), w.top = peak;
+      if (n == 0) {
+        w.mx = now;
+      } else if (__any_sync(0xffffffffu, now > w.mx + 8.f)) {  // the products so far move to the new maximum
+        const bool more = now > w.mx + 8.f;
+        const float down = more ? exp2_fast(w.mx - now) : 1.f;
+        if (BUFS == 2) {
+          if (!__all_sync(0xffffffffu, tc::mbar_wait(w.o_done, (uint32_t)(n - 1) & 1u))) {
+            ok = false;
+            break;
+          }
+          tc::fence_after_sync();
+        }
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          tc::tmem_ld32_issue(w.o_col + c, o);
+          tc::tmem_ld32_wait(o);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * down);
+          tc::tmem_st32(w.o_col + c, o);
+        }
+        tc::tmem_st_wait();
+        if (more) w.mx = now;
+      }
+      const float less = w.top == -INFINITY ? 0.f : -w.top, neg = w.mx == -INFINITY ? 0.f : kLift8 - w.mx;
+      // (probabilities of 64 keys take the 32 columns whose scores were read first)
+#pragma unroll 1
+      for (int c = 0; c < 4; c += 2) {
+        uint32_t p[32];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float s[32], d[2];
+          load(c + h, s, d);
+          float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            acc[i / 2 & 3] += exp2_fast(s[i] + less) + exp2_fast(s[i + 1] + less);
+            const float e = neg + d[i / 16];
+            p[16 * h + i / 2] = Bits<__half>::pack(exp2_fast(s[i] + e), exp2_fast(s[i + 1] + e));
+          }
+          w.sum += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+        }
+        tc::tmem_st32(s_col + 16 * c, p);
+      }
+      tc::tmem_st_wait();
+    }
+    tc::fence_before_sync();
+    tc::mbar_arrive(w.p_full + 8u * buf);
+  }
+  row = w;
+  return ok;
+}
+
 template <typename T, int D, int MT>
 __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
     k_attend8(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -190,7 +303,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
   auto scale_full = [&](int s) { return scale_bars + 8u * s; };
   const uint32_t tmem_slot = scale_bars + 32u;
   __shared__ int bad_values;     // some were taken out of the tiles
-  __shared__ int top_of[4], low_of[4], ref;  // largest and smallest exponents, R
+  __shared__ int top_of[4], low_of[4], ref, wide_sum;  // largest and smallest exponents, R, whether they lie far apart
   // Of tile t in slot t % 4: when the codes of tile t + 4 are turned, the
   // scores of tile t + 2 are done, and with them the softmax of tile t.
   __shared__ __align__(16) TileScales tile_scales[4];
@@ -298,13 +411,14 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
       }
       top = __reduce_max_sync(0xffffffffu, top), low = __reduce_min_sync(0xffffffffu, low);
       int r = 0;  // R
+      bool wide = false;
       if (t0 < t1) {
         if (lane == 0) top_of[w] = top, low_of[w] = low;
         codes_sync();
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = max(top, top_of[i]), low = min(low, low_of[i]);
-        r = min(top, low - kLeast);
-        if (w == 0 && lane == 0) ref = r;
+        r = top, wide = low < top + kLeast;
+        if (w == 0 && lane == 0) ref = r, wide_sum = wide;
       }
       // scales of 16 tiles at a time, this warp's two blocks of one tile in two lanes
       auto scales = [&](int t) {
@@ -327,10 +441,11 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
           const uint32_t s = t - held0 < 16 ? s0 : s1;
           if (lane < 2) {
             TileScales &out = tile_scales[n & 3];
-            const int d = min(max((s >> 8 < 255u ? (int)(s >> 8) - 127 : -127) - r, kLeast), kMost);
+            int d = (s >> 8 < 255u ? (int)(s >> 8) - 127 : -127) - r;
+            if (!wide) d = max(d, kLeast);
             out.k[2 * w + lane] = pow2((int)(s & 0xffu) - 127);
             out.v[2 * w + lane] = (float)d;
-            out.undo[2 * w + lane] = pow2(-d / 2) * pow2(-d - -d / 2);
+            out.undo[2 * w + lane] = pow2(min(-d, -kLeast));
           }
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(scale_full(n & 3));
@@ -451,8 +566,8 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
     const int lo = valid && g.window > 0 ? window_start(own, g.window) : 0;
     const bool live = __any_sync(0xffffffffu, valid);
     const int ta = MT > 1 && m == 1 ? a[MT - 1] : a[0], tb = MT > 1 && m == 1 ? b[MT - 1] : b[0];
-    float mx = -INFINITY, sum = 0.f;
-    bool ok = true;
+    float mx = -INFINITY, top = -INFINITY, sum = 0.f;  // maxima of scores + d and (wide) of scores
+    bool ok = true, wide = false;
     const uint32_t lane_col = (uint32_t)(32 * quarter) << 16;
     const uint32_t o_col = tmem + lane_col + (uint32_t)(S::kColO + m * D);
     if (ta < tb) {
@@ -498,13 +613,26 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
       // what a score of the row is multiplied by, its key's scale apart
       const float row_scale = g.scale * pow2(eq);
 
-      for (int t = ta; t < tb && ok; ++t) {
+      // Whether the CTA is wide is known with the scales of its first tile.  (Their
+      // barrier has no second phase yet: that is the fifth tile's, turned after
+      // the third tile's scores, and those come after this block's first tile,
+      // the CTA's first or second.  With one block and few tiles this wait before
+      // that for the scores would take a microsecond: there it is read after it.)
+      if (MT == 2) {
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(scale_full(0), 0));
+        wide = ok && wide_sum;
+      }
+      for (int t = ta; !wide && t < tb && ok; ++t) {
         const int n = t - ta;
         const int buf = S::kSBuf == 2 ? n & 1 : 0;
         const uint32_t s_par = S::kSBuf == 2 ? (uint32_t)(n >> 1) & 1u : (uint32_t)n & 1u;
         const int ts = t - t0;
         ok = __all_sync(0xffffffffu, tc::mbar_wait(s_full(m, buf), s_par) && tc::mbar_wait(scale_full(ts & 3), (uint32_t)(ts >> 2) & 1u));
         if (!ok) break;
+        if (MT == 1 && n == 0 && wide_sum) {
+          wide = true;
+          break;
+        }
         tc::fence_after_sync();
         if (live) {
           const uint32_t s_col = tmem + lane_col + (uint32_t)((MT == 1 ? buf : m) * kTile);
@@ -594,6 +722,12 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
         tc::fence_before_sync();
         tc::mbar_arrive(p_full(m, buf));
       }
+      if (wide) {
+        WideRow w{tmem + lane_col + (uint32_t)((MT == 1 ? 0 : m) * kTile), o_col, s_full(m, 0), p_full(m, 0), o_done(m), scale_full(0),
+                  tc::smem_u32(tile_scales), t0, ta, tb, lo, hi, row_scale, -INFINITY, -INFINITY, 0.f, live};
+        ok = softmax_wide<D, S::kSBuf>(w);
+        mx = w.mx, top = w.top, sum = w.sum;
+      }
       // A barrier of its own: of one that every product completes, a thread
       // that comes late could not tell the last phase from the one before.
       if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(o_last(m), 0));
@@ -608,11 +742,11 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
       const bool parts = g.splits > 1;
       const long long all_rows = (long long)g.c.total_new * g.q_heads;
       float *prow = g.part + ((long long)split * all_rows + out_row) * g.c.d;
-      // divided by the sum before V's scale, up to 2^127, enters (a small sum: R is small too; none, of a row that
-      // sees no key: R may be any)
-      const float more = sum > 0.f && sum < 0x1p-100f ? 0x1p40f : 1.f;
-      const float inv = sum > 0.f || sum != sum ? 1.f / (sum * more) : 0.f;
-      const float up = ta < tb ? pow2(ref) * more : 0.f;
+      // divided by the sum before V's scale, up to 2^127, enters (wide: with what the sum was taken against, in two
+      // steps, because it may be 2^-140)
+      const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+      const float half = top == -INFINITY ? 0.f : exp2_fast(0.5f * (mx - kLift8 + (ta < tb ? (float)ref : 0.f) - top));
+      const float up0 = wide ? half : ta < tb ? pow2(ref) : 0.f, up1 = wide ? half : 1.f;
       // staged in the place of this row's queries, whose products are done
       const uint32_t stage_row = sbase + m * S::kTileBytes + row * 128;
 #pragma unroll 1
@@ -631,7 +765,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
             if (c + i >= g.c.d) break;
             float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(o[i + j]) * inv * up;
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(o[i + j]) * inv * up0 * up1;
             if (parts) {
               *reinterpret_cast<float4 *>(prow + c + i) = make_float4(v[0], v[1], v[2], v[3]);
               *reinterpret_cast<float4 *>(prow + c + i + 4) = make_float4(v[4], v[5], v[6], v[7]);
@@ -660,8 +794,8 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
         __syncwarp();
       }
       if (valid) {
-        const float against = mx - kLift8;  // what the probabilities were taken against
-        const bool any = sum > 0.f;         // (the parts' sums, of any size, join as exponents)
+        const float against = wide ? top : mx - kLift8;  // what the sum was taken against
+        const bool any = sum > 0.f;  // (the parts' sums, of any size, join as exponents)
         if (parts) g.part_ml[(long long)split * all_rows + out_row] = any ? make_float2(against + log2f(sum), 1.f) : make_float2(against, sum);
         else if (g.lse) g.lse[out_row] = any || sum != sum ? against * 0.693147180559945309f + logf(sum) : -INFINITY;
       }

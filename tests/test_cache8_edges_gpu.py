@@ -120,3 +120,59 @@ def test_values_that_outweigh_their_small_probability(new, group, length, width,
     _within(o, ro, to, "o")
     _within(lse, rl, tl, "lse")
 
+
+FAR = [(73, -60), (17, -116), (119, -100), (101, 0)]  # exponents of the values' scales, in turn
+
+
+@pytest.mark.parametrize("length", [200, 7000])
+@pytest.mark.parametrize("new,group", [(1, 4), (8, 4), (40, 1), (40, 4), (300, 4)])
+@pytest.mark.parametrize("scales", FAR, ids=str)
+def test_values_whose_scales_lie_far_apart(scales, new, group, length):
+    """Every second block's values are smaller by far than the others': their keys count in the sum all the same."""
+    n, hk, d = length + new, 2, 64
+    table, pages = _table([n], 16, 211)
+    c = _cache(pages, hk, 16, d, 212)
+    at = _blocks(table, n)
+    _bytes(c.v_scale)[at[0::2]], _bytes(c.v_scale)[at[1::2]] = 127 + scales[0], 127 + scales[1]
+    q = _randn(new, group * hk, d, dtype=BF, seed=213, gain=0.1)
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), return_lse=True)
+    assert length < 1000 or new <= 8 or _parts(c)
+    ro, rl, to, tl = _seen_reference(c, q, table, n)
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
+
+@pytest.mark.parametrize("new,group", [(8, 4), (40, 1), (40, 4), (300, 4)])
+@pytest.mark.parametrize("hidden", [90, 119])
+def test_small_values_beside_hidden_large_ones(hidden, new, group):
+    """Rows that see values of 2^-20 alone, where the last rows see ones of 2^90 and more too."""
+    n, hk, d = 636 + new, 2, 128
+    table, pages = _table([n], 16, 221)
+    c = _cache(pages, hk, 16, d, 222)
+    at = _blocks(table, n)
+    _bytes(c.v_scale)[at], _bytes(c.v_scale)[at[-1]] = 127 - 20, 127 + hidden
+    q = _randn(new, group * hk, d, dtype=BF, seed=223, gain=0.1)
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), return_lse=True)
+    ro, rl, to, tl = _seen_reference(c, q, table, n)
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
+
+def test_the_sum_over_small_values_does_not_overflow():
+    """40 000 keys whose values are 2^100 smaller than those of the last block, their scores 2^8 above the first tile's."""
+    n, new, heads, d = 40016, 40, 152, 64
+    table = torch.arange(n // 16, dtype=torch.int32, device=DEV)[None]
+    c = _alt().PagedCache8.empty(n // 16, heads, 16, d, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(231)
+    _bytes(c.v).copy_(torch.randint(0, 0x7f, c.v.shape, generator=g, device=DEV, dtype=torch.uint8))
+    _bytes(c.k)[:], _bytes(c.k_scale)[:] = 0, 127
+    _bytes(c.k)[8:, :, :, 0] = 0x4b  # 5.5: 2^7.93, below the 2^8 that the softmax's maximum may lag by
+    _bytes(c.v_scale)[:], _bytes(c.v_scale)[-1] = 127 - 27, 127 + 73
+    q = torch.zeros(new, heads, d, dtype=BF, device=DEV)
+    q[:, :, 0] = 1
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), scale=1.0, return_lse=True)
+    assert not _parts(c)
+    ro, rl, to, tl = _seen_reference(c, q, table, n, scale=1.0)
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
