@@ -77,9 +77,9 @@ constexpr float kLift8 = 6.f;   // probabilities are taken times 2^6 (and grow b
 // at most, and the sums, up to 2^94 a key, are fp32 numbers.  Where the exponents
 // lie further apart (but for blocks of zeros: a wide CTA) the sum is taken from
 // exponentials of its own, against the maximum of the scores alone
-// (softmax_wide: 2048 tokens over 32768 keys 1800 us, else 692).
+// (softmax_wide: 2048 tokens over 32768 keys 1820 us, else 703).
 constexpr int kLeast = -80;
-constexpr int kZeros = -117;  // the exponent of a block of zeros, as the append leaves it
+constexpr int kZeros = -117;  // the exponent of a block of zeros, as the append leaves it; but it may hold small values too
 
 // What the softmax needs of a tile's blocks.
 struct TileScales {
@@ -164,6 +164,29 @@ __device__ __forceinline__ bool to_halves(uint32_t codes, uint32_t tile, int row
     }
   }
   return found;
+}
+
+// Whether some of the key blocks from, from + 128, .. (a warp's 32 each time)
+// whose exponent is kZeros or less hold anything but zeros, by a warp.  (With
+// every second page of 32768 keys zeros, 2048 tokens take 962 us, without zeros
+// 703; taking them for small values, as a wide CTA, would be 1820.)
+__device__ __noinline__ bool holds_small_values(const Attend8Args &p, int seq, int hk, int len, int from, int blocks) {
+  const AttendArgs &g = p.a;
+  const uint8_t *codes = static_cast<const uint8_t *>(g.c.v);
+  for (int i0 = from; i0 < blocks; i0 += 128) {
+    const int i = i0 + (int)(threadIdx.x & 31);
+    const uint32_t s = i < blocks ? block_scales(p, seq, hk, len, kBlock * i) : kNoScales;
+    uint32_t any = 0u;
+    if (s != kNoScales && (int)(s >> 8) - 127 <= kZeros) {
+      // (the rows of a block lie one after the other)
+      const uint4 *v = reinterpret_cast<const uint4 *>(codes + key_offset(g, seq, hk, kBlock * i) / 2);
+      const int n = min(len - kBlock * i, kBlock) * (g.c.d / 16);
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) any |= v[j].x | v[j].y | v[j].z | v[j].w;
+    }
+    if (__any_sync(0xffffffffu, (any & 0x7f7f7f7fu) != 0u)) return true;
+  }
+  return false;
 }
 
 // The softmax of a row's tiles in a wide CTA (see kLeast), by the warps of a
@@ -303,7 +326,8 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
   auto scale_full = [&](int s) { return scale_bars + 8u * s; };
   const uint32_t tmem_slot = scale_bars + 32u;
   __shared__ int bad_values;     // some were taken out of the tiles
-  __shared__ int top_of[4], low_of[4], ref, wide_sum;  // largest and smallest exponents, R, whether they lie far apart
+  __shared__ int top_of[4], low_of[4], tiny_of[4], ref, wide_sum;  // largest and smallest exponents, R, whether they lie far apart
+  __shared__ bool small_of[4];
   // Of tile t in slot t % 4: when the codes of tile t + 4 are turned, the
   // scores of tile t + 2 are done, and with them the softmax of tile t.
   __shared__ __align__(16) TileScales tile_scales[4];
@@ -400,7 +424,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
     } else if (warp >= 4 * MT + 4) {
       // ---------------------------------------------------------------- codes to halves
       const int w = warp - 4 * MT - 4;  // its rows: 32 w to 32 w + 31 of each tile
-      int top = -127, low = 127;
+      int top = -127, low = 127, tiny = 127;
       const int blocks = min(8 * t1, (k.len + kBlock - 1) / kBlock);
 #pragma unroll 4
       for (int i = 8 * t0 + 32 * w + lane; i < blocks; i += 128) {
@@ -408,15 +432,23 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
         const int e = s != kNoScales ? (int)(s >> 8) - 127 : -127;
         top = max(top, e);
         if (e > kZeros) low = min(low, e);
+        else if (s != kNoScales) tiny = min(tiny, e);
       }
       top = __reduce_max_sync(0xffffffffu, top), low = __reduce_min_sync(0xffffffffu, low);
+      tiny = __reduce_min_sync(0xffffffffu, tiny);
       int r = 0;  // R
       bool wide = false;
       if (t0 < t1) {
-        if (lane == 0) top_of[w] = top, low_of[w] = low;
+        if (lane == 0) top_of[w] = top, low_of[w] = low, tiny_of[w] = tiny;
         codes_sync();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = max(top, top_of[i]), low = min(low, low_of[i]);
+        for (int i = 0; i < 4; ++i) top = max(top, top_of[i]), low = min(low, low_of[i]), tiny = min(tiny, tiny_of[i]);
+        if (tiny < top + kLeast && top + kLeast <= low) {  // only these are so far off: if they hold more than zeros
+          const bool small = holds_small_values(p, k.seq, hk, k.len, 8 * t0 + 32 * w, blocks);
+          if (lane == 0) small_of[w] = small;
+          codes_sync();
+          if (small_of[0] | small_of[1] | small_of[2] | small_of[3]) low = tiny;
+        }
         r = top, wide = low < top + kLeast;
         if (w == 0 && lane == 0) ref = r, wide_sum = wide;
       }

@@ -176,3 +176,54 @@ def test_the_sum_over_small_values_does_not_overflow():
     _within(o, ro, to, "o")
     _within(lse, rl, tl, "lse")
 
+
+@pytest.mark.parametrize("new,group", [(1, 4), (8, 4), (40, 1), (40, 4), (300, 4)])
+def test_the_largest_and_the_smallest_scales_side_by_side(new, group):
+    """Bytes 254 and 11 (2^127 and 2^-116): every scale is taken as it stands."""
+    n, hk, d = 200 + new, 2, 64
+    table, pages = _table([n], 16, 241)
+    c = _cache(pages, hk, 16, d, 242)
+    at = _blocks(table, n)
+    _bytes(c.v)[at[0::2]] &= 0xb7  # codes below 1, so that the values are numbers of 32 bits
+    _bytes(c.v_scale)[at[0::2]], _bytes(c.v_scale)[at[1::2]] = 254, 11
+    q = _randn(new, group * hk, d, dtype=BF, seed=243, gain=0.1)
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), return_lse=True)
+    ro, rl, to, tl = _seen_reference(c, q, table, n)
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
+
+@pytest.mark.parametrize("hidden", [127, 127 - 40, 127 + 80])
+@pytest.mark.parametrize("new,group", [(8, 4), (40, 1), (40, 4), (300, 4)])
+def test_rows_that_see_the_smallest_scales_alone(new, group, hidden):
+    """Values held with bytes 0 to 10, beside others that the last rows see too."""
+    n, hk, d = 636 + new, 2, 64
+    table, pages = _table([n], 16, 251)
+    c = _cache(pages, hk, 16, d, 252)
+    at = _blocks(table, n)
+    g = torch.Generator().manual_seed(253)
+    _bytes(c.v_scale)[at] = torch.randint(0, 11, (len(at), hk, 1), generator=g, dtype=torch.uint8).to(DEV)
+    _bytes(c.v_scale)[at[-1]] = hidden
+    q = _randn(new, group * hk, d, dtype=BF, seed=254, gain=0.1)
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), return_lse=True)
+    ro, rl, to, tl = _seen_reference(c, q, table, n)
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
+
+@pytest.mark.parametrize("new,group", [(8, 4), (40, 4), (300, 4)])
+def test_blocks_of_zeros_beside_others(new, group):
+    """Blocks of zeros as the append leaves them (byte 10): seen alone, and beside large values."""
+    n, hk, d = 7000 + new, 2, 64
+    table, pages = _table([n], 16, 261)
+    c = _cache(pages, hk, 16, d, 262)
+    at = _blocks(table, n)
+    _bytes(c.v)[at[3:-2]], _bytes(c.v_scale)[at[3:-2]] = 0, 10
+    _bytes(c.v_scale)[at[-1]] = 127 + 60
+    q = _randn(new, group * hk, d, dtype=BF, seed=263, gain=0.1)
+    for window in (0, 300):
+        o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), window=window, return_lse=True)
+        ro, rl, to, tl = _seen_reference(c, q, table, n, window=window)
+        _within(o, ro, to, "o")
+        _within(lse, rl, tl, "lse")
+
