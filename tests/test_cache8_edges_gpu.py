@@ -227,3 +227,188 @@ def test_blocks_of_zeros_beside_others(new, group):
         _within(o, ro, to, "o")
         _within(lse, rl, tl, "lse")
 
+
+# ---------------------------------------------------------------- the keys in parts
+@pytest.mark.parametrize("new", [40, 300])
+@pytest.mark.parametrize("d", [64, 128])
+def test_parts_of_the_keys_with_codes_that_are_no_numbers(new, d):
+    n, page, hq, hk = 6200 + new, 16, 8, 2
+    table, pages = _table([n], page, 281)
+    c = _cache(pages, hk, page, d, 282)
+    clean = [_bytes(x).clone() for x in (c.k, c.v)]
+    q = _randn(new, hq, d, dtype=BF, seed=283)
+    own = n - new + torch.arange(new, device=DEV)
+    for window in (0, 6000):
+        for x, y in zip((c.k, c.v), clean):
+            _bytes(x).copy_(y)
+        want = torch.zeros(new, hq, d, dtype=torch.bool, device=DEV)
+        for j in (n - 1, n - new // 2, n - new - 200, n - 6000 - new // 3, 17):
+            _bytes(c.v)[table[0, j // page].long(), 1, j % page, (7 * j) % d] = 0xff
+            sees = own >= j
+            if window:
+                sees &= j > own - window
+            want[:, hq // 2:, (7 * j) % d] |= sees[:, None]
+        o = c.attend(q, table, _i32([n]), _i32([0, new]), window=window)
+        assert _parts(c) and torch.equal(o.isnan(), want)
+        _bytes(c.v).copy_(clean[1])
+        ro, _, to, _ = _reference(c, q, table, [n], [0, new], window=window)
+        _within(o[~want], ro[~want], to[~want], "rows that do not see it")
+        j = n - new // 2  # a key that is not a number
+        _bytes(c.k)[table[0, j // page].long(), 0, j % page, 3] = 0x7f
+        o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), window=window, return_lse=True)
+        want = torch.zeros(new, hq, dtype=torch.bool, device=DEV)
+        want[:, :hq // 2] = (own >= j)[:, None]
+        assert torch.equal(lse.isnan(), want) and torch.equal(o.isnan().all(-1), want) and torch.equal(o.isnan().any(-1), want)
+
+
+@pytest.mark.parametrize("new", [40, 300])
+@pytest.mark.parametrize("power", [30, 90])
+def test_parts_of_the_keys_whose_scales_differ_by_far(new, power):
+    """One part holds values 2^power times the others', behind every window and before it; one none but zeros."""
+    n, page, hq, hk, d, window = 9000 + new, 16, 8, 2, 128, 8000
+    table, pages = _table([n], page, 291)
+    c = _cache(pages, hk, page, d, 292)
+    at = _blocks(table, n)
+    _bytes(c.v_scale)[at[:40]] += power                       # before the windows
+    _bytes(c.v_scale)[at[300:380]] -= power                   # a part's
+    _bytes(c.v)[at[400:480]], _bytes(c.v_scale)[at[400:480]] = 0, 10
+    _bytes(c.v_scale)[at[-1]] += power                        # seen by the last rows alone
+    q = _randn(new, hq, d, dtype=BF, seed=293, gain=0.1)
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), window=window, return_lse=True)
+    assert _parts(c)
+    ro, rl, to, tl = _seen_reference(c, q, table, n, window=window)
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
+
+@pytest.mark.parametrize("new", [40, 300])
+def test_parts_of_the_keys_with_pages_outside_the_cache(new):
+    n, page, hq, hk, d = 6200 + new, 16, 4, 2, 64
+    table, pages = _table([n], page, 301)
+    c = _cache(pages, hk, page, d, 302)
+    q = _randn(new, hq, d, dtype=BF, seed=303)
+    table[0, 150:290] = -1  # whole tiles, and a part of a part
+    table[0, 300] = pages
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), return_lse=True)
+    assert _parts(c) and int(c.error) == 1
+    ro, rl, to, tl = _reference(c, q, table, [n], [0, new])
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
+
+@pytest.mark.parametrize("new", [1, 5, 70])
+def test_a_request_alone_as_among_others(new):
+    """Within what either may be off, and bit for bit when nothing but the stream differs."""
+    lens, page, hq, hk, d = [new + 6200, new + 333, new], 32, 8, 2, 128
+    table, pages = _table(lens, page, 311)
+    c = _cache(pages, hk, page, d, 312)
+    cu = _cum([new] * 3)
+    q = _randn(3 * new, hq, d, dtype=BF, seed=313)
+    both, lse = c.attend(q, table, _i32(lens), _i32(cu), max_new=new, max_len=max(lens), return_lse=True)
+    ro, rl, to, tl = _reference(c, q, table, lens, cu)
+    _within(both, ro, to, "among others")
+    for b, n in enumerate(lens):
+        mine = slice(cu[b], cu[b + 1])
+        o, l = c.attend(q[mine], table[b:b + 1], _i32([n]), _i32([0, new]), return_lse=True)
+        _within(o, ro[mine], to[mine], "alone")
+        _within(o, both[mine].double(), 2 * to[mine], "alone as among others")
+        _within(l, rl[mine], tl[mine], "lse alone")
+    if new > 32:
+        c._sizes.clear()
+        c.attend(q[:new], table[:1], _i32(lens[:1]), _i32([0, new]))
+        assert _parts(c)  # the first has a workspace
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ts, ls, cs = table, _i32(lens), _i32(cu)
+    first, one = c.attend(q[:new], ts[:1], ls[:1], _i32([0, new])), _i32([0, new])
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(5):
+        for s in streams:
+            with torch.cuda.stream(s):
+                outs.append((c.attend(q, ts, ls, cs, max_new=new, max_len=max(lens)), c.attend(q[:new], ts[:1], ls[:1], one)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, both) and torch.equal(b, first) for a, b in outs)
+
+
+# ---------------------------------------------------------------- many sequences, large caches
+def _single_tokens(c, table, lens, q, **kw):
+    """One new token of each sequence, all keys short enough for one padded computation."""
+    n, d, group = int(lens.max()), q.shape[2], q.shape[1] // c.heads
+    o, lse = c.attend(q, table, lens, torch.arange(len(lens) + 1, dtype=torch.int32, device=DEV), max_new=1, return_lse=True, **kw)
+    assert int(c.error) == 0
+    pages = (n + c.page - 1) // c.page
+    at = table[:, :pages].long()
+    k, v = ((x.view(torch.uint8)[at].view(torch.float8_e4m3fn).double() *
+             torch.exp2(_bytes(s)[at].double() - 127).repeat_interleave(16, 3)[..., None]).transpose(1, 2).flatten(2, 3)[:, :, :n]
+            for x, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+    x = q.double().view(len(lens), c.heads, group, d)
+    seen = (torch.arange(n, device=DEV) < lens[:, None])[:, None, None]
+    s = (x @ k.transpose(2, 3) / math.sqrt(d)).masked_fill(~seen, -math.inf)
+    z = torch.logsumexp(s, -1)
+    p = torch.where(seen, torch.exp(s - torch.where(z.isinf(), 0.0, z)[..., None]), 0.0)
+    e = torch.where(seen, x.abs() @ k.abs().transpose(2, 3), 0.0).amax(-1) / math.sqrt(d) * d * 2.0 ** -23
+    e = e + x.abs().sum(-1) * 2.0 ** -38 * k.abs().amax((2, 3))[..., None] / math.sqrt(d)
+    ref, pv, top = p @ v, p @ v.abs(), v.abs().amax((2, 3))[..., None, None]
+    _within(o.view(ref.shape), ref, U[q.dtype] * ref.abs() + (2.0 ** -11 + 2 * e + 2.0 ** -17)[..., None] * pv
+            + (n * 2.0 ** -25 + 2.0 ** -38) * top, "o")
+    lse = lse.view(z.shape)
+    assert torch.equal(lse.isinf(), z.isinf())
+    some = ~z.isinf()
+    _within(lse[some], z[some], (e + 2.0 ** -17 * (1 + z.abs()))[some], "lse")
+
+
+def test_more_sequences_than_the_kernel_of_few_rows_counts():
+    g = torch.Generator(device=DEV).manual_seed(321)
+    batch, page, d = 8300, 16, 64
+    c = _cache(500, 1, page, d, 322)
+    table = torch.randint(0, 500, (batch, 13), device=DEV, generator=g, dtype=torch.int32)
+    lens = torch.randint(0, 13 * page + 1, (batch,), device=DEV, generator=g, dtype=torch.int32)
+    q = _randn(batch, 2, d, dtype=BF, seed=323, gain=1.5)
+    _single_tokens(c, table, lens, q)
+    _single_tokens(c, table[:8192], lens[:8192], q[:8192])
+
+
+def test_tables_whose_tiles_pass_31_bits():
+    heads, page, d, most = 80, 256, 64, 2 ** 23 - 257
+    c = _cache(5, heads, page, d, 331)
+    table = torch.full((2, most), -1, dtype=torch.int32, device=DEV)
+    table[0, :2], table[1, :3] = _i32([4, 0]), _i32([1, 3, 2])
+    lens = _i32([300, 517])
+    q = _randn(2, heads, d, dtype=BF, seed=332, gain=1.5)
+    _single_tokens(c, table, lens, q)
+    _single_tokens(c, table, lens, q, max_len=517)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_a_cache_past_32_bits(new):
+    """4.5 GB of codes each of keys and of values: pages at both ends, appended to and read."""
+    heads, page, d, pages = 8, 256, 128, 17200
+    assert pages * heads * page * d > 2 ** 32
+    c = _alt().PagedCache8.empty(pages, heads, page, d, device=DEV)
+    table = _i32([[pages - 1, 0, pages // 2], [pages - 2, 1, pages // 2 + 1]])
+    for x in (c.k, c.v, c.k_scale, c.v_scale):
+        _bytes(x)[table.flatten().long()] = 127 if x.dim() == 3 else 0x38
+    lens, cu, t = [600 + new, 300 + new], [0, new, 2 * new], 2 * new
+    near = {p: [_bytes(x)[p].clone() for x in (c.k, c.v)] for p in (2, 3, pages // 2 - 1, pages - 3)}
+    past, batch = [600, 300], 2
+    rows = _randn(sum(past), 2 * heads, d, dtype=BF, seed=341)
+    assert c.append(rows[:, :heads], rows[:, heads:], table, _i32(past), _i32(_cum(past))) is None
+    x = _randn(t, 4 * heads, d, dtype=BF, seed=342)
+    c.append(x[:, :heads], x[:, heads:2 * heads], table, _i32(lens), _i32(cu))
+    for b in range(batch):  # (every row is where the table says: off by half a code's step at most)
+        want = torch.cat([rows[_cum(past)[b]:_cum(past)[b + 1]], x[cu[b]:cu[b + 1], :2 * heads]]).double()
+        for y, s, w in ((c.k, c.k_scale, want[:, :heads]), (c.v, c.v_scale, want[:, heads:])):
+            j = torch.arange(lens[b], device=DEV)
+            home = table[b].long()[j // page]
+            sc = torch.exp2(_bytes(s)[home, :, j % page // 16].double() - 127)[..., None]
+            got = _bytes(y)[home, :, j % page].view(torch.float8_e4m3fn).double() * sc
+            # (twice for the keys that a larger scale coded anew)
+            _within(got, w, 2.0 ** -4 * w.abs() + 2 * 2.0 ** -10 * sc, "where the table says")
+    assert all(torch.equal(_bytes(y)[p], z) for p, was in near.items() for y, z in zip((c.k, c.v), was))
+    o, lse = c.attend(x[:, 2 * heads:], table, _i32(lens), _i32(cu), max_new=new, return_lse=True)
+    small = _alt().PagedCache8.empty(6, heads, page, d, device=DEV)
+    for y, z in ((small.k, c.k), (small.v, c.v), (small.k_scale, c.k_scale), (small.v_scale, c.v_scale)):
+        _bytes(y).copy_(_bytes(z)[table.flatten().long()])
+    again, lse2 = small.attend(x[:, 2 * heads:], _i32([[0, 1, 2], [3, 4, 5]]), _i32(lens), _i32(cu), max_new=new, return_lse=True)
+    assert torch.equal(o, again) and torch.equal(lse, lse2) and int(c.error) == 0
+
