@@ -291,6 +291,8 @@ class PagedCache:
     collects TR_CACHE_ERR_PAGE / TR_CACHE_ERR_WAIT.  No gradient goes through
     a cache: what ``append`` and ``attend`` return is no part of a graph."""
 
+    _name = "tr_cache_"  # of the entry points
+
     def __init__(self, k, v):
         self.calls = _library()
         if k.device.type != "cuda" or v.device != k.device:
@@ -348,7 +350,7 @@ class PagedCache:
             rc = at(i, self.calls.cache_append)(c, hk, hv, r, p, wk, hq, wq, hqo, eps, self.error.data_ptr(),
                                                 _stream(i))
             if rc:
-                check("tr_cache_append", rc)
+                check(self._name + "append", rc)
         return None if q is None else q_out
 
     def attend(self, q, table, lens, cu_new, scale=None, causal=True, window=0, max_new=None, max_len=None, out=None,
@@ -387,7 +389,7 @@ class PagedCache:
                 1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0, window, max_new, max_len,
                 None if ws is None else ws.data_ptr(), nbytes, self.error.data_ptr(), _stream(i))
             if rc:
-                check("tr_cache_attend", rc)
+                check(self._name + "attend", rc)
         return (out, lse) if return_lse else out
 
 
@@ -403,6 +405,8 @@ class PagedCache8(PagedCache):
     scale is the least that holds what was appended to it, and grows with it:
     its older keys are then coded anew, by a power of two.  What is not finite
     is held as NaN."""
+
+    _name = "tr_cache8_"
 
     def __init__(self, k, v, k_scale, v_scale):
         self.calls = _library().cache8
