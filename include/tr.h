@@ -560,10 +560,14 @@ tr_status tr_cache_attend(const tr_cache *c, const tr_heads *q, const tr_heads *
  * magnitudes of the rows it gets by the call (magnitude <= 448 * scale, 10 <=
  * e <= 246), and not below the block's old one if it has keys before the
  * call's; those keys are then coded anew by the scales' quotient, a power of
- * two, which rounds nothing but what falls under the codes' smallest step.  Codes are the nearest (ties to even, 448 at most); a value
- * that is not finite is held as NaN.  k_weight, r, pos, q as in
- * tr_cache_append: norm and rotation in fp32, rounded once into the codes.
- * Two sequences of a call may not share a page that it writes.
+ * two, which rounds nothing but what falls under the codes' smallest step.
+ * Codes are the nearest (ties to even, 448 at most); a value that is not
+ * finite is held as NaN.  k_weight, r, pos, q as in tr_cache_append: norm and
+ * rotation in fp32, rounded once into the codes.  Two sequences of a call may
+ * not share a page that it writes.
+ *   Tokens that are taken back later (drafts that are refused) leave the block
+ * that they shared with older keys as they made it: with the larger scale, if
+ * they needed one, and the older codes rounded for it.
  */
 #define TR_CACHE8_BLOCK 16
 typedef struct {
@@ -580,8 +584,9 @@ tr_status tr_cache8_append(const tr_cache8 *c, const tr_heads *k, const tr_heads
  * products take codes, which fit exactly, queries and probabilities as halves:
  * bf16 queries in units of a power of two of each row's own, probabilities with
  * the values' scales on them: whole down to 2^-20, and lost below 2^-31, of the
- * greatest that the row sees.  Scales of values below 2^-100 of the greatest
- * that it sees may count as that.  Sums are fp32.
+ * greatest that the row sees.  Sums are fp32.  So are the scores: a row with one
+ * of 2^23 or more (or its negative), where fp32 no longer tells apart what
+ * differs by one, gets no result to rely on.
  */
 size_t tr_cache8_attend_workspace_bytes(const tr_cache8 *c, int32_t q_heads, int32_t window, int32_t max_new,
                                         int32_t max_len);
@@ -613,8 +618,10 @@ tr_status tr_cache8_attend(const tr_cache8 *c, const tr_heads *q, const tr_heads
  * tr_pages_truncate: sequence b keeps its first d_keep[b] tokens at most
  * (negative: none); pages that hold none of these go back to the stack in the
  * opposite of the order in which they were taken, and their entries become -1.
- * Directly after an extend, to the lengths before it, everything is as it was.
- * Refused as above (TR_PAGES_ERR_STATE).
+ * Directly after an extend, to the lengths before it, table, lens and stack are
+ * as they were (what was appended in between stays in the cache: see
+ * tr_cache8_append for the block that it shares with older keys).  Refused as
+ * above (TR_PAGES_ERR_STATE).
  *
  * Calls on one table come one after another (a stream, or events between
  * streams); all of it may be captured and replayed.  ticket is one int32 of

@@ -245,7 +245,10 @@ struct BlockRows {
 // CTA waits for one load after the other (its sequence, rows, page), and its
 // keys' warps take longer than its values'; with two blocks, and each warp
 // keys and then values, that is once for both (29.6k tokens 113 us, so 108).
-// It costs registers, so few blocks go without.
+// Single tokens gain as well, although every second slot of theirs stays empty
+// (448 sequences 12.0 us, so 11.3; 512 13.9, so 14.3; 1024 28.3, so 24.1; 4096
+// 233, so 143: there every CTA's search for its sequence tells).  It costs
+// registers, so few blocks go without.
 template <typename T, int V, bool PAIRS, bool NORM, bool PACK>
 __global__ void __launch_bounds__(kRotThreads, 3) k_append8(const __grid_constant__ Append8Args a) {
   __shared__ __align__(16) float cs[(1 + PACK) * kMaxTrig], sn[(1 + PACK) * kMaxTrig];

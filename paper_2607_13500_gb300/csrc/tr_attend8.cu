@@ -22,7 +22,8 @@
 //   values  d = e - R, R one exponent of the CTA's, is added to the block's 16
 //           scores, and the softmax's maximum is that of these sums: what
 //           enters the second product is p 2^d.  R enters the results, and the
-//           sum of the p is taken block by block, times 2^-d.
+//           sum of the p is taken block by block, times 2^-d (kLeast says how
+//           far the d may lie apart for that, and what is done beyond).
 // So what enters the second product, 2^14 at most, is rounded to halves: it
 // keeps its bits down to 2^-20 of what the row's greatest key adds, and what is
 // lost below is 2^-31 of it.  Sums and everything else are fp32.
@@ -229,7 +230,7 @@ __device__ __noinline__ bool softmax_wide(WideRow &row) {
         for (int b = 0; b < 2; ++b) {
           asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[b]) : "r"(at + 4 * (2 * c + b)));
           asm volatile("ld.shared.f32 %0, [%1];" : "=f"(d[b]) : "r"(at + 32 + 4 * (2 * c + b)));
-          f[b] = fminf(fmaxf(w.row_scale * f[b], 1e-30f), 1e30f);
+          f[b] = block_factor(w.row_scale, f[b]);
         }
         const int key0 = t * kTile + 32 * c;
 #pragma unroll
@@ -683,7 +684,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
               undo[b] = __uint_as_float(z.x), undo[b + 1] = __uint_as_float(z.y), undo[b + 2] = __uint_as_float(z.z), undo[b + 3] = __uint_as_float(z.w);
             }
 #pragma unroll
-            for (int b = 0; b < 8; ++b) f[b] = fminf(fmaxf(row_scale * f[b], 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
+            for (int b = 0; b < 8; ++b) f[b] = block_factor(row_scale, f[b]);
           }
 #pragma unroll
           for (int i = 0; i < kTile; i += 32) tc::tmem_ld32_wait(s + i);

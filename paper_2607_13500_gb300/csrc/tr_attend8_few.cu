@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(kAllThreads, 1)
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          fs[i][h] = fminf(fmaxf(fr[i] * fk[h], 1e-30f), 1e30f);  // (-inf and 0 times it stay what they are)
+          fs[i][h] = block_factor(fr[i], fk[h]);
           peak[i][h] = fmaxf(fmaxf(s[2 * h][2 * i], s[2 * h][2 * i + 1]), fmaxf(s[2 * h + 1][2 * i], s[2 * h + 1][2 * i + 1])) * fs[i][h];
           over |= peak[i][h] > mx[i] + 8.f || peak[i][h] + (float)ev[h] > wx[i] + 8.f;
         }

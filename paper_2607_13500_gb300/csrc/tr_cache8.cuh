@@ -26,13 +26,7 @@ __device__ __forceinline__ long long scale_at(const CacheView &c, int page, int 
   return ((long long)page * c.heads + h) * (c.page / kBlock) + s / kBlock;
 }
 
-// Two codes (the low byte first) as two halves, exactly; NaN stays NaN.
-__device__ __forceinline__ uint32_t halves(uint16_t codes) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(codes));
-  return r;
-}
-// The same of four.
+// Four codes (the low byte first) as two pairs of halves, exactly; NaN stays NaN.
 __device__ __forceinline__ void halves4(uint32_t codes, uint32_t &lo, uint32_t &hi) {
   asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}"
       : "=r"(lo), "=r"(hi)

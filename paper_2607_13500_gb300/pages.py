@@ -109,7 +109,9 @@ class PageTable:
         """Every sequence keeps its first ``keep`` int32 [batch] tokens at
         most (0 or less: none), and the pages behind them are free again
         (tr_pages_truncate).  Directly after an extend, to the lengths before
-        it, everything is as it was."""
+        it, table, lens and free pages are as they were; the cache keeps what
+        was appended meanwhile (a PagedCache8 the larger scale of a block that
+        older keys share with tokens taken back)."""
         i = self.index
         p = attention._ints(keep, "keep", (self.batch,), i)
         rc = at(i, self.calls.truncate)(self._struct, p, self._error, attention._stream(i))

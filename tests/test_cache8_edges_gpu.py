@@ -228,6 +228,30 @@ def test_blocks_of_zeros_beside_others(new, group):
         _within(lse, rl, tl, "lse")
 
 
+@pytest.mark.parametrize("new,group", [(1, 4), (8, 4), (40, 1), (40, 4), (300, 4)])
+@pytest.mark.parametrize("length", [200, 7000])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_up_to_2_to_the_22(new, group, length, sign):
+    """One key of 16 has the greatest score, 2^22, and is the result; the next is 2^18 below it.  (Scores and their
+    difference are exact, so that nothing but the value's probability, 1, and the result is rounded.)"""
+    n, hk, d = length + new, 2, 64
+    table, pages = _table([n], 16, 351)
+    c = _cache(pages, hk, 16, d, 352, spread=30)
+    at = _blocks(table, n)
+    _bytes(c.k)[:], _bytes(c.k_scale)[:] = 0, 127 + 2
+    _bytes(c.k)[at, :, :, 0] = 0x77  # 240
+    best = length // 2
+    _bytes(c.k)[at[best // 16], :, best % 16, 0] = 0x78  # 256
+    if sign < 0:
+        _bytes(c.k)[at, :, :, 0] ^= 0x80
+    q = torch.zeros(new, group * hk, d, dtype=BF, device=DEV)
+    q[:, :, 0] = 2.0 ** 12
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), scale=float(sign), return_lse=True)
+    v = _held(c.v, c.v_scale, table, 0, n)[best].repeat_interleave(group, 0)[None].expand(new, -1, -1)
+    _within(o, v, (U[BF] + 2.0 ** -11 + 2.0 ** -17) * v.abs() + 2.0 ** -133, "o")
+    _within(lse, torch.full_like(lse, 2.0 ** 22, dtype=torch.float64), torch.full_like(lse, 2.0 ** 22 * 2.0 ** -17, dtype=torch.float64), "lse")
+
+
 # ---------------------------------------------------------------- the keys in parts
 @pytest.mark.parametrize("new", [40, 300])
 @pytest.mark.parametrize("d", [64, 128])
