@@ -86,7 +86,7 @@ constexpr int kZeros = -117;  // the exponent of a block of zeros, as the append
 struct TileScales {
   float k[8];     // 2^e of keys
   float v[8];     // d of values
-  float undo[8];  // 2^-d (wide CTAs: not used)
+  float undo[8];  // 2^-d (wide CTAs: none)
 };
 
 // The values taken out of open tiles among [t0, t1) to those rows of the warp
@@ -426,9 +426,11 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
       // ---------------------------------------------------------------- codes to halves
       const int w = warp - 4 * MT - 4;  // its rows: 32 w to 32 w + 31 of each tile
       int top = -127, low = 127, tiny = 127;
+      // (from the first block that some row sees: those before a window may be given away and hold any scale)
+      const int first = max(8 * t0, keys_of_rows(g, k, k.first, min(k.first + kRows, k.rows)).lo / kBlock) + 32 * w;
       const int blocks = min(8 * t1, (k.len + kBlock - 1) / kBlock);
 #pragma unroll 4
-      for (int i = 8 * t0 + 32 * w + lane; i < blocks; i += 128) {
+      for (int i = first + lane; i < blocks; i += 128) {
         const uint32_t s = block_scales(p, k.seq, hk, k.len, kBlock * i);
         const int e = s != kNoScales ? (int)(s >> 8) - 127 : -127;
         top = max(top, e);
@@ -445,7 +447,7 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = max(top, top_of[i]), low = min(low, low_of[i]), tiny = min(tiny, tiny_of[i]);
         if (tiny < top + kLeast && top + kLeast <= low) {  // only these are so far off: if they hold more than zeros
-          const bool small = holds_small_values(p, k.seq, hk, k.len, 8 * t0 + 32 * w, blocks);
+          const bool small = holds_small_values(p, k.seq, hk, k.len, first, blocks);
           if (lane == 0) small_of[w] = small;
           codes_sync();
           if (small_of[0] | small_of[1] | small_of[2] | small_of[3]) low = tiny;
@@ -475,10 +477,10 @@ __global__ void __launch_bounds__(Shape8<D, MT>::kThreads, 1)
           if (lane < 2) {
             TileScales &out = tile_scales[n & 3];
             int d = (s >> 8 < 255u ? (int)(s >> 8) - 127 : -127) - r;
-            if (!wide) d = max(d, kLeast);
+            if (!wide) d = min(max(d, kLeast), 0);  // (above 0: seen by no row)
             out.k[2 * w + lane] = pow2((int)(s & 0xffu) - 127);
             out.v[2 * w + lane] = (float)d;
-            out.undo[2 * w + lane] = pow2(min(-d, -kLeast));
+            out.undo[2 * w + lane] = wide ? 0.f : pow2(-d);
           }
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(scale_full(n & 3));

@@ -228,6 +228,28 @@ def test_blocks_of_zeros_beside_others(new, group):
         _within(lse, rl, tl, "lse")
 
 
+@pytest.mark.parametrize("new,group", [(8, 4), (40, 1), (40, 4), (300, 4)])
+@pytest.mark.parametrize("garbage", [0, 10, 255])
+def test_scales_of_pages_given_away(new, group, garbage):
+    """Pages before every window hold any scales and codes: nothing of them enters."""
+    n, hk, d, window = 2000 + new, 2, 64, 700
+    table, pages = _table([n], 16, 361)
+    c = _cache(pages, hk, 16, d, 362)
+    at = _blocks(table, n)
+    gone = at[:(n - new - window + 1) // 16]
+    for x in (c.k_scale, c.v_scale):
+        _bytes(x)[gone] = garbage
+    for x in (c.k, c.v):
+        _bytes(x)[gone] = 0x7f
+    q = _randn(new, group * hk, d, dtype=BF, seed=363, gain=0.5)
+    o, lse = c.attend(q, table, _i32([n]), _i32([0, new]), window=window, return_lse=True)
+    for x in (c.k, c.v):
+        _bytes(x)[gone] = 0
+    ro, rl, to, tl = _seen_reference(c, q, table, n, window=window)
+    _within(o, ro, to, "o")
+    _within(lse, rl, tl, "lse")
+
+
 @pytest.mark.parametrize("new,group", [(1, 4), (8, 4), (40, 1), (40, 4), (300, 4)])
 @pytest.mark.parametrize("length", [200, 7000])
 @pytest.mark.parametrize("sign", [1, -1])
