@@ -35,13 +35,12 @@
 // and the chain of a block's scores, softmax and second product has one score
 // buffer (with heads of 64 channels, half the bytes, a tile takes 0.86 of it).
 //
-// 28 heads of 128 over 4: 2048 tokens over 32768 keys 701 us (1.33 PFLOP/s, 0.70
+// 28 heads of 128 over 4: 2048 tokens over 32768 keys 700 us (1.33 PFLOP/s, 0.70
 // of the measured cuBLAS); 5 tokens of 32 sequences over 1000 to 12000 keys (35
-// rows a key head, MT = 1) 65 us; chunks of 784 tokens of 4 sequences over 1000
-// to 6272 keys, in fp16, 83 us, where each CTA's start and end, 11 us, tell.
+// rows a key head, MT = 1) 67 us; chunks of 784 tokens of 4 sequences over 1000
+// to 6272 keys, in fp16, 84 us, where each CTA's start and end, 11 us, tell.
 #include <atomic>
 #include <cmath>
-#include <type_traits>
 
 #include "tr_attend8.cuh"
 #include "tr_pack.cuh"
@@ -78,7 +77,7 @@ constexpr float kLift8 = 6.f;   // probabilities are taken times 2^6 (and grow b
 // at most, and the sums, up to 2^94 a key, are fp32 numbers.  Where the exponents
 // lie further apart (but for blocks of zeros: a wide CTA) the sum is taken from
 // exponentials of its own, against the maximum of the scores alone
-// (softmax_wide: 2048 tokens over 32768 keys 1820 us, else 703).
+// (softmax_wide: 2048 tokens over 32768 keys 1820 us, else 700).
 constexpr int kLeast = -80;
 constexpr int kZeros = -117;  // the exponent of a block of zeros, as the append leaves it; but it may hold small values too
 
@@ -170,7 +169,7 @@ __device__ __forceinline__ bool to_halves(uint32_t codes, uint32_t tile, int row
 // Whether some of the key blocks from, from + 128, .. (a warp's 32 each time)
 // whose exponent is kZeros or less hold anything but zeros, by a warp.  (With
 // every second page of 32768 keys zeros, 2048 tokens take 962 us, without zeros
-// 703; taking them for small values, as a wide CTA, would be 1820.)
+// 700; taking them for small values, as a wide CTA, would be 1820.)
 __device__ __noinline__ bool holds_small_values(const Attend8Args &p, int seq, int hk, int len, int from, int blocks) {
   const AttendArgs &g = p.a;
   const uint8_t *codes = static_cast<const uint8_t *>(g.c.v);

@@ -21,9 +21,9 @@
 // requests over 256 to 16384 keys 86 us, so 76).  A piece's queries and first
 // scales come from a warp of their own, a piece ahead (62, so 59).
 //
-// 28 heads of 128 over 4, bf16: those 64 requests 59 us (4.1 TB/s: ragged
+// 28 heads of 128 over 4, bf16: those 64 requests 60 us (4.1 TB/s: ragged
 // lengths end in part tiles, and the join takes 3), with 16384 keys each 183 us
-// (5.9 TB/s, 0.88 of a copy).  One token over 611 keys, 32 heads: 12.5 us of
+// (5.9 TB/s, 0.88 of a copy).  One token over 611 keys, 32 heads: 12.7 us of
 // latencies in a row, and a second launch.
 #include <atomic>
 
