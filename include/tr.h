@@ -584,7 +584,9 @@ tr_status tr_cache8_append(const tr_cache8 *c, const tr_heads *k, const tr_heads
  * products take codes, which fit exactly, queries and probabilities as halves:
  * bf16 queries in units of a power of two of each row's own, probabilities with
  * the values' scales on them: whole down to 2^-20, and lost below 2^-31, of the
- * greatest that the row sees.  Sums are fp32.  So are the scores: a row with one
+ * greatest that the row sees (where blocks of zeros, held with e <= 10, count
+ * with 2^-80 of the largest scale among the sequence's keys, if that is more than
+ * theirs).  Sums are fp32.  So are the scores: a row with one
  * of 2^23 or more (or its negative), where fp32 no longer tells apart what
  * differs by one, gets no result to rely on.
  */
